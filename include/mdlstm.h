@@ -424,6 +424,155 @@ mdlstm_status mdlstm_head_backward(const mdlstm_head_desc* desc, int32_t canvas_
                                    float* d_dy, float* d_dw, float* d_db,
                                    void* d_workspace, size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Sequence operators: layers along the packed frames of the examples (the
+ * columns the output layer sees, or any other packed tokens).
+ *
+ * Token tensors are [tokens][heads][dim], example after example without
+ * padding, like the frames of mdlstm_head_forward. Inputs may be views (the
+ * three parts of one projection's output): element strides between tokens and
+ * between heads are given, the last dimension is contiguous and strides are
+ * not negative. Outputs are contiguous. Outputs must not overlap inputs or
+ * each other.
+ */
+typedef struct {
+    const void* d_data;
+    int64_t token_stride, head_stride; /* in elements */
+} mdlstm_heads;
+
+/*
+ * Linear attention with a decay for each head. Per example and head h, with
+ * the rate a_h >= 0 and the fp32 state S [dim_k][dim_v],
+ *     S_t = exp(-a_h) S_{t-1} + k_t v_t^T          o_t = scale * q_t^T S_t
+ * The state restarts at every example's edge (S_{-1} = 0, or d_state), so the
+ * packed result equals each example computed alone. Query heads h share the
+ * key and value head h / (heads / kv_heads).
+ * dtype: storage of q, k, v, o and their gradients; states and sums are fp32.
+ * 1 <= dim_k, dim_v <= 128, 1 <= kv_heads <= heads <= 1024, heads a multiple of
+ * kv_heads.
+ */
+typedef struct {
+    int32_t heads, kv_heads, dim_k, dim_v, dtype;
+    float scale;
+} mdlstm_attention_desc;
+
+/* Workspace of a forward call, or with backward != 0 of a backward call: n
+ * examples of at most `longest` tokens, `tokens` in all. 0 when an argument is
+ * invalid; otherwise at least 16. */
+size_t mdlstm_attention_workspace_bytes(const mdlstm_attention_desc* desc, int32_t n, int64_t tokens,
+                                        int64_t longest, int32_t backward);
+
+/*
+ * d_offsets [n + 1] (device): example i is tokens d_offsets[i] to
+ * d_offsets[i + 1] - 1; ascending from 0 to `tokens`, no example longer than
+ * `longest`, empty ones allowed. The host does not read them: the kernels cut
+ * them to [0, tokens] and to `longest` tokens, so wrong offsets give wrong
+ * results but no access outside the tensors.
+ * d_rates [heads]: a_h, fp32.
+ * d_state [n][heads][dim_k][dim_v] (may be NULL: zero): the state each example
+ * starts from; d_final (out, may be NULL): the state it leaves (an empty
+ * example leaves the one it starts from).
+ * d_o (out) [tokens][heads][dim_v]. Asynchronous on `stream`; capturable into
+ * a graph.
+ */
+mdlstm_status mdlstm_attention_forward(const mdlstm_attention_desc* desc, int32_t n, int64_t tokens, int64_t longest,
+                                       const int64_t* d_offsets, const float* d_rates, const mdlstm_heads* q,
+                                       const mdlstm_heads* k, const mdlstm_heads* v, const float* d_state,
+                                       void* d_o, float* d_final, void* d_workspace, size_t workspace_bytes,
+                                       void* stream);
+
+/*
+ * Gradients of sum(o * do) + sum(final * dfinal) with respect to q, k, v and
+ * the initial state (the rates are constants). grad_o: a view of do. d_dfinal
+ * and d_dstate (out) may be NULL. d_dq [tokens][heads][dim_k], d_dk
+ * [tokens][kv_heads][dim_k] and d_dv [tokens][kv_heads][dim_v] (out) are
+ * overwritten; those of shared heads are summed in fp32 in a fixed order
+ * before they are rounded. Needs nothing of the forward call.
+ */
+mdlstm_status mdlstm_attention_backward(const mdlstm_attention_desc* desc, int32_t n, int64_t tokens, int64_t longest,
+                                        const int64_t* d_offsets, const float* d_rates, const mdlstm_heads* q,
+                                        const mdlstm_heads* k, const mdlstm_heads* v, const float* d_state,
+                                        const mdlstm_heads* grad_o, const float* d_dfinal, void* d_dq, void* d_dk,
+                                        void* d_dv, float* d_dstate, void* d_workspace, size_t workspace_bytes,
+                                        void* stream);
+
+/*
+ * One token for each of n sequences: row i of q, k, v advances the state at
+ * d_state [slots][heads][dim_k][dim_v] (in and out, fp32) of slot d_slots[i]
+ * (device; NULL: slot i, then n <= slots) and gives o_i (d_o [n][heads][dim_v]).
+ * A slot outside [0, slots) marks an idle row: its o is zero and no state
+ * changes. Two rows must not name the same slot (which of them the state then
+ * holds is undefined).
+ */
+mdlstm_status mdlstm_attention_step(const mdlstm_attention_desc* desc, int32_t n, const float* d_rates,
+                                    const mdlstm_heads* q, const mdlstm_heads* k, const mdlstm_heads* v,
+                                    float* d_state, int64_t slots, const int32_t* d_slots, void* d_o, void* stream);
+
+/*
+ * Dropout from a counter-based generator; the mask is never stored. Element
+ * e = row * cols + col of the tensor belongs to block b = e / 8, place j = e % 8:
+ * the four 32-bit words of Philox 4x32-10 (Salmon et al. 2011) with counter
+ * (b, call) and key seed, 64 bits each, low word first, give eight 16-bit
+ * numbers u_j (word j / 2, low half first). The element is kept where
+ * u_j >= t, t = 65536 p rounded to the nearest integer (ties to even), and then
+ * scaled by 65536 / (65536 - t); a dropped element is 0 whatever it held.
+ * p is thus taken to the nearest 2^-16 and the scale keeps the expectation
+ * exact. `call` numbers the draws under one seed (a layer's id, the step).
+ *
+ * d_y (out, contiguous [rows][cols]) = d_residual + dropout(d_x); d_residual may
+ * be NULL. x and residual rows are x_stride and residual_stride >= cols
+ * elements apart. 0 <= p <= 1. The gradient with respect to x is the same call on
+ * the gradient of y without a residual. d_y may be d_x or d_residual where that
+ * one is contiguous.
+ */
+mdlstm_status mdlstm_dropout(int32_t dtype, int64_t rows, int64_t cols, const void* d_x, int64_t x_stride, double p,
+                             uint64_t seed, uint64_t call, const void* d_residual, int64_t residual_stride,
+                             void* d_y, void* stream);
+
+/*
+ * Root-mean-square norm of a residual sum, rows of `cols` elements
+ * (1 <= cols <= 32768), weights fp32:
+ *     h = residual + dropout(x)     y = h * rsqrt(mean(h^2) + eps) * w
+ * with mdlstm_dropout's mask for (p, seed, call). Sums are fp32 and y is
+ * computed from h before h is rounded to its storage type.
+ */
+typedef struct {
+    int32_t cols, dtype;
+    float eps; /* > 0 */
+    double p;  /* dropout, in [0, 1] */
+} mdlstm_norm_desc;
+
+/*
+ * d_residual [rows][residual_stride >= cols] may be NULL (h = dropout(x)).
+ * d_h (out) [rows][cols]: may be NULL only without residual and dropout, when
+ * h is x itself. Output, one of the two, the other NULL:
+ *   d_y  (out) [rows][cols], storage type;
+ *   d_y8 (out) [rows][cols], float8 e4m3, and d_scale (out) [rows], fp32:
+ *        y / scale rounded to nearest even, scale = max(max_row |y| / 448,
+ *        2^-126) (a row with a NaN or an infinity among its y has scale NaN).
+ * d_rstd (out, may be NULL) [rows]: rsqrt(mean(h^2) + eps), for the backward.
+ */
+mdlstm_status mdlstm_norm_forward(const mdlstm_norm_desc* desc, int64_t rows, const void* d_x, int64_t x_stride,
+                                  const void* d_residual, int64_t residual_stride, const float* d_w, uint64_t seed,
+                                  uint64_t call, void* d_h, void* d_y, uint8_t* d_y8, float* d_scale, float* d_rstd,
+                                  void* stream);
+
+/* Workspace of mdlstm_norm_backward; 0 for invalid arguments, otherwise at least 16. */
+size_t mdlstm_norm_workspace_bytes(const mdlstm_norm_desc* desc, int64_t rows);
+
+/*
+ * Gradients of sum(y * dy) + sum(h * dh), contiguous [rows][cols] tensors; dh
+ * may be NULL. With g = dy w and c = h rstd,
+ *     dresidual = dh + rstd (g - c mean(g c))     dx = dropout'(dresidual)
+ *     dw = sum over rows of dy c  (fp32, fixed order, overwritten)
+ * h is read as stored (d_h, or x with its stride where the forward wrote none).
+ * d_dresidual may be NULL (then only dx is written).
+ */
+mdlstm_status mdlstm_norm_backward(const mdlstm_norm_desc* desc, int64_t rows, const void* d_h, int64_t h_stride,
+                                   const float* d_rstd, const float* d_w, const void* d_dy, const void* d_dh,
+                                   uint64_t seed, uint64_t call, void* d_dx, void* d_dresidual, float* d_dw,
+                                   void* d_workspace, size_t workspace_bytes, void* stream);
+
 /* Message for the last non-OK status returned on the calling thread. */
 const char* mdlstm_last_error(void);
 

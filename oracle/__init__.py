@@ -13,6 +13,8 @@ Plain, slow, float64 NumPy definitions of what the GPU path computes:
   and tensor-list chunking (Section V-B).
 * ``oracle.head``   — the output layer shared by the four directions with the
   collapse of the rows (Section II), and the CTC loss with its gradient.
+* ``oracle.sequence`` — linear attention with a decay for each head, residual
+  norm and dropout over packed frames.
 
 Only ``tests/``, ``__graft_entry__.smoke()`` and the CPU-baseline leg of
 ``bench.py`` may import this package. The product path (the HIP library and

@@ -13,6 +13,7 @@ LIB_PATH = os.path.join(_HERE, "libmdlstm.so")
 
 # names and argument types of every exported entry point
 c_i32, c_size, c_void, c_char_p = ctypes.c_int32, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_char_p
+c_i64, c_u64 = ctypes.c_int64, ctypes.c_uint64
 
 
 class Rect(ctypes.Structure):
@@ -32,6 +33,24 @@ P_RECT = ctypes.POINTER(Rect)
 P_DESC = ctypes.POINTER(LayerDesc)
 P_HEAD = ctypes.POINTER(HeadDesc)
 P_VOIDP = ctypes.POINTER(c_void)
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("d_data", c_void), ("token_stride", c_i64), ("head_stride", c_i64)]
+
+
+class AttentionDesc(ctypes.Structure):
+    _fields_ = [("heads", c_i32), ("kv_heads", c_i32), ("dim_k", c_i32), ("dim_v", c_i32), ("dtype", c_i32),
+                ("scale", ctypes.c_float)]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("cols", c_i32), ("dtype", c_i32), ("eps", ctypes.c_float), ("p", ctypes.c_double)]
+
+
+P_HEADS = ctypes.POINTER(Heads)
+P_ATTENTION = ctypes.POINTER(AttentionDesc)
+P_NORM = ctypes.POINTER(NormDesc)
 
 SIGNATURES = {
     "mdlstm_pack_workspace_bytes": (c_size, [c_i32]),
@@ -67,6 +86,21 @@ SIGNATURES = {
     "mdlstm_block_conv_backward": (c_i32, [c_i32, c_i32, c_i32, c_i32, c_i32, P_RECT, c_i32, c_i32, c_void, c_void,
                                            P_RECT, c_i32, c_i32, c_void, c_void, c_void, c_void, c_void, c_void, c_size,
                                            c_void]),
+    "mdlstm_attention_workspace_bytes": (c_size, [P_ATTENTION, c_i32, c_i64, c_i64, c_i32]),
+    "mdlstm_attention_forward": (c_i32, [P_ATTENTION, c_i32, c_i64, c_i64, c_void, c_void, P_HEADS, P_HEADS, P_HEADS,
+                                         c_void, c_void, c_void, c_void, c_size, c_void]),
+    "mdlstm_attention_backward": (c_i32, [P_ATTENTION, c_i32, c_i64, c_i64, c_void, c_void, P_HEADS, P_HEADS, P_HEADS,
+                                          c_void, P_HEADS, c_void, c_void, c_void, c_void, c_void, c_void, c_size,
+                                          c_void]),
+    "mdlstm_attention_step": (c_i32, [P_ATTENTION, c_i32, c_void, P_HEADS, P_HEADS, P_HEADS, c_void, c_i64, c_void,
+                                      c_void, c_void]),
+    "mdlstm_dropout": (c_i32, [c_i32, c_i64, c_i64, c_void, c_i64, ctypes.c_double, c_u64, c_u64, c_void, c_i64, c_void,
+                               c_void]),
+    "mdlstm_norm_forward": (c_i32, [P_NORM, c_i64, c_void, c_i64, c_void, c_i64, c_void, c_u64, c_u64, c_void, c_void,
+                                    c_void, c_void, c_void, c_void]),
+    "mdlstm_norm_workspace_bytes": (c_size, [P_NORM, c_i64]),
+    "mdlstm_norm_backward": (c_i32, [P_NORM, c_i64, c_void, c_i64, c_void, c_void, c_void, c_void, c_u64, c_u64, c_void,
+                                     c_void, c_void, c_void, c_size, c_void]),
 }
 
 STATUS = {0: "OK", 1: "INVALID_ARG", 2: "TOO_WIDE", 3: "BAD_LAYOUT", 4: "WORKSPACE", 5: "UNSUPPORTED", 6: "DEVICE",

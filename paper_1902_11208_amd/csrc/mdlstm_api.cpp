@@ -15,6 +15,7 @@
 #include <unordered_map>
 #include <vector>
 
+#include "host.hpp"
 #include "kernels.hpp"
 
 namespace {
@@ -36,6 +37,12 @@ mdlstm_status fail(mdlstm_status st, const char* fmt, ...) {
     g_last_error = buf;
     return st;
 }
+
+}  // namespace
+
+mdlstm_status mdl::set_error(mdlstm_status st, const char* message) { return fail(st, "%s", message); }
+
+namespace {
 
 mdlstm_status device_fail(hipError_t e, const char* where) {
     return fail(MDLSTM_ERR_DEVICE, "%s: %s", where, hipGetErrorString(e));
