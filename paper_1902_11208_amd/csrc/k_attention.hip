@@ -1,5 +1,7 @@
 // Linear attention with a decay for each head: the scan over packed sequences,
 // the sum over shared heads, and the single-token step.
+#include <algorithm>
+
 #include "common.hpp"
 #include "sequence.hpp"
 
@@ -19,48 +21,489 @@ __device__ __forceinline__ void sequence(const int64_t* offsets, int i, int64_t 
     len = min(t1 - t0, longest);
 }
 
-// One workgroup per (sequence, head), a thread per column of the state, which
-// lies in LDS; one token at a time.
+// ---------------------------------------------------------------------------
+// The scan in chunks of C = 32 tokens, on matrix instructions. With the state S
+// [dk][dv] before a chunk and g the decay, for tokens i, j of the chunk
+//     o_i = g^(i+1) q_i S + sum_(j<=i) g^(i-j) (q_i . k_j) v_j
+//     S'  = g^C S + sum_j g^(C-1-j) k_j v_j^T
+// so a chunk costs products of 32-row tiles instead of 32 dependent steps.
+//
+// A wave owns 32 (or 16) of the dv columns of one head's state and keeps them
+// in MFMA accumulators for its whole sequence; a workgroup's waves share the
+// chunk's q, k and v rows in LDS, and each computes the chunk's q k^T itself
+// (that costs less than passing it through LDS and a barrier). All products
+// are computed transposed, O^T = S^T Q^T + V^T P^T with P^T = K Q^T: a tile's
+// accumulators hold, in lane 16 g + n, rows 4 g .. 4 g + 3 of column n, and a
+// reduction may run in any order, so S and P^T are operands of the next product
+// as they stand, with the reduction slots of lane group g taken as rows 4 g + r
+// (and 16 + 4 g + r). Neither passes through LDS.
+//
+// bf16: P and S are rounded to bf16 as operands, one rounding of each on its
+// way to an output that is rounded to bf16 itself. The state's own sum takes
+// g^(C-1-j) v_j in PIECES bf16 pieces (2: 2^-17 of a term is left out, 3: 2^-25,
+// where the state is a result of the call), so it is as good as its fp32
+// accumulators.
+// ---------------------------------------------------------------------------
+constexpr int C = 32;
+
 template <typename T>
-__global__ __launch_bounds__(128) void k_scan(ScanArgs a) {
-    extern __shared__ float lds[];
-    const ScanRole& R = a.role[blockIdx.z];
-    const int seq = blockIdx.x, head = blockIdx.y, c = threadIdx.x, dk = R.q.dim, dv = R.v.dim;
-    float* S = lds;  // [dk][dv]
-    float* q = S + dk * dv;
-    float* k = q + dk;
-    int64_t t0, len;
-    sequence(a.offsets, seq, a.tokens, a.longest, t0, len);
-    const int64_t so = ((int64_t)seq * a.heads + head) * dk * dv;
-    if (c < dv)
-        for (int i = 0; i < dk; ++i) S[i * dv + c] = R.state ? R.state[so + (R.state_t ? c * dk + i : i * dv + c)] : 0.0f;
-    const float g = expf(-a.rates[head]);
-    for (int64_t j = 0; j < len; ++j) {
-        const int64_t t = t0 + (R.reverse ? len - 1 - j : j);
-        __syncthreads();
-        if (c < dk) {
-            q[c] = St<T>::ld1(at<T>(R.q, t, head) + c);
-            k[c] = St<T>::ld1(at<T>(R.k, t, head) + c);
-        }
-        __syncthreads();
-        if (c < dv) {
-            const float v = St<T>::ld1(at<T>(R.v, t, head) + c) * R.in_scale, f = R.reverse && j == 0 ? 1.0f : g;
-            float o = 0.0f;
-            for (int i = 0; i < dk; ++i) {
-                const float s = fmaf(k[i], v, S[i * dv + c] * f);
-                S[i * dv + c] = s;
-                o = fmaf(q[i], s, o);
+struct Mx;
+template <>
+struct Mx<float> {
+    typedef floatx4 Frag;  // reduction over 16: slots 4 g + r
+    static constexpr int KB = 16, PAD = 4;
+    static __device__ __forceinline__ floatx4 mma(Frag a, Frag b, floatx4 c) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) c = mfma_f32(a[r], b[r], c);
+        return c;
+    }
+    // row `row` of a staged tile, reduction along it
+    static __device__ __forceinline__ Frag along(const float* tile, int pitch, int row, int k, int g) {
+        return *reinterpret_cast<const floatx4*>(tile + row * pitch + k + 4 * g);
+    }
+    // column `col0 + n`, reduction down the rows
+    static __device__ __forceinline__ Frag down(const float* tile, int pitch, int row0, int col0, int g, int n) {
+        Frag f;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) f[r] = tile[(row0 + 4 * g + r) * pitch + col0 + n];
+        return f;
+    }
+    static __device__ __forceinline__ Frag from(const floatx4* t) { return t[0]; }
+};
+template <>
+struct Mx<bf16_t> {
+    typedef bf16x8 Frag;  // reduction over 32: slots 4 g + r, then 16 + 4 g + r
+    static constexpr int KB = 32, PAD = 8;
+    typedef short s4 __attribute__((ext_vector_type(4)));
+    static __device__ __forceinline__ floatx4 mma(Frag a, Frag b, floatx4 c) { return mfma_bf16(a, b, c); }
+    static __device__ __forceinline__ Frag along(const bf16_t* tile, int pitch, int row, int k, int g) {
+        const uint2 lo = *reinterpret_cast<const uint2*>(tile + row * pitch + k + 4 * g);
+        const uint2 hi = *reinterpret_cast<const uint2*>(tile + row * pitch + k + 16 + 4 * g);
+        return as_bf16x8(make_uint4(lo.x, lo.y, hi.x, hi.y));
+    }
+    // The LDS transpose read: in each sixteen lanes, lane 4 j + c points at four
+    // consecutive values of row j, and lane n receives column n of the four rows.
+    static __device__ __forceinline__ uint2 tr(const bf16_t* p) {
+        const s4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)(p));
+        uint2 r;
+        __builtin_memcpy(&r, &v, 8);
+        return r;
+    }
+    static __device__ __forceinline__ Frag down(const bf16_t* tile, int pitch, int row0, int col0, int g, int n) {
+        const bf16_t* p = tile + (row0 + 4 * g + (n >> 2)) * pitch + col0 + 4 * (n & 3);
+        const uint2 lo = tr(p), hi = tr(p + 16 * pitch);
+        return as_bf16x8(make_uint4(lo.x, lo.y, hi.x, hi.y));
+    }
+    static __device__ __forceinline__ Frag from(const floatx4* t) {
+        return as_bf16x8(make_uint4(f2bf2(t[0][0], t[0][1]), f2bf2(t[0][2], t[0][3]), f2bf2(t[1][0], t[1][1]),
+                                    f2bf2(t[1][2], t[1][3])));
+    }
+};
+
+// exp(-rate n) for n >= 0; 1 at n = 0 for every rate.
+__device__ __forceinline__ float power(float l2, int n) { return n == 0 ? 1.0f : __builtin_amdgcn_exp2f(l2 * (float)n); }
+
+// Sequences are cut into segments of `seg` tokens that are scanned side by
+// side where there are too few sequences to fill the chip. Segment j of
+// sequence i has slot i + offsets[i] / seg + j; slots in between stay empty.
+__device__ __forceinline__ int find_sequence(const int64_t* offsets, int n, int64_t tokens, int64_t seg, int64_t slot) {
+    int lo = 0, hi = n;  // the last sequence whose first slot is at most `slot`
+    const int lane = threadIdx.x & 63;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 63) / 64, i = lo + lane * step;
+        const bool in = i < hi && i + min(max(offsets[i], (int64_t)0), tokens) / seg <= slot;
+        const int below = __popcll(__ballot(in));
+        if (below == 0) break;
+        lo += (below - 1) * step;
+        hi = min(hi, lo + step);
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+
+struct Unit {
+    int role, head, seq;
+    int64_t slot, j;  // slot and segment; without segments slot = seq, j = 0
+};
+
+// Units in launch order: workgroup b runs on XCD b % 8, which takes the roles
+// and the query heads of one (slot, key head) one after the other, as they read
+// the same tokens. False: no unit.
+__device__ __forceinline__ bool unit_of(const ScanArgs& a, Unit& u) {
+    const int group = a.group, kv = a.heads / group, inner = a.n_roles * group;
+    const int64_t i = blockIdx.x >> 3, rest = i / inner * 8 + (blockIdx.x & 7);
+    const int in = (int)(i % inner);
+    u.slot = rest / kv;
+    if (u.slot >= a.slots) return false;
+    u.role = in % a.n_roles;
+    u.head = (int)(rest % kv) * group + in / a.n_roles;
+    u.j = 0;
+    u.seq = (int)u.slot;
+    if (a.seg) {
+        u.seq = find_sequence(a.offsets, a.n, a.tokens, a.seg, u.slot);
+        u.j = u.slot - u.seq - min(max(a.offsets[u.seq], (int64_t)0), a.tokens) / a.seg;
+    }
+    return true;
+}
+
+// A thread's share of a chunk's q, k or v rows, on its way from memory to LDS.
+template <typename T, int D, int THREADS, bool WIDE>
+struct Stage {
+    static constexpr int EPV = 16 / sizeof(T), VPR = D / EPV, N = C * VPR / THREADS;
+    u32x4 v[N];
+    // rows 0 .. count - 1 of the chunk are tokens first, first + dir, ...; others and columns >= dim are zero
+    __device__ __forceinline__ void load(const T* base, int64_t token_stride, int dim, int64_t first, int dir, int count) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int x = threadIdx.x + i * THREADS, row = x / VPR, col = x % VPR * EPV;
+            const T* p = base + (first + (int64_t)dir * row) * token_stride + col;
+            v[i] = u32x4{0, 0, 0, 0};
+            if (row < count) {
+                if (WIDE) {
+                    if (col < dim) v[i] = *reinterpret_cast<const u32x4*>(p);
+                } else {
+                    T e[EPV];
+#pragma unroll
+                    for (int j = 0; j < EPV; ++j) e[j] = col + j < dim ? p[j] : T(0);
+                    __builtin_memcpy(&v[i], e, 16);
+                }
             }
-            const int64_t oo = (t * a.heads + head) * dv + c;
-            if (R.out_f32)
-                static_cast<float*>(R.out)[oo] = o * R.out_scale;
-            else
-                St<T>::st1(static_cast<T*>(R.out) + oo, o * R.out_scale);
         }
     }
-    if (R.final_state && c < dv)
-        for (int i = 0; i < dk; ++i)
-            R.final_state[so + (R.state_t ? c * dk + i : i * dv + c)] = S[i * dv + c] * (R.reverse && len > 0 ? g : 1.0f);
+    __device__ __forceinline__ void store(T* tile, int pitch) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int x = threadIdx.x + i * THREADS;
+            *reinterpret_cast<u32x4*>(tile + x / VPR * pitch + x % VPR * EPV) = v[i];
+        }
+    }
+};
+
+// WIDE: rows of q, k, v are whole 16-byte vectors. LOCAL: only the state that
+// a segment adds to zero, for all segments but a sequence's last.
+template <typename T, int D, int SLAB, bool WIDE, int PIECES, bool LOCAL>
+__global__ __launch_bounds__(64 * D / SLAB) void k_scan(ScanArgs a) {
+    typedef Mx<T> M;
+    typedef typename M::Frag Frag;
+    constexpr int THREADS = 64 * D / SLAB, NT = SLAB / 16, KT = D / 16, PITCH = D + M::PAD, TPF = M::KB / 16;
+    __shared__ __align__(16) T lds[3 * C * PITCH];
+    T *Q = lds, *K = lds + C * PITCH, *V = lds + 2 * C * PITCH;
+    Unit u;
+    if (!unit_of(a, u)) return;
+    const ScanRole& R = a.role[u.role];
+    int64_t t0, len;
+    sequence(a.offsets, u.seq, a.tokens, a.longest, t0, len);
+    const int64_t from = u.j * a.seg, to = a.seg ? min(len, from + a.seg) : len;
+    if (u.j > 0 && from >= len) return;
+    if (LOCAL && to >= len) return;
+    const int l = threadIdx.x & 63, g = l >> 4, n = l & 15, slab = (threadIdx.x >> 6) * SLAB;
+    const int dk = R.q.dim, dv = R.v.dim, head = u.head, e = R.reverse;
+    const float l2 = -1.4426950408889634f * a.rates[head];
+
+    // decays inside the chunk; a token j beyond i meets it with 0
+    const float ps = R.in_scale * R.out_scale;
+    float same[4], lower[4], late[2], w[2][4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int i = n, j = 4 * g + r;
+        same[r] = j <= i ? ps * power(l2, i - j) : 0.0f;
+        lower[r] = ps * power(l2, 16 + i - j);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) w[h][r] = R.in_scale * power(l2, C - 1 - (16 * h + j) + e);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) late[h] = R.out_scale * power(l2, 16 * h + n + 1 - e);
+    // g^C, in two parts where the state has to stand for itself: a rounded one
+    // would be off by the same 2^-24 every chunk
+    constexpr bool EXACT = PIECES == 3 || sizeof(T) == 4;
+    float gc = power(l2, C), gc_lo = 0.0f;
+    if (EXACT) {
+        const double x = exp(-(double)a.rates[head] * C);
+        gc = (float)x;
+        gc_lo = (float)(x - (double)gc);
+    }
+
+    floatx4 S[KT][NT];  // S[t][m][r] = state[16 t + 4 g + r][slab + 16 m + n]
+    {
+        const float* from_state = nullptr;
+        const int64_t size = (int64_t)dk * dv;
+        bool transposed = false;
+        if (u.j > 0)  // the slot before holds the state that this segment starts from
+            from_state = LOCAL ? nullptr : a.states + (((int64_t)u.role * a.slots + u.slot - 1) * a.heads + head) * size;
+        else if (!LOCAL && R.state) {
+            from_state = R.state + ((int64_t)u.seq * a.heads + head) * size;
+            transposed = R.state_t;
+        }
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int m = 0; m < NT; ++m)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = 16 * t + 4 * g + r, c = slab + 16 * m + n;
+                    S[t][m][r] = from_state && i < dk && c < dv ? from_state[transposed ? c * dk + i : i * dv + c] : 0.0f;
+                }
+    }
+
+    const T* qp = at<T>(R.q, 0, head);
+    const T* kp = at<T>(R.k, 0, head);
+    const T* vp = at<T>(R.v, 0, head);
+    const int dir = R.reverse ? -1 : 1;
+    const int64_t first = R.reverse ? t0 + len - 1 : t0;  // token at scan position 0
+    Stage<T, D, THREADS, WIDE> sq, sk, sv;
+    auto fetch = [&](int64_t pos) {
+        const int count = (int)min((int64_t)C, to - pos);
+        if (!LOCAL) sq.load(qp, R.q.token_stride, dk, first + dir * pos, dir, count);
+        sk.load(kp, R.k.token_stride, dk, first + dir * pos, dir, count);
+        sv.load(vp, R.v.token_stride, dv, first + dir * pos, dir, count);
+    };
+    if (from < to) fetch(from);
+    for (int64_t pos = from; pos < to; pos += C) {
+        const int count = (int)min((int64_t)C, to - pos);
+        if (!LOCAL) sq.store(Q, PITCH);
+        sk.store(K, PITCH);
+        sv.store(V, PITCH);
+        lds_barrier();
+        if (pos + C < to) fetch(pos + C);
+        if (count < C) {  // the sequence's last chunk
+            gc = power(l2, count);
+            if (EXACT) {
+                const double x = exp(-(double)a.rates[head] * count);
+                gc = (float)x;
+                gc_lo = (float)(x - (double)gc);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int j = 16 * h + 4 * g + r;
+                    w[h][r] = j < count ? R.in_scale * power(l2, count - 1 - j + e) : 0.0f;
+                }
+        }
+        Frag vf[NT][2 / TPF];
+#pragma unroll
+        for (int m = 0; m < NT; ++m)
+#pragma unroll
+            for (int h = 0; h < 2 / TPF; ++h) vf[m][h] = M::down(V, PITCH, h * M::KB, slab + 16 * m, g, n);
+        if (!LOCAL) {
+            floatx4 o[NT][2], p[3];  // p: (j tile, i tile) (0, 0), (0, 1), (1, 1)
+            const floatx4 zero = {0, 0, 0, 0};
+            auto state_part = [&](bool scores) {
+#pragma unroll
+                for (int m = 0; m < NT; ++m) o[m][0] = o[m][1] = zero;
+#pragma unroll
+                for (int k = 0; k < D / M::KB; ++k) {
+                    const Frag q0 = M::along(Q, PITCH, n, k * M::KB, g), q1 = M::along(Q, PITCH, 16 + n, k * M::KB, g);
+                    if (scores) {
+                        const Frag k0 = M::along(K, PITCH, n, k * M::KB, g), k1 = M::along(K, PITCH, 16 + n, k * M::KB, g);
+                        p[0] = M::mma(k0, q0, p[0]);
+                        p[1] = M::mma(k0, q1, p[1]);
+                        p[2] = M::mma(k1, q1, p[2]);
+                    }
+#pragma unroll
+                    for (int m = 0; m < NT; ++m) {
+                        floatx4 t[TPF];
+#pragma unroll
+                        for (int x = 0; x < TPF; ++x) t[x] = S[k * TPF + x][m];
+                        const Frag s = M::from(t);
+                        o[m][0] = M::mma(s, q0, o[m][0]);
+                        o[m][1] = M::mma(s, q1, o[m][1]);
+                    }
+                }
+#pragma unroll
+                for (int m = 0; m < NT; ++m) o[m][0] *= late[0], o[m][1] *= late[1];
+            };
+            p[0] = p[1] = p[2] = zero;
+            state_part(true);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {  // a select: what lies beyond i may be infinite
+                p[0][r] = 4 * g + r <= n ? p[0][r] * same[r] : 0.0f;
+                p[2][r] = 4 * g + r <= n ? p[2][r] * same[r] : 0.0f;
+                p[1][r] *= lower[r];
+            }
+            {
+                const floatx4 b0[2] = {p[0], zero}, b1[2] = {p[1], p[2]};
+#pragma unroll
+                for (int h = 0; h < 2 / TPF; ++h) {
+                    const Frag f0 = M::from(b0 + h), f1 = M::from(b1 + h);
+#pragma unroll
+                    for (int m = 0; m < NT; ++m) {
+                        if (h == 0) o[m][0] = M::mma(vf[m][h], f0, o[m][0]);
+                        o[m][1] = M::mma(vf[m][h], f1, o[m][1]);
+                    }
+                }
+            }
+            // A v_j that is not finite reaches tokens before it as 0 v_j = NaN: their
+            // sums are taken again without it.
+            float bad = 0.0f;
+#pragma unroll
+            for (int m = 0; m < NT; ++m)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) bad = fmaf(o[m][0][r], 0.0f, fmaf(o[m][1][r], 0.0f, bad));
+            if (__any(bad != bad)) {
+                floatx4 was[NT][2];
+#pragma unroll
+                for (int m = 0; m < NT; ++m) was[m][0] = o[m][0], was[m][1] = o[m][1];
+                state_part(false);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int i = 16 * h + n;
+#pragma nounroll
+                    for (int j = 0; j <= i; ++j) {
+                        float s = 0.0f;
+#pragma nounroll
+                        for (int k = 0; k < dk; ++k) s = fmaf(St<T>::ld1(Q + i * PITCH + k), St<T>::ld1(K + j * PITCH + k), s);
+                        s *= ps * power(l2, i - j);
+#pragma unroll
+                        for (int m = 0; m < NT; ++m)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                o[m][h][r] = fmaf(s, St<T>::ld1(V + j * PITCH + slab + 16 * m + 4 * g + r), o[m][h][r]);
+                    }
+                }
+#pragma unroll
+                for (int m = 0; m < NT; ++m)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (was[m][h][r] - was[m][h][r] == 0.0f) o[m][h][r] = was[m][h][r];
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int i = 16 * h + n;
+                if (i < count) {
+                    const int64_t row = ((first + dir * (pos + i)) * a.heads + head) * dv;
+#pragma unroll
+                    for (int m = 0; m < NT; ++m) {
+                        const int c = slab + 16 * m + 4 * g;
+                        if (R.out_f32) {
+                            float* d = static_cast<float*>(R.out) + row + c;
+                            if (dv % 4 == 0) {
+                                if (c < dv) St<float>::st4(d, o[m][h]);
+                            } else {
+#pragma unroll
+                                for (int r = 0; r < 4; ++r)
+                                    if (c + r < dv) d[r] = o[m][h][r];
+                            }
+                        } else {
+                            T* d = static_cast<T*>(R.out) + row + c;
+                            if (dv % 4 == 0) {
+                                if (c < dv) St<T>::st4(d, o[m][h]);
+                            } else {
+#pragma unroll
+                                for (int r = 0; r < 4; ++r)
+                                    if (c + r < dv) St<T>::st1(d + r, o[m][h][r]);
+                            }
+                        }
+                    }
+                }
+            }
+        }
+        // S = g^C S + K^T (w V)
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int m = 0; m < NT; ++m) {
+                if (EXACT) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[t][m][r] = fmaf(S[t][m][r], gc, S[t][m][r] * gc_lo);
+                } else {
+                    S[t][m] *= gc;
+                }
+            }
+        Frag wv[NT][2 / TPF][sizeof(T) == 4 ? 1 : PIECES];
+#pragma unroll
+        for (int m = 0; m < NT; ++m) {
+            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) wv[m][h][0][r] = vf[m][h][r] * w[h][r];
+            } else {
+                floatx4 x[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[h][r] = (float)vf[m][0][4 * h + r] * w[h][r];
+#pragma unroll
+                for (int c = 0; c < PIECES; ++c) {
+                    wv[m][0][c] = M::from(x);
+                    if (c + 1 < PIECES)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) x[h][r] -= (float)wv[m][0][c][4 * h + r];
+                }
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int h = 0; h < 2 / TPF; ++h) {
+                const Frag kt = M::down(K, PITCH, h * M::KB, 16 * t, g, n);
+#pragma unroll
+                for (int m = 0; m < NT; ++m)
+#pragma unroll
+                    for (int c = (sizeof(T) == 4 ? 1 : PIECES) - 1; c >= 0; --c) S[t][m] = M::mma(kt, wv[m][h][c], S[t][m]);
+            }
+        lds_barrier();
+    }
+
+    const int64_t size = (int64_t)dk * dv;
+    float* to_state = nullptr;
+    bool transposed = false;
+    if (LOCAL) {
+        to_state = a.states + (((int64_t)u.role * a.slots + u.slot) * a.heads + head) * size;
+    } else if (R.final_state && to >= len) {
+        to_state = R.final_state + ((int64_t)u.seq * a.heads + head) * size;
+        transposed = R.state_t;
+    }
+    if (to_state) {
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int m = 0; m < NT; ++m)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = 16 * t + 4 * g + r, c = slab + 16 * m + n;
+                    if (i < dk && c < dv) to_state[transposed ? c * dk + i : i * dv + c] = S[t][m][r];
+                }
+    }
+}
+
+// The states that segments start from: for every sequence, head and element of
+// the state, over its segments in order. Slot j holds what segment j adds to
+// zero and receives the state that segment j + 1 starts from.
+__global__ __launch_bounds__(256) void k_join_segments(ScanArgs a) {
+    const ScanRole& R = a.role[blockIdx.z];
+    const int seq = blockIdx.y / a.heads, head = blockIdx.y % a.heads, size = R.q.dim * R.v.dim;
+    const int x = blockIdx.x * 256 + threadIdx.x;
+    int64_t t0, len;
+    sequence(a.offsets, seq, a.tokens, a.longest, t0, len);
+    if (len <= a.seg || x >= size) return;
+    const double gd = exp(-(double)a.rates[head] * (double)a.seg);
+    const float gs = (float)gd, gs_lo = (float)(gd - (double)gs);
+    float s = 0.0f;
+    if (R.state) {
+        const int i = x / R.v.dim, c = x % R.v.dim;
+        s = R.state[((int64_t)seq * a.heads + head) * size + (R.state_t ? c * R.q.dim + i : x)];
+    }
+    const int64_t slot0 = seq + t0 / a.seg;
+    float* p = a.states + (((int64_t)blockIdx.z * a.slots + slot0) * a.heads + head) * size + x;
+    const int64_t step = (int64_t)a.heads * size;
+    const int joins = (int)((len - 1) / a.seg);
+    for (int j = 0; j < joins; j += 8) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = j + i < joins ? p[i * step] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (j + i < joins) {
+                s = fmaf(s, gs, fmaf(s, gs_lo, v[i]));
+                p[i * step] = s;
+            }
+        p += 8 * step;
+    }
 }
 
 template <typename T>
@@ -103,19 +546,74 @@ __global__ __launch_bounds__(128) void k_step(StepArgs a) {
 
 }  // namespace
 
-size_t scan_workspace_bytes(const ScanArgs&) { return 16; }
+// Tokens of a segment, 0: sequences are scanned whole. Segments cost a second
+// pass over k and v and the states between them, so they are taken only where
+// whole sequences would leave most of the chip idle.
+static int64_t segment_of(const ScanArgs& a) {
+    const int64_t units = (int64_t)a.n * a.heads * a.n_roles;
+    if (units >= 512 || a.longest <= 256) return 0;
+    const int64_t want = 1024 / ((int64_t)a.heads * a.n_roles) + 1;  // slots
+    const int64_t seg = (a.tokens / want + C - 1) / C * C;
+    return std::max<int64_t>(seg, 128);
+}
 
-hipError_t launch_scan(const ScanArgs& a, hipStream_t s) {
-    int dk = 0, dv = 0;
-    for (int r = 0; r < a.n_roles; ++r) dk = std::max(dk, a.role[r].q.dim), dv = std::max(dv, a.role[r].v.dim);
-    const dim3 grid(a.n, a.heads, a.n_roles);
-    const size_t lds = (size_t)(dk * dv + 2 * dk) * 4;
-    auto f = a.dtype ? k_scan<bf16_t> : k_scan<float>;
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                       (int)lds);
-    if (e != hipSuccess) return e;
-    f<<<grid, 128, lds, s>>>(a);
+static int64_t slots_of(const ScanArgs& a, int64_t seg) { return seg ? a.n + a.tokens / seg : a.n; }
+
+size_t scan_workspace_bytes(const ScanArgs& a) {
+    const int64_t seg = segment_of(a);
+    return seg ? (size_t)a.n_roles * slots_of(a, seg) * a.heads * a.role[0].q.dim * a.role[0].v.dim * 4 : 16;
+}
+
+template <typename T, int D, int SLAB, bool WIDE, int PIECES>
+static hipError_t scan(const ScanArgs& a, hipStream_t s) {
+    const int group = a.group, inner = a.n_roles * group;
+    const int64_t rest = (a.slots * (a.heads / group) + 7) / 8, blocks = rest * 8 * inner;
+    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+    if (a.seg) {
+        k_scan<T, D, SLAB, WIDE, 3, true><<<(unsigned)blocks, 64 * D / SLAB, 0, s>>>(a);
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        const int size = a.role[0].q.dim * a.role[0].v.dim;
+        k_join_segments<<<dim3((size + 255) / 256, a.n * a.heads, a.n_roles), 256, 0, s>>>(a);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    k_scan<T, D, SLAB, WIDE, PIECES, false><<<(unsigned)blocks, 64 * D / SLAB, 0, s>>>(a);
     return hipGetLastError();
+}
+
+template <typename T, int D, int SLAB>
+static hipError_t scan_any(const ScanArgs& a, hipStream_t s) {
+    bool wide = true, state = false;
+    constexpr int V = 16 / sizeof(T);
+    for (int r = 0; r < a.n_roles; ++r) {
+        for (const HeadView* v : {&a.role[r].q, &a.role[r].k, &a.role[r].v})
+            wide = wide && (reinterpret_cast<uintptr_t>(v->p) & 15) == 0 && v->dim % V == 0 && v->token_stride % V == 0 &&
+                   v->head_stride % V == 0;
+        state = state || a.role[r].final_state;
+    }
+    if constexpr (sizeof(T) == 4) {
+        return wide ? scan<T, D, SLAB, true, 1>(a, s) : scan<T, D, SLAB, false, 1>(a, s);
+    } else {
+        if (state) return wide ? scan<T, D, SLAB, true, 3>(a, s) : scan<T, D, SLAB, false, 3>(a, s);
+        return wide ? scan<T, D, SLAB, true, 2>(a, s) : scan<T, D, SLAB, false, 2>(a, s);
+    }
+}
+
+hipError_t launch_scan(const ScanArgs& in, hipStream_t s) {
+    ScanArgs a = in;
+    a.seg = segment_of(a);
+    a.slots = slots_of(a, a.seg);
+    a.states = static_cast<float*>(a.ws);
+    const int d = std::max(a.role[0].q.dim, a.role[0].v.dim);
+    if (a.dtype) {
+        if (d <= 32) return scan_any<bf16_t, 32, 32>(a, s);
+        if (d <= 64) return scan_any<bf16_t, 64, 32>(a, s);
+        return scan_any<bf16_t, 128, 32>(a, s);
+    }
+    if (d <= 16) return scan_any<float, 16, 16>(a, s);
+    if (d <= 32) return scan_any<float, 32, 32>(a, s);
+    if (d <= 64) return scan_any<float, 64, 32>(a, s);
+    return scan_any<float, 128, 32>(a, s);
 }
 
 hipError_t launch_sum_heads(int64_t tokens, int kv_heads, int group, int dim, int dtype, const float* src, void* dst,

@@ -43,7 +43,12 @@ struct ScanArgs {
     const float* rates;
     int n_roles;
     ScanRole role[3];
+    int group;             // query heads of a key head
     void* ws;              // scan_workspace_bytes
+    // set by launch_scan: tokens of a segment (0: whole sequences), slots of
+    // segments or sequences, the states between segments [role][slot][head][q.dim][v.dim]
+    int64_t seg, slots;
+    float* states;
 };
 
 size_t scan_workspace_bytes(const ScanArgs& a);

@@ -100,6 +100,7 @@ mdl::ScanArgs scan_args(const mdlstm_attention_desc* d, int32_t n, int64_t token
     mdl::ScanArgs a{};
     a.n = n;
     a.heads = d->heads;
+    a.group = d->heads / d->kv_heads;
     a.dtype = d->dtype;
     a.tokens = tokens;
     a.longest = longest;

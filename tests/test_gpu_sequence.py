@@ -169,6 +169,38 @@ def test_attention_keeps_nan_in_its_example(dtype):
         assert not torch.isfinite(dv2[95, 0]).all()
 
 
+@pytest.mark.parametrize("dtype,d", [("f32", 16), ("f32", 64), ("bf16", 32), ("bf16", 128)])
+def test_attention_keeps_earlier_tokens_from_a_later_nan_value(dtype, d):
+    """A value that is not finite reaches its own column of the outputs, from its token on; as a key it is a value of
+    dq's scan, as a gradient of o one of dv's, which runs from the end."""
+    rng = np.random.default_rng(16)
+    lengths, heads, at = [45, 100], 2, 45 + 40
+    q, k, v = _qkv(rng, 145, heads, heads, d, d, dtype, "contiguous")
+    do, a = _rand(rng, 145, heads, d, dtype=dtype), _rates(rng, heads)
+    op = _seq().DecayAttention(lengths, heads, d, d, a, dtype=DT[dtype])
+    o = op.forward(q, k, v).clone()
+    dq, dk, dv = (g.clone() for g in op.backward(do))
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        v2, k2, do2 = v.clone(), k.clone(), do.clone()
+        for t in (v2, k2, do2):
+            t[at, 1, 5] = bad
+        o2 = op.forward(q, k, v2)
+        others = [c for c in range(d) if c != 5]
+        _check("before", o2[:at], _np(o[:at]), TOL[dtype])
+        _check("other columns", o2[:, :, others], _np(o[:, :, others]), TOL[dtype])
+        assert not torch.isfinite(o2[at:, 1, 5]).any()
+        op.forward(q, k2, v)
+        dq2 = op.backward(do)[0]
+        _check("before", dq2[:at], _np(dq[:at]), TOL[dtype])
+        _check("other columns", dq2[:, :, others], _np(dq[:, :, others]), TOL[dtype])
+        assert not torch.isfinite(dq2[at:, 1, 5]).any()
+        op.forward(q, k, v)
+        dv2 = op.backward(do2)[2]
+        _check("after", dv2[at + 1:], _np(dv[at + 1:]), TOL[dtype])
+        _check("other columns", dv2[:, :, others], _np(dv[:, :, others]), TOL[dtype])
+        assert not torch.isfinite(dv2[45:at + 1, 1, 5]).any()
+
+
 @pytest.mark.parametrize("dtype,dim", [("f32", 16), ("bf16", 128)])
 def test_attention_does_not_depend_on_its_neighbours(dtype, dim):
     """Examples packed together against each alone: the same up to the order of sums; twice the same call: the same bits."""
