@@ -148,43 +148,111 @@ __device__ __forceinline__ bool unit_of(const ScanArgs& a, Unit& u) {
 // A thread's share of a chunk's q, k or v rows, on its way from memory to LDS.
 template <typename T, int D, int THREADS, bool WIDE>
 struct Stage {
-    static constexpr int EPV = 16 / sizeof(T), VPR = D / EPV, N = C * VPR / THREADS;
+    static constexpr int EPV = 16 / sizeof(T), VPR = D / EPV, N = C * VPR / THREADS, STEP = THREADS / VPR;
     u32x4 v[N];
-    // rows 0 .. count - 1 of the chunk are tokens first, first + dir, ...; others and columns >= dim are zero
-    __device__ __forceinline__ void load(const T* base, int64_t token_stride, int dim, int64_t first, int dir, int count) {
+    // Rows row0 .. C - 1 of the chunk, row r at base + r stride (bytes); the rows before and columns >= dim are zero.
+    // WIDE: offsets within a chunk fit 32 bits.
+    __device__ __forceinline__ void load(const char* base, int64_t stride, int dim, int row0) {
+        const int first = threadIdx.x / VPR, col = threadIdx.x % VPR * EPV;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int x = threadIdx.x + i * THREADS, row = x / VPR, col = x % VPR * EPV;
-            const T* p = base + (first + (int64_t)dir * row) * token_stride + col;
+            const int row = first + i * STEP;
             v[i] = u32x4{0, 0, 0, 0};
-            if (row < count) {
-                if (WIDE) {
-                    if (col < dim) v[i] = *reinterpret_cast<const u32x4*>(p);
-                } else {
-                    T e[EPV];
+            if (WIDE) {
+                if (row >= row0 && col < dim)
+                    v[i] = *reinterpret_cast<const u32x4*>(base + (int)(row * (int)stride + col * (int)sizeof(T)));
+            } else if (row >= row0) {
+                const T* p = reinterpret_cast<const T*>(base + row * stride) + col;
+                T e[EPV];
 #pragma unroll
-                    for (int j = 0; j < EPV; ++j) e[j] = col + j < dim ? p[j] : T(0);
-                    __builtin_memcpy(&v[i], e, 16);
-                }
+                for (int j = 0; j < EPV; ++j) e[j] = col + j < dim ? p[j] : T(0);
+                __builtin_memcpy(&v[i], e, 16);
             }
         }
     }
     __device__ __forceinline__ void store(T* tile, int pitch) const {
+        T* p = tile + threadIdx.x / VPR * pitch + threadIdx.x % VPR * EPV;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int x = threadIdx.x + i * THREADS;
-            *reinterpret_cast<u32x4*>(tile + x / VPR * pitch + x % VPR * EPV) = v[i];
-        }
+        for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(p + i * STEP * pitch) = v[i];
     }
 };
 
+template <typename T>
+__device__ __forceinline__ void store4(T* d, int c, int dv, floatx4 o) {
+    if (dv % 4 == 0) {
+        if (c < dv) St<T>::st4(d, o);
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (c + r < dv) St<T>::st1(d + r, o[r]);
+    }
+}
+
+// Outputs of a wave that came out infinite or NaN, taken again one token at a
+// time: in a chunk's product a value that is not finite reaches the tokens
+// before it as 0 v = NaN. Finite outputs stay as they are.
+template <typename T, int KT, int NT, typename Init>
+__device__ __forceinline__ void scan_plain(const ScanArgs& a, const ScanRole& R, int head, int64_t t0, int64_t len, int64_t from,
+                                        int64_t to, int slab, Init init) {
+    const int l = threadIdx.x & 63, g = l >> 4, n = l & 15, dk = R.q.dim, dv = R.v.dim;
+    const float decay = expf(-a.rates[head]);
+    floatx4 S[KT][NT];
+    init(S);
+    for (int64_t pos = from; pos < to; ++pos) {
+        const int64_t t = R.reverse ? t0 + len - 1 - pos : t0 + pos;
+        const T *q = at<T>(R.q, t, head), *k = at<T>(R.k, t, head), *v = at<T>(R.v, t, head);
+        const float f = R.reverse && pos == 0 ? 1.0f : decay;
+        float o[NT], x[NT];
+#pragma unroll
+        for (int m = 0; m < NT; ++m) {
+            const int c = slab + 16 * m + n;
+            o[m] = 0.0f;
+            x[m] = c < dv ? St<T>::ld1(v + c) * R.in_scale : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < KT; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int row = 16 * i + 4 * g + r;
+                const float kr = row < dk ? St<T>::ld1(k + row) : 0.0f, qr = row < dk ? St<T>::ld1(q + row) : 0.0f;
+#pragma unroll
+                for (int m = 0; m < NT; ++m) {
+                    S[i][m][r] = row < dk ? fmaf(kr, x[m], S[i][m][r] * f) : 0.0f;
+                    o[m] = fmaf(qr, S[i][m][r], o[m]);
+                }
+            }
+#pragma unroll
+        for (int m = 0; m < NT; ++m) {
+            o[m] += __shfl_xor(o[m], 16);
+            o[m] += __shfl_xor(o[m], 32);
+            const int c = slab + 16 * m + n;
+            if (g == 0 && c < dv) {
+                const int64_t at_o = (t * a.heads + head) * dv + c;
+                if (R.out_f32) {
+                    float* d = static_cast<float*>(R.out) + at_o;
+                    if (!(*d - *d == 0.0f)) *d = o[m] * R.out_scale;
+                } else {
+                    T* d = static_cast<T*>(R.out) + at_o;
+                    const float was = St<T>::ld1(d);
+                    if (!(was - was == 0.0f)) St<T>::st1(d, o[m] * R.out_scale);
+                }
+            }
+        }
+    }
+}
+
 // WIDE: rows of q, k, v are whole 16-byte vectors. LOCAL: only the state that
 // a segment adds to zero, for all segments but a sequence's last.
+//
+// The scan's length need not be a multiple of C: its first chunk starts before
+// the first token, with rows of zeros, so that distances to a chunk's end are
+// the same in every chunk.
 template <typename T, int D, int SLAB, bool WIDE, int PIECES, bool LOCAL>
-__global__ __launch_bounds__(64 * D / SLAB) void k_scan(ScanArgs a) {
+__global__ __launch_bounds__(64 * D / SLAB, 2) void k_scan(ScanArgs a) {
     typedef Mx<T> M;
     typedef typename M::Frag Frag;
     constexpr int THREADS = 64 * D / SLAB, NT = SLAB / 16, KT = D / 16, PITCH = D + M::PAD, TPF = M::KB / 16;
+    constexpr int NP = sizeof(T) == 4 ? 1 : PIECES;
     __shared__ __align__(16) T lds[3 * C * PITCH];
     T *Q = lds, *K = lds + C * PITCH, *V = lds + 2 * C * PITCH;
     Unit u;
@@ -199,37 +267,42 @@ __global__ __launch_bounds__(64 * D / SLAB) void k_scan(ScanArgs a) {
     const int dk = R.q.dim, dv = R.v.dim, head = u.head, e = R.reverse;
     const float l2 = -1.4426950408889634f * a.rates[head];
 
-    // decays inside the chunk; a token j beyond i meets it with 0
-    const float ps = R.in_scale * R.out_scale;
-    float same[4], lower[4], late[2], w[2][4];
+    // decays inside a chunk; a token j beyond i meets it with 0
+    float same[4], lower[4], w[2][4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         const int i = n, j = 4 * g + r;
+        const float ps = R.in_scale * R.out_scale;
         same[r] = j <= i ? ps * power(l2, i - j) : 0.0f;
         lower[r] = ps * power(l2, 16 + i - j);
 #pragma unroll
         for (int h = 0; h < 2; ++h) w[h][r] = R.in_scale * power(l2, C - 1 - (16 * h + j) + e);
     }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) late[h] = R.out_scale * power(l2, 16 * h + n + 1 - e);
-    // g^C, in two parts where the state has to stand for itself: a rounded one
-    // would be off by the same 2^-24 every chunk
+    // what is left of the state before the chunk: at its tokens, and at its end,
+    // there in two parts where the state has to stand for itself: a rounded
+    // g^C would be off by the same 2^-24 every chunk
     constexpr bool EXACT = PIECES == 3 || sizeof(T) == 4;
-    float gc = power(l2, C), gc_lo = 0.0f;
-    if (EXACT) {
-        const double x = exp(-(double)a.rates[head] * C);
-        gc = (float)x;
-        gc_lo = (float)(x - (double)gc);
-    }
+    const int skip = (int)(-(to - from) & (C - 1));  // rows of zeros in the first chunk
+    float late[2], gc, gc_lo = 0.0f;
+    auto decays = [&](int skip) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) late[h] = R.out_scale * power(l2, max(16 * h + n - skip, 0) + 1 - e);
+        gc = power(l2, C - skip);
+        if (EXACT) {
+            const double x = exp(-(double)a.rates[head] * (C - skip));
+            if (skip < C) gc = (float)x, gc_lo = (float)(x - (double)gc);
+        }
+    };
+    decays(skip);
 
-    floatx4 S[KT][NT];  // S[t][m][r] = state[16 t + 4 g + r][slab + 16 m + n]
-    {
+    auto init = [&](floatx4 (&S)[KT][NT]) {
         const float* from_state = nullptr;
         const int64_t size = (int64_t)dk * dv;
         bool transposed = false;
-        if (u.j > 0)  // the slot before holds the state that this segment starts from
-            from_state = LOCAL ? nullptr : a.states + (((int64_t)u.role * a.slots + u.slot - 1) * a.heads + head) * size;
-        else if (!LOCAL && R.state) {
+        if (LOCAL) {
+        } else if (u.j > 0) {  // the slot before holds the state that this segment starts from
+            from_state = a.states + (((int64_t)u.role * a.slots + u.slot - 1) * a.heads + head) * size;
+        } else if (R.state) {
             from_state = R.state + ((int64_t)u.seq * a.heads + head) * size;
             transposed = R.state_t;
         }
@@ -242,176 +315,112 @@ __global__ __launch_bounds__(64 * D / SLAB) void k_scan(ScanArgs a) {
                     const int i = 16 * t + 4 * g + r, c = slab + 16 * m + n;
                     S[t][m][r] = from_state && i < dk && c < dv ? from_state[transposed ? c * dk + i : i * dv + c] : 0.0f;
                 }
-    }
-
-    const T* qp = at<T>(R.q, 0, head);
-    const T* kp = at<T>(R.k, 0, head);
-    const T* vp = at<T>(R.v, 0, head);
-    const int dir = R.reverse ? -1 : 1;
-    const int64_t first = R.reverse ? t0 + len - 1 : t0;  // token at scan position 0
-    Stage<T, D, THREADS, WIDE> sq, sk, sv;
-    auto fetch = [&](int64_t pos) {
-        const int count = (int)min((int64_t)C, to - pos);
-        if (!LOCAL) sq.load(qp, R.q.token_stride, dk, first + dir * pos, dir, count);
-        sk.load(kp, R.k.token_stride, dk, first + dir * pos, dir, count);
-        sv.load(vp, R.v.token_stride, dv, first + dir * pos, dir, count);
     };
-    if (from < to) fetch(from);
-    for (int64_t pos = from; pos < to; pos += C) {
-        const int count = (int)min((int64_t)C, to - pos);
+    floatx4 S[KT][NT];  // S[t][m][r] = state[16 t + 4 g + r][slab + 16 m + n]
+    init(S);
+
+    // bytes between rows and from a chunk to the next; the chunk's row 0 is scan position pos
+    const int dir = R.reverse ? -1 : 1;
+    const int64_t first = (R.reverse ? t0 + len - 1 : t0) + dir * (from - skip);
+    const int64_t qs = dir * R.q.token_stride * (int64_t)sizeof(T), ks = dir * R.k.token_stride * (int64_t)sizeof(T),
+                  vs = dir * R.v.token_stride * (int64_t)sizeof(T);
+    const char* qp = reinterpret_cast<const char*>(at<T>(R.q, 0, head)) + first * dir * qs;
+    const char* kp = reinterpret_cast<const char*>(at<T>(R.k, 0, head)) + first * dir * ks;
+    const char* vp = reinterpret_cast<const char*>(at<T>(R.v, 0, head)) + first * dir * vs;
+    const int os = dir * a.heads * dv;  // elements between output rows
+    int64_t out = (first * a.heads + head) * dv;
+    Stage<T, D, THREADS, WIDE> sq, sk, sv;
+    auto fetch = [&](int skip) {
+        if (!LOCAL) sq.load(qp, qs, dk, skip);
+        sk.load(kp, ks, dk, skip);
+        sv.load(vp, vs, dv, skip);
+        qp += C * qs;
+        kp += C * ks;
+        vp += C * vs;
+    };
+    const int chunks = (int)((to - from + C - 1) / C);
+    float bad = 0.0f;  // NaN once an output was not finite
+    if (chunks > 0) fetch(skip);
+    for (int chunk = 0; chunk < chunks; ++chunk) {
         if (!LOCAL) sq.store(Q, PITCH);
         sk.store(K, PITCH);
         sv.store(V, PITCH);
         lds_barrier();
-        if (pos + C < to) fetch(pos + C);
-        if (count < C) {  // the sequence's last chunk
-            gc = power(l2, count);
-            if (EXACT) {
-                const double x = exp(-(double)a.rates[head] * count);
-                gc = (float)x;
-                gc_lo = (float)(x - (double)gc);
-            }
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int j = 16 * h + 4 * g + r;
-                    w[h][r] = j < count ? R.in_scale * power(l2, count - 1 - j + e) : 0.0f;
-                }
-        }
+        if (chunk + 1 < chunks) fetch(0);
         Frag vf[NT][2 / TPF];
 #pragma unroll
         for (int m = 0; m < NT; ++m)
 #pragma unroll
             for (int h = 0; h < 2 / TPF; ++h) vf[m][h] = M::down(V, PITCH, h * M::KB, slab + 16 * m, g, n);
         if (!LOCAL) {
-            floatx4 o[NT][2], p[3];  // p: (j tile, i tile) (0, 0), (0, 1), (1, 1)
             const floatx4 zero = {0, 0, 0, 0};
-            auto state_part = [&](bool scores) {
+            floatx4 o[NT][2], p[3] = {zero, zero, zero};  // p: (j tile, i tile) (0, 0), (0, 1), (1, 1)
 #pragma unroll
-                for (int m = 0; m < NT; ++m) o[m][0] = o[m][1] = zero;
+            for (int m = 0; m < NT; ++m) o[m][0] = o[m][1] = zero;
 #pragma unroll
-                for (int k = 0; k < D / M::KB; ++k) {
-                    const Frag q0 = M::along(Q, PITCH, n, k * M::KB, g), q1 = M::along(Q, PITCH, 16 + n, k * M::KB, g);
-                    if (scores) {
-                        const Frag k0 = M::along(K, PITCH, n, k * M::KB, g), k1 = M::along(K, PITCH, 16 + n, k * M::KB, g);
-                        p[0] = M::mma(k0, q0, p[0]);
-                        p[1] = M::mma(k0, q1, p[1]);
-                        p[2] = M::mma(k1, q1, p[2]);
-                    }
+            for (int k = 0; k < D / M::KB; ++k) {
+                const Frag q0 = M::along(Q, PITCH, n, k * M::KB, g), q1 = M::along(Q, PITCH, 16 + n, k * M::KB, g);
+                const Frag k0 = M::along(K, PITCH, n, k * M::KB, g), k1 = M::along(K, PITCH, 16 + n, k * M::KB, g);
+                p[0] = M::mma(k0, q0, p[0]);
+                p[1] = M::mma(k0, q1, p[1]);
+                p[2] = M::mma(k1, q1, p[2]);
 #pragma unroll
-                    for (int m = 0; m < NT; ++m) {
-                        floatx4 t[TPF];
+                for (int m = 0; m < NT; ++m) {
+                    floatx4 t[TPF];
 #pragma unroll
-                        for (int x = 0; x < TPF; ++x) t[x] = S[k * TPF + x][m];
-                        const Frag s = M::from(t);
-                        o[m][0] = M::mma(s, q0, o[m][0]);
-                        o[m][1] = M::mma(s, q1, o[m][1]);
-                    }
+                    for (int x = 0; x < TPF; ++x) t[x] = S[k * TPF + x][m];
+                    const Frag s = M::from(t);
+                    o[m][0] = M::mma(s, q0, o[m][0]);
+                    o[m][1] = M::mma(s, q1, o[m][1]);
                 }
+            }
 #pragma unroll
-                for (int m = 0; m < NT; ++m) o[m][0] *= late[0], o[m][1] *= late[1];
-            };
-            p[0] = p[1] = p[2] = zero;
-            state_part(true);
+            for (int m = 0; m < NT; ++m) o[m][0] *= late[0], o[m][1] *= late[1];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {  // a select: what lies beyond i may be infinite
                 p[0][r] = 4 * g + r <= n ? p[0][r] * same[r] : 0.0f;
                 p[2][r] = 4 * g + r <= n ? p[2][r] * same[r] : 0.0f;
                 p[1][r] *= lower[r];
             }
-            {
-                const floatx4 b0[2] = {p[0], zero}, b1[2] = {p[1], p[2]};
+            const floatx4 b0[2] = {p[0], zero}, b1[2] = {p[1], p[2]};
 #pragma unroll
-                for (int h = 0; h < 2 / TPF; ++h) {
-                    const Frag f0 = M::from(b0 + h), f1 = M::from(b1 + h);
+            for (int h = 0; h < 2 / TPF; ++h) {
+                const Frag f0 = M::from(b0 + h), f1 = M::from(b1 + h);
 #pragma unroll
-                    for (int m = 0; m < NT; ++m) {
-                        if (h == 0) o[m][0] = M::mma(vf[m][h], f0, o[m][0]);
-                        o[m][1] = M::mma(vf[m][h], f1, o[m][1]);
-                    }
+                for (int m = 0; m < NT; ++m) {
+                    if (h == 0) o[m][0] = M::mma(vf[m][h], f0, o[m][0]);
+                    o[m][1] = M::mma(vf[m][h], f1, o[m][1]);
                 }
             }
-            // A v_j that is not finite reaches tokens before it as 0 v_j = NaN: their
-            // sums are taken again without it.
-            float bad = 0.0f;
-#pragma unroll
-            for (int m = 0; m < NT; ++m)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) bad = fmaf(o[m][0][r], 0.0f, fmaf(o[m][1][r], 0.0f, bad));
-            if (__any(bad != bad)) {
-                floatx4 was[NT][2];
-#pragma unroll
-                for (int m = 0; m < NT; ++m) was[m][0] = o[m][0], was[m][1] = o[m][1];
-                state_part(false);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int i = 16 * h + n;
-#pragma nounroll
-                    for (int j = 0; j <= i; ++j) {
-                        float s = 0.0f;
-#pragma nounroll
-                        for (int k = 0; k < dk; ++k) s = fmaf(St<T>::ld1(Q + i * PITCH + k), St<T>::ld1(K + j * PITCH + k), s);
-                        s *= ps * power(l2, i - j);
-#pragma unroll
-                        for (int m = 0; m < NT; ++m)
-#pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                o[m][h][r] = fmaf(s, St<T>::ld1(V + j * PITCH + slab + 16 * m + 4 * g + r), o[m][h][r]);
-                    }
-                }
-#pragma unroll
-                for (int m = 0; m < NT; ++m)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (was[m][h][r] - was[m][h][r] == 0.0f) o[m][h][r] = was[m][h][r];
-            }
+            const int row0 = chunk == 0 ? skip : 0;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int i = 16 * h + n;
-                if (i < count) {
-                    const int64_t row = ((first + dir * (pos + i)) * a.heads + head) * dv;
 #pragma unroll
-                    for (int m = 0; m < NT; ++m) {
-                        const int c = slab + 16 * m + 4 * g;
-                        if (R.out_f32) {
-                            float* d = static_cast<float*>(R.out) + row + c;
-                            if (dv % 4 == 0) {
-                                if (c < dv) St<float>::st4(d, o[m][h]);
-                            } else {
+                for (int m = 0; m < NT; ++m) {
 #pragma unroll
-                                for (int r = 0; r < 4; ++r)
-                                    if (c + r < dv) d[r] = o[m][h][r];
-                            }
-                        } else {
-                            T* d = static_cast<T*>(R.out) + row + c;
-                            if (dv % 4 == 0) {
-                                if (c < dv) St<T>::st4(d, o[m][h]);
-                            } else {
-#pragma unroll
-                                for (int r = 0; r < 4; ++r)
-                                    if (c + r < dv) St<T>::st1(d + r, o[m][h][r]);
-                            }
-                        }
+                    for (int r = 0; r < 4; ++r) bad = fmaf(o[m][h][r], 0.0f, bad);
+                    const int c = slab + 16 * m + 4 * g;
+                    if (i >= row0) {
+                        if (R.out_f32)
+                            store4(static_cast<float*>(R.out) + out + (i * os + c), c, dv, o[m][h]);
+                        else
+                            store4(static_cast<T*>(R.out) + out + (i * os + c), c, dv, o[m][h]);
                     }
                 }
             }
+            out += (int64_t)C * os;
         }
         // S = g^C S + K^T (w V)
 #pragma unroll
         for (int t = 0; t < KT; ++t)
 #pragma unroll
-            for (int m = 0; m < NT; ++m) {
-                if (EXACT) {
+            for (int m = 0; m < NT; ++m)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) S[t][m][r] = fmaf(S[t][m][r], gc, S[t][m][r] * gc_lo);
-                } else {
-                    S[t][m] *= gc;
-                }
-            }
-        Frag wv[NT][2 / TPF][sizeof(T) == 4 ? 1 : PIECES];
+                for (int r = 0; r < 4; ++r)
+                    S[t][m][r] = EXACT ? fmaf(S[t][m][r], gc, S[t][m][r] * gc_lo) : S[t][m][r] * gc;
+        if (chunk == 0) decays(0);
+        Frag wv[NT][2 / TPF][NP];
 #pragma unroll
         for (int m = 0; m < NT; ++m) {
             if constexpr (sizeof(T) == 4) {
@@ -426,9 +435,9 @@ __global__ __launch_bounds__(64 * D / SLAB) void k_scan(ScanArgs a) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) x[h][r] = (float)vf[m][0][4 * h + r] * w[h][r];
 #pragma unroll
-                for (int c = 0; c < PIECES; ++c) {
+                for (int c = 0; c < NP; ++c) {
                     wv[m][0][c] = M::from(x);
-                    if (c + 1 < PIECES)
+                    if (c + 1 < NP)
 #pragma unroll
                         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -444,7 +453,7 @@ __global__ __launch_bounds__(64 * D / SLAB) void k_scan(ScanArgs a) {
 #pragma unroll
                 for (int m = 0; m < NT; ++m)
 #pragma unroll
-                    for (int c = (sizeof(T) == 4 ? 1 : PIECES) - 1; c >= 0; --c) S[t][m] = M::mma(kt, wv[m][h][c], S[t][m]);
+                    for (int c = NP - 1; c >= 0; --c) S[t][m] = M::mma(kt, wv[m][h][c], S[t][m]);
             }
         lds_barrier();
     }
@@ -468,6 +477,10 @@ __global__ __launch_bounds__(64 * D / SLAB) void k_scan(ScanArgs a) {
                     const int i = 16 * t + 4 * g + r, c = slab + 16 * m + n;
                     if (i < dk && c < dv) to_state[transposed ? c * dk + i : i * dv + c] = S[t][m][r];
                 }
+    }
+    if (!LOCAL && __any(bad != bad)) {
+        __threadfence_block();  // the outputs as written
+        scan_plain<T, KT, NT>(a, R, head, t0, len, from, to, slab, init);
     }
 }
 
@@ -588,7 +601,7 @@ static hipError_t scan_any(const ScanArgs& a, hipStream_t s) {
     for (int r = 0; r < a.n_roles; ++r) {
         for (const HeadView* v : {&a.role[r].q, &a.role[r].k, &a.role[r].v})
             wide = wide && (reinterpret_cast<uintptr_t>(v->p) & 15) == 0 && v->dim % V == 0 && v->token_stride % V == 0 &&
-                   v->head_stride % V == 0;
+                   v->head_stride % V == 0 && v->token_stride < (1 << 22);
         state = state || a.role[r].final_state;
     }
     if constexpr (sizeof(T) == 4) {
