@@ -45,6 +45,7 @@ __device__ __forceinline__ void sequence(const int64_t* offsets, int i, int64_t 
 // accumulators.
 // ---------------------------------------------------------------------------
 constexpr int C = 32;
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 template <typename T>
 struct Mx;
@@ -145,28 +146,50 @@ __device__ __forceinline__ bool unit_of(const ScanArgs& a, Unit& u) {
     return true;
 }
 
-// A thread's share of a chunk's q, k or v rows, on its way from memory to LDS.
+// 32 rows of a tensor as a buffer: row r of a chunk lies r `stride` bytes from
+// its row 0, backwards in a scan from the end. Offsets count from the row at
+// the lowest address; OUT is outside the buffer: such loads give 0 and such
+// stores write nothing, without a branch.
+constexpr int OUT = 0x7fffffff;
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ __forceinline__ Buffer buffer(const char* row_0, int64_t stride) {
+    const char* p = stride < 0 ? row_0 + (C - 1) * stride : row_0;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, 0x7ffffff0, 0x00027000);
+}
+__device__ __forceinline__ int row_offset(int row, int stride) { return stride < 0 ? (row - (C - 1)) * stride : row * stride; }
+
+// A thread's share of a chunk's q, k or v rows, on its way from memory to LDS:
+// rows first, first + STEP, ... of it, 16 bytes each. Rows before row0 and
+// columns from dim on are zero. WIDE: rows are whole aligned 16-byte vectors
+// and a chunk spans less than 2^31 bytes.
 template <typename T, int D, int THREADS, bool WIDE>
 struct Stage {
     static constexpr int EPV = 16 / sizeof(T), VPR = D / EPV, N = C * VPR / THREADS, STEP = THREADS / VPR;
     u32x4 v[N];
-    // Rows row0 .. C - 1 of the chunk, row r at base + r stride (bytes); the rows before and columns >= dim are zero.
-    // WIDE: offsets within a chunk fit 32 bits.
+    int offset;  // of the first vector
+    __device__ __forceinline__ void init(int64_t stride, int dim) {
+        const int first = threadIdx.x / VPR, col = threadIdx.x % VPR * EPV;
+        offset = col < dim ? row_offset(first, (int)stride) + col * (int)sizeof(T) : OUT;
+    }
     __device__ __forceinline__ void load(const char* base, int64_t stride, int dim, int row0) {
         const int first = threadIdx.x / VPR, col = threadIdx.x % VPR * EPV;
+        if constexpr (WIDE) {
+            const Buffer b = buffer(base, stride);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int row = first + i * STEP;
-            v[i] = u32x4{0, 0, 0, 0};
-            if (WIDE) {
-                if (row >= row0 && col < dim)
-                    v[i] = *reinterpret_cast<const u32x4*>(base + (int)(row * (int)stride + col * (int)sizeof(T)));
-            } else if (row >= row0) {
-                const T* p = reinterpret_cast<const T*>(base + row * stride) + col;
-                T e[EPV];
+            for (int i = 0; i < N; ++i)
+                v[i] = __builtin_amdgcn_raw_buffer_load_b128(
+                    b, first + i * STEP >= row0 && offset != OUT ? offset + i * STEP * (int)stride : OUT, 0, 0);
+        } else {
 #pragma unroll
-                for (int j = 0; j < EPV; ++j) e[j] = col + j < dim ? p[j] : T(0);
-                __builtin_memcpy(&v[i], e, 16);
+            for (int i = 0; i < N; ++i) {
+                v[i] = u32x4{0, 0, 0, 0};
+                if (first + i * STEP >= row0) {
+                    const T* p = reinterpret_cast<const T*>(base + (first + i * STEP) * stride) + col;
+                    T e[EPV];
+#pragma unroll
+                    for (int j = 0; j < EPV; ++j) e[j] = col + j < dim ? p[j] : T(0);
+                    __builtin_memcpy(&v[i], e, 16);
+                }
             }
         }
     }
@@ -177,16 +200,13 @@ struct Stage {
     }
 };
 
-template <typename T>
-__device__ __forceinline__ void store4(T* d, int c, int dv, floatx4 o) {
-    if (dv % 4 == 0) {
-        if (c < dv) St<T>::st4(d, o);
-    } else {
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if (c + r < dv) St<T>::st1(d + r, o[r]);
-    }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 |
+                     (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
 }
+
+// Keeps a value in its register where the compiler would rather compute it again.
+__device__ __forceinline__ void keep(float& x) { asm volatile("" : "+v"(x)); }
 
 // Outputs of a wave that came out infinite or NaN, taken again one token at a
 // time: in a chunk's product a value that is not finite reaches the tokens
@@ -248,24 +268,26 @@ __device__ __forceinline__ void scan_plain(const ScanArgs& a, const ScanRole& R,
 // the first token, with rows of zeros, so that distances to a chunk's end are
 // the same in every chunk.
 template <typename T, int D, int SLAB, bool WIDE, int PIECES, bool LOCAL>
-__global__ __launch_bounds__(64 * D / SLAB, 2) void k_scan(ScanArgs a) {
+__global__ __launch_bounds__(64 * D / SLAB, SLAB == 16 ? 4 : 2) void k_scan(ScanArgs a) {
     typedef Mx<T> M;
     typedef typename M::Frag Frag;
     constexpr int THREADS = 64 * D / SLAB, NT = SLAB / 16, KT = D / 16, PITCH = D + M::PAD, TPF = M::KB / 16;
     constexpr int NP = sizeof(T) == 4 ? 1 : PIECES;
-    __shared__ __align__(16) T lds[3 * C * PITCH];
-    T *Q = lds, *K = lds + C * PITCH, *V = lds + 2 * C * PITCH;
+    constexpr int BUF = 3 * C * PITCH, BUFS = 2 * BUF * sizeof(T) <= 53 * 1024 ? 2 : 1;
+    __shared__ __align__(16) T lds[BUFS * BUF];
     Unit u;
     if (!unit_of(a, u)) return;
     const ScanRole& R = a.role[u.role];
     int64_t t0, len;
     sequence(a.offsets, u.seq, a.tokens, a.longest, t0, len);
+    t0 = uniform(t0);
+    len = uniform(len);
     const int64_t from = u.j * a.seg, to = a.seg ? min(len, from + a.seg) : len;
     if (u.j > 0 && from >= len) return;
     if (LOCAL && to >= len) return;
     const int l = threadIdx.x & 63, g = l >> 4, n = l & 15, slab = (threadIdx.x >> 6) * SLAB;
     const int dk = R.q.dim, dv = R.v.dim, head = u.head, e = R.reverse;
-    const float l2 = -1.4426950408889634f * a.rates[head];
+    const float l2 = -1.4426950408889634f * a.rates[head];  // log2 g
 
     // decays inside a chunk; a token j beyond i meets it with 0
     float same[4], lower[4], w[2][4];
@@ -278,22 +300,27 @@ __global__ __launch_bounds__(64 * D / SLAB, 2) void k_scan(ScanArgs a) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) w[h][r] = R.in_scale * power(l2, C - 1 - (16 * h + j) + e);
     }
-    // what is left of the state before the chunk: at its tokens, and at its end,
-    // there in two parts where the state has to stand for itself: a rounded
-    // g^C would be off by the same 2^-24 every chunk
-    constexpr bool EXACT = PIECES == 3 || sizeof(T) == 4;
-    const int skip = (int)(-(to - from) & (C - 1));  // rows of zeros in the first chunk
-    float late[2], gc, gc_lo = 0.0f;
-    auto decays = [&](int skip) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) late[h] = R.out_scale * power(l2, max(16 * h + n - skip, 0) + 1 - e);
-        gc = power(l2, C - skip);
-        if (EXACT) {
-            const double x = exp(-(double)a.rates[head] * (C - skip));
-            if (skip < C) gc = (float)x, gc_lo = (float)(x - (double)gc);
-        }
-    };
-    decays(skip);
+    for (int r = 0; r < 4; ++r) {
+        keep(same[r]);
+        keep(lower[r]);
+        keep(w[0][r]);
+        keep(w[1][r]);
+    }
+    // The state in registers is S / g^age: what it has decayed by since it was
+    // last scaled is left out until that reaches 2^-8 (64 multiplications a chunk
+    // less; beyond, exponents would cost precision). late: weight of the registers' state at the
+    // chunk's tokens.
+    const int skip = (int)(-(to - from) & (C - 1));  // rows of zeros in the first chunk
+    const int oldest = __builtin_amdgcn_readfirstlane((int)fminf(8.0f / fabsf(l2), 1e9f));
+    int age = 0;
+    float full[2], late[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        full[h] = R.out_scale * power(l2, 16 * h + n + 1 - e);
+        late[h] = R.out_scale * power(l2, max(16 * h + n - skip, 0) + 1 - e);
+        keep(full[h]);
+    }
 
     auto init = [&](floatx4 (&S)[KT][NT]) {
         const float* from_state = nullptr;
@@ -327,9 +354,13 @@ __global__ __launch_bounds__(64 * D / SLAB, 2) void k_scan(ScanArgs a) {
     const char* qp = reinterpret_cast<const char*>(at<T>(R.q, 0, head)) + first * dir * qs;
     const char* kp = reinterpret_cast<const char*>(at<T>(R.k, 0, head)) + first * dir * ks;
     const char* vp = reinterpret_cast<const char*>(at<T>(R.v, 0, head)) + first * dir * vs;
-    const int os = dir * a.heads * dv;  // elements between output rows
-    int64_t out = (first * a.heads + head) * dv;
+    const bool f32 = sizeof(T) == 4 || R.out_f32;
+    const int osize = f32 ? 4 : (int)sizeof(T), os = dir * a.heads * dv * osize;  // bytes between output rows
+    char* out = static_cast<char*>(R.out) + (first * a.heads + head) * dv * osize;
     Stage<T, D, THREADS, WIDE> sq, sk, sv;
+    if (!LOCAL) sq.init(qs, dk);
+    sk.init(ks, dk);
+    sv.init(vs, dv);
     auto fetch = [&](int skip) {
         if (!LOCAL) sq.load(qp, qs, dk, skip);
         sk.load(kp, ks, dk, skip);
@@ -338,23 +369,32 @@ __global__ __launch_bounds__(64 * D / SLAB, 2) void k_scan(ScanArgs a) {
         kp += C * ks;
         vp += C * vs;
     };
+    auto put = [&](T* buf) {
+        if (!LOCAL) sq.store(buf, PITCH);
+        sk.store(buf + C * PITCH, PITCH);
+        sv.store(buf + 2 * C * PITCH, PITCH);
+    };
     const int chunks = (int)((to - from + C - 1) / C);
-    float bad = 0.0f;  // NaN once an output was not finite
-    if (chunks > 0) fetch(skip);
+    floatx4 bad = {0, 0, 0, 0};  // NaN once a value was not finite
+    int row0 = skip;
+    if (chunks > 0) {
+        fetch(skip);
+        put(lds);
+    }
     for (int chunk = 0; chunk < chunks; ++chunk) {
-        if (!LOCAL) sq.store(Q, PITCH);
-        sk.store(K, PITCH);
-        sv.store(V, PITCH);
-        lds_barrier();
+        const T* Q = lds + (BUFS == 2 ? (chunk & 1) * BUF : 0);
+        const T *K = Q + C * PITCH, *V = K + C * PITCH;
+        lds_barrier();  // this chunk's rows are there; with two buffers no wave reads the other one any more
         if (chunk + 1 < chunks) fetch(0);
         Frag vf[NT][2 / TPF];
 #pragma unroll
         for (int m = 0; m < NT; ++m)
 #pragma unroll
             for (int h = 0; h < 2 / TPF; ++h) vf[m][h] = M::down(V, PITCH, h * M::KB, slab + 16 * m, g, n);
+        floatx4 o[NT][2];
         if (!LOCAL) {
             const floatx4 zero = {0, 0, 0, 0};
-            floatx4 o[NT][2], p[3] = {zero, zero, zero};  // p: (j tile, i tile) (0, 0), (0, 1), (1, 1)
+            floatx4 p[3] = {zero, zero, zero};  // (j tile, i tile) (0, 0), (0, 1), (1, 1)
 #pragma unroll
             for (int m = 0; m < NT; ++m) o[m][0] = o[m][1] = zero;
 #pragma unroll
@@ -392,34 +432,36 @@ __global__ __launch_bounds__(64 * D / SLAB, 2) void k_scan(ScanArgs a) {
                     o[m][1] = M::mma(vf[m][h], f1, o[m][1]);
                 }
             }
-            const int row0 = chunk == 0 ? skip : 0;
+            // A value that is not finite reaches the tokens before it as 0 v = NaN.
+            if constexpr (sizeof(T) == 2) {
+                const Frag none = {};
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int i = 16 * h + n;
+                for (int m = 0; m < NT; ++m) bad = M::mma(vf[m][0], none, bad);
+            } else {
 #pragma unroll
-                for (int m = 0; m < NT; ++m) {
+                for (int m = 0; m < NT; ++m)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) bad = fmaf(o[m][h][r], 0.0f, bad);
-                    const int c = slab + 16 * m + 4 * g;
-                    if (i >= row0) {
-                        if (R.out_f32)
-                            store4(static_cast<float*>(R.out) + out + (i * os + c), c, dv, o[m][h]);
-                        else
-                            store4(static_cast<T*>(R.out) + out + (i * os + c), c, dv, o[m][h]);
-                    }
-                }
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) bad[r] = fmaf(vf[m][h][r], 0.0f, bad[r]);
             }
-            out += (int64_t)C * os;
         }
         // S = g^C S + K^T (w V)
+        const int length = C - row0;
+        float fresh = 1.0f;
+        age += length;
+        if (age > oldest) {
+            const float f = power(l2, age);
 #pragma unroll
-        for (int t = 0; t < KT; ++t)
+            for (int t = 0; t < KT; ++t)
 #pragma unroll
-            for (int m = 0; m < NT; ++m)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    S[t][m][r] = EXACT ? fmaf(S[t][m][r], gc, S[t][m][r] * gc_lo) : S[t][m][r] * gc;
-        if (chunk == 0) decays(0);
+                for (int m = 0; m < NT; ++m) S[t][m] *= f;
+            age = 0;
+        } else {
+            fresh = __builtin_amdgcn_exp2f(-l2 * (float)age);
+        }
+        late[0] = full[0] * power(l2, age);
+        late[1] = full[1] * power(l2, age);
         Frag wv[NT][2 / TPF][NP];
 #pragma unroll
         for (int m = 0; m < NT; ++m) {
@@ -427,13 +469,13 @@ __global__ __launch_bounds__(64 * D / SLAB, 2) void k_scan(ScanArgs a) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) wv[m][h][0][r] = vf[m][h][r] * w[h][r];
+                    for (int r = 0; r < 4; ++r) wv[m][h][0][r] = vf[m][h][r] * (w[h][r] * fresh);
             } else {
                 floatx4 x[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) x[h][r] = (float)vf[m][0][4 * h + r] * w[h][r];
+                    for (int r = 0; r < 4; ++r) x[h][r] = (float)vf[m][0][4 * h + r] * (w[h][r] * fresh);
 #pragma unroll
                 for (int c = 0; c < NP; ++c) {
                     wv[m][0][c] = M::from(x);
@@ -455,7 +497,49 @@ __global__ __launch_bounds__(64 * D / SLAB, 2) void k_scan(ScanArgs a) {
 #pragma unroll
                     for (int c = NP - 1; c >= 0; --c) S[t][m] = M::mma(kt, wv[m][h][c], S[t][m]);
             }
-        lds_barrier();
+        // the next chunk's rows before the outputs: a wait for them would wait for those too
+        if (BUFS == 1) lds_barrier();
+        if (chunk + 1 < chunks) put(lds + (BUFS == 2 ? ((chunk + 1) & 1) * BUF : 0));
+        if (!LOCAL) {
+            const Buffer to_out = buffer(out, os);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int i = 16 * h + n;
+#pragma unroll
+                for (int m = 0; m < NT; ++m) {
+                    const int c = slab + 16 * m + 4 * g;
+                    if (WIDE) {
+                        const int at = i >= row0 && c < dv ? row_offset(i, os) + c * osize : OUT;
+                        if (f32) {
+                            u32x4 x;
+                            __builtin_memcpy(&x, &o[m][h], 16);
+                            __builtin_amdgcn_raw_buffer_store_b128(x, to_out, at, 0, 0);
+                        } else {
+                            __builtin_amdgcn_raw_buffer_store_b64(u32x2{f2bf2(o[m][h][0], o[m][h][1]), f2bf2(o[m][h][2], o[m][h][3])},
+                                                                  to_out, at, 0, 0);
+                        }
+                    } else if (i >= row0) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (c + r < dv) {
+                                if (f32)
+                                    reinterpret_cast<float*>(out + i * os)[c + r] = o[m][h][r];
+                                else
+                                    St<T>::st1(reinterpret_cast<T*>(out + i * os) + c + r, o[m][h][r]);
+                            }
+                    }
+                }
+            }
+            out += (int64_t)C * os;
+        }
+        row0 = 0;
+    }
+    {
+        const float f = power(l2, age);
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int m = 0; m < NT; ++m) S[t][m] *= f;
     }
 
     const int64_t size = (int64_t)dk * dv;
@@ -478,7 +562,7 @@ __global__ __launch_bounds__(64 * D / SLAB, 2) void k_scan(ScanArgs a) {
                     if (i < dk && c < dv) to_state[transposed ? c * dk + i : i * dv + c] = S[t][m][r];
                 }
     }
-    if (!LOCAL && __any(bad != bad)) {
+    if (!LOCAL && __any(bad[0] + bad[1] + bad[2] + bad[3] != 0.0f)) {
         __threadfence_block();  // the outputs as written
         scan_plain<T, KT, NT>(a, R, head, t0, len, from, to, slab, init);
     }

@@ -33,7 +33,7 @@ mdlstm_status fail(mdlstm_status st, const char* fmt, ...) {
         if (_st != MDLSTM_OK) return _st;         \
     } while (0)
 
-constexpr int64_t kMaxTokens = (int64_t)1 << 40;  // products with a dimension or a head count stay within int64
+constexpr int64_t kMaxTokens = (int64_t)1 << 35;  // products with a dimension or a head count stay within int64
 constexpr int64_t kMaxStride = (int64_t)1 << 62;
 
 size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
