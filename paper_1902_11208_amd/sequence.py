@@ -17,48 +17,61 @@ import numpy as np
 import torch
 
 from ._lib import AttentionDesc, Heads, NormDesc, check, lib
-from .api import _ptr, _stream, check_tensor, dtype_code
+from .api import _ptr, check_tensor, dtype_code
 
 FP8 = torch.float8_e4m3fn
+_raw_stream = torch._C._cuda_getCurrentRawStream  # the handle without a Stream object: these calls are short
+
+
+def _stream(stream, device) -> int:
+    return _raw_stream(device.index) if stream is None else stream.cuda_stream
+
+
+def _matches(t, name: str, shape, dtype: torch.dtype, device) -> None:
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} must be a torch.Tensor")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
 
 
 def _heads(t, name: str, tokens: int, heads: int, dim: int, dtype: torch.dtype, device) -> Heads:
     """A [tokens, heads, dim] tensor, possibly a view with a contiguous last dimension, as the C ABI takes it."""
-    if not isinstance(t, torch.Tensor):
-        raise ValueError(f"{name} must be a torch.Tensor")
-    if t.shape != (tokens, heads, dim):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(tokens, heads, dim)}")
-    if t.dtype != dtype:
-        raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    _matches(t, name, (tokens, heads, dim), dtype, device)
     st, sh, sd = t.stride()
     if sd != 1 and dim > 1 and t.numel():
         raise ValueError(f"{name} must be contiguous along its last dimension")
     return Heads(t.data_ptr(), st, sh)
 
 
+def _full(t, name: str, shape, dtype: torch.dtype, device) -> int:
+    """The pointer of a contiguous tensor."""
+    _matches(t, name, shape, dtype, device)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
 def _rows(t, name: str, shape, dtype: torch.dtype, device) -> int:
     """Stride between the rows of a [rows, cols] tensor that is contiguous along its rows."""
-    if not isinstance(t, torch.Tensor):
-        raise ValueError(f"{name} must be a torch.Tensor")
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
-    if t.dtype != dtype:
-        raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, expected {device}")
-    if shape[0] < 2 or shape[1] == 0:
-        if shape[1] > 1 and shape[0] and t.stride(1) != 1:
-            raise ValueError(f"{name} must be contiguous along its rows")
-        return shape[1]
-    if (shape[1] > 1 and t.stride(1) != 1) or t.stride(0) < shape[1]:
-        raise ValueError(f"{name} must be contiguous along its rows, which must not overlap")
-    return t.stride(0)
+    _matches(t, name, shape, dtype, device)
+    rows, cols = shape
+    sr, sc = t.stride()
+    if rows and cols > 1 and sc != 1:
+        raise ValueError(f"{name} must be contiguous along its rows")
+    if rows < 2 or cols == 0:
+        return cols
+    if sr < cols:
+        raise ValueError(f"the rows of {name} must not overlap")
+    return sr
 
 
 def _u64(v, name: str) -> int:
-    v = int(v)
+    if type(v) is not int:
+        v = int(v)
     if not 0 <= v < 1 << 64:
         raise ValueError(f"{name} {v} is not a 64-bit unsigned number")
     return v
@@ -93,6 +106,7 @@ class DecayAttention:
                                                                   self.longest, b)) for b in (0, 1)]
         if not all(self._bytes):
             raise ValueError(lib().mdlstm_last_error().decode(errors="replace"))
+        self._state_shape = (self.n, self.heads, self.dim_k, self.dim_v)
         self.offsets = torch.from_numpy(np.concatenate([[0], np.cumsum(n)])).to(self.device)
         self._ws = [None, None]
         self._o = self._final = self._grads = self._dstate = None
@@ -108,25 +122,22 @@ class DecayAttention:
         return (_heads(q, "q", t, self.heads, self.dim_k, dt, dev), _heads(k, "k", t, self.kv_heads, self.dim_k, dt, dev),
                 _heads(v, "v", t, self.kv_heads, self.dim_v, dt, dev))
 
-    def _check_state(self, t, name):
-        if t is not None:
-            check_tensor(t, name, (self.n, self.heads, self.dim_k, self.dim_v), torch.float32, self.device)
+    def _state(self, t, name):
+        return None if t is None else _full(t, name, self._state_shape, torch.float32, self.device)
 
     def forward(self, q, k, v, state=None, final_state: bool = False, stream=None):
         """o [tokens, heads, dim_v]; with final_state also the states the sequences leave [n, heads, dim_k, dim_v].
         state: the states they start from (None: zero). q, k, v may be views of one projection's output."""
         hq, hk, hv = self._qkv(q, k, v)
-        self._check_state(state, "state")
+        pstate = self._state(state, "state")
         if self._o is None:
             self._o = torch.empty((self.tokens, self.heads, self.dim_v), dtype=self.dtype, device=self.device)
         if final_state and self._final is None:
-            self._final = torch.empty((self.n, self.heads, self.dim_k, self.dim_v), dtype=torch.float32,
-                                      device=self.device)
-        ws = self._workspace(0)
+            self._final = torch.empty(self._state_shape, dtype=torch.float32, device=self.device)
         check(lib().mdlstm_attention_forward(self.desc, self.n, self.tokens, self.longest, self.offsets.data_ptr(),
-                                             self.rates.data_ptr(), hq, hk, hv, _ptr(state), self._o.data_ptr(),
-                                             self._final.data_ptr() if final_state else None, ws.data_ptr(),
-                                             ws.numel(), _stream(stream)))
+                                             self.rates.data_ptr(), hq, hk, hv, pstate, self._o.data_ptr(),
+                                             self._final.data_ptr() if final_state else None,
+                                             self._workspace(0).data_ptr(), self._bytes[0], _stream(stream, self.device)))
         self._saved = (q, k, v, state)
         return (self._o, self._final) if final_state else self._o
 
@@ -138,20 +149,19 @@ class DecayAttention:
         q, k, v, state = self._saved
         hq, hk, hv = self._qkv(q, k, v)
         hdo = _heads(do, "do", self.tokens, self.heads, self.dim_v, self.dtype, self.device)
-        self._check_state(dstate, "dstate")
+        pdstate = self._state(dstate, "dstate")
         if self._grads is None:
             self._grads = tuple(torch.empty((self.tokens, h, d), dtype=self.dtype, device=self.device) for h, d in (
                 (self.heads, self.dim_k), (self.kv_heads, self.dim_k), (self.kv_heads, self.dim_v)))
         if state is not None and self._dstate is None:
-            self._dstate = torch.empty((self.n, self.heads, self.dim_k, self.dim_v), dtype=torch.float32,
-                                       device=self.device)
+            self._dstate = torch.empty(self._state_shape, dtype=torch.float32, device=self.device)
         dq, dk, dv = self._grads
-        ws = self._workspace(1)
         check(lib().mdlstm_attention_backward(self.desc, self.n, self.tokens, self.longest, self.offsets.data_ptr(),
-                                              self.rates.data_ptr(), hq, hk, hv, _ptr(state), hdo, _ptr(dstate),
+                                              self.rates.data_ptr(), hq, hk, hv, _ptr(state), hdo, pdstate,
                                               dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
-                                              None if state is None else self._dstate.data_ptr(), ws.data_ptr(),
-                                              ws.numel(), _stream(stream)))
+                                              None if state is None else self._dstate.data_ptr(),
+                                              self._workspace(1).data_ptr(), self._bytes[1],
+                                              _stream(stream, self.device)))
         return self._grads if state is None else self._grads + (self._dstate,)
 
 
@@ -164,21 +174,20 @@ def decay_attention_step(q, k, v, state, rates, slots=None, scale: float = None,
         raise ValueError("q must be [n, heads, dim_k] and k [n, kv_heads, dim_k]")
     if not isinstance(state, torch.Tensor) or state.dim() != 4:
         raise ValueError("state must be [slots, heads, dim_k, dim_v]")
-    n, heads, dk = q.shape
-    dv, kv, dev, dt = state.shape[3], k.shape[1], q.device, q.dtype
-    check_tensor(state, "state", (state.shape[0], heads, dk, dv), torch.float32, dev)
-    check_tensor(rates, "rates", (heads,), torch.float32, dev)
-    if slots is not None:
-        check_tensor(slots, "slots", (n,), torch.int32, dev)
-    desc = AttentionDesc(heads, kv, dk, dv, dtype_code(dt), float(dk ** -0.5 if scale is None else scale))
+    (n, heads, dk), kv, dev, dt = q.shape, k.shape[1], q.device, q.dtype
+    count, _, _, dv = state.shape
+    if not q.is_cuda:
+        raise ValueError("q must be a device tensor")
+    pstate = _full(state, "state", (count, heads, dk, dv), torch.float32, dev)
+    prates = _full(rates, "rates", (heads,), torch.float32, dev)
+    pslots = None if slots is None else _full(slots, "slots", (n,), torch.int32, dev)
+    desc = AttentionDesc(heads, kv, dk, dv, dtype_code(dt), dk ** -0.5 if scale is None else scale)
     hq, hk, hv = (_heads(q, "q", n, heads, dk, dt, dev), _heads(k, "k", n, kv, dk, dt, dev),
                   _heads(v, "v", n, kv, dv, dt, dev))
     if out is None:
         out = torch.empty((n, heads, dv), dtype=dt, device=dev)
-    else:
-        check_tensor(out, "out", (n, heads, dv), dt, dev)
-    check(lib().mdlstm_attention_step(desc, n, rates.data_ptr(), hq, hk, hv, state.data_ptr(), state.shape[0],
-                                      _ptr(slots), out.data_ptr(), _stream(stream)))
+    check(lib().mdlstm_attention_step(desc, n, prates, hq, hk, hv, pstate, count, pslots,
+                                      _full(out, "out", (n, heads, dv), dt, dev), _stream(stream, dev)))
     return out
 
 
@@ -234,7 +243,7 @@ class ResidualNorm:
         check(lib().mdlstm_norm_forward(self.desc, self.rows, x.data_ptr(), xs, _ptr(residual), rs,
                                         self.weight.data_ptr(), seed, call, None if plain else h.data_ptr(),
                                         None if self.fp8 else y, y if self.fp8 else None, _ptr(self._scale),
-                                        _ptr(self._rstd), _stream(stream)))
+                                        _ptr(self._rstd), _stream(stream, self.device)))
         if self.fp8:
             return self._y, self._scale, h
         self._saved = (h, xs if plain else self.cols, seed, call, residual is not None)
@@ -247,9 +256,8 @@ class ResidualNorm:
             raise ValueError("backward needs a forward call on this norm first (and no 8-bit output)")
         h, hs, seed, call, residual = self._saved
         shape = (self.rows, self.cols)
-        check_tensor(dy, "dy", shape, self.dtype, self.device)
-        if dh is not None:
-            check_tensor(dh, "dh", shape, self.dtype, self.device)
+        pdy = _full(dy, "dy", shape, self.dtype, self.device)
+        pdh = None if dh is None else _full(dh, "dh", shape, self.dtype, self.device)
         if self._dx is None:
             self._dx = torch.empty(shape, dtype=self.dtype, device=self.device)
             self._dw = torch.empty(self.cols, dtype=torch.float32, device=self.device)
@@ -258,9 +266,10 @@ class ResidualNorm:
         if both and self._dres is None:
             self._dres = torch.empty(shape, dtype=self.dtype, device=self.device)
         check(lib().mdlstm_norm_backward(self.desc, self.rows, h.data_ptr(), hs, self._rstd.data_ptr(),
-                                         self.weight.data_ptr(), dy.data_ptr(), _ptr(dh), seed, call,
+                                         self.weight.data_ptr(), pdy, pdh, seed, call,
                                          self._dx.data_ptr(), self._dres.data_ptr() if both else None,
-                                         self._dw.data_ptr(), self._ws.data_ptr(), self._ws.numel(), _stream(stream)))
+                                         self._dw.data_ptr(), self._ws.data_ptr(), self._ws_bytes,
+                                         _stream(stream, self.device)))
         return self._dx, (self._dres if both else self._dx) if residual else None, self._dw
 
 
@@ -271,24 +280,22 @@ def dropout(x, p: float, seed: int, call: int = 0, residual=None, out=None, stre
     contiguous, or two-dimensional with contiguous rows. out: contiguous; may be x or residual."""
     if not isinstance(x, torch.Tensor) or not x.is_cuda:
         raise ValueError("x must be a device tensor")
+    shape, dt, dev = x.shape, x.dtype, x.device
+    rows, cols = shape if len(shape) == 2 else (1, x.numel())
 
-    def as_rows(t, name):
-        if not isinstance(t, torch.Tensor) or t.shape != x.shape or t.dtype != x.dtype or t.device != x.device:
-            raise ValueError(f"{name} must be a tensor of x's shape, dtype and device")
+    def stride(t, name):
         if t.is_contiguous():
-            return t.shape[-1] if t.dim() == 2 else t.numel()
-        if t.dim() != 2:
+            return cols
+        if len(shape) != 2:
             raise ValueError(f"{name} must be contiguous or two-dimensional")
-        return _rows(t, name, tuple(t.shape), t.dtype, t.device)
+        return _rows(t, name, shape, dt, dev)
 
-    code = dtype_code(x.dtype)
-    rows, cols = x.shape if x.dim() == 2 else (1, x.numel())
-    xs = as_rows(x, "x")
-    rs = 0 if residual is None else as_rows(residual, "residual")
+    xs, rs, pres = stride(x, "x"), 0, None
+    if residual is not None:
+        _matches(residual, "residual", shape, dt, dev)
+        rs, pres = stride(residual, "residual"), residual.data_ptr()
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    else:
-        check_tensor(out, "out", tuple(x.shape), x.dtype, x.device)
-    check(lib().mdlstm_dropout(code, rows, cols, x.data_ptr(), xs, float(p), _u64(seed, "seed"), _u64(call, "call"),
-                               _ptr(residual), rs, out.data_ptr(), _stream(stream)))
+        out = torch.empty(shape, dtype=dt, device=dev)
+    check(lib().mdlstm_dropout(dtype_code(dt), rows, cols, x.data_ptr(), xs, p, _u64(seed, "seed"), _u64(call, "call"),
+                               pres, rs, _full(out, "out", shape, dt, dev), _stream(stream, dev)))
     return out
