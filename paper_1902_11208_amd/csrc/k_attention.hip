@@ -614,31 +614,89 @@ __global__ __launch_bounds__(256) void k_sum_heads(int64_t n, int group, int dim
     St<T>::st1(dst + i, s);
 }
 
-template <typename T>
-__global__ __launch_bounds__(128) void k_step(StepArgs a) {
-    __shared__ float q[128], k[128];
-    const int row = blockIdx.x, head = blockIdx.y, c = threadIdx.x, dk = a.q.dim, dv = a.v.dim;
+// ---------------------------------------------------------------------------
+// One token: the state is read and written once and nothing else counts, so a
+// workgroup per (row, head) issues all its loads of the state at once. CG
+// threads share a row of it, V columns each; the workgroup's other threads take
+// other rows, and their sums for o meet by shuffles and in LDS.
+// ---------------------------------------------------------------------------
+template <int V>
+struct Cols {
+    float x[V];
+};
+
+template <typename T, int V, int CG>
+__global__ __launch_bounds__(256) void k_step(StepArgs a) {
+    constexpr int RG = 256 / CG, N = (128 + RG - 1) / RG;  // rows at once, rows of a thread
+    __shared__ float q[128], k[128], part[4][CG * V];
+    const int row = blockIdx.x, head = blockIdx.y, dk = a.q.dim, dv = a.v.dim;
+    const int c = threadIdx.x % CG * V, r0 = threadIdx.x / CG;
     const int64_t slot = a.slot ? a.slot[row] : row;
-    const int64_t oo = ((int64_t)row * a.heads + head) * dv + c;
+    T* out = static_cast<T*>(a.out) + ((int64_t)row * a.heads + head) * dv;
     if (slot < 0 || slot >= a.slots) {
-        if (c < dv) St<T>::st1(static_cast<T*>(a.out) + oo, 0.0f);
+        if ((int)threadIdx.x < dv) St<T>::st1(out + threadIdx.x, 0.0f);
         return;
     }
-    if (c < dk) {
-        q[c] = St<T>::ld1(at<T>(a.q, row, head) + c);
-        k[c] = St<T>::ld1(at<T>(a.k, row, head) + c);
-    }
-    __syncthreads();
-    if (c >= dv) return;
-    const float g = expf(-a.rates[head]), v = St<T>::ld1(at<T>(a.v, row, head) + c);
     float* S = a.state + (slot * a.heads + head) * dk * dv + c;
-    float o = 0.0f;
-    for (int i = 0; i < dk; ++i) {
-        const float s = fmaf(k[i], v, S[(int64_t)i * dv] * g);
-        S[(int64_t)i * dv] = s;
-        o = fmaf(q[i], s, o);
+    Cols<V> s[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (r0 + i * RG < dk && c < dv) {
+            if constexpr (V == 4) {
+                const floatx4 t = __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(S + (r0 + i * RG) * dv));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[i].x[j] = t[j];
+            } else {
+                s[i].x[0] = S[(r0 + i * RG) * dv];
+            }
+        }
+    if ((int)threadIdx.x < dk)
+        q[threadIdx.x] = St<T>::ld1(at<T>(a.q, row, head) + threadIdx.x);
+    else if (threadIdx.x >= 128 && (int)threadIdx.x - 128 < dk)
+        k[threadIdx.x - 128] = St<T>::ld1(at<T>(a.k, row, head) + threadIdx.x - 128);
+    float v[V], o[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        v[j] = c < dv ? St<T>::ld1(at<T>(a.v, row, head) + c + j) : 0.0f;
+        o[j] = 0.0f;
     }
-    St<T>::st1(static_cast<T*>(a.out) + oo, o * a.scale);
+    const float g = expf(-a.rates[head]);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (r0 + i * RG < dk && c < dv) {
+            const float ki = k[r0 + i * RG], qi = q[r0 + i * RG];
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                s[i].x[j] = fmaf(ki, v[j], s[i].x[j] * g);
+                o[j] = fmaf(qi, s[i].x[j], o[j]);
+            }
+            if constexpr (V == 4)
+                __builtin_nontemporal_store(floatx4{s[i].x[0], s[i].x[1], s[i].x[2], s[i].x[3]},
+                                            reinterpret_cast<floatx4*>(S + (r0 + i * RG) * dv));
+            else
+                S[(r0 + i * RG) * dv] = s[i].x[0];
+        }
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int d = CG; d < 64; d *= 2) o[j] += __shfl_xor(o[j], d);
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    // a wave's columns: all CG threads' where they fit in it, else its half of them
+    if constexpr (CG <= 64) {
+        if (lane < CG)
+#pragma unroll
+            for (int j = 0; j < V; ++j) part[wave][lane * V + j] = o[j];
+        __syncthreads();
+        if ((int)threadIdx.x < dv) {
+            const int x = threadIdx.x;
+            St<T>::st1(out + x, (part[0][x] + part[1][x] + part[2][x] + part[3][x]) * a.scale);
+        }
+    } else {
+        part[wave >> 1][threadIdx.x % CG] = o[0];
+        __syncthreads();
+        if ((int)threadIdx.x < dv) St<T>::st1(out + threadIdx.x, (part[0][threadIdx.x] + part[1][threadIdx.x]) * a.scale);
+    }
 }
 
 }  // namespace
@@ -724,13 +782,27 @@ hipError_t launch_sum_heads(int64_t tokens, int kv_heads, int group, int dim, in
     return hipGetLastError();
 }
 
-hipError_t launch_step(const StepArgs& a, hipStream_t s) {
+template <typename T>
+static hipError_t step(const StepArgs& a, hipStream_t s) {
     const dim3 grid(a.n, a.heads);
-    if (a.dtype)
-        k_step<bf16_t><<<grid, 128, 0, s>>>(a);
-    else
-        k_step<float><<<grid, 128, 0, s>>>(a);
+    const int dv = a.v.dim;
+    if (dv % 4 == 0) {  // rows of the state are whole 16-byte vectors
+        if (dv <= 16)
+            k_step<T, 4, 4><<<grid, 256, 0, s>>>(a);
+        else if (dv <= 32)
+            k_step<T, 4, 8><<<grid, 256, 0, s>>>(a);
+        else if (dv <= 64)
+            k_step<T, 4, 16><<<grid, 256, 0, s>>>(a);
+        else
+            k_step<T, 4, 32><<<grid, 256, 0, s>>>(a);
+    } else if (dv <= 32) {
+        k_step<T, 1, 32><<<grid, 256, 0, s>>>(a);
+    } else {
+        k_step<T, 1, 128><<<grid, 256, 0, s>>>(a);
+    }
     return hipGetLastError();
 }
+
+hipError_t launch_step(const StepArgs& a, hipStream_t s) { return a.dtype ? step<bf16_t>(a, s) : step<float>(a, s); }
 
 }  // namespace mdl
