@@ -4,6 +4,9 @@
 // All three are elementwise or one reduction along a row, so HBM bounds them:
 // every kernel reads each input once and writes each output once, a row's
 // values staying in registers between the reduction and their use.
+#include <algorithm>
+#include <type_traits>
+
 #include "common.hpp"
 #include "philox.hpp"
 #include "sequence.hpp"
@@ -12,42 +15,50 @@ namespace mdl {
 namespace {
 
 // Eight consecutive elements, `valid` of them inside the row (the others read
-// as 0 and are not written). WIDE: a whole vector is 16-byte aligned.
+// as 0 and are not written). WIDE: a whole vector is 16-byte aligned; else it is
+// moved by the same 16-byte instructions at its element's alignment (rows of 100
+// bf16, 60 million elements: 182 us forward, 330 us with single elements).
+template <typename V, bool WIDE>
+struct Vec;
+template <typename V>
+struct Vec<V, true> {
+    typedef V type;
+};
+template <typename V>
+struct Vec<V, false> {
+    typedef V type __attribute__((aligned(1)));
+};
 template <typename T, bool WIDE>
 __device__ __forceinline__ void load8(const T* p, int valid, float (&v)[8]) {
-    if (WIDE && valid == 8) {
-        const floatx4 a = St<T>::ld4(p), b = St<T>::ld4(p + 4);
+    if (valid == 8) {
+        if constexpr (sizeof(T) == 2) {
+            const u32x4 u = *reinterpret_cast<const typename Vec<u32x4, WIDE>::type*>(p);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+            for (int i = 0; i < 4; ++i) {
+                v[2 * i] = __uint_as_float(u[i] << 16);
+                v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+            }
+        } else {
+            typedef typename Vec<floatx4, WIDE>::type V;
+            const floatx4 a = *reinterpret_cast<const V*>(p), b = *reinterpret_cast<const V*>(p + 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = i < valid ? St<T>::ld1(p + i) : 0.0f;
     }
 }
-template <>
-__device__ __forceinline__ void load8<bf16_t, true>(const bf16_t* p, int valid, float (&v)[8]) {
-    if (valid == 8) {
-        const uint4 u = *reinterpret_cast<const uint4*>(p);
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = __uint_as_float(w[i] << 16);
-            v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < valid ? bf2f(p[i]) : 0.0f;
-    }
-}
 template <typename T, bool WIDE>
 __device__ __forceinline__ void store8(T* p, int valid, const float (&v)[8]) {
-    if (WIDE && valid == 8) {
+    if (valid == 8) {
         if constexpr (sizeof(T) == 2) {
-            *reinterpret_cast<uint4*>(p) =
-                make_uint4(f2bf2(v[0], v[1]), f2bf2(v[2], v[3]), f2bf2(v[4], v[5]), f2bf2(v[6], v[7]));
+            *reinterpret_cast<typename Vec<u32x4, WIDE>::type*>(p) =
+                u32x4{f2bf2(v[0], v[1]), f2bf2(v[2], v[3]), f2bf2(v[4], v[5]), f2bf2(v[6], v[7])};
         } else {
-            St<T>::st4(p, floatx4{v[0], v[1], v[2], v[3]});
-            St<T>::st4(p + 4, floatx4{v[4], v[5], v[6], v[7]});
+            typedef typename Vec<floatx4, WIDE>::type V;
+            *reinterpret_cast<V*>(p) = floatx4{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<V*>(p + 4) = floatx4{v[4], v[5], v[6], v[7]};
         }
     } else {
 #pragma unroll
@@ -105,11 +116,10 @@ __global__ __launch_bounds__(256) void k_dropout(DropoutArgs a, int64_t vecs) {
 }
 
 // ---------------------------------------------------------------------------
-// Norm. LANES threads share a row, each holding NV vectors of 8 of it.
+// Norm. LANES threads share a row, each holding NV vectors of 8 of it: up to a
+// wave, with several rows in a workgroup of 256, or (LANES 0) a workgroup of as
+// many waves as the row needs (with_shape below).
 // ---------------------------------------------------------------------------
-template <int LANES>
-constexpr int block_of() { return LANES <= 256 ? 256 : LANES; }
-
 // max that keeps a NaN
 __device__ __forceinline__ float max_nan(float a, float b) { return a > b || a != a ? a : b; }
 
@@ -117,36 +127,39 @@ template <int LANES, bool MAX>
 __device__ __forceinline__ float row_reduce(float s, float* lds) {
     auto join = [](float x, float y) { return MAX ? max_nan(x, y) : x + y; };
 #pragma unroll
-    for (int o = (LANES < 64 ? LANES : 64) / 2; o > 0; o >>= 1) s = join(s, __shfl_xor(s, o));
-    if (LANES > 64) {
+    for (int o = (LANES ? LANES : 64) / 2; o > 0; o >>= 1) s = join(s, __shfl_xor(s, o));
+    if (LANES == 0) {
         __syncthreads();
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
         __syncthreads();
         s = lds[0];
-#pragma unroll
-        for (int i = 1; i < LANES / 64; ++i) s = join(s, lds[i]);
+        for (int i = 1; i < (int)blockDim.x / 64; ++i) s = join(s, lds[i]);
     }
     return s;
 }
 
+template <int LANES>
+constexpr int threads_of() { return LANES ? 256 : 1024; }
+
 template <typename T, bool WIDE, int LANES, int NV, bool F8>
-__global__ __launch_bounds__(block_of<LANES>()) void k_norm_fwd(NormArgs a) {
-    __shared__ float lds[LANES > 64 ? LANES / 64 : 1];
-    const int64_t row = (int64_t)blockIdx.x * (block_of<LANES>() / LANES) + threadIdx.x / LANES;
+__global__ __launch_bounds__(threads_of<LANES>()) void k_norm_fwd(NormArgs a) {
+    __shared__ float lds[16];
+    const int lanes = LANES ? LANES : blockDim.x;
+    const int64_t row = LANES ? (int64_t)blockIdx.x * (256 / lanes) + threadIdx.x / lanes : blockIdx.x;
     if (row >= a.rows) return;
-    const int lane = threadIdx.x % LANES;
+    const int lane = LANES ? threadIdx.x % lanes : threadIdx.x;
     const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
     const T* r = a.residual ? static_cast<const T*>(a.residual) + row * a.r_stride : nullptr;
     const int64_t e0 = row * a.cols;
     float v[NV][8], sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (lane + i * LANES) * 8, valid = min(8, a.cols - c);
+        const int c = (lane + i * lanes) * 8, valid = min(8, a.cols - c);
         load8<T, WIDE>(x + c, valid, v[i]);
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (lane + i * LANES) * 8, valid = min(8, a.cols - c);
+        const int c = (lane + i * lanes) * 8, valid = min(8, a.cols - c);
         if (valid > 0) drop8<WIDE>(a.drop, e0 + c, v[i]);
         if (r) {
             float t[8];
@@ -164,7 +177,7 @@ __global__ __launch_bounds__(block_of<LANES>()) void k_norm_fwd(NormArgs a) {
     float top = 0.0f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (lane + i * LANES) * 8, valid = min(8, a.cols - c);
+        const int c = (lane + i * lanes) * 8, valid = min(8, a.cols - c);
         float w[8];
         load8<float, WIDE>(a.w + c, valid, w);
 #pragma unroll
@@ -181,7 +194,7 @@ __global__ __launch_bounds__(block_of<LANES>()) void k_norm_fwd(NormArgs a) {
         const float inv = 1.0f / scale;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = (lane + i * LANES) * 8, valid = min(8, a.cols - c);
+            const int c = (lane + i * lanes) * 8, valid = min(8, a.cols - c);
             uint32_t q[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
@@ -190,8 +203,9 @@ __global__ __launch_bounds__(block_of<LANES>()) void k_norm_fwd(NormArgs a) {
                 q[j] = (uint32_t)p;
             }
             uint8_t* y = a.y8 + e0 + c;
-            if (WIDE && valid == 8) {
-                *reinterpret_cast<uint2*>(y) = make_uint2(q[0], q[1]);
+            if (valid == 8) {
+                typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+                *reinterpret_cast<typename Vec<u32x2, WIDE>::type*>(y) = u32x2{q[0], q[1]};
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -202,11 +216,12 @@ __global__ __launch_bounds__(block_of<LANES>()) void k_norm_fwd(NormArgs a) {
 }
 
 template <typename T, bool WIDE, int LANES, int NV>
-__global__ __launch_bounds__(block_of<LANES>()) void k_norm_bwd(NormArgs a, int64_t groups) {
-    constexpr int ROWS = block_of<LANES>() / LANES;  // rows of a workgroup at once
-    __shared__ float lds[LANES > 64 ? LANES / 64 : 1];
+__global__ __launch_bounds__(threads_of<LANES>()) void k_norm_bwd(NormArgs a, int64_t groups) {
+    constexpr int ROWS = LANES ? 256 / LANES : 1;  // rows of a workgroup at once
+    __shared__ float lds[16];
     __shared__ float acc[ROWS > 1 ? ROWS * LANES * NV * 8 : 1];
-    const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES;
+    const int lanes = LANES ? LANES : blockDim.x;
+    const int lane = LANES ? threadIdx.x % lanes : threadIdx.x, sub = LANES ? threadIdx.x / lanes : 0;
     float dw[NV][8] = {};
     for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < a.rows; r0 += groups * ROWS) {
         const int64_t row = r0 + sub;
@@ -217,7 +232,7 @@ __global__ __launch_bounds__(block_of<LANES>()) void k_norm_bwd(NormArgs a, int6
         float g[NV][8], c[NV][8], sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int col = (lane + i * LANES) * 8, valid = min(8, a.cols - col);
+            const int col = (lane + i * lanes) * 8, valid = min(8, a.cols - col);
             float w[8];
             load8<T, WIDE>(h + col, valid, c[i]);
             load8<T, WIDE>(static_cast<const T*>(a.dy) + e0 + col, valid, g[i]);
@@ -233,7 +248,7 @@ __global__ __launch_bounds__(block_of<LANES>()) void k_norm_bwd(NormArgs a, int6
         const float mean = row_reduce<LANES, false>(sum, lds) / (float)a.cols;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int col = (lane + i * LANES) * 8, valid = min(8, a.cols - col);
+            const int col = (lane + i * lanes) * 8, valid = min(8, a.cols - col);
             float d[8] = {};
             if (a.dh) load8<T, WIDE>(static_cast<const T*>(a.dh) + e0 + col, valid, d);
 #pragma unroll
@@ -251,7 +266,7 @@ __global__ __launch_bounds__(block_of<LANES>()) void k_norm_bwd(NormArgs a, int6
 #pragma unroll
             for (int j = 0; j < 8; ++j) acc[(sub * NV + i) * LANES * 8 + lane * 8 + j] = dw[i][j];
         __syncthreads();
-        for (int c = threadIdx.x; c < a.cols; c += block_of<LANES>()) {
+        for (int c = threadIdx.x; c < a.cols; c += 256) {
             float s = 0.0f;
 #pragma unroll
             for (int k = 0; k < ROWS; ++k) s += acc[k * NV * LANES * 8 + c];
@@ -260,87 +275,103 @@ __global__ __launch_bounds__(block_of<LANES>()) void k_norm_bwd(NormArgs a, int6
     } else {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int col = (lane + i * LANES) * 8;
+            const int col = (lane + i * lanes) * 8;
             store8<float, WIDE>(part + col, min(8, a.cols - col), dw[i]);
         }
     }
 }
 
-// dw[c] = sum of the workgroups' shares: 16 slices of them, each in order, added in order.
+// dw[c] = sum of the workgroups' shares: 64 slices of them, each in order, added
+// in order. 16 columns a workgroup, eight loads of a thread in flight.
 __global__ __launch_bounds__(1024) void k_norm_dw(int cols, int groups, const float* part, float* dw) {
-    __shared__ float lds[16][64];
-    const int c = blockIdx.x * 64 + threadIdx.x % 64, slice = threadIdx.x / 64;
-    const int lo = (int)((int64_t)groups * slice / 16), hi = (int)((int64_t)groups * (slice + 1) / 16);
+    __shared__ float lds[64][17];
+    const int c = blockIdx.x * 16 + threadIdx.x % 16, slice = threadIdx.x / 16;
+    const int lo = (int)((int64_t)groups * slice / 64), hi = (int)((int64_t)groups * (slice + 1) / 64);
     float s = 0.0f;
     if (c < cols)
-        for (int g = lo; g < hi; ++g) s += part[(int64_t)g * cols + c];
-    lds[slice][threadIdx.x % 64] = s;
+        for (int g = lo; g < hi; g += 8) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = g + i < hi ? part[(int64_t)(g + i) * cols + c] : 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += v[i];
+        }
+    lds[slice][threadIdx.x % 16] = s;
     __syncthreads();
-    if (slice == 0 && c < cols) {
+    if (threadIdx.x < 64) {  // four threads a column, a quarter of the slices each
         s = 0.0f;
-        for (int i = 0; i < 16; ++i) s += lds[i][threadIdx.x];
-        dw[c] = s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s += lds[threadIdx.x / 16 * 16 + i][threadIdx.x % 16];
+        const float s1 = __shfl(s, threadIdx.x % 16 + 16), s2 = __shfl(s, threadIdx.x % 16 + 32), s3 = __shfl(s, threadIdx.x % 16 + 48);
+        if (threadIdx.x < 16 && c < cols) dw[c] = ((s + s1) + s2) + s3;
     }
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-// Calls f with the number of lanes of a row and of vectors a lane holds.
+// Calls f with the lanes of a row (0: a workgroup of `threads`), the vectors a
+// lane holds and the threads of a workgroup. Measured at 60 million elements:
+// two bytes an element leave a lane 16 bytes of a tensor a vector, and then two
+// vectors in one wave beat two waves (rows of 1000: backward 125 against 143 us;
+// four bytes: forward 113 against 92), and a forward pass wants at most about
+// four waves on a row's barriers (8-bit output, rows of 4096: 78 against 86 us, of
+// 5000: 87 with three vectors, 116 with ten waves; backward 4096: 184 against 133).
 template <typename F>
-hipError_t with_shape(int cols, F&& f) {
-    const int v = (cols + 7) / 8;
-#define SHAPE(L, N) \
-    if (v <= L * N) return f(std::integral_constant<int, L>(), std::integral_constant<int, N>());
-    SHAPE(8, 1)
-    SHAPE(16, 1)
-    SHAPE(32, 1)
-    SHAPE(64, 1)
-    SHAPE(64, 2)
-    SHAPE(64, 4)
-    SHAPE(256, 2)
-    SHAPE(256, 4)
-    SHAPE(1024, 2)
-    SHAPE(1024, 4)
-#undef SHAPE
+hipError_t with_shape(int cols, int dtype, bool forward, F&& f) {
+    const int v = (cols + 7) / 8, waves = (v + 63) / 64;
+    const bool half = dtype == 1;
+    const std::integral_constant<int, 1> one;
+    const std::integral_constant<int, 2> two;
+    const std::integral_constant<int, 0> block;
+    if (v <= 8) return f(std::integral_constant<int, 8>(), one, 256);
+    if (v <= 16) return f(std::integral_constant<int, 16>(), one, 256);
+    if (v <= 32) return f(std::integral_constant<int, 32>(), one, 256);
+    if (v <= 64) return f(std::integral_constant<int, 64>(), one, 256);
+    if (v <= 128 && half) return f(std::integral_constant<int, 64>(), two, 256);
+    if (waves <= (half && forward ? 4 : 16)) return f(block, one, waves * 64);
+    if (half && forward && waves > 8 && waves <= 12) return f(block, std::integral_constant<int, 3>(), 256);
+    if (waves <= 32) return f(block, two, (waves + 1) / 2 * 64);
+    if (waves <= 64) return f(block, std::integral_constant<int, 4>(), (waves + 3) / 4 * 64);
     return hipErrorInvalidValue;
 }
 
 template <typename T, bool WIDE>
 hipError_t norm_fwd(const NormArgs& a, hipStream_t s) {
-    return with_shape(a.cols, [&](auto L, auto N) {
-        constexpr int rows = block_of<L()>() / L();
+    return with_shape(a.cols, a.dtype, true, [&](auto L, auto N, int threads) {
+        constexpr int rows = L() ? 256 / (L() ? L() : 1) : 1;
         const dim3 grid((unsigned)((a.rows + rows - 1) / rows));
         if (a.y8)
-            k_norm_fwd<T, WIDE, L(), N(), true><<<grid, block_of<L()>(), 0, s>>>(a);
+            k_norm_fwd<T, WIDE, L(), N(), true><<<grid, threads, 0, s>>>(a);
         else
-            k_norm_fwd<T, WIDE, L(), N(), false><<<grid, block_of<L()>(), 0, s>>>(a);
+            k_norm_fwd<T, WIDE, L(), N(), false><<<grid, threads, 0, s>>>(a);
         return hipGetLastError();
     });
 }
 
 template <typename T, bool WIDE>
 hipError_t norm_bwd(const NormArgs& a, hipStream_t s) {
-    const int groups = norm_bwd_groups(a.cols, a.rows);
-    hipError_t e = with_shape(a.cols, [&](auto L, auto N) {
+    const int groups = norm_bwd_groups(a.cols, a.dtype, a.rows);
+    hipError_t e = with_shape(a.cols, a.dtype, false, [&](auto L, auto N, int threads) {
         if (groups == 0) return hipSuccess;  // no rows: dw is zero
-        k_norm_bwd<T, WIDE, L(), N()><<<groups, block_of<L()>(), 0, s>>>(a, groups);
+        k_norm_bwd<T, WIDE, L(), N()><<<groups, threads, 0, s>>>(a, groups);
         return hipGetLastError();
     });
     if (e != hipSuccess) return e;
-    k_norm_dw<<<(a.cols + 63) / 64, 1024, 0, s>>>(a.cols, groups, a.part, a.dw);
+    k_norm_dw<<<(a.cols + 15) / 16, 1024, 0, s>>>(a.cols, groups, a.part, a.dw);
     return hipGetLastError();
 }
 
 }  // namespace
 
-int norm_bwd_groups(int cols, int64_t rows) {
-    int per = 1;
-    (void)with_shape(cols, [&](auto L, auto) {
-        per = block_of<L()>() / L();
+// Workgroups of a backward call: 16 waves a CU, each with a share of dw.
+int norm_bwd_groups(int cols, int dtype, int64_t rows) {
+    int64_t want = 1;
+    (void)with_shape(cols, dtype, false, [&](auto L, auto, int threads) {
+        const int64_t per = L() ? 256 / (L() ? L() : 1) : 1;
+        want = std::min<int64_t>((rows + per - 1) / per, 4096 / (threads / 64));
         return hipSuccess;
     });
-    const int64_t want = (rows + per - 1) / per;
-    return (int)(want < 1024 ? want : 1024);
+    return (int)want;
 }
 
 hipError_t launch_dropout(const DropoutArgs& in, hipStream_t s) {

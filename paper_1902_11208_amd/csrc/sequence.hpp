@@ -114,7 +114,7 @@ struct NormArgs {
     float* dw;
 };
 constexpr int MAX_NORM_COLS = 32768;
-int norm_bwd_groups(int cols, int64_t rows);
+int norm_bwd_groups(int cols, int dtype, int64_t rows);
 hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t s);
 hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t s);
 

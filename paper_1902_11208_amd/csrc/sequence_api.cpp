@@ -182,7 +182,7 @@ mdlstm_status check_norm(const mdlstm_norm_desc* d, int64_t rows) {
 }
 
 size_t norm_workspace(const mdlstm_norm_desc* d, int64_t rows) {
-    return align_up((size_t)mdl::norm_bwd_groups(d->cols, rows) * d->cols * 4 + 16);
+    return align_up((size_t)mdl::norm_bwd_groups(d->cols, d->dtype, rows) * d->cols * 4 + 16);
 }
 
 }  // namespace
