@@ -52,16 +52,20 @@ struct Mx;
 template <>
 struct Mx<float> {
     typedef floatx4 Frag;  // reduction over 16: slots 4 g + r
-    static constexpr int KB = 16, PAD = 4;
+    static constexpr int KB = 16, PAD_Q = 4, PAD = 4;
     static __device__ __forceinline__ floatx4 mma(Frag a, Frag b, floatx4 c) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) c = mfma_f32(a[r], b[r], c);
         return c;
     }
-    // row `row` of a staged tile, reduction along it
+    // row `row` of a staged tile, reduction along it; of a q tile, whose slots lie together
     static __device__ __forceinline__ Frag along(const float* tile, int pitch, int row, int k, int g) {
         return *reinterpret_cast<const floatx4*>(tile + row * pitch + k + 4 * g);
     }
+    static __device__ __forceinline__ Frag along_q(const float* tile, int pitch, int row, int k, int g) {
+        return along(tile, pitch, row, k, g);
+    }
+    static __device__ __forceinline__ void put_q(float* row, int col, u32x4 v) { *reinterpret_cast<u32x4*>(row + col) = v; }
     // column `col0 + n`, reduction down the rows
     static __device__ __forceinline__ Frag down(const float* tile, int pitch, int row0, int col0, int g, int n) {
         Frag f;
@@ -74,13 +78,22 @@ struct Mx<float> {
 template <>
 struct Mx<bf16_t> {
     typedef bf16x8 Frag;  // reduction over 32: slots 4 g + r, then 16 + 4 g + r
-    static constexpr int KB = 32, PAD = 8;
+    static constexpr int KB = 32, PAD_Q = 8, PAD = 16;
     typedef short s4 __attribute__((ext_vector_type(4)));
     static __device__ __forceinline__ floatx4 mma(Frag a, Frag b, floatx4 c) { return mfma_bf16(a, b, c); }
     static __device__ __forceinline__ Frag along(const bf16_t* tile, int pitch, int row, int k, int g) {
         const uint2 lo = *reinterpret_cast<const uint2*>(tile + row * pitch + k + 4 * g);
         const uint2 hi = *reinterpret_cast<const uint2*>(tile + row * pitch + k + 16 + 4 * g);
         return as_bf16x8(make_uint4(lo.x, lo.y, hi.x, hi.y));
+    }
+    // q rows are only read along, so a lane group's eight slots of 32 columns are staged side by side
+    static __device__ __forceinline__ Frag along_q(const bf16_t* tile, int pitch, int row, int k, int g) {
+        return as_bf16x8(*reinterpret_cast<const uint4*>(tile + row * pitch + k + 8 * g));
+    }
+    static __device__ __forceinline__ void put_q(bf16_t* row, int col, u32x4 v) {
+        bf16_t* p = row + (col & ~31) + (col & 15) * 2 + ((col >> 4) & 1) * 4;
+        *reinterpret_cast<u32x2*>(p) = u32x2{v[0], v[1]};
+        *reinterpret_cast<u32x2*>(p + 8) = u32x2{v[2], v[3]};
     }
     // The LDS transpose read: in each sixteen lanes, lane 4 j + c points at four
     // consecutive values of row j, and lane n receives column n of the four rows.
@@ -127,10 +140,12 @@ struct Unit {
 };
 
 // Units in launch order: workgroup b runs on XCD b % 8, which takes the roles
-// and the query heads of one (slot, key head) one after the other, as they read
-// the same tokens. False: no unit.
+// and `together` heads of one slot one after the other: they read the same
+// tokens, and the heads of a token share cache lines where they are narrow (1024
+// units of 32 bf16 columns, 32 chunks each: 76 us by (slot, key head), 50 by slot).
+// False: no unit.
 __device__ __forceinline__ bool unit_of(const ScanArgs& a, Unit& u) {
-    const int group = a.group, kv = a.heads / group, inner = a.n_roles * group;
+    const int group = a.together, kv = a.heads / group, inner = a.n_roles * group;
     const int64_t i = blockIdx.x >> 3, rest = i / inner * 8 + (blockIdx.x & 7);
     const int in = (int)(i % inner);
     u.slot = rest / kv;
@@ -164,12 +179,13 @@ __device__ __forceinline__ int row_offset(int row, int stride) { return stride <
 // and a chunk spans less than 2^31 bytes.
 template <typename T, int D, int THREADS, bool WIDE>
 struct Stage {
-    static constexpr int EPV = 16 / sizeof(T), VPR = D / EPV, N = C * VPR / THREADS, STEP = THREADS / VPR;
+    // (32 columns of bf16 in four waves: half of the threads suffice)
+    static constexpr int EPV = 16 / sizeof(T), VPR = D / EPV, ALL = C * VPR, N = (ALL + THREADS - 1) / THREADS, STEP = THREADS / VPR;
     u32x4 v[N];
     int offset;  // of the first vector
     __device__ __forceinline__ void init(int64_t stride, int dim) {
         const int first = threadIdx.x / VPR, col = threadIdx.x % VPR * EPV;
-        offset = col < dim ? row_offset(first, (int)stride) + col * (int)sizeof(T) : OUT;
+        offset = col < dim && (int)threadIdx.x < ALL ? row_offset(first, (int)stride) + col * (int)sizeof(T) : OUT;
     }
     __device__ __forceinline__ void load(const char* base, int64_t stride, int dim, int row0) {
         const int first = threadIdx.x / VPR, col = threadIdx.x % VPR * EPV;
@@ -183,7 +199,7 @@ struct Stage {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 v[i] = u32x4{0, 0, 0, 0};
-                if (first + i * STEP >= row0) {
+                if (first + i * STEP >= row0 && (int)threadIdx.x < ALL) {
                     const T* p = reinterpret_cast<const T*>(base + (first + i * STEP) * stride) + col;
                     T e[EPV];
 #pragma unroll
@@ -193,10 +209,18 @@ struct Stage {
             }
         }
     }
+    template <bool IS_Q>
     __device__ __forceinline__ void store(T* tile, int pitch) const {
-        T* p = tile + threadIdx.x / VPR * pitch + threadIdx.x % VPR * EPV;
+        if (ALL < THREADS && (int)threadIdx.x >= ALL) return;
+        T* p = tile + threadIdx.x / VPR * pitch;
+        const int col = threadIdx.x % VPR * EPV;
 #pragma unroll
-        for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(p + i * STEP * pitch) = v[i];
+        for (int i = 0; i < N; ++i) {
+            if (IS_Q)
+                Mx<T>::put_q(p + i * STEP * pitch, col, v[i]);
+            else
+                *reinterpret_cast<u32x4*>(p + i * STEP * pitch + col) = v[i];
+        }
     }
 };
 
@@ -261,20 +285,33 @@ __device__ __forceinline__ void scan_plain(const ScanArgs& a, const ScanRole& R,
     }
 }
 
+// A workgroup's waves share a unit's chunk. A wave has NT column tiles of the
+// state and TI of the chunk's two token tiles: with TI 2 each wave's columns are
+// its own and P^T comes from three of the waves through LDS; with TI 1 (up to 32
+// columns) two waves keep the same columns, each computes its own part of P.
+//
 // WIDE: rows of q, k, v are whole 16-byte vectors. LOCAL: only the state that
 // a segment adds to zero, for all segments but a sequence's last.
 //
 // The scan's length need not be a multiple of C: its first chunk starts before
 // the first token, with rows of zeros, so that distances to a chunk's end are
 // the same in every chunk.
-template <typename T, int D, int SLAB, bool WIDE, int PIECES, bool LOCAL>
-__global__ __launch_bounds__(64 * D / SLAB, SLAB == 16 ? 4 : 2) void k_scan(ScanArgs a) {
+template <int D, int NT, int TI>
+constexpr int scan_threads() { return 64 * (D / 16 / NT) * (2 / TI); }
+
+template <typename T, int D, int NT, int TI, bool WIDE, int PIECES, bool LOCAL>
+__global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArgs a) {
     typedef Mx<T> M;
     typedef typename M::Frag Frag;
-    constexpr int THREADS = 64 * D / SLAB, NT = SLAB / 16, KT = D / 16, PITCH = D + M::PAD, TPF = M::KB / 16;
+    constexpr int THREADS = scan_threads<D, NT, TI>(), KT = D / 16, TPF = M::KB / 16, COLS = KT / NT;
+    constexpr int PQ = D + M::PAD_Q, PK = D + M::PAD;
     constexpr int NP = sizeof(T) == 4 ? 1 : PIECES;
-    constexpr int BUF = 3 * C * PITCH, BUFS = 2 * BUF * sizeof(T) <= 53 * 1024 ? 2 : 1;
+    constexpr bool SHARE = TI == 2 && !LOCAL && THREADS >= 192;
+    constexpr int AT_K = LOCAL ? 0 : C * PQ, AT_V = AT_K + C * PK, BUF = AT_V + C * PK;
+    constexpr int BUFS = 2 * BUF * sizeof(T) <= 60 * 1024 ? 2 : 1;
     __shared__ __align__(16) T lds[BUFS * BUF];
+    typedef T Tile[64][4];  // P^T tile, four values of a lane together
+    __shared__ __align__(16) Tile shared_p[SHARE ? 3 : 1];
     Unit u;
     if (!unit_of(a, u)) return;
     const ScanRole& R = a.role[u.role];
@@ -285,11 +322,14 @@ __global__ __launch_bounds__(64 * D / SLAB, SLAB == 16 ? 4 : 2) void k_scan(Scan
     const int64_t from = u.j * a.seg, to = a.seg ? min(len, from + a.seg) : len;
     if (u.j > 0 && from >= len) return;
     if (LOCAL && to >= len) return;
-    const int l = threadIdx.x & 63, g = l >> 4, n = l & 15, slab = (threadIdx.x >> 6) * SLAB;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l = threadIdx.x & 63, g = l >> 4, n = l & 15, slab = wave % COLS * NT * 16, i0 = TI == 2 ? 0 : wave / COLS;
     const int dk = R.q.dim, dv = R.v.dim, head = u.head, e = R.reverse;
     const float l2 = -1.4426950408889634f * a.rates[head];  // log2 g
 
-    // decays inside a chunk; a token j beyond i meets it with 0
+    // Decays inside a chunk; a token j beyond i meets it with 0. SHARE: of the tile
+    // that this wave computes, (j, i) = (0, 0), (0, 1) or (1, 1); else of those of
+    // its token tiles.
     float same[4], lower[4], w[2][4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -297,28 +337,27 @@ __global__ __launch_bounds__(64 * D / SLAB, SLAB == 16 ? 4 : 2) void k_scan(Scan
         const float ps = R.in_scale * R.out_scale;
         same[r] = j <= i ? ps * power(l2, i - j) : 0.0f;
         lower[r] = ps * power(l2, 16 + i - j);
+        if (SHARE && wave == 1) same[r] = lower[r];
 #pragma unroll
         for (int h = 0; h < 2; ++h) w[h][r] = R.in_scale * power(l2, C - 1 - (16 * h + j) + e);
-    }
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
         keep(same[r]);
         keep(lower[r]);
         keep(w[0][r]);
         keep(w[1][r]);
     }
     // The state in registers is S / g^age: what it has decayed by since it was
-    // last scaled is left out until that reaches 2^-8 (64 multiplications a chunk
-    // less; beyond, exponents would cost precision). late: weight of the registers' state at the
-    // chunk's tokens.
+    // last scaled is left out until that reaches 2^-8 (a multiplication a chunk
+    // and element less; beyond, exponents would cost precision). late: weight of
+    // the registers' state at the chunk's tokens.
     const int skip = (int)(-(to - from) & (C - 1));  // rows of zeros in the first chunk
     const int oldest = __builtin_amdgcn_readfirstlane((int)fminf(8.0f / fabsf(l2), 1e9f));
     int age = 0;
-    float full[2], late[2];
+    float full[TI], late[TI];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        full[h] = R.out_scale * power(l2, 16 * h + n + 1 - e);
-        late[h] = R.out_scale * power(l2, max(16 * h + n - skip, 0) + 1 - e);
+    for (int h = 0; h < TI; ++h) {
+        const int i = 16 * (i0 + h) + n;
+        full[h] = R.out_scale * power(l2, i + 1 - e);
+        late[h] = R.out_scale * power(l2, max(i - skip, 0) + 1 - e);
         keep(full[h]);
     }
 
@@ -370,12 +409,13 @@ __global__ __launch_bounds__(64 * D / SLAB, SLAB == 16 ? 4 : 2) void k_scan(Scan
         vp += C * vs;
     };
     auto put = [&](T* buf) {
-        if (!LOCAL) sq.store(buf, PITCH);
-        sk.store(buf + C * PITCH, PITCH);
-        sv.store(buf + 2 * C * PITCH, PITCH);
+        if (!LOCAL) sq.template store<true>(buf, PQ);
+        sk.template store<false>(buf + AT_K, PK);
+        sv.template store<false>(buf + AT_V, PK);
     };
     const int chunks = (int)((to - from + C - 1) / C);
-    floatx4 bad = {0, 0, 0, 0};  // NaN once a value was not finite
+    const floatx4 zero = {0, 0, 0, 0};
+    floatx4 bad = zero;  // NaN once a value was not finite
     int row0 = skip;
     if (chunks > 0) {
         fetch(skip);
@@ -383,53 +423,101 @@ __global__ __launch_bounds__(64 * D / SLAB, SLAB == 16 ? 4 : 2) void k_scan(Scan
     }
     for (int chunk = 0; chunk < chunks; ++chunk) {
         const T* Q = lds + (BUFS == 2 ? (chunk & 1) * BUF : 0);
-        const T *K = Q + C * PITCH, *V = K + C * PITCH;
+        const T *K = Q + AT_K, *V = Q + AT_V;
         lds_barrier();  // this chunk's rows are there; with two buffers no wave reads the other one any more
         if (chunk + 1 < chunks) fetch(0);
+        floatx4 o[NT][TI];
         Frag vf[NT][2 / TPF];
-#pragma unroll
-        for (int m = 0; m < NT; ++m)
-#pragma unroll
-            for (int h = 0; h < 2 / TPF; ++h) vf[m][h] = M::down(V, PITCH, h * M::KB, slab + 16 * m, g, n);
-        floatx4 o[NT][2];
         if (!LOCAL) {
-            const floatx4 zero = {0, 0, 0, 0};
             floatx4 p[3] = {zero, zero, zero};  // (j tile, i tile) (0, 0), (0, 1), (1, 1)
+            if (SHARE && wave < 3) {
+                const int j0 = wave == 2 ? 16 : 0, q0 = wave == 0 ? 0 : 16;
 #pragma unroll
-            for (int m = 0; m < NT; ++m) o[m][0] = o[m][1] = zero;
+                for (int k = 0; k < D / M::KB; ++k)
+                    p[0] = M::mma(M::along(K, PK, j0 + n, k * M::KB, g), M::along_q(Q, PQ, q0 + n, k * M::KB, g), p[0]);
+                // a select: what lies beyond i may be infinite
+                if (wave == 1) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) p[0][r] *= same[r];
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) p[0][r] = 4 * g + r <= n ? p[0][r] * same[r] : 0.0f;
+                }
+                St<T>::st4(shared_p[wave][l], p[0]);
+            }
+#pragma unroll
+            for (int m = 0; m < NT; ++m)
+#pragma unroll
+                for (int h = 0; h < TI; ++h) o[m][h] = zero;
 #pragma unroll
             for (int k = 0; k < D / M::KB; ++k) {
-                const Frag q0 = M::along(Q, PITCH, n, k * M::KB, g), q1 = M::along(Q, PITCH, 16 + n, k * M::KB, g);
-                const Frag k0 = M::along(K, PITCH, n, k * M::KB, g), k1 = M::along(K, PITCH, 16 + n, k * M::KB, g);
-                p[0] = M::mma(k0, q0, p[0]);
-                p[1] = M::mma(k0, q1, p[1]);
-                p[2] = M::mma(k1, q1, p[2]);
+                Frag q[TI];
+#pragma unroll
+                for (int h = 0; h < TI; ++h) q[h] = M::along_q(Q, PQ, 16 * (i0 + h) + n, k * M::KB, g);
+                if (!SHARE) {
+                    const Frag k0 = M::along(K, PK, n, k * M::KB, g);
+                    if (TI == 2) {
+                        p[0] = M::mma(k0, q[0], p[0]);
+                        p[1] = M::mma(k0, q[TI - 1], p[1]);
+                        p[2] = M::mma(M::along(K, PK, 16 + n, k * M::KB, g), q[TI - 1], p[2]);
+                    } else if (i0 == 0) {
+                        p[0] = M::mma(k0, q[0], p[0]);
+                    } else {
+                        p[1] = M::mma(k0, q[0], p[1]);
+                        p[2] = M::mma(M::along(K, PK, 16 + n, k * M::KB, g), q[0], p[2]);
+                    }
+                }
 #pragma unroll
                 for (int m = 0; m < NT; ++m) {
                     floatx4 t[TPF];
 #pragma unroll
                     for (int x = 0; x < TPF; ++x) t[x] = S[k * TPF + x][m];
                     const Frag s = M::from(t);
-                    o[m][0] = M::mma(s, q0, o[m][0]);
-                    o[m][1] = M::mma(s, q1, o[m][1]);
+#pragma unroll
+                    for (int h = 0; h < TI; ++h) o[m][h] = M::mma(s, q[h], o[m][h]);
                 }
             }
 #pragma unroll
-            for (int m = 0; m < NT; ++m) o[m][0] *= late[0], o[m][1] *= late[1];
+            for (int m = 0; m < NT; ++m)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {  // a select: what lies beyond i may be infinite
-                p[0][r] = 4 * g + r <= n ? p[0][r] * same[r] : 0.0f;
-                p[2][r] = 4 * g + r <= n ? p[2][r] * same[r] : 0.0f;
-                p[1][r] *= lower[r];
+                for (int h = 0; h < 2 / TPF; ++h) vf[m][h] = M::down(V, PK, h * M::KB, slab + 16 * m, g, n);
+#pragma unroll
+            for (int m = 0; m < NT; ++m)
+#pragma unroll
+                for (int h = 0; h < TI; ++h) o[m][h] *= late[h];
+            Frag f0[2 / TPF], f1[2 / TPF];  // P^T for the token tiles 0 and 1
+            if (SHARE) {
+                lds_barrier();
+                if constexpr (sizeof(T) == 2) {
+                    const uint2 x = *reinterpret_cast<const uint2*>(shared_p[0][l]), y = *reinterpret_cast<const uint2*>(shared_p[1][l]),
+                                z = *reinterpret_cast<const uint2*>(shared_p[2][l]);
+                    f0[0] = as_bf16x8(make_uint4(x.x, x.y, 0, 0));
+                    f1[0] = as_bf16x8(make_uint4(y.x, y.y, z.x, z.y));
+                } else {
+                    f0[0] = St<T>::ld4(shared_p[0][l]);
+                    f1[0] = St<T>::ld4(shared_p[1][l]);
+                    f1[1] = St<T>::ld4(shared_p[2][l]);
+                }
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    p[0][r] = 4 * g + r <= n ? p[0][r] * same[r] : 0.0f;
+                    p[2][r] = 4 * g + r <= n ? p[2][r] * same[r] : 0.0f;
+                    p[1][r] *= lower[r];
+                }
+                const floatx4 b0[2] = {p[0], zero}, b1[2] = {p[1], p[2]};
+#pragma unroll
+                for (int h = 0; h < 2 / TPF; ++h) {
+                    f0[h] = M::from(b0 + h);
+                    f1[h] = M::from(b1 + h);
+                }
             }
-            const floatx4 b0[2] = {p[0], zero}, b1[2] = {p[1], p[2]};
 #pragma unroll
-            for (int h = 0; h < 2 / TPF; ++h) {
-                const Frag f0 = M::from(b0 + h), f1 = M::from(b1 + h);
+            for (int m = 0; m < NT; ++m) {
+                if (TI == 2 || i0 == 0) o[m][0] = M::mma(vf[m][0], f0[0], o[m][0]);
+                if (TI == 2 || i0 == 1) {
 #pragma unroll
-                for (int m = 0; m < NT; ++m) {
-                    if (h == 0) o[m][0] = M::mma(vf[m][h], f0, o[m][0]);
-                    o[m][1] = M::mma(vf[m][h], f1, o[m][1]);
+                    for (int h = 0; h < 2 / TPF; ++h) o[m][TI - 1] = M::mma(vf[m][h], f1[h], o[m][TI - 1]);
                 }
             }
             // A value that is not finite reaches the tokens before it as 0 v = NaN.
@@ -445,11 +533,15 @@ __global__ __launch_bounds__(64 * D / SLAB, SLAB == 16 ? 4 : 2) void k_scan(Scan
 #pragma unroll
                         for (int r = 0; r < 4; ++r) bad[r] = fmaf(vf[m][h][r], 0.0f, bad[r]);
             }
+        } else {
+#pragma unroll
+            for (int m = 0; m < NT; ++m)
+#pragma unroll
+                for (int h = 0; h < 2 / TPF; ++h) vf[m][h] = M::down(V, PK, h * M::KB, slab + 16 * m, g, n);
         }
         // S = g^C S + K^T (w V)
-        const int length = C - row0;
         float fresh = 1.0f;
-        age += length;
+        age += C - row0;
         if (age > oldest) {
             const float f = power(l2, age);
 #pragma unroll
@@ -460,8 +552,8 @@ __global__ __launch_bounds__(64 * D / SLAB, SLAB == 16 ? 4 : 2) void k_scan(Scan
         } else {
             fresh = __builtin_amdgcn_exp2f(-l2 * (float)age);
         }
-        late[0] = full[0] * power(l2, age);
-        late[1] = full[1] * power(l2, age);
+#pragma unroll
+        for (int h = 0; h < TI; ++h) late[h] = full[h] * power(l2, age);
         Frag wv[NT][2 / TPF][NP];
 #pragma unroll
         for (int m = 0; m < NT; ++m) {
@@ -491,11 +583,11 @@ __global__ __launch_bounds__(64 * D / SLAB, SLAB == 16 ? 4 : 2) void k_scan(Scan
         for (int t = 0; t < KT; ++t)
 #pragma unroll
             for (int h = 0; h < 2 / TPF; ++h) {
-                const Frag kt = M::down(K, PITCH, h * M::KB, 16 * t, g, n);
+                const Frag kt = M::down(K, PK, h * M::KB, 16 * t, g, n);
 #pragma unroll
-                for (int m = 0; m < NT; ++m)
+                for (int c = NP - 1; c >= 0; --c)
 #pragma unroll
-                    for (int c = NP - 1; c >= 0; --c) S[t][m] = M::mma(kt, wv[m][h][c], S[t][m]);
+                    for (int m = 0; m < NT; ++m) S[t][m] = M::mma(kt, wv[m][h][c], S[t][m]);
             }
         // the next chunk's rows before the outputs: a wait for them would wait for those too
         if (BUFS == 1) lds_barrier();
@@ -503,8 +595,8 @@ __global__ __launch_bounds__(64 * D / SLAB, SLAB == 16 ? 4 : 2) void k_scan(Scan
         if (!LOCAL) {
             const Buffer to_out = buffer(out, os);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int i = 16 * h + n;
+            for (int h = 0; h < TI; ++h) {
+                const int i = 16 * (i0 + h) + n;
 #pragma unroll
                 for (int m = 0; m < NT; ++m) {
                     const int c = slab + 16 * m + 4 * g;
@@ -551,7 +643,7 @@ __global__ __launch_bounds__(64 * D / SLAB, SLAB == 16 ? 4 : 2) void k_scan(Scan
         to_state = R.final_state + ((int64_t)u.seq * a.heads + head) * size;
         transposed = R.state_t;
     }
-    if (to_state) {
+    if (to_state && i0 == 0) {
 #pragma unroll
         for (int t = 0; t < KT; ++t)
 #pragma unroll
@@ -562,9 +654,10 @@ __global__ __launch_bounds__(64 * D / SLAB, SLAB == 16 ? 4 : 2) void k_scan(Scan
                     if (i < dk && c < dv) to_state[transposed ? c * dk + i : i * dv + c] = S[t][m][r];
                 }
     }
-    if (!LOCAL && __any(bad[0] + bad[1] + bad[2] + bad[3] != 0.0f)) {
-        __threadfence_block();  // the outputs as written
-        scan_plain<T, KT, NT>(a, R, head, t0, len, from, to, slab, init);
+    if (!LOCAL && __syncthreads_or(bad[0] + bad[1] + bad[2] + bad[3] != 0.0f)) {
+        __threadfence();  // the outputs as written, also by the wave of the other token tile
+        __syncthreads();
+        if (i0 == 0) scan_plain<T, KT, NT>(a, R, head, t0, len, from, to, slab, init);
     }
 }
 
@@ -719,24 +812,24 @@ size_t scan_workspace_bytes(const ScanArgs& a) {
     return seg ? (size_t)a.n_roles * slots_of(a, seg) * a.heads * a.role[0].q.dim * a.role[0].v.dim * 4 : 16;
 }
 
-template <typename T, int D, int SLAB, bool WIDE, int PIECES>
+template <typename T, int D, int NT, int TI, bool WIDE, int PIECES>
 static hipError_t scan(const ScanArgs& a, hipStream_t s) {
-    const int group = a.group, inner = a.n_roles * group;
-    const int64_t rest = (a.slots * (a.heads / group) + 7) / 8, blocks = rest * 8 * inner;
+    const int inner = a.n_roles * a.together;
+    const int64_t rest = (a.slots * (a.heads / a.together) + 7) / 8, blocks = rest * 8 * inner;
     if (blocks > 0x7fffffff) return hipErrorInvalidValue;
     if (a.seg) {
-        k_scan<T, D, SLAB, WIDE, 3, true><<<(unsigned)blocks, 64 * D / SLAB, 0, s>>>(a);
+        k_scan<T, D, NT, 2, WIDE, 3, true><<<(unsigned)blocks, scan_threads<D, NT, 2>(), 0, s>>>(a);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         const int size = a.role[0].q.dim * a.role[0].v.dim;
         k_join_segments<<<dim3((size + 255) / 256, a.n * a.heads, a.n_roles), 256, 0, s>>>(a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    k_scan<T, D, SLAB, WIDE, PIECES, false><<<(unsigned)blocks, 64 * D / SLAB, 0, s>>>(a);
+    k_scan<T, D, NT, TI, WIDE, PIECES, false><<<(unsigned)blocks, scan_threads<D, NT, TI>(), 0, s>>>(a);
     return hipGetLastError();
 }
 
-template <typename T, int D, int SLAB>
+template <typename T, int D, int NT, int TI>
 static hipError_t scan_any(const ScanArgs& a, hipStream_t s) {
     bool wide = true, state = false;
     constexpr int V = 16 / sizeof(T);
@@ -747,10 +840,10 @@ static hipError_t scan_any(const ScanArgs& a, hipStream_t s) {
         state = state || a.role[r].final_state;
     }
     if constexpr (sizeof(T) == 4) {
-        return wide ? scan<T, D, SLAB, true, 1>(a, s) : scan<T, D, SLAB, false, 1>(a, s);
+        return wide ? scan<T, D, NT, TI, true, 1>(a, s) : scan<T, D, NT, TI, false, 1>(a, s);
     } else {
-        if (state) return wide ? scan<T, D, SLAB, true, 3>(a, s) : scan<T, D, SLAB, false, 3>(a, s);
-        return wide ? scan<T, D, SLAB, true, 2>(a, s) : scan<T, D, SLAB, false, 2>(a, s);
+        if (state) return wide ? scan<T, D, NT, TI, true, 3>(a, s) : scan<T, D, NT, TI, false, 3>(a, s);
+        return wide ? scan<T, D, NT, TI, true, 2>(a, s) : scan<T, D, NT, TI, false, 2>(a, s);
     }
 }
 
@@ -759,16 +852,17 @@ hipError_t launch_scan(const ScanArgs& in, hipStream_t s) {
     a.seg = segment_of(a);
     a.slots = slots_of(a, a.seg);
     a.states = static_cast<float*>(a.ws);
+    a.together = a.slots >= 64 ? a.heads : a.group;  // fewer slots would leave XCDs idle
     const int d = std::max(a.role[0].q.dim, a.role[0].v.dim);
     if (a.dtype) {
-        if (d <= 32) return scan_any<bf16_t, 32, 32>(a, s);
-        if (d <= 64) return scan_any<bf16_t, 64, 32>(a, s);
-        return scan_any<bf16_t, 128, 32>(a, s);
+        if (d <= 32) return scan_any<bf16_t, 32, 1, 1>(a, s);
+        if (d <= 64) return scan_any<bf16_t, 64, 1, 2>(a, s);
+        return scan_any<bf16_t, 128, 2, 2>(a, s);
     }
-    if (d <= 16) return scan_any<float, 16, 16>(a, s);
-    if (d <= 32) return scan_any<float, 32, 32>(a, s);
-    if (d <= 64) return scan_any<float, 64, 32>(a, s);
-    return scan_any<float, 128, 32>(a, s);
+    if (d <= 16) return scan_any<float, 16, 1, 1>(a, s);
+    if (d <= 32) return scan_any<float, 32, 1, 1>(a, s);
+    if (d <= 64) return scan_any<float, 64, 1, 2>(a, s);
+    return scan_any<float, 128, 2, 2>(a, s);
 }
 
 hipError_t launch_sum_heads(int64_t tokens, int kv_heads, int group, int dim, int dtype, const float* src, void* dst,
