@@ -291,7 +291,8 @@ __device__ __forceinline__ void scan_plain(const ScanArgs& a, const ScanRole& R,
 // columns) two waves keep the same columns, each computes its own part of P.
 //
 // WIDE: rows of q, k, v are whole 16-byte vectors. LOCAL: only the state that
-// a segment adds to zero, for all segments but a sequence's last.
+// a segment adds to zero; of a sequence's last segment where the final state is
+// asked for.
 //
 // The scan's length need not be a multiple of C: its first chunk starts before
 // the first token, with rows of zeros, so that distances to a chunk's end are
@@ -310,6 +311,11 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
     constexpr int AT_K = LOCAL ? 0 : C * PQ, AT_V = AT_K + C * PK, BUF = AT_V + C * PK;
     constexpr int BUFS = 2 * BUF * sizeof(T) <= 60 * 1024 ? 2 : 1;
     __shared__ __align__(16) T lds[BUFS * BUF];
+    // bf16 outputs pass through LDS, to leave as whole rows a chunk later: a wave's
+    // own stores are 32 bytes of a row (wide batch forward 117 -> 104 us)
+    constexpr bool ROWS_OUT = sizeof(T) == 2 && WIDE && !LOCAL;
+    constexpr int PO = D + 8, OUT_PIECES = C * D / 8, OBUFS = SHARE ? 1 : 2;
+    __shared__ __align__(16) T out_rows[ROWS_OUT ? OBUFS * C * PO : 8];
     typedef T Tile[64][4];  // P^T tile, four values of a lane together
     __shared__ __align__(16) Tile shared_p[SHARE ? 3 : 1];
     Unit u;
@@ -321,7 +327,7 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
     len = uniform(len);
     const int64_t from = u.j * a.seg, to = a.seg ? min(len, from + a.seg) : len;
     if (u.j > 0 && from >= len) return;
-    if (LOCAL && to >= len) return;
+    if (LOCAL && to >= len && !R.final_state) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l = threadIdx.x & 63, g = l >> 4, n = l & 15, slab = wave % COLS * NT * 16, i0 = TI == 2 ? 0 : wave / COLS;
     const int dk = R.q.dim, dv = R.v.dim, head = u.head, e = R.reverse;
@@ -367,7 +373,7 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
         bool transposed = false;
         if (LOCAL) {
         } else if (u.j > 0) {  // the slot before holds the state that this segment starts from
-            from_state = a.states + (((int64_t)u.role * a.slots + u.slot - 1) * a.heads + head) * size;
+            from_state = a.states + (((int64_t)u.role * a.heads + head) * a.slots + u.slot - 1) * size;
         } else if (R.state) {
             from_state = R.state + ((int64_t)u.seq * a.heads + head) * size;
             transposed = R.state_t;
@@ -413,10 +419,21 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
         sk.template store<false>(buf + AT_K, PK);
         sv.template store<false>(buf + AT_V, PK);
     };
+    // rows of the chunk at `row`, from row0 on, as staged in out_rows
+    auto flush = [&](const T* staged, char* row, int row0) {
+        const Buffer to_out = buffer(row, os);
+#pragma unroll
+        for (int x = threadIdx.x; x < (OUT_PIECES + THREADS - 1) / THREADS * THREADS; x += THREADS) {
+            const int i = x / (D / 8), c = x % (D / 8) * 8;
+            const bool in = x < OUT_PIECES && i >= row0 && c < dv;
+            const u32x4 v = *reinterpret_cast<const u32x4*>(staged + (x < OUT_PIECES ? i * PO + c : 0));
+            __builtin_amdgcn_raw_buffer_store_b128(v, to_out, in ? row_offset(i, os) + c * 2 : OUT, 0, 2);
+        }
+    };
     const int chunks = (int)((to - from + C - 1) / C);
     const floatx4 zero = {0, 0, 0, 0};
     floatx4 bad = zero;  // NaN once a value was not finite
-    int row0 = skip;
+    int row0 = skip, flush0 = skip;
     if (chunks > 0) {
         fetch(skip);
         put(lds);
@@ -485,6 +502,11 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
             for (int m = 0; m < NT; ++m)
 #pragma unroll
                 for (int h = 0; h < TI; ++h) o[m][h] *= late[h];
+            if (ROWS_OUT && !f32 && chunk > 0) {  // the outputs of the chunk before
+                flush(out_rows + (OBUFS == 2 ? ((chunk - 1) & 1) * C * PO : 0), out, flush0);
+                out += (int64_t)C * os;
+                flush0 = 0;
+            }
             Frag f0[2 / TPF], f1[2 / TPF];  // P^T for the token tiles 0 and 1
             if (SHARE) {
                 lds_barrier();
@@ -600,16 +622,12 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
 #pragma unroll
                 for (int m = 0; m < NT; ++m) {
                     const int c = slab + 16 * m + 4 * g;
-                    if (WIDE) {
-                        const int at = i >= row0 && c < dv ? row_offset(i, os) + c * osize : OUT;
-                        if (f32) {
-                            u32x4 x;
-                            __builtin_memcpy(&x, &o[m][h], 16);
-                            __builtin_amdgcn_raw_buffer_store_b128(x, to_out, at, 0, 0);
-                        } else {
-                            __builtin_amdgcn_raw_buffer_store_b64(u32x2{f2bf2(o[m][h][0], o[m][h][1]), f2bf2(o[m][h][2], o[m][h][3])},
-                                                                  to_out, at, 0, 0);
-                        }
+                    if (ROWS_OUT && !f32) {
+                        St<T>::st4(out_rows + (OBUFS == 2 ? (chunk & 1) * C * PO : 0) + i * PO + c, o[m][h]);
+                    } else if (WIDE) {
+                        u32x4 x;
+                        __builtin_memcpy(&x, &o[m][h], 16);
+                        __builtin_amdgcn_raw_buffer_store_b128(x, to_out, i >= row0 && c < dv ? row_offset(i, os) + c * 4 : OUT, 0, 2);
                     } else if (i >= row0) {
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
@@ -622,9 +640,13 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
                     }
                 }
             }
-            out += (int64_t)C * os;
+            if (!ROWS_OUT || f32) out += (int64_t)C * os;
         }
         row0 = 0;
+    }
+    if (ROWS_OUT && !f32 && chunks > 0) {
+        lds_barrier();
+        flush(out_rows + (OBUFS == 2 ? ((chunks - 1) & 1) * C * PO : 0), out, flush0);
     }
     {
         const float f = power(l2, age);
@@ -638,8 +660,8 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
     float* to_state = nullptr;
     bool transposed = false;
     if (LOCAL) {
-        to_state = a.states + (((int64_t)u.role * a.slots + u.slot) * a.heads + head) * size;
-    } else if (R.final_state && to >= len) {
+        to_state = a.states + (((int64_t)u.role * a.heads + head) * a.slots + u.slot) * size;
+    } else if (R.final_state && !a.seg) {  // with segments it comes from k_join_segments
         to_state = R.final_state + ((int64_t)u.seq * a.heads + head) * size;
         transposed = R.state_t;
     }
@@ -663,36 +685,41 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
 
 // The states that segments start from: for every sequence, head and element of
 // the state, over its segments in order. Slot j holds what segment j adds to
-// zero and receives the state that segment j + 1 starts from.
+// zero and receives the state that segment j + 1 starts from; the last one's
+// goes to the final states.
 __global__ __launch_bounds__(256) void k_join_segments(ScanArgs a) {
     const ScanRole& R = a.role[blockIdx.z];
     const int seq = blockIdx.y / a.heads, head = blockIdx.y % a.heads, size = R.q.dim * R.v.dim;
     const int x = blockIdx.x * 256 + threadIdx.x;
     int64_t t0, len;
     sequence(a.offsets, seq, a.tokens, a.longest, t0, len);
-    if (len <= a.seg || x >= size) return;
-    const double gd = exp(-(double)a.rates[head] * (double)a.seg);
+    if (x >= size || (len <= a.seg && !R.final_state)) return;
+    const double rate = a.rates[head];
+    const double gd = exp(-rate * (double)a.seg);
     const float gs = (float)gd, gs_lo = (float)(gd - (double)gs);
-    float s = 0.0f;
-    if (R.state) {
-        const int i = x / R.v.dim, c = x % R.v.dim;
-        s = R.state[((int64_t)seq * a.heads + head) * size + (R.state_t ? c * R.q.dim + i : x)];
-    }
+    const int64_t outside = ((int64_t)seq * a.heads + head) * size + (R.state_t ? x % R.v.dim * R.q.dim + x / R.v.dim : x);
+    float s = R.state ? R.state[outside] : 0.0f;
     const int64_t slot0 = seq + t0 / a.seg;
-    float* p = a.states + (((int64_t)blockIdx.z * a.slots + slot0) * a.heads + head) * size + x;
-    const int64_t step = (int64_t)a.heads * size;
-    const int joins = (int)((len - 1) / a.seg);
-    for (int j = 0; j < joins; j += 8) {
-        float v[8];
+    float* p = a.states + (((int64_t)blockIdx.z * a.heads + head) * a.slots + slot0) * size + x;
+    const int64_t step = size;
+    const int joins = len > 0 ? (int)((len - 1) / a.seg) : 0;
+    constexpr int N = 32;  // loads in flight
+    for (int j = 0; j < joins; j += N) {
+        float v[N];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = j + i < joins ? p[i * step] : 0.0f;
+        for (int i = 0; i < N; ++i) v[i] = j + i < joins ? p[i * step] : 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < N; ++i)
             if (j + i < joins) {
                 s = fmaf(s, gs, fmaf(s, gs_lo, v[i]));
                 p[i * step] = s;
             }
-        p += 8 * step;
+        p += N * step;
+    }
+    if (R.final_state) {
+        const float last = a.states[(((int64_t)blockIdx.z * a.heads + head) * a.slots + slot0 + joins) * size + x];
+        const double g = exp(-rate * (double)(len - joins * a.seg));
+        R.final_state[outside] = len > 0 ? (float)(g * (double)s + (double)last) : s;
     }
 }
 
@@ -795,12 +822,18 @@ __global__ __launch_bounds__(256) void k_step(StepArgs a) {
 }  // namespace
 
 // Tokens of a segment, 0: sequences are scanned whole. Segments cost a second
-// pass over k and v and the states between them, so they are taken only where
-// whole sequences would leave most of the chip idle.
+// pass over k and v, the states between them and two more launches, so they are
+// taken only where whole sequences would leave most of the chip idle for long
+// (64 sequences of 200 to 600 tokens, 4 heads of 32 fp32: 28 us whole, 37 us in
+// segments; one of 2048, 8 heads of 64: 27 us in segments, about 60 whole). They
+// are as long as fills the chip once: four workgroups a CU, two above 64
+// columns (one sequence of 32768, 8 heads of 128 bf16: 105 us with two, 127 with
+// four; of 65536, 8 heads of 64: 88 us with four, 103 with one and a half).
 static int64_t segment_of(const ScanArgs& a) {
     const int64_t units = (int64_t)a.n * a.heads * a.n_roles;
-    if (units >= 512 || a.longest <= 256) return 0;
-    const int64_t want = 1024 / ((int64_t)a.heads * a.n_roles) + 1;  // slots
+    if (units >= 512 || a.longest <= 768) return 0;
+    const int d = std::max(a.role[0].q.dim, a.role[0].v.dim);
+    const int64_t want = (d > 64 ? 512 : 1024) / ((int64_t)a.heads * a.n_roles) + 1;  // slots
     const int64_t seg = (a.tokens / want + C - 1) / C * C;
     return std::max<int64_t>(seg, 128);
 }
@@ -837,7 +870,7 @@ static hipError_t scan_any(const ScanArgs& a, hipStream_t s) {
         for (const HeadView* v : {&a.role[r].q, &a.role[r].k, &a.role[r].v})
             wide = wide && (reinterpret_cast<uintptr_t>(v->p) & 15) == 0 && v->dim % V == 0 && v->token_stride % V == 0 &&
                    v->head_stride % V == 0 && v->token_stride < (1 << 22);
-        state = state || a.role[r].final_state;
+        state = state || (a.role[r].final_state && !a.seg);
     }
     if constexpr (sizeof(T) == 4) {
         return wide ? scan<T, D, NT, TI, true, 1>(a, s) : scan<T, D, NT, TI, false, 1>(a, s);

@@ -47,7 +47,7 @@ struct ScanArgs {
     void* ws;              // scan_workspace_bytes
     // set by launch_scan: tokens of a segment (0: whole sequences), slots of
     // segments or sequences, heads that one XCD takes together, the states between
-    // segments [role][slot][head][q.dim][v.dim]
+    // segments [role][head][slot][q.dim][v.dim]
     int64_t seg, slots;
     int together;
     float* states;
