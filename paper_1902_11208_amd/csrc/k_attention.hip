@@ -158,7 +158,7 @@ __device__ __forceinline__ bool unit_of(const ScanArgs& a, Unit& u) {
         u.seq = find_sequence(a.offsets, a.n, a.tokens, a.seg, u.slot);
         u.j = u.slot - u.seq - min(max(a.offsets[u.seq], (int64_t)0), a.tokens) / a.seg;
     }
-    return true;
+    return u.j >= 0;  // negative only where the offsets do not ascend
 }
 
 // 32 rows of a tensor as a buffer: row r of a chunk lies r `stride` bytes from
@@ -689,8 +689,8 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
 // goes to the final states.
 __global__ __launch_bounds__(256) void k_join_segments(ScanArgs a) {
     const ScanRole& R = a.role[blockIdx.z];
-    const int seq = blockIdx.y / a.heads, head = blockIdx.y % a.heads, size = R.q.dim * R.v.dim;
-    const int x = blockIdx.x * 256 + threadIdx.x;
+    const int seq = blockIdx.x / a.heads, head = blockIdx.x % a.heads, size = R.q.dim * R.v.dim;
+    const int x = blockIdx.y * 256 + threadIdx.x;
     int64_t t0, len;
     sequence(a.offsets, seq, a.tokens, a.longest, t0, len);
     if (x >= size || (len <= a.seg && !R.final_state)) return;
@@ -823,19 +823,17 @@ __global__ __launch_bounds__(256) void k_step(StepArgs a) {
 
 // Tokens of a segment, 0: sequences are scanned whole. Segments cost a second
 // pass over k and v, the states between them and two more launches, so they are
-// taken only where whole sequences would leave most of the chip idle for long
+// taken only where the longest sequence would keep half of the chip or more idle
 // (64 sequences of 200 to 600 tokens, 4 heads of 32 fp32: 28 us whole, 37 us in
 // segments; one of 2048, 8 heads of 64: 27 us in segments, about 60 whole). They
 // are as long as fills the chip once: four workgroups a CU, two above 64
 // columns (one sequence of 32768, 8 heads of 128 bf16: 105 us with two, 127 with
 // four; of 65536, 8 heads of 64: 88 us with four, 103 with one and a half).
 static int64_t segment_of(const ScanArgs& a) {
-    const int64_t units = (int64_t)a.n * a.heads * a.n_roles;
-    if (units >= 512 || a.longest <= 768) return 0;
-    const int d = std::max(a.role[0].q.dim, a.role[0].v.dim);
-    const int64_t want = (d > 64 ? 512 : 1024) / ((int64_t)a.heads * a.n_roles) + 1;  // slots
-    const int64_t seg = (a.tokens / want + C - 1) / C * C;
-    return std::max<int64_t>(seg, 128);
+    const int64_t resident = std::max(a.role[0].q.dim, a.role[0].v.dim) > 64 ? 512 : 1024, lanes = (int64_t)a.heads * a.n_roles;
+    if (a.longest <= 768 || a.longest * resident <= 2 * a.tokens * lanes) return 0;
+    const int64_t want = resident / lanes + 1;  // slots
+    return std::max<int64_t>((a.tokens / want + C - 1) / C * C, 128);
 }
 
 static int64_t slots_of(const ScanArgs& a, int64_t seg) { return seg ? a.n + a.tokens / seg : a.n; }
@@ -855,7 +853,8 @@ static hipError_t scan(const ScanArgs& a, hipStream_t s) {
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         const int size = a.role[0].q.dim * a.role[0].v.dim;
-        k_join_segments<<<dim3((size + 255) / 256, a.n * a.heads, a.n_roles), 256, 0, s>>>(a);
+        if ((int64_t)a.n * a.heads > 0x7fffffff) return hipErrorInvalidValue;
+        k_join_segments<<<dim3(a.n * a.heads, (size + 255) / 256, a.n_roles), 256, 0, s>>>(a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     k_scan<T, D, NT, TI, WIDE, PIECES, false><<<(unsigned)blocks, scan_threads<D, NT, TI>(), 0, s>>>(a);
@@ -888,12 +887,17 @@ hipError_t launch_scan(const ScanArgs& in, hipStream_t s) {
     a.together = a.slots >= 64 ? a.heads : a.group;  // fewer slots would leave XCDs idle
     const int d = std::max(a.role[0].q.dim, a.role[0].v.dim);
     if (a.dtype) {
-        if (d <= 32) return scan_any<bf16_t, 32, 1, 1>(a, s);
+        if (d <= 32) return scan_any<bf16_t, 32, 1, 2>(a, s);
         if (d <= 64) return scan_any<bf16_t, 64, 1, 2>(a, s);
         return scan_any<bf16_t, 128, 2, 2>(a, s);
     }
-    if (d <= 16) return scan_any<float, 16, 1, 1>(a, s);
-    if (d <= 32) return scan_any<float, 32, 1, 1>(a, s);
+    // The fp32 MFMA takes longest: with few units, a wave for each token tile (256
+    // units of 32 columns, 16 chunks: 26 us against 29); with many, one wave for both
+    // keeps the state once (1024 units: 52 against 66; 2048 of 16 columns, backward:
+    // 129 against 149). bf16 gains nothing from the split (32 units 15 us both ways).
+    const bool few = a.slots * a.heads * a.n_roles <= 512;
+    if (d <= 16) return few ? scan_any<float, 16, 1, 1>(a, s) : scan_any<float, 16, 1, 2>(a, s);
+    if (d <= 32) return few ? scan_any<float, 32, 1, 1>(a, s) : scan_any<float, 32, 1, 2>(a, s);
     if (d <= 64) return scan_any<float, 64, 1, 2>(a, s);
     return scan_any<float, 128, 2, 2>(a, s);
 }

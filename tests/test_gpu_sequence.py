@@ -223,6 +223,37 @@ def test_attention_does_not_depend_on_its_neighbours(dtype, dim):
         t += n
 
 
+@pytest.mark.parametrize("dtype,d,heads,n", [("f32", 16, 8, 9000), ("bf16", 64, 2, 40), ("bf16", 128, 4, 3)])
+def test_attention_one_long_among_short(dtype, d, heads, n):
+    """One long example among short and empty ones, which segments are made for; the long one in the middle, its
+    states in and out."""
+    rng = np.random.default_rng(n)
+    lengths = rng.integers(0, 3, n)
+    lengths[n // 2] = 3333
+    T = int(lengths.sum())
+    print(f"case: {n} examples, one of 3333 tokens, {heads} heads of {d}, {dtype}", flush=True)
+    q, k, v = _qkv(rng, T, heads, heads, d, d, dtype, "fused")
+    do, a = _rand(rng, T, heads, d, dtype=dtype), _rates(rng, heads)
+    st, ds = _rand(rng, n, heads, d, d), _rand(rng, n, heads, d, d)
+    op = _seq().DecayAttention(lengths, heads, d, d, a, dtype=DT[dtype])
+    o, final = op.forward(q, k, v, state=st, final_state=True)
+    got = op.backward(do, dstate=ds)
+    some = slice(n // 2 - 1, n // 2 + 2)  # the oracle walks three examples
+    t0 = int(lengths[:n // 2 - 1].sum())
+    t = slice(t0, t0 + int(lengths[some].sum()))
+    cut = lambda x: _np(x[t])  # noqa: E731
+    args = cut(q), cut(k), cut(v), lengths[some], _np(a), d ** -0.5
+    wo, wf = orc.attention_forward(*args, _np(st[some]))
+    want = orc.attention_backward(*args, cut(do), _np(st[some]), _np(ds[some]))
+    _check("o", o[t], wo, TOL[dtype])
+    _check("final", final[some], wf, TOL32[dtype])
+    for name, g, w in zip(("dq", "dk", "dv"), got, want):
+        _check(name, g[t], w, TOL[dtype])
+    _check("dstate", got[3][some], want[3], TOL32[dtype])
+    empty = torch.from_numpy(lengths == 0).cuda()
+    assert torch.equal(final[empty], st[empty]) and torch.equal(got[3][empty], ds[empty])
+
+
 def test_attention_gradient_by_differences():
     """o is linear in q, k and v each, so a difference quotient with a step of 1 is exact up to rounding."""
     rng = np.random.default_rng(8)
@@ -257,7 +288,7 @@ def test_attention_cuts_wrong_offsets():
     desc = _lib.AttentionDesc(heads, heads, d, d, 0, 1.0)
     view = lambda t: _lib.Heads(t.data_ptr(), t.stride(0), t.stride(1))  # noqa: E731
     for offsets, rows in (([0, 1 << 40, 1 << 41], slice(0, 50)), ([-5, 20, 10], slice(0, 20)), ([60, 70, 80], slice(0, 0)),
-                          ([0, 45, 50], slice(0, 50))):
+                          ([0, 45, 50], slice(0, 50)), ([50, 0, 50], slice(0, 50))):
         off = torch.tensor(offsets, device="cuda")
         buf = torch.full((T + 64, heads, d), 7.0, device="cuda")
         ws = torch.empty(int(L.mdlstm_attention_workspace_bytes(ctypes.byref(desc), 2, T, 50, 0)), dtype=torch.uint8,
@@ -268,6 +299,20 @@ def test_attention_cuts_wrong_offsets():
         torch.cuda.synchronize()
         assert bool((buf[rows.stop:] == 7.0).all()), offsets
         assert not bool((buf[rows] == 7.0).any()), offsets
+    # in segments: offsets that descend, with the long example's length given as the longest
+    T = 2000
+    q, k, v = _qkv(rng, T, heads, heads, d, d, "f32", "contiguous")
+    for offsets in ([0, 1500, 300, 2000], [2000, 0, 1 << 50, -7], [1900, 100, 1000, 1], [0, 0, 0, 0]):
+        buf = torch.full((T + 64, heads, d), 7.0, device="cuda")
+        ws = torch.empty(int(L.mdlstm_attention_workspace_bytes(ctypes.byref(desc), 3, T, T, 0)), dtype=torch.uint8,
+                         device="cuda")
+        assert ws.numel() > 1 << 16  # segments
+        off = torch.tensor(offsets, device="cuda")
+        _lib.check(L.mdlstm_attention_forward(desc, 3, T, T, off.data_ptr(), a.data_ptr(), view(q), view(k), view(v),
+                                              None, buf.data_ptr(), None, ws.data_ptr(), ws.numel(),
+                                              torch.cuda.current_stream().cuda_stream))
+        torch.cuda.synchronize()
+        assert bool((buf[T:] == 7.0).all()), offsets
 
 
 @pytest.mark.parametrize("heads,kv,dk,dv,dtype,layout,n", [
