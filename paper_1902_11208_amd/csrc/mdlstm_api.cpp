@@ -87,6 +87,14 @@ mdlstm_status poison(char* ws, size_t from, size_t to, hipStream_t s) {
     return MDLSTM_OK;
 }
 
+}  // namespace
+
+mdlstm_status mdl::poison_workspace(void* ws, size_t bytes, void* stream) {
+    return poison_requested() ? poison(static_cast<char*>(ws), 0, bytes, as_stream(stream)) : MDLSTM_OK;
+}
+
+namespace {
+
 // ---------------------------------------------------------------------------
 // Layer descriptor and workspace plan.
 // ---------------------------------------------------------------------------

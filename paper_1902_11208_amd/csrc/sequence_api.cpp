@@ -213,6 +213,7 @@ mdlstm_status mdlstm_attention_forward(const mdlstm_attention_desc* desc, int32_
     const AttentionPlan p = attention_plan(desc, n, tokens, longest, false);
     OK_OR_RETURN(check_workspace(d_workspace, workspace_bytes, p.total));
     if (n == 0) return MDLSTM_OK;
+    OK_OR_RETURN(mdl::poison_workspace(d_workspace, p.total, stream));
     mdl::ScanArgs a = scan_args(desc, n, tokens, longest, d_offsets, d_rates);
     a.n_roles = 1;
     a.ws = static_cast<char*>(d_workspace) + p.scan;
@@ -246,6 +247,7 @@ mdlstm_status mdlstm_attention_backward(const mdlstm_attention_desc* desc, int32
     const AttentionPlan p = attention_plan(desc, n, tokens, longest, true);
     OK_OR_RETURN(check_workspace(d_workspace, workspace_bytes, p.total));
     if (n == 0) return MDLSTM_OK;
+    OK_OR_RETURN(mdl::poison_workspace(d_workspace, p.total, stream));
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     char* ws = static_cast<char*>(d_workspace);
     const mdl::HeadView qv = view(q, 1, desc->dim_k), kv = view(k, group, desc->dim_k), vv = view(v, group, desc->dim_v),
@@ -378,6 +380,7 @@ mdlstm_status mdlstm_norm_backward(const mdlstm_norm_desc* desc, int64_t rows, c
     OK_OR_RETURN(check_out(d_w, "w", true, 4));
     OK_OR_RETURN(check_out(d_dw, "dw", true, 4));
     OK_OR_RETURN(check_workspace(d_workspace, workspace_bytes, norm_workspace(desc, rows)));
+    OK_OR_RETURN(mdl::poison_workspace(d_workspace, norm_workspace(desc, rows), stream));
     mdl::NormArgs a{};
     a.cols = desc->cols;
     a.dtype = desc->dtype;

@@ -541,3 +541,26 @@ def test_other_stream_and_graph():
         torch.cuda.synchronize()
         assert all(torch.equal(g, w) for g, w in zip(got, want))
         _ = (x.float() @ x.float().t()).sum().item()
+
+
+def test_poisoned_workspaces_change_nothing(monkeypatch):
+    """With MDLSTM_POISON_WORKSPACE=1 the workspaces are NaN at the start of a call: the same bits come out."""
+    rng = np.random.default_rng(23)
+    for lengths, heads, kv, d, dtype in (([3000, 1, 0], 2, 2, 32, "f32"), ([2500], 4, 2, 64, "bf16"), ([70, 9], 4, 1, 16, "f32")):
+        T = sum(lengths)
+        q, k, v = _qkv(rng, T, heads, kv, d, d, dtype, "contiguous")
+        do, a, st = _rand(rng, T, heads, d, dtype=dtype), _rates(rng, heads), _rand(rng, len(lengths), heads, d, d)
+        op = _seq().DecayAttention(lengths, heads, d, d, a, dtype=DT[dtype], kv_heads=kv)
+        norm = _seq().ResidualNorm(torch.ones(heads * d, device="cuda"), T, dtype=DT[dtype])
+        x, dy = _rand(rng, T, heads * d, dtype=dtype), _rand(rng, T, heads * d, dtype=dtype)
+
+        def run():
+            norm.forward(x)
+            return [t.clone() for t in (*op.forward(q, k, v, state=st, final_state=True), *op.backward(do, dstate=st),
+                                        norm.backward(dy)[0], norm.backward(dy)[2])]
+
+        want = run()
+        monkeypatch.setenv("MDLSTM_POISON_WORKSPACE", "1")
+        got = run()
+        monkeypatch.delenv("MDLSTM_POISON_WORKSPACE")
+        assert all(torch.equal(g, w) for g, w in zip(got, want))
