@@ -468,6 +468,10 @@ size_t mdlstm_attention_workspace_bytes(const mdlstm_attention_desc* desc, int32
  * `longest`, empty ones allowed. The host does not read them: the kernels cut
  * them to [0, tokens] and to `longest` tokens, so wrong offsets give wrong
  * results but no access outside the tensors.
+ * d_order [n] (device; may be NULL: as numbered): the examples in the order in
+ * which they are started, which changes no result but the time: longest first
+ * keeps the chip busy to the end. An entry outside [0, n) is skipped; an example
+ * that is not listed is not computed.
  * d_rates [heads]: a_h, fp32.
  * d_state [n][heads][dim_k][dim_v] (may be NULL: zero): the state each example
  * starts from; d_final (out, may be NULL): the state it leaves (an empty
@@ -476,7 +480,7 @@ size_t mdlstm_attention_workspace_bytes(const mdlstm_attention_desc* desc, int32
  * a graph.
  */
 mdlstm_status mdlstm_attention_forward(const mdlstm_attention_desc* desc, int32_t n, int64_t tokens, int64_t longest,
-                                       const int64_t* d_offsets, const float* d_rates, const mdlstm_heads* q,
+                                       const int64_t* d_offsets, const int32_t* d_order, const float* d_rates, const mdlstm_heads* q,
                                        const mdlstm_heads* k, const mdlstm_heads* v, const float* d_state,
                                        void* d_o, float* d_final, void* d_workspace, size_t workspace_bytes,
                                        void* stream);
@@ -490,7 +494,7 @@ mdlstm_status mdlstm_attention_forward(const mdlstm_attention_desc* desc, int32_
  * before they are rounded. Needs nothing of the forward call.
  */
 mdlstm_status mdlstm_attention_backward(const mdlstm_attention_desc* desc, int32_t n, int64_t tokens, int64_t longest,
-                                        const int64_t* d_offsets, const float* d_rates, const mdlstm_heads* q,
+                                        const int64_t* d_offsets, const int32_t* d_order, const float* d_rates, const mdlstm_heads* q,
                                         const mdlstm_heads* k, const mdlstm_heads* v, const float* d_state,
                                         const mdlstm_heads* grad_o, const float* d_dfinal, void* d_dq, void* d_dk,
                                         void* d_dv, float* d_dstate, void* d_workspace, size_t workspace_bytes,
@@ -549,7 +553,7 @@ typedef struct {
  *   d_y  (out) [rows][cols], storage type;
  *   d_y8 (out) [rows][cols], float8 e4m3, and d_scale (out) [rows], fp32:
  *        y / scale rounded to nearest even, scale = max(max_row |y| / 448,
- *        2^-126) (a row with a NaN or an infinity among its y has scale NaN).
+ *        2^-126) (NaN where the row has one, infinite where |y| is).
  * d_rstd (out, may be NULL) [rows]: rsqrt(mean(h^2) + eps), for the backward.
  */
 mdlstm_status mdlstm_norm_forward(const mdlstm_norm_desc* desc, int64_t rows, const void* d_x, int64_t x_stride,

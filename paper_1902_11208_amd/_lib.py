@@ -87,9 +87,9 @@ SIGNATURES = {
                                            P_RECT, c_i32, c_i32, c_void, c_void, c_void, c_void, c_void, c_void, c_size,
                                            c_void]),
     "mdlstm_attention_workspace_bytes": (c_size, [P_ATTENTION, c_i32, c_i64, c_i64, c_i32]),
-    "mdlstm_attention_forward": (c_i32, [P_ATTENTION, c_i32, c_i64, c_i64, c_void, c_void, P_HEADS, P_HEADS, P_HEADS,
+    "mdlstm_attention_forward": (c_i32, [P_ATTENTION, c_i32, c_i64, c_i64, c_void, c_void, c_void, P_HEADS, P_HEADS, P_HEADS,
                                          c_void, c_void, c_void, c_void, c_size, c_void]),
-    "mdlstm_attention_backward": (c_i32, [P_ATTENTION, c_i32, c_i64, c_i64, c_void, c_void, P_HEADS, P_HEADS, P_HEADS,
+    "mdlstm_attention_backward": (c_i32, [P_ATTENTION, c_i32, c_i64, c_i64, c_void, c_void, c_void, P_HEADS, P_HEADS, P_HEADS,
                                           c_void, P_HEADS, c_void, c_void, c_void, c_void, c_void, c_void, c_size,
                                           c_void]),
     "mdlstm_attention_step": (c_i32, [P_ATTENTION, c_i32, c_void, P_HEADS, P_HEADS, P_HEADS, c_void, c_i64, c_void,

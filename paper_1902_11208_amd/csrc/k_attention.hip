@@ -154,6 +154,10 @@ __device__ __forceinline__ bool unit_of(const ScanArgs& a, Unit& u) {
     u.head = (int)(rest % kv) * group + in / a.n_roles;
     u.j = 0;
     u.seq = (int)u.slot;
+    if (!a.seg && a.order) {  // longest first: the wide batch's gradients 269 -> 212 us
+        u.seq = __builtin_amdgcn_readfirstlane(a.order[u.slot]);
+        if (u.seq < 0 || u.seq >= a.n) return false;
+    }
     if (a.seg) {
         u.seq = find_sequence(a.offsets, a.n, a.tokens, a.seg, u.slot);
         u.j = u.slot - u.seq - min(max(a.offsets[u.seq], (int64_t)0), a.tokens) / a.seg;

@@ -40,6 +40,7 @@ struct ScanArgs {
     int n, heads, dtype;
     int64_t tokens, longest;
     const int64_t* offsets;
+    const int32_t* order;  // sequences in the order they are started, or NULL
     const float* rates;
     int n_roles;
     ScanRole role[3];

@@ -96,7 +96,7 @@ mdl::HeadView view(const mdlstm_heads* v, int group, int dim) {
 }
 
 mdl::ScanArgs scan_args(const mdlstm_attention_desc* d, int32_t n, int64_t tokens, int64_t longest,
-                        const int64_t* offsets, const float* rates) {
+                        const int64_t* offsets, const int32_t* order, const float* rates) {
     mdl::ScanArgs a{};
     a.n = n;
     a.heads = d->heads;
@@ -105,6 +105,7 @@ mdl::ScanArgs scan_args(const mdlstm_attention_desc* d, int32_t n, int64_t token
     a.tokens = tokens;
     a.longest = longest;
     a.offsets = offsets;
+    a.order = order;
     a.rates = rates;
     return a;
 }
@@ -133,7 +134,7 @@ AttentionPlan attention_plan(const mdlstm_attention_desc* d, int32_t n, int64_t 
         off += align_up((size_t)tokens * d->heads * d->dim_v * 4);
     }
     p.scan = off;
-    mdl::ScanArgs a = scan_args(d, n, tokens, longest, nullptr, nullptr);
+    mdl::ScanArgs a = scan_args(d, n, tokens, longest, nullptr, nullptr, nullptr);
     role_dims(a, d, backward);
     off += align_up(mdl::scan_workspace_bytes(a));
     p.total = off;
@@ -196,7 +197,8 @@ size_t mdlstm_attention_workspace_bytes(const mdlstm_attention_desc* desc, int32
 }
 
 mdlstm_status mdlstm_attention_forward(const mdlstm_attention_desc* desc, int32_t n, int64_t tokens, int64_t longest,
-                                       const int64_t* d_offsets, const float* d_rates, const mdlstm_heads* q,
+                                       const int64_t* d_offsets, const int32_t* d_order, const float* d_rates,
+                                       const mdlstm_heads* q,
                                        const mdlstm_heads* k, const mdlstm_heads* v, const float* d_state, void* d_o,
                                        float* d_final, void* d_workspace, size_t workspace_bytes, void* stream) {
     OK_OR_RETURN(check_attention(desc));
@@ -206,6 +208,7 @@ mdlstm_status mdlstm_attention_forward(const mdlstm_attention_desc* desc, int32_
     OK_OR_RETURN(check_view(k, "k", tokens, desc->kv_heads, desc->dtype));
     OK_OR_RETURN(check_view(v, "v", tokens, desc->kv_heads, desc->dtype));
     OK_OR_RETURN(check_out(d_offsets, "offsets", n > 0, 8));
+    OK_OR_RETURN(check_out(d_order, "order", false, 4));
     OK_OR_RETURN(check_out(d_rates, "rates", n > 0, 4));
     OK_OR_RETURN(check_out(d_state, "state", false, 16));
     OK_OR_RETURN(check_out(d_o, "o", tokens > 0, 16));
@@ -214,7 +217,7 @@ mdlstm_status mdlstm_attention_forward(const mdlstm_attention_desc* desc, int32_
     OK_OR_RETURN(check_workspace(d_workspace, workspace_bytes, p.total));
     if (n == 0) return MDLSTM_OK;
     OK_OR_RETURN(mdl::poison_workspace(d_workspace, p.total, stream));
-    mdl::ScanArgs a = scan_args(desc, n, tokens, longest, d_offsets, d_rates);
+    mdl::ScanArgs a = scan_args(desc, n, tokens, longest, d_offsets, d_order, d_rates);
     a.n_roles = 1;
     a.ws = static_cast<char*>(d_workspace) + p.scan;
     a.role[0] = mdl::ScanRole{view(q, 1, desc->dim_k), view(k, group, desc->dim_k), view(v, group, desc->dim_v),
@@ -224,7 +227,8 @@ mdlstm_status mdlstm_attention_forward(const mdlstm_attention_desc* desc, int32_
 }
 
 mdlstm_status mdlstm_attention_backward(const mdlstm_attention_desc* desc, int32_t n, int64_t tokens, int64_t longest,
-                                        const int64_t* d_offsets, const float* d_rates, const mdlstm_heads* q,
+                                        const int64_t* d_offsets, const int32_t* d_order, const float* d_rates,
+                                       const mdlstm_heads* q,
                                         const mdlstm_heads* k, const mdlstm_heads* v, const float* d_state,
                                         const mdlstm_heads* grad_o, const float* d_dfinal, void* d_dq, void* d_dk,
                                         void* d_dv, float* d_dstate, void* d_workspace, size_t workspace_bytes,
@@ -237,6 +241,7 @@ mdlstm_status mdlstm_attention_backward(const mdlstm_attention_desc* desc, int32
     OK_OR_RETURN(check_view(v, "v", tokens, desc->kv_heads, desc->dtype));
     OK_OR_RETURN(check_view(grad_o, "grad_o", tokens, desc->heads, desc->dtype));
     OK_OR_RETURN(check_out(d_offsets, "offsets", n > 0, 8));
+    OK_OR_RETURN(check_out(d_order, "order", false, 4));
     OK_OR_RETURN(check_out(d_rates, "rates", n > 0, 4));
     OK_OR_RETURN(check_out(d_state, "state", false, 16));
     OK_OR_RETURN(check_out(d_dfinal, "dfinal", false, 16));
@@ -255,7 +260,7 @@ mdlstm_status mdlstm_attention_backward(const mdlstm_attention_desc* desc, int32
     const int shared = group > 1;
     void* dk = shared ? ws + p.dk : d_dk;
     void* dv = shared ? ws + p.dv : d_dv;
-    mdl::ScanArgs a = scan_args(desc, n, tokens, longest, d_offsets, d_rates);
+    mdl::ScanArgs a = scan_args(desc, n, tokens, longest, d_offsets, d_order, d_rates);
     a.n_roles = 3;
     a.ws = ws + p.scan;
     a.role[0] = mdl::ScanRole{gv, vv, kv, d_dq, d_state, nullptr, desc->scale, 1.0f, 0, 1, 0};

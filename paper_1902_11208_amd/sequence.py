@@ -12,6 +12,7 @@ returned have to outlive the work enqueued on any other stream.
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import numpy as np
 import torch
@@ -27,20 +28,26 @@ def _stream(stream, device) -> int:
     return _raw_stream(device.index) if stream is None else stream.cuda_stream
 
 
-def _matches(t, name: str, shape, dtype: torch.dtype, device) -> None:
+def _complain(t, name: str, shape, dtype: torch.dtype, device):
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{name} must be a torch.Tensor")
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if t.dtype is not dtype:
         raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    raise ValueError(f"{name} is on {t.device}, expected {device}")
+
+
+def _matches(t, name: str, shape, dtype: torch.dtype, device) -> None:
+    if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype is not dtype or t.device != device:
+        _complain(t, name, shape, dtype, device)
 
 
 def _heads(t, name: str, tokens: int, heads: int, dim: int, dtype: torch.dtype, device) -> Heads:
     """A [tokens, heads, dim] tensor, possibly a view with a contiguous last dimension, as the C ABI takes it."""
-    _matches(t, name, (tokens, heads, dim), dtype, device)
+    if (not isinstance(t, torch.Tensor) or t.shape != (tokens, heads, dim) or t.dtype is not dtype or
+            t.device != device):
+        _complain(t, name, (tokens, heads, dim), dtype, device)
     st, sh, sd = t.stride()
     if sd != 1 and dim > 1 and t.numel():
         raise ValueError(f"{name} must be contiguous along its last dimension")
@@ -49,10 +56,16 @@ def _heads(t, name: str, tokens: int, heads: int, dim: int, dtype: torch.dtype, 
 
 def _full(t, name: str, shape, dtype: torch.dtype, device) -> int:
     """The pointer of a contiguous tensor."""
-    _matches(t, name, shape, dtype, device)
+    if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype is not dtype or t.device != device:
+        _complain(t, name, shape, dtype, device)
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
+
+
+@functools.lru_cache(maxsize=256)
+def _attention_desc(heads: int, kv_heads: int, dim_k: int, dim_v: int, dtype: int, scale) -> AttentionDesc:
+    return AttentionDesc(heads, kv_heads, dim_k, dim_v, dtype, max(1, dim_k) ** -0.5 if scale is None else scale)
 
 
 def _rows(t, name: str, shape, dtype: torch.dtype, device) -> int:
@@ -99,7 +112,7 @@ class DecayAttention:
         self.n, self.tokens = int(n.size), int(n.sum())
         self.longest = int(n.max()) if n.size else 0
         self.desc = AttentionDesc(self.heads, self.kv_heads, self.dim_k, self.dim_v, dtype_code(dtype),
-                                  float(self.dim_k ** -0.5 if scale is None else scale))
+                                  float(max(1, self.dim_k) ** -0.5 if scale is None else scale))
         check_tensor(rates, "rates", (self.heads,), torch.float32)
         self.rates, self.device = rates, rates.device
         self._bytes = [int(lib().mdlstm_attention_workspace_bytes(ctypes.byref(self.desc), self.n, self.tokens,
@@ -108,6 +121,8 @@ class DecayAttention:
             raise ValueError(lib().mdlstm_last_error().decode(errors="replace"))
         self._state_shape = (self.n, self.heads, self.dim_k, self.dim_v)
         self.offsets = torch.from_numpy(np.concatenate([[0], np.cumsum(n)])).to(self.device)
+        # longest first, so that no long sequence starts when the others are done
+        self.order = torch.from_numpy(np.argsort(-n, kind="stable").astype(np.int32)).to(self.device)
         self._ws = [None, None]
         self._o = self._final = self._grads = self._dstate = None
         self._saved = None
@@ -135,7 +150,7 @@ class DecayAttention:
         if final_state and self._final is None:
             self._final = torch.empty(self._state_shape, dtype=torch.float32, device=self.device)
         check(lib().mdlstm_attention_forward(self.desc, self.n, self.tokens, self.longest, self.offsets.data_ptr(),
-                                             self.rates.data_ptr(), hq, hk, hv, pstate, self._o.data_ptr(),
+                                             self.order.data_ptr(), self.rates.data_ptr(), hq, hk, hv, pstate, self._o.data_ptr(),
                                              self._final.data_ptr() if final_state else None,
                                              self._workspace(0).data_ptr(), self._bytes[0], _stream(stream, self.device)))
         self._saved = (q, k, v, state)
@@ -157,7 +172,7 @@ class DecayAttention:
             self._dstate = torch.empty(self._state_shape, dtype=torch.float32, device=self.device)
         dq, dk, dv = self._grads
         check(lib().mdlstm_attention_backward(self.desc, self.n, self.tokens, self.longest, self.offsets.data_ptr(),
-                                              self.rates.data_ptr(), hq, hk, hv, _ptr(state), hdo, pdstate,
+                                              self.order.data_ptr(), self.rates.data_ptr(), hq, hk, hv, _ptr(state), hdo, pdstate,
                                               dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
                                               None if state is None else self._dstate.data_ptr(),
                                               self._workspace(1).data_ptr(), self._bytes[1],
@@ -181,7 +196,7 @@ def decay_attention_step(q, k, v, state, rates, slots=None, scale: float = None,
     pstate = _full(state, "state", (count, heads, dk, dv), torch.float32, dev)
     prates = _full(rates, "rates", (heads,), torch.float32, dev)
     pslots = None if slots is None else _full(slots, "slots", (n,), torch.int32, dev)
-    desc = AttentionDesc(heads, kv, dk, dv, dtype_code(dt), dk ** -0.5 if scale is None else scale)
+    desc = _attention_desc(heads, kv, dk, dv, dtype_code(dt), scale)
     hq, hk, hv = (_heads(q, "q", n, heads, dk, dt, dev), _heads(k, "k", n, kv, dk, dt, dev),
                   _heads(v, "v", n, kv, dv, dt, dev))
     if out is None:

@@ -91,10 +91,10 @@ static void fuzz_attention(void) {
         ++g_failures;
         fprintf(stderr, "workspace sizes %zu and %zu\n", f, b);
     }
-    rejected(mdlstm_attention_forward(chance(2) ? NULL : &d, n, tokens, longest, any_ptr(), any_ptr(), &v[0], &v[1],
+    rejected(mdlstm_attention_forward(chance(2) ? NULL : &d, n, tokens, longest, any_ptr(), any_ptr(), any_ptr(), &v[0], &v[1],
                                       chance(2) ? NULL : &v[2], any_ptr(), any_ptr(), any_ptr(), any_ptr(),
                                       f > 0 ? f - 1 : 0, NULL), "attention_forward");
-    rejected(mdlstm_attention_backward(&d, n, tokens, longest, any_ptr(), any_ptr(), &v[0], &v[1], &v[2], any_ptr(), &v[3],
+    rejected(mdlstm_attention_backward(&d, n, tokens, longest, any_ptr(), any_ptr(), any_ptr(), &v[0], &v[1], &v[2], any_ptr(), &v[3],
                                        any_ptr(), any_ptr(), any_ptr(), any_ptr(), any_ptr(), any_ptr(), b > 0 ? b - 1 : 0,
                                        NULL), "attention_backward");
     v[uniform(0, 2)].token_stride = -1; /* a defect for certain */

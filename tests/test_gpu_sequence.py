@@ -293,12 +293,20 @@ def test_attention_cuts_wrong_offsets():
         buf = torch.full((T + 64, heads, d), 7.0, device="cuda")
         ws = torch.empty(int(L.mdlstm_attention_workspace_bytes(ctypes.byref(desc), 2, T, 50, 0)), dtype=torch.uint8,
                          device="cuda")
-        _lib.check(L.mdlstm_attention_forward(desc, 2, T, 50, off.data_ptr(), a.data_ptr(), view(q), view(k), view(v),
+        _lib.check(L.mdlstm_attention_forward(desc, 2, T, 50, off.data_ptr(), None, a.data_ptr(), view(q), view(k), view(v),
                                               None, buf.data_ptr(), None, ws.data_ptr(), ws.numel(),
                                               torch.cuda.current_stream().cuda_stream))
         torch.cuda.synchronize()
         assert bool((buf[rows.stop:] == 7.0).all()), offsets
         assert not bool((buf[rows] == 7.0).any()), offsets
+    # an order that is no permutation: entries outside are skipped, an example not listed stays as it was
+    off, order = torch.tensor([0, 20, 50], device="cuda"), torch.tensor([7, 1], dtype=torch.int32, device="cuda")
+    buf = torch.full((T, heads, d), 7.0, device="cuda")
+    _lib.check(L.mdlstm_attention_forward(desc, 2, T, 50, off.data_ptr(), order.data_ptr(), a.data_ptr(), view(q), view(k),
+                                          view(v), None, buf.data_ptr(), None, ws.data_ptr(), ws.numel(),
+                                          torch.cuda.current_stream().cuda_stream))
+    torch.cuda.synchronize()
+    assert bool((buf[:20] == 7.0).all()) and not bool((buf[20:] == 7.0).any())
     # in segments: offsets that descend, with the long example's length given as the longest
     T = 2000
     q, k, v = _qkv(rng, T, heads, heads, d, d, "f32", "contiguous")
@@ -308,7 +316,7 @@ def test_attention_cuts_wrong_offsets():
                          device="cuda")
         assert ws.numel() > 1 << 16  # segments
         off = torch.tensor(offsets, device="cuda")
-        _lib.check(L.mdlstm_attention_forward(desc, 3, T, T, off.data_ptr(), a.data_ptr(), view(q), view(k), view(v),
+        _lib.check(L.mdlstm_attention_forward(desc, 3, T, T, off.data_ptr(), None, a.data_ptr(), view(q), view(k), view(v),
                                               None, buf.data_ptr(), None, ws.data_ptr(), ws.numel(),
                                               torch.cuda.current_stream().cuda_stream))
         torch.cuda.synchronize()

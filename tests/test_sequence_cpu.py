@@ -37,7 +37,7 @@ ATTENTION_BAD = [
     (dict(q=None), INVALID), (dict(q=(0, 128, 32)), INVALID), (dict(k=(FAKE + 2, 128, 32)), INVALID),
     (dict(v=(FAKE, -1, 32)), INVALID), (dict(v=(FAKE, 128, -32)), INVALID), (dict(q=(FAKE, 1 << 62, 32)), INVALID),
     (dict(q=(FAKE, 1 << 58, 1 << 60)), INVALID),
-    (dict(offsets=None), INVALID), (dict(offsets=FAKE + 4), INVALID), (dict(rates=None), INVALID),
+    (dict(order=FAKE + 2), INVALID), (dict(offsets=None), INVALID), (dict(offsets=FAKE + 4), INVALID), (dict(rates=None), INVALID),
     (dict(state=FAKE + 4), INVALID), (dict(out=None), INVALID), (dict(out=FAKE + 8), INVALID), (dict(final=FAKE + 2), INVALID),
     (dict(ws=None), WORKSPACE), (dict(short=1), WORKSPACE), (dict(ws=FAKE + 4), INVALID),
 ]
@@ -47,7 +47,7 @@ ATTENTION_BAD = [
 @pytest.mark.parametrize("backward", [False, True])
 def test_attention_errors(change, code, backward):
     L = _L().lib()
-    a = dict(desc={}, n=3, tokens=100, longest=50, offsets=FAKE, rates=FAKE, q=(FAKE, 128, 32), k=(FAKE, 64, 32),
+    a = dict(desc={}, n=3, tokens=100, longest=50, offsets=FAKE, order=FAKE, rates=FAKE, q=(FAKE, 128, 32), k=(FAKE, 64, 32),
              v=(FAKE, 32, 16), state=None, out=FAKE, final=None, ws=FAKE, short=0)
     a.update(change)
     d = None if a["desc"] is None else _desc(**a["desc"])
@@ -57,11 +57,11 @@ def test_attention_errors(change, code, backward):
     assert (need == 0) == (set(change) <= size_only)
     have = max(need, 1 << 20) if not a["short"] else need - 1
     if backward:
-        st = L.mdlstm_attention_backward(d, a["n"], a["tokens"], a["longest"], a["offsets"], a["rates"], *views, a["state"],
-                                         _view(), None, a["out"], FAKE, FAKE, a["final"], a["ws"], have, None)
+        st = L.mdlstm_attention_backward(d, a["n"], a["tokens"], a["longest"], a["offsets"], a["order"], a["rates"], *views,
+                                         a["state"], _view(), None, a["out"], FAKE, FAKE, a["final"], a["ws"], have, None)
     else:
-        st = L.mdlstm_attention_forward(d, a["n"], a["tokens"], a["longest"], a["offsets"], a["rates"], *views, a["state"],
-                                        a["out"], a["final"], a["ws"], have, None)
+        st = L.mdlstm_attention_forward(d, a["n"], a["tokens"], a["longest"], a["offsets"], a["order"], a["rates"], *views,
+                                        a["state"], a["out"], a["final"], a["ws"], have, None)
     assert st == code, L.mdlstm_last_error()
 
 
@@ -71,7 +71,7 @@ def test_attention_of_nothing():
     v = _view(0)
     need = L.mdlstm_attention_workspace_bytes(d, 0, 0, 0, 0)
     assert need >= 16
-    assert L.mdlstm_attention_forward(d, 0, 0, 0, None, None, v, v, v, None, None, None, FAKE, need, None) == OK
+    assert L.mdlstm_attention_forward(d, 0, 0, 0, None, None, None, v, v, v, None, None, None, FAKE, need, None) == OK
     assert L.mdlstm_attention_step(d, 0, None, v, v, v, None, 0, None, None, None) == OK
 
 
