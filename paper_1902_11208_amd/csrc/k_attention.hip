@@ -1,6 +1,7 @@
 // Linear attention with a decay for each head: the scan over packed sequences,
 // the sum over shared heads, and the single-token step.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.hpp"
 #include "sequence.hpp"
@@ -245,7 +246,7 @@ __device__ __forceinline__ void scan_plain(const ScanArgs& a, const ScanRole& R,
     const int l = threadIdx.x & 63, g = l >> 4, n = l & 15, dk = R.q.dim, dv = R.v.dim;
     const float decay = expf(-a.rates[head]);
     floatx4 S[KT][NT];
-    init(S);
+    init(S, 0);
     for (int64_t pos = from; pos < to; ++pos) {
         const int64_t t = R.reverse ? t0 + len - 1 - pos : t0 + pos;
         const T *q = at<T>(R.q, t, head), *k = at<T>(R.k, t, head), *v = at<T>(R.v, t, head);
@@ -290,9 +291,11 @@ __device__ __forceinline__ void scan_plain(const ScanArgs& a, const ScanRole& R,
 }
 
 // A workgroup's waves share a unit's chunk. A wave has NT column tiles of the
-// state and TI of the chunk's two token tiles: with TI 2 each wave's columns are
-// its own and P^T comes from three of the waves through LDS; with TI 1 (up to 32
-// columns) two waves keep the same columns, each computes its own part of P.
+// state and TI of the chunk's two token tiles. With TI 2 each wave's columns are
+// its own, and from four waves on P^T comes from three of them through LDS. With
+// TI 1 two waves share columns: of 32 by 32 states (SPLIT) each keeps 16 of the
+// rows, multiplies both token tiles by them and passes on the tile that is the
+// other's; of 16 by 16 ones both keep the state, and each computes its part of P.
 //
 // WIDE: rows of q, k, v are whole 16-byte vectors. LOCAL: only the state that
 // a segment adds to zero; of a sequence's last segment where the final state is
@@ -308,10 +311,13 @@ template <typename T, int D, int NT, int TI, bool WIDE, int PIECES, bool LOCAL>
 __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArgs a) {
     typedef Mx<T> M;
     typedef typename M::Frag Frag;
-    constexpr int THREADS = scan_threads<D, NT, TI>(), KT = D / 16, TPF = M::KB / 16, COLS = KT / NT;
+    constexpr int THREADS = scan_threads<D, NT, TI>(), TPF = M::KB / 16, COLS = D / 16 / NT;
+    constexpr bool SPLIT = TI == 1 && D == 32;
+    constexpr int KT = SPLIT ? 1 : D / 16, OT = SPLIT ? 2 : TI;  // state tiles of a column tile, token tiles they meet
+    static_assert(!SPLIT || (TPF == 1 && NT == 1), "a split state is built for fp32");
     constexpr int PQ = D + M::PAD_Q, PK = D + M::PAD;
     constexpr int NP = sizeof(T) == 4 ? 1 : PIECES;
-    constexpr bool SHARE = TI == 2 && !LOCAL && THREADS >= 192;
+    constexpr bool SHARE = SPLIT || (TI == 2 && !LOCAL && THREADS >= 192);
     constexpr int AT_K = LOCAL ? 0 : C * PQ, AT_V = AT_K + C * PK, BUF = AT_V + C * PK;
     constexpr int BUFS = 2 * BUF * sizeof(T) <= 60 * 1024 ? 2 : 1;
     __shared__ __align__(16) T lds[BUFS * BUF];
@@ -322,6 +328,7 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
     __shared__ __align__(16) T out_rows[ROWS_OUT ? OBUFS * C * PO : 8];
     typedef T Tile[64][4];  // P^T tile, four values of a lane together
     __shared__ __align__(16) Tile shared_p[SHARE ? 3 : 1];
+    __shared__ __align__(16) float passed[SPLIT ? 4 : 1][64][4];
     Unit u;
     if (!unit_of(a, u)) return;
     const ScanRole& R = a.role[u.role];
@@ -362,16 +369,16 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
     const int skip = (int)(-(to - from) & (C - 1));  // rows of zeros in the first chunk
     const int oldest = __builtin_amdgcn_readfirstlane((int)fminf(8.0f / fabsf(l2), 1e9f));
     int age = 0;
-    float full[TI], late[TI];
+    float full[OT], late[OT];
 #pragma unroll
-    for (int h = 0; h < TI; ++h) {
-        const int i = 16 * (i0 + h) + n;
+    for (int h = 0; h < OT; ++h) {
+        const int i = 16 * ((SPLIT ? 0 : i0) + h) + n;
         full[h] = R.out_scale * power(l2, i + 1 - e);
         late[h] = R.out_scale * power(l2, max(i - skip, 0) + 1 - e);
         keep(full[h]);
     }
 
-    auto init = [&](floatx4 (&S)[KT][NT]) {
+    auto init = [&](auto& S, int tile0) {
         const float* from_state = nullptr;
         const int64_t size = (int64_t)dk * dv;
         bool transposed = false;
@@ -383,17 +390,18 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
             transposed = R.state_t;
         }
 #pragma unroll
-        for (int t = 0; t < KT; ++t)
+        for (int t = 0; t < (int)std::extent<std::remove_reference_t<decltype(S)>>(); ++t)
 #pragma unroll
             for (int m = 0; m < NT; ++m)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int i = 16 * t + 4 * g + r, c = slab + 16 * m + n;
+                    const int i = 16 * (tile0 + t) + 4 * g + r, c = slab + 16 * m + n;
                     S[t][m][r] = from_state && i < dk && c < dv ? from_state[transposed ? c * dk + i : i * dv + c] : 0.0f;
                 }
     };
-    floatx4 S[KT][NT];  // S[t][m][r] = state[16 t + 4 g + r][slab + 16 m + n]
-    init(S);
+    const int tile0 = SPLIT ? i0 : 0;
+    floatx4 S[KT][NT];  // S[t][m][r] = state[16 (tile0 + t) + 4 g + r][slab + 16 m + n]
+    init(S, tile0);
 
     // bytes between rows and from a chunk to the next; the chunk's row 0 is scan position pos
     const int dir = R.reverse ? -1 : 1;
@@ -447,7 +455,7 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
         const T *K = Q + AT_K, *V = Q + AT_V;
         lds_barrier();  // this chunk's rows are there; with two buffers no wave reads the other one any more
         if (chunk + 1 < chunks) fetch(0);
-        floatx4 o[NT][TI];
+        floatx4 o[NT][OT];
         Frag vf[NT][2 / TPF];
         if (!LOCAL) {
             floatx4 p[3] = {zero, zero, zero};  // (j tile, i tile) (0, 0), (0, 1), (1, 1)
@@ -469,12 +477,13 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
 #pragma unroll
             for (int m = 0; m < NT; ++m)
 #pragma unroll
-                for (int h = 0; h < TI; ++h) o[m][h] = zero;
+                for (int h = 0; h < OT; ++h) o[m][h] = zero;
 #pragma unroll
-            for (int k = 0; k < D / M::KB; ++k) {
-                Frag q[TI];
+            for (int k = 0; k < KT / TPF; ++k) {
+                Frag q[OT];
 #pragma unroll
-                for (int h = 0; h < TI; ++h) q[h] = M::along_q(Q, PQ, 16 * (i0 + h) + n, k * M::KB, g);
+                for (int h = 0; h < OT; ++h)
+                    q[h] = M::along_q(Q, PQ, 16 * ((SPLIT ? 0 : i0) + h) + n, k * M::KB + 16 * tile0, g);
                 if (!SHARE) {
                     const Frag k0 = M::along(K, PK, n, k * M::KB, g);
                     if (TI == 2) {
@@ -495,7 +504,7 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
                     for (int x = 0; x < TPF; ++x) t[x] = S[k * TPF + x][m];
                     const Frag s = M::from(t);
 #pragma unroll
-                    for (int h = 0; h < TI; ++h) o[m][h] = M::mma(s, q[h], o[m][h]);
+                    for (int h = 0; h < OT; ++h) o[m][h] = M::mma(s, q[h], o[m][h]);
                 }
             }
 #pragma unroll
@@ -505,7 +514,8 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
 #pragma unroll
             for (int m = 0; m < NT; ++m)
 #pragma unroll
-                for (int h = 0; h < TI; ++h) o[m][h] *= late[h];
+                for (int h = 0; h < OT; ++h) o[m][h] *= late[h];
+            if (SPLIT) St<float>::st4(passed[wave][l], i0 == 0 ? o[0][OT - 1] : o[0][0]);
             if (ROWS_OUT && !f32 && chunk > 0) {  // the outputs of the chunk before
                 flush(out_rows + (OBUFS == 2 ? ((chunk - 1) & 1) * C * PO : 0), out, flush0);
                 out += (int64_t)C * os;
@@ -523,6 +533,7 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
                     f0[0] = St<T>::ld4(shared_p[0][l]);
                     f1[0] = St<T>::ld4(shared_p[1][l]);
                     f1[1] = St<T>::ld4(shared_p[2][l]);
+                    if (SPLIT) o[0][0] = (i0 == 0 ? o[0][0] : o[0][OT - 1]) + St<float>::ld4(passed[wave ^ COLS][l]);
                 }
             } else {
 #pragma unroll
@@ -579,7 +590,7 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
             fresh = __builtin_amdgcn_exp2f(-l2 * (float)age);
         }
 #pragma unroll
-        for (int h = 0; h < TI; ++h) late[h] = full[h] * power(l2, age);
+        for (int h = 0; h < OT; ++h) late[h] = full[h] * power(l2, age);
         Frag wv[NT][2 / TPF][NP];
 #pragma unroll
         for (int m = 0; m < NT; ++m) {
@@ -609,7 +620,7 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
         for (int t = 0; t < KT; ++t)
 #pragma unroll
             for (int h = 0; h < 2 / TPF; ++h) {
-                const Frag kt = M::down(K, PK, h * M::KB, 16 * t, g, n);
+                const Frag kt = M::down(K, PK, h * M::KB, 16 * (tile0 + t), g, n);
 #pragma unroll
                 for (int c = NP - 1; c >= 0; --c)
 #pragma unroll
@@ -669,21 +680,21 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
         to_state = R.final_state + ((int64_t)u.seq * a.heads + head) * size;
         transposed = R.state_t;
     }
-    if (to_state && i0 == 0) {
+    if (to_state && (SPLIT || i0 == 0)) {
 #pragma unroll
         for (int t = 0; t < KT; ++t)
 #pragma unroll
             for (int m = 0; m < NT; ++m)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int i = 16 * t + 4 * g + r, c = slab + 16 * m + n;
+                    const int i = 16 * (tile0 + t) + 4 * g + r, c = slab + 16 * m + n;
                     if (i < dk && c < dv) to_state[transposed ? c * dk + i : i * dv + c] = S[t][m][r];
                 }
     }
     if (!LOCAL && __syncthreads_or(bad[0] + bad[1] + bad[2] + bad[3] != 0.0f)) {
         __threadfence();  // the outputs as written, also by the wave of the other token tile
         __syncthreads();
-        if (i0 == 0) scan_plain<T, KT, NT>(a, R, head, t0, len, from, to, slab, init);
+        if (i0 == 0) scan_plain<T, D / 16, NT>(a, R, head, t0, len, from, to, slab, init);
     }
 }
 
@@ -895,13 +906,14 @@ hipError_t launch_scan(const ScanArgs& in, hipStream_t s) {
         if (d <= 64) return scan_any<bf16_t, 64, 1, 2>(a, s);
         return scan_any<bf16_t, 128, 2, 2>(a, s);
     }
-    // The fp32 MFMA takes longest: with few units, a wave for each token tile (256
-    // units of 32 columns, 16 chunks: 26 us against 29); with many, one wave for both
-    // keeps the state once (1024 units: 52 against 66; 2048 of 16 columns, backward:
-    // 129 against 149). bf16 gains nothing from the split (32 units 15 us both ways).
-    const bool few = a.slots * a.heads * a.n_roles <= 512;
-    if (d <= 16) return few ? scan_any<float, 16, 1, 1>(a, s) : scan_any<float, 16, 1, 2>(a, s);
-    if (d <= 32) return few ? scan_any<float, 32, 1, 1>(a, s) : scan_any<float, 32, 1, 2>(a, s);
+    // The fp32 MFMA takes longest, so up to 32 columns a wave takes one token tile:
+    // at 32 with half of the state (2048 units of 16 chunks 121 us, 139 with whole
+    // states and both tiles; 256 units 24 and 29), at 16 only where units are few
+    // (32 units 18 us against 22; 2048 units' gradients 149 against 130). bf16 gains
+    // nothing from it (32 units 15 us both ways, 2048 units 61 against 57).
+    if (d <= 16)
+        return a.slots * a.heads * a.n_roles <= 512 ? scan_any<float, 16, 1, 1>(a, s) : scan_any<float, 16, 1, 2>(a, s);
+    if (d <= 32) return scan_any<float, 32, 1, 1>(a, s);
     if (d <= 64) return scan_any<float, 64, 1, 2>(a, s);
     return scan_any<float, 128, 2, 2>(a, s);
 }
