@@ -1,13 +1,18 @@
 """Build libmdlstm.so (the C-ABI library and its HIP kernels) for gfx950, in-tree.
 
+The sequence operators' Python binding (_binding.so, csrc/binding.cpp) is built
+beside it with the host compiler against torch's headers.
+
 Usage: python -m paper_1902_11208_amd.build [--verbose]
 """
 from __future__ import annotations
 
 import concurrent.futures as cf
+import importlib.util
 import os
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -15,7 +20,10 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libmdlstm.so")
+BINDING = os.path.join(PKG, "_binding.so")
+ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+CXX = os.environ.get("CXX", "g++")
 ARCH = "gfx950"
 
 SOURCES = ["mdlstm_api.cpp", "k_pack.hip", "k_proj.hip", "k_wave.hip", "k_wave_fwd_f32_h4.hip", "k_wave_fwd_f32_h8.hip",
@@ -55,17 +63,44 @@ def _compile(src: str, verbose: bool) -> str:
     return obj
 
 
+def _torch() -> str:
+    return os.path.dirname(importlib.util.find_spec("torch").origin)  # found, not imported: that takes longer
+
+
+def _compile_binding() -> str:
+    obj, t = os.path.join(BUILD, "binding.o"), _torch()
+    includes = [os.path.join(t, "include"), os.path.join(t, "include", "torch", "csrc", "api", "include"),
+                sysconfig.get_paths()["include"], os.path.join(ROCM, "include")]
+    cmd = [CXX, "-O2", "-fPIC", "-std=c++17", "-DTORCH_EXTENSION_NAME=_binding", "-D_GLIBCXX_USE_CXX11_ABI=1", "-DUSE_ROCM",
+           "-D__HIP_PLATFORM_AMD__", "-I", INCLUDE, *[x for i in includes for x in ("-isystem", i)], "-c",
+           os.path.join(CSRC, "binding.cpp"), "-o", obj]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{CXX} failed on binding.cpp:\n{r.stdout}\n{r.stderr}")
+    return obj
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
-    jobs = min(len(SOURCES), max(1, min(16, os.cpu_count() or 1)))
+    jobs = min(len(SOURCES) + 1, max(1, min(16, os.cpu_count() or 1)))
     with cf.ThreadPoolExecutor(jobs) as ex:
+        binding = ex.submit(_compile_binding)
         objs = list(ex.map(lambda s: _compile(s, verbose), SOURCES))
+        binding = binding.result()
     tmp = LIB + ".tmp"
     cmd = [HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-Wl,--no-undefined", *objs, "-o", tmp]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, LIB)
+    lib = os.path.join(_torch(), "lib")
+    tmp = BINDING + ".tmp"
+    cmd = [CXX, "-shared", binding, "-o", tmp, "-L", lib, "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_hip",
+           "-L", PKG, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"link of the binding failed:\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, BINDING)
     return LIB
 
 

@@ -368,6 +368,50 @@ def test_steps_follow_a_prompt():
     _check("state", st, _np(final), 1e-5)
 
 
+def test_binding_refuses_wrong_tensors():
+    """Shapes, types, devices and layouts that the kernels would misread."""
+    sq = _seq()
+    op = sq.DecayAttention([3, 4], 4, 8, 6, torch.zeros(4, device="cuda"), dtype=torch.float32, kv_heads=2)
+    q, k, v = (torch.zeros(7, h, d, device="cuda") for h, d in ((4, 8), (2, 8), (2, 6)))
+    st = torch.zeros(2, 4, 8, 6, device="cuda")
+    with pytest.raises(ValueError, match="forward call"):
+        op.backward(torch.zeros(7, 4, 6, device="cuda"))
+    for a, says in (((q[:6], k, v), "q has shape"), ((q, q, v), "k has shape"), ((q, k, k), "v has shape"),
+                    ((q.bfloat16(), k, v), "q has dtype"), ((q.cpu(), k, v), "q is on"),
+                    ((torch.zeros(7, 4, 16, device="cuda")[:, :, ::2], k, v), "last dimension")):
+        with pytest.raises(ValueError, match=says):
+            op.forward(*a)
+    with pytest.raises(ValueError, match="state has shape"):
+        op.forward(q, k, v, state=st[:1])
+    with pytest.raises(ValueError, match="state must be contiguous"):
+        op.forward(q, k, v, state=torch.zeros(2, 4, 6, 8, device="cuda").transpose(2, 3))
+    op.forward(q, k, v, state=st)
+    with pytest.raises(ValueError, match="do has shape"):
+        op.backward(q)
+    with pytest.raises(ValueError, match="dstate has dtype"):
+        op.backward(torch.zeros(7, 4, 6, device="cuda"), dstate=st.double())
+    norm = sq.ResidualNorm(torch.ones(8, device="cuda"), 5, dtype=torch.float32)
+    x = torch.zeros(5, 8, device="cuda")
+    with pytest.raises(ValueError, match="forward call"):
+        norm.backward(x)
+    for t, r, says in ((x[:4], None, "x has shape"), (x.bfloat16(), None, "x has dtype"), (x, x.cpu(), "residual is on"),
+                       (torch.zeros(8, 5, device="cuda").t(), None, "contiguous along its rows"),
+                       (x[:1].expand(5, 8), None, "overlap")):
+        with pytest.raises(ValueError, match=says):
+            norm.forward(t, r)
+    norm.forward(x)
+    with pytest.raises(ValueError, match="dy must be contiguous"):
+        norm.backward(torch.zeros(5, 16, device="cuda")[:, :8])
+    with pytest.raises(ValueError, match="not a 64-bit"):
+        norm.forward(x, seed=-1)
+    from paper_1902_11208_amd import MdlstmError
+
+    with pytest.raises(MdlstmError, match="probability"):  # what the library refuses
+        sq.dropout(x, 1.5, 0)
+    with pytest.raises(ValueError, match="at most 128"):
+        sq.DecayAttention([3], 4, 200, 6, torch.zeros(4, device="cuda"))
+
+
 # --- norm and dropout ----------------------------------------------------------
 def _strided(rng, rows, cols, dtype, layout):
     if layout == "contiguous":

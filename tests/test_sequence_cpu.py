@@ -159,17 +159,32 @@ def test_binding_refusals():
         sequence.DecayAttention([1, 1], 2, 4, 4, torch.zeros(2), dtype=torch.float16)
     with pytest.raises(ValueError):
         sequence.decay_attention_step(x, x, x, x, x)
-    # views as the kernels index them
-    t = torch.zeros(5, 3, 8)
-    h = sequence._heads(t[:, :, ::1], "t", 5, 3, 8, torch.float32, t.device)
-    assert (h.token_stride, h.head_stride) == (24, 8)
-    for bad in (t[:, :, ::2], t.transpose(0, 1), t.double(), t[:4], None):
-        with pytest.raises(ValueError):
-            sequence._heads(bad, "t", 5, 3, 8, torch.float32, t.device)
-    assert sequence._rows(torch.zeros(4, 20)[:, :8], "x", (4, 8), torch.float32, x.device) == 20
-    for bad in (torch.zeros(8, 4).t(), torch.zeros(4, 16)[:, ::2], torch.zeros(1, 8).expand(4, 8), torch.zeros(4, 8).half()):
-        with pytest.raises(ValueError):
-            sequence._rows(bad, "x", (4, 8), torch.float32, x.device)
+    # the step's and dropout's defects are told before they find no device
+    q, st, rates = torch.zeros(5, 4, 8), torch.zeros(9, 4, 8, 6), torch.zeros(4)
+    k, v, slots = torch.zeros(5, 2, 8), torch.zeros(5, 2, 6), torch.zeros(5, dtype=torch.int32)
+    good = dict(q=q, k=k, v=v, state=st, rates=rates, slots=slots, out=torch.zeros(5, 4, 6))
+    wide = torch.zeros(5, 4, 16)
+    for change, says in ((dict(), "device"), (dict(q=wide[:, :, :8]), "device"), (dict(q=wide[:, :, ::2]), "last dimension"),
+                         (dict(q=torch.zeros(5, 32)), "3 dimensions"), (dict(k=torch.zeros(4, 2, 8)), "k has shape"),
+                         (dict(v=v.double()), "v has dtype"), (dict(state=st.transpose(1, 2).contiguous()), "state has shape"),
+                         (dict(state=st.bfloat16()), "state has dtype"), (dict(state=st.transpose(0, 1)), "shape"),
+                         (dict(rates=torch.zeros(3)), "rates"), (dict(slots=slots.long()), "slots has dtype"),
+                         (dict(slots=slots[:3]), "slots has shape"), (dict(out=torch.zeros(5, 4, 12)[:, :, ::2]), "contiguous")):
+        a = dict(good, **change)
+        with pytest.raises(ValueError, match=says):
+            sequence.decay_attention_step(a["q"], a["k"], a["v"], a["state"], a["rates"], slots=a["slots"], out=a["out"])
+    with pytest.raises(TypeError):
+        sequence.decay_attention_step(q.half(), k.half(), v.half(), st, rates)
+    with pytest.raises(TypeError):
+        sequence.decay_attention_step(None, k, v, st, rates)
+    for t, r, o, says in ((x, x[:3], None, "residual has shape"), (x, x.double(), None, "residual has dtype"),
+                          (x, None, torch.zeros(8, 4).t(), "out must be contiguous"), (torch.zeros(4, 16)[:, ::2], None, None, "rows"),
+                          (torch.zeros(1, 8).expand(4, 8), None, None, "overlap"), (torch.zeros(2, 3, 4).transpose(0, 1), None, None, "two-dim"),
+                          (torch.zeros(4, 20)[:, :8], None, None, "device")):
+        with pytest.raises(ValueError, match=says):
+            sequence.dropout(t, 0.5, 1, residual=r, out=o)
+    with pytest.raises(TypeError):
+        sequence.dropout(x.half(), 0.5, 1)
     with pytest.raises(ValueError):
         sequence._u64(-1, "seed")
     with pytest.raises(ValueError):
