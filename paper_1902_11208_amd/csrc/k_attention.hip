@@ -917,11 +917,13 @@ hipError_t launch_scan(const ScanArgs& in, hipStream_t s) {
     }
     // The fp32 MFMA takes longest, so up to 32 columns a wave takes one token tile:
     // at 32 with half of the state (2048 units of 16 chunks 121 us, 139 with whole
-    // states and both tiles; 256 units 24 and 29), at 16 only where units are few
-    // (32 units 18 us against 22; 2048 units' gradients 149 against 130). bf16 gains
-    // nothing from it (32 units 15 us both ways, 2048 units 61 against 57).
+    // states and both tiles; 256 units 24 and 29), at 16 only up to a unit a SIMD
+    // (32 units 18 us against 22; 1024 units of 8 to 400 tokens, log-normal about 100,
+    // 16.4 against 19.0, of 200 each 13.7 against 13.8; gradients as 1536 units of 50
+    // tokens 11.1 against 8.6). bf16 gains nothing from it (32 units 15 us both ways,
+    // 2048 units 61 against 57).
     if (d <= 16)
-        return a.slots * a.heads * a.n_roles <= 512 ? scan_any<float, 16, 1, 1>(a, s) : scan_any<float, 16, 1, 2>(a, s);
+        return a.slots * a.heads * a.n_roles <= 1024 ? scan_any<float, 16, 1, 1>(a, s) : scan_any<float, 16, 1, 2>(a, s);
     if (d <= 32) return scan_any<float, 32, 1, 1>(a, s);
     if (d <= 64) return scan_any<float, 64, 1, 2>(a, s);
     return scan_any<float, 128, 2, 2>(a, s);
