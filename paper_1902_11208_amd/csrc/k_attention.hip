@@ -48,8 +48,8 @@ __device__ __forceinline__ void sequence(const int64_t* offsets, int i, int64_t 
 // What bounds it: memory where the heads are 64 and more wide and units are many
 // (1024 units of 1024 tokens, 128 columns bf16, 1.07 GB: 240 us, 4.5 TB/s; 64
 // columns 115 us, 4.7 TB/s, where a copy reaches 5.5), the latency of a chunk
-// where they are few (a unit alone: 0.9 us a chunk at 64 bf16 columns, 2.0 at 128,
-// 1.0 at 32 fp32), and the fp32 MFMA at 128 fp32 columns (3.1 TB/s). C = 32 and not
+// where they are few (a unit alone: 0.9 us a chunk at 64 bf16 columns, 1.7 at 128,
+// 1.1 at 32 fp32), and the fp32 MFMA at 128 fp32 columns (3.1 TB/s). C = 32 and not
 // 64: the products inside a chunk grow with C, the state's do not, and a chunk of
 // 64 rows would leave one workgroup a CU at 128 columns.
 // ---------------------------------------------------------------------------
@@ -163,7 +163,7 @@ __device__ __forceinline__ bool unit_of(const ScanArgs& a, Unit& u) {
     u.head = (int)(rest % kv) * group + in / a.n_roles;
     u.j = 0;
     u.seq = (int)u.slot;
-    if (!a.seg && a.order) {  // longest first: the wide batch's gradients 269 -> 212 us
+    if (!a.seg && a.order) {  // longest first: the wide batch's gradients 255 -> 229 us
         u.seq = __builtin_amdgcn_readfirstlane(a.order[u.slot]);
         if (u.seq < 0 || u.seq >= a.n) return false;
     }
@@ -716,6 +716,8 @@ __global__ __launch_bounds__(256) void k_join_segments(ScanArgs a) {
     const int x = blockIdx.y * 256 + threadIdx.x;
     int64_t t0, len;
     sequence(a.offsets, seq, a.tokens, a.longest, t0, len);
+    t0 = uniform(t0);
+    len = uniform(len);
     if (x >= size || (len <= a.seg && !R.final_state)) return;
     const double rate = a.rates[head];
     const double gd = exp(-rate * (double)a.seg);
@@ -726,19 +728,33 @@ __global__ __launch_bounds__(256) void k_join_segments(ScanArgs a) {
     float* p = a.states + (((int64_t)blockIdx.z * a.heads + head) * a.slots + slot0) * size + x;
     const int64_t step = size;
     const int joins = len > 0 ? (int)((len - 1) / a.seg) : 0;
-    constexpr int N = 32;  // loads in flight
-    for (int j = 0; j < joins; j += N) {
-        float v[N];
+    // Latency bounds it: N loads are in flight while the N before are joined, and
+    // the last ones read a slot again rather than branch (128 segments of 8 heads of
+    // 64 x 64, 34 MB: 10.4 us, 13.0 with rounds of 32 one after the other).
+    constexpr int N = 16;
+    float v[N], next[N];
+    auto load = [&](float(&to)[N], int j) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = j + i < joins ? p[i * step] : 0.0f;
+        for (int i = 0; i < N; ++i) to[i] = p[min(j + i, joins - 1) * step];
+    };
+    if (joins > 0) load(v, 0);
+    int j = 0;
+    for (; j + N < joins; j += N) {
+        load(next, j + N);
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (j + i < joins) {
-                s = fmaf(s, gs, fmaf(s, gs_lo, v[i]));
-                p[i * step] = s;
-            }
-        p += N * step;
+        for (int i = 0; i < N; ++i) {
+            s = fmaf(s, gs, fmaf(s, gs_lo, v[i]));
+            p[(j + i) * step] = s;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = next[i];
     }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (j + i < joins) {
+            s = fmaf(s, gs, fmaf(s, gs_lo, v[i]));
+            p[(j + i) * step] = s;
+        }
     if (R.final_state) {
         const float last = a.states[(((int64_t)blockIdx.z * a.heads + head) * a.slots + slot0 + joins) * size + x];
         const double g = exp(-rate * (double)(len - joins * a.seg));
@@ -849,7 +865,7 @@ __global__ __launch_bounds__(256) void k_step(StepArgs a) {
 // pass over k and v, the states between them and two more launches, so they are
 // taken only where the longest sequence would keep half of the chip or more idle
 // (64 sequences of 200 to 600 tokens, 4 heads of 32 fp32: 28 us whole, 37 us in
-// segments; one of 2048, 8 heads of 64: 27 us in segments, about 60 whole). They
+// segments; one of 2048, 8 heads of 64: 21 us in segments, 63 whole). They
 // are as long as fills the chip once: four workgroups a CU, two above 64
 // columns (one sequence of 32768, 8 heads of 128 bf16: 105 us with two, 127 with
 // four; of 65536, 8 heads of 64: 88 us with four, 103 with one and a half).
