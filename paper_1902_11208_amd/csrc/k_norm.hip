@@ -8,8 +8,7 @@
 // residual and dropout, 96000 x 512 bf16, 66 us forward (6.0 TB/s) and 100 us
 // backward (4.9 TB/s) with 4 us for dw's shares; 8-bit output, 16383 x 5000 bf16,
 // 116 us (4.9 TB/s). A block of the generator (ten rounds of two 32-bit products)
-// serves eight elements, 16 bits each, so it stays below the memory's time; with
-// 32 bits an element it would be about even with it at two bytes an element.
+// serves eight elements, 16 bits each, so it stays below the memory's time.
 #include <algorithm>
 #include <type_traits>
 
