@@ -254,11 +254,11 @@ __device__ __forceinline__ void scan_plain(const ScanArgs& a, const ScanRole& R,
     const int l = threadIdx.x & 63, g = l >> 4, n = l & 15, dk = R.q.dim, dv = R.v.dim;
     const float decay = expf(-a.rates[head]);
     floatx4 S[KT][NT];
-    init(S, 0);
+    init(S, 0);  // in reverse, also that of a later segment has decayed up to its first token
     for (int64_t pos = from; pos < to; ++pos) {
         const int64_t t = R.reverse ? t0 + len - 1 - pos : t0 + pos;
         const T *q = at<T>(R.q, t, head), *k = at<T>(R.k, t, head), *v = at<T>(R.v, t, head);
-        const float f = R.reverse && pos == 0 ? 1.0f : decay;
+        const float f = R.reverse && pos == from ? 1.0f : decay;
         float o[NT], x[NT];
 #pragma unroll
         for (int m = 0; m < NT; ++m) {
