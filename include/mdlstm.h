@@ -433,7 +433,8 @@ mdlstm_status mdlstm_head_backward(const mdlstm_head_desc* desc, int32_t canvas_
  * three parts of one projection's output): element strides between tokens and
  * between heads are given, the last dimension is contiguous and strides are
  * not negative. Outputs are contiguous. Outputs must not overlap inputs or
- * each other.
+ * each other, where a call does not say otherwise; the packed attention calls
+ * refuse buffers that do (a view counts from its first element to its last).
  */
 typedef struct {
     const void* d_data;

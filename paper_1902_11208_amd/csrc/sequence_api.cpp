@@ -91,6 +91,31 @@ mdlstm_status check_out(const void* p, const char* name, bool needed, size_t to)
     return MDLSTM_OK;
 }
 
+// The bytes of an argument, and whether the call writes them.
+struct Span {
+    const char* name;
+    uintptr_t from, size;
+    bool written;
+};
+Span span(const char* name, const void* p, int64_t bytes, bool written) {
+    return Span{name, reinterpret_cast<uintptr_t>(p), p ? (uintptr_t)bytes : 0, written};
+}
+// From a view's first element to its last.
+Span span(const char* name, const mdlstm_heads* v, int64_t tokens, int32_t heads, int32_t dim, int32_t dtype) {
+    const int64_t last = (tokens - 1) * v->token_stride + (heads - 1) * v->head_stride + dim;
+    return span(name, v->d_data, tokens > 0 ? last * (int64_t)element(dtype) : 0, false);
+}
+
+// Nothing that the call writes may overlap anything else: workgroups read and write in no order.
+template <size_t N>
+mdlstm_status check_apart(const Span (&s)[N]) {
+    for (size_t i = 0; i < N; ++i)
+        for (size_t j = 0; j < N && s[i].written; ++j)
+            if (j != i && s[i].size && s[j].size && s[i].from < s[j].from + s[j].size && s[j].from < s[i].from + s[i].size)
+                return fail(MDLSTM_ERR_INVALID_ARG, "%s overlaps %s", s[i].name, s[j].name);
+    return MDLSTM_OK;
+}
+
 mdl::HeadView view(const mdlstm_heads* v, int group, int dim) {
     return mdl::HeadView{v->d_data, v->token_stride, v->head_stride, group, dim};
 }
@@ -215,6 +240,14 @@ mdlstm_status mdlstm_attention_forward(const mdlstm_attention_desc* desc, int32_
     OK_OR_RETURN(check_out(d_final, "final", false, 16));
     const AttentionPlan p = attention_plan(desc, n, tokens, longest, false);
     OK_OR_RETURN(check_workspace(d_workspace, workspace_bytes, p.total));
+    const int64_t es = (int64_t)element(desc->dtype), states = (int64_t)n * desc->heads * desc->dim_k * desc->dim_v * 4;
+    OK_OR_RETURN(check_apart({span("o", d_o, tokens * desc->heads * desc->dim_v * es, true), span("final", d_final, states, true),
+                              span("the workspace", d_workspace, (int64_t)p.total, true),
+                              span("q", q, tokens, desc->heads, desc->dim_k, desc->dtype),
+                              span("k", k, tokens, desc->kv_heads, desc->dim_k, desc->dtype),
+                              span("v", v, tokens, desc->kv_heads, desc->dim_v, desc->dtype), span("state", d_state, states, false),
+                              span("offsets", d_offsets, ((int64_t)n + 1) * 8, false), span("order", d_order, (int64_t)n * 4, false),
+                              span("rates", d_rates, (int64_t)desc->heads * 4, false)}));
     if (n == 0) return MDLSTM_OK;
     OK_OR_RETURN(mdl::poison_workspace(d_workspace, p.total, stream));
     mdl::ScanArgs a = scan_args(desc, n, tokens, longest, d_offsets, d_order, d_rates);
@@ -251,6 +284,18 @@ mdlstm_status mdlstm_attention_backward(const mdlstm_attention_desc* desc, int32
     OK_OR_RETURN(check_out(d_dstate, "dstate", false, 16));
     const AttentionPlan p = attention_plan(desc, n, tokens, longest, true);
     OK_OR_RETURN(check_workspace(d_workspace, workspace_bytes, p.total));
+    const int64_t es = (int64_t)element(desc->dtype), states = (int64_t)n * desc->heads * desc->dim_k * desc->dim_v * 4;
+    OK_OR_RETURN(check_apart({span("dq", d_dq, tokens * desc->heads * desc->dim_k * es, true),
+                              span("dk", d_dk, tokens * desc->kv_heads * desc->dim_k * es, true),
+                              span("dv", d_dv, tokens * desc->kv_heads * desc->dim_v * es, true),
+                              span("dstate", d_dstate, states, true), span("the workspace", d_workspace, (int64_t)p.total, true),
+                              span("q", q, tokens, desc->heads, desc->dim_k, desc->dtype),
+                              span("k", k, tokens, desc->kv_heads, desc->dim_k, desc->dtype),
+                              span("v", v, tokens, desc->kv_heads, desc->dim_v, desc->dtype), span("state", d_state, states, false),
+                              span("grad_o", grad_o, tokens, desc->heads, desc->dim_v, desc->dtype),
+                              span("dfinal", d_dfinal, states, false), span("offsets", d_offsets, ((int64_t)n + 1) * 8, false),
+                              span("order", d_order, (int64_t)n * 4, false),
+                              span("rates", d_rates, (int64_t)desc->heads * 4, false)}));
     if (n == 0) return MDLSTM_OK;
     OK_OR_RETURN(mdl::poison_workspace(d_workspace, p.total, stream));
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);

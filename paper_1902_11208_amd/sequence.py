@@ -40,6 +40,12 @@ def _u64(v, name: str) -> int:
     return v
 
 
+def _apart(a: torch.Tensor, b) -> bool:
+    """False where two contiguous tensors share memory."""
+    return not isinstance(b, torch.Tensor) or (a.data_ptr() + a.nbytes <= b.data_ptr() or
+                                               b.data_ptr() + b.nbytes <= a.data_ptr())
+
+
 class DecayAttention:
     """Linear attention with a decay for each head over packed sequences.
 
@@ -50,6 +56,11 @@ class DecayAttention:
     widths of an output layer's rectangles; zero is allowed. rates: [heads] fp32
     device tensor, >= 0. kv_heads: heads of k and v, shared by heads / kv_heads
     query heads each. scale: 1 / sqrt(dim_k) unless given.
+
+    States that a call returned may be given back to the object, to go through
+    sequences piece by piece: a call writes to a buffer that neither its
+    arguments nor the forward call it belongs to use. Its other outputs must not
+    be its inputs.
     """
 
     def __init__(self, lengths, heads: int, dim_k: int, dim_v: int, rates: torch.Tensor, dtype=torch.bfloat16,
@@ -76,8 +87,16 @@ class DecayAttention:
         self._op = _binding.Attention(self.heads, self.kv_heads, self.dim_k, self.dim_v, desc.dtype, desc.scale, self.n,
                                       self.tokens, self.longest, self.offsets, self.order, rates)
         self._ws = [None, None]
-        self._o = self._final = self._grads = self._dstate = None
-        self._saved = None
+        self._o = self._grads = self._saved = None
+        self._finals, self._dstates = [], []
+
+    def _spare(self, buffers: list, *used) -> torch.Tensor:
+        """The first of the buffers of states that none of `used` lies in."""
+        for b in buffers:
+            if all(_apart(b, u) for u in used):
+                return b
+        buffers.append(torch.empty(self._state_shape, dtype=torch.float32, device=self.device))
+        return buffers[-1]
 
     def _workspace(self, backward: int) -> torch.Tensor:
         if self._ws[backward] is None:
@@ -89,11 +108,10 @@ class DecayAttention:
         state: the states they start from (None: zero). q, k, v may be views of one projection's output."""
         if self._o is None:
             self._o = torch.empty((self.tokens, self.heads, self.dim_v), dtype=self.dtype, device=self.device)
-        if final_state and self._final is None:
-            self._final = torch.empty(self._state_shape, dtype=torch.float32, device=self.device)
-        self._op.forward(q, k, v, state, self._o, self._final if final_state else None, self._workspace(0), _stream(stream))
+        final = self._spare(self._finals, state) if final_state else None
+        self._op.forward(q, k, v, state, self._o, final, self._workspace(0), _stream(stream))
         self._saved = (q, k, v, state)
-        return (self._o, self._final) if final_state else self._o
+        return (self._o, final) if final_state else self._o
 
     def backward(self, do, dstate=None, stream=None):
         """(dq, dk, dv) after a forward call, from the gradient of o (and of the final states, dstate); where the
@@ -104,11 +122,9 @@ class DecayAttention:
         if self._grads is None:
             self._grads = tuple(torch.empty((self.tokens, h, d), dtype=self.dtype, device=self.device) for h, d in (
                 (self.heads, self.dim_k), (self.kv_heads, self.dim_k), (self.kv_heads, self.dim_v)))
-        if state is not None and self._dstate is None:
-            self._dstate = torch.empty(self._state_shape, dtype=torch.float32, device=self.device)
-        self._op.backward(q, k, v, state, do, dstate, *self._grads, None if state is None else self._dstate,
-                          self._workspace(1), _stream(stream))
-        return self._grads if state is None else self._grads + (self._dstate,)
+        out = None if state is None else self._spare(self._dstates, state, dstate)
+        self._op.backward(q, k, v, state, do, dstate, *self._grads, out, self._workspace(1), _stream(stream))
+        return self._grads if state is None else self._grads + (out,)
 
 
 def decay_attention_step(q, k, v, state, rates, slots=None, scale: float = None, out=None, stream=None) -> torch.Tensor:

@@ -72,3 +72,51 @@ def test_gradients_before_a_bad_value_in_a_later_segment(dtype, d, bad):
     for got, want in ((dk, wk), (dv, wv)):
         assert torch.isfinite(got[T - at:]).all() and not torch.isfinite(got[:T - at, 1, 5]).any()
         _check("other columns", got[:, :, :5], want[:, :, :5], TOL[dtype])
+
+
+@pytest.mark.parametrize("lengths,d,dtype", [([33, 0, 70], 32, "f32"), ([33, 0, 70], 64, "bf16"), ([1500, 900], 64, "f32"),
+                                             ([1500, 900], 128, "bf16")])
+def test_states_of_an_object_passed_back_to_it(lengths, d, dtype):
+    """Three pieces of the same sequences through one object, whole and in segments: each piece starts from the states
+    that the one before left, each backward call takes the state gradients that the one before gave."""
+    rng = np.random.default_rng(sum(lengths) + d)
+    T, n, heads = sum(lengths), len(lengths), 2
+    print(f"case: three pieces of {lengths}, {d} columns, {dtype}", flush=True)
+    a = torch.from_numpy(rng.uniform(0.01, 0.1, heads).astype(np.float32)).cuda()
+    op = _seq().DecayAttention(lengths, heads, d, d, a, dtype=DT[dtype])
+    state, dstate = _rand(rng, n, heads, d, d), _rand(rng, n, heads, d, d)
+    for piece in range(3):
+        q, k, v, do = (_rand(rng, T, heads, d, dtype=dtype) for _ in range(4))
+        before = state.clone()
+        args = _np(q), _np(k), _np(v), lengths, _np(a), d ** -0.5
+        o, final = op.forward(q, k, v, state=state, final_state=True)
+        wo, wf = orc.attention_forward(*args, _np(before))
+        _check("o", o, wo, TOL[dtype])
+        _check("final", final, wf, TOL32[dtype])
+        assert torch.equal(state, before), "the call wrote to its own input"
+        for _ in range(2):
+            given = dstate.clone()
+            *grads, ds = op.backward(do, dstate=dstate)
+            want = orc.attention_backward(*args, _np(do), _np(before), _np(given))
+            for name, g, w in zip(("dq", "dk", "dv"), grads, want):
+                _check(name, g, w, TOL[dtype])
+            _check("dstate", ds, want[3], TOL32[dtype])
+            assert torch.equal(dstate, given), "the call wrote to its own input"
+            dstate = ds
+        state = final
+
+
+def test_attention_refuses_its_other_outputs_as_inputs():
+    """Outputs and gradients of an object as its own inputs, which workgroups would read and write in no order."""
+    from paper_1902_11208_amd import MdlstmError
+
+    op = _seq().DecayAttention([40, 30], 2, 32, 32, torch.zeros(2, device="cuda"), dtype=torch.float32)
+    q = torch.ones(70, 2, 32, device="cuda")
+    o = op.forward(q, q, q)
+    for args in ((o, q, q), (q, o, q), (q, q, o)):
+        with pytest.raises(MdlstmError, match="o overlaps"):
+            op.forward(*args)
+    dq, dk, dv = op.backward(o)  # o is no output of that call
+    for g in (dq, dk, dv):
+        with pytest.raises(MdlstmError, match="overlaps grad_o"):
+            op.backward(g)
