@@ -242,23 +242,45 @@ __device__ __forceinline__ int64_t uniform(int64_t x) {
                      (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
 }
 
-// Keeps a value in its register where the compiler would rather compute it again.
-__device__ __forceinline__ void keep(float& x) { asm volatile("" : "+v"(x)); }
+// Has a value computed here, not again or later on.
+template <typename V>
+__device__ __forceinline__ void keep(V& x) {
+    asm volatile("" : "+v"(x));
+}
 
-// Outputs of a wave that came out infinite or NaN, taken again one token at a
-// time: in a chunk's product a value that is not finite reaches the tokens
-// before it as 0 v = NaN. Finite outputs stay as they are.
-template <typename T, int KT, int NT, typename Init>
+// exp(x) to about 2^-48 as a sum of two positive numbers, so that an infinite
+// state times it stays infinite.
+struct Decay {
+    float hi, lo;
+};
+__device__ __forceinline__ Decay decay_of(double x) {
+    constexpr float least = 0x1p-149f;
+    const double e = exp(x);
+    float hi = (float)e;
+    if ((double)hi > e) hi = __uint_as_float(__float_as_uint(hi) - 1);
+    if (hi < least) hi = least;
+    const float lo = (float)(e - (double)hi);
+    return Decay{hi, lo < least ? least : lo};
+}
+
+__device__ __forceinline__ bool not_finite(float x) { return !(x - x == 0.0f); }
+
+// Outputs and states of a wave that came out infinite or NaN, taken again one
+// token at a time. In a chunk's products a value that is not finite reaches
+// other tokens and rows as 0 v = NaN, and a bf16 operand's pieces as v - v; a
+// state beyond 2^120 overflows in registers that hold up to 2^8 times of it.
+// What came out finite stays as it is.
+template <typename T, int KT, int NT, bool LOCAL, typename Init>
 __device__ __forceinline__ void scan_plain(const ScanArgs& a, const ScanRole& R, int head, int64_t t0, int64_t len, int64_t from,
-                                        int64_t to, int slab, Init init) {
+                                        int64_t to, int slab, float* to_state, bool transposed, Init init) {
     const int l = threadIdx.x & 63, g = l >> 4, n = l & 15, dk = R.q.dim, dv = R.v.dim;
-    const float decay = expf(-a.rates[head]);
+    const Decay once = decay_of(-(double)a.rates[head]), none = decay_of(0.0);
     floatx4 S[KT][NT];
     init(S, 0);  // in reverse, also that of a later segment has decayed up to its first token
     for (int64_t pos = from; pos < to; ++pos) {
         const int64_t t = R.reverse ? t0 + len - 1 - pos : t0 + pos;
         const T *q = at<T>(R.q, t, head), *k = at<T>(R.k, t, head), *v = at<T>(R.v, t, head);
-        const float f = R.reverse && pos == from ? 1.0f : decay;
+        const Decay f = R.reverse && pos == from ? none : once;
         float o[NT], x[NT];
 #pragma unroll
         for (int m = 0; m < NT; ++m) {
@@ -271,15 +293,15 @@ __device__ __forceinline__ void scan_plain(const ScanArgs& a, const ScanRole& R,
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int row = 16 * i + 4 * g + r;
-                const float kr = row < dk ? St<T>::ld1(k + row) : 0.0f, qr = row < dk ? St<T>::ld1(q + row) : 0.0f;
+                const float kr = row < dk ? St<T>::ld1(k + row) : 0.0f, qr = !LOCAL && row < dk ? St<T>::ld1(q + row) : 0.0f;
 #pragma unroll
                 for (int m = 0; m < NT; ++m) {
-                    S[i][m][r] = row < dk ? fmaf(kr, x[m], S[i][m][r] * f) : 0.0f;
+                    S[i][m][r] = row < dk ? fmaf(S[i][m][r], f.hi, fmaf(S[i][m][r], f.lo, kr * x[m])) : 0.0f;
                     o[m] = fmaf(qr, S[i][m][r], o[m]);
                 }
             }
 #pragma unroll
-        for (int m = 0; m < NT; ++m) {
+        for (int m = 0; m < NT && !LOCAL; ++m) {
             o[m] += __shfl_xor(o[m], 16);
             o[m] += __shfl_xor(o[m], 32);
             const int c = slab + 16 * m + n;
@@ -287,15 +309,28 @@ __device__ __forceinline__ void scan_plain(const ScanArgs& a, const ScanRole& R,
                 const int64_t at_o = (t * a.heads + head) * dv + c;
                 if (R.out_f32) {
                     float* d = static_cast<float*>(R.out) + at_o;
-                    if (!(*d - *d == 0.0f)) *d = o[m] * R.out_scale;
+                    if (not_finite(*d)) *d = o[m] * R.out_scale;
                 } else {
                     T* d = static_cast<T*>(R.out) + at_o;
-                    const float was = St<T>::ld1(d);
-                    if (!(was - was == 0.0f)) St<T>::st1(d, o[m] * R.out_scale);
+                    if (not_finite(St<T>::ld1(d))) St<T>::st1(d, o[m] * R.out_scale);
                 }
             }
         }
     }
+    if (!to_state) return;
+    const Decay f = R.reverse && to > from ? once : none;
+#pragma unroll
+    for (int i = 0; i < KT; ++i)
+#pragma unroll
+        for (int m = 0; m < NT; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int row = 16 * i + 4 * g + r, c = slab + 16 * m + n;
+                if (row < dk && c < dv) {
+                    float* d = to_state + (transposed ? c * dk + row : row * dv + c);
+                    if (not_finite(*d)) *d = fmaf(S[i][m][r], f.hi, S[i][m][r] * f.lo);
+                }
+            }
 }
 
 // A workgroup's waves share a unit's chunk. A wave has NT column tiles of the
@@ -452,7 +487,7 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
     };
     const int chunks = (int)((to - from + C - 1) / C);
     const floatx4 zero = {0, 0, 0, 0};
-    floatx4 bad = zero;  // NaN once a value was not finite
+    floatx4 bad = zero;  // NaN once an output was not finite
     int row0 = skip, flush0 = skip;
     if (chunks > 0) {
         fetch(skip);
@@ -522,7 +557,10 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
 #pragma unroll
             for (int m = 0; m < NT; ++m)
 #pragma unroll
-                for (int h = 0; h < OT; ++h) o[m][h] *= late[h];
+                for (int h = 0; h < OT; ++h) {
+                    o[m][h] *= late[h];
+                    keep(o[m][h]);  // beyond the branch below it was read before the matrix instruction had written it
+                }
             if (SPLIT) St<float>::st4(passed[wave][l], i0 == 0 ? o[0][OT - 1] : o[0][0]);
             if (ROWS_OUT && !f32 && chunk > 0) {  // the outputs of the chunk before
                 flush(out_rows + (OBUFS == 2 ? ((chunk - 1) & 1) * C * PO : 0), out, flush0);
@@ -564,19 +602,6 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
 #pragma unroll
                     for (int h = 0; h < 2 / TPF; ++h) o[m][TI - 1] = M::mma(vf[m][h], f1[h], o[m][TI - 1]);
                 }
-            }
-            // A value that is not finite reaches the tokens before it as 0 v = NaN.
-            if constexpr (sizeof(T) == 2) {
-                const Frag none = {};
-#pragma unroll
-                for (int m = 0; m < NT; ++m) bad = M::mma(vf[m][0], none, bad);
-            } else {
-#pragma unroll
-                for (int m = 0; m < NT; ++m)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) bad[r] = fmaf(vf[m][h][r], 0.0f, bad[r]);
             }
         } else {
 #pragma unroll
@@ -663,6 +688,22 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
                     }
                 }
             }
+            // An output that is not finite leaves 0 o = NaN.
+            if constexpr (sizeof(T) == 2) {
+                const Frag none = {};
+#pragma unroll
+                for (int m = 0; m < NT; ++m) {
+                    const floatx4 out2[2] = {o[m][0], o[m][OT - 1]};
+                    bad = M::mma(M::from(out2), none, bad);
+                }
+            } else {
+#pragma unroll
+                for (int m = 0; m < NT; ++m)
+#pragma unroll
+                    for (int h = 0; h < TI; ++h)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) bad[r] = fmaf(o[m][h][r], 0.0f, bad[r]);
+            }
             if (!ROWS_OUT || f32) out += (int64_t)C * os;
         }
         row0 = 0;
@@ -699,10 +740,17 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
                     if (i < dk && c < dv) to_state[transposed ? c * dk + i : i * dv + c] = S[t][m][r];
                 }
     }
-    if (!LOCAL && __syncthreads_or(bad[0] + bad[1] + bad[2] + bad[3] != 0.0f)) {
-        __threadfence();  // the outputs as written, also by the wave of the other token tile
+    // A state that was not finite once is so at the end.
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int m = 0; m < NT; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) bad[r] = fmaf(S[t][m][r], 0.0f, bad[r]);
+    if (__syncthreads_or(not_finite(bad[0] + bad[1] + bad[2] + bad[3]))) {
+        __threadfence();  // outputs and states as written, also by the waves that share this one's columns
         __syncthreads();
-        if (i0 == 0) scan_plain<T, D / 16, NT>(a, R, head, t0, len, from, to, slab, init);
+        if (i0 == 0) scan_plain<T, D / 16, NT, LOCAL>(a, R, head, t0, len, from, to, slab, to_state, transposed, init);
     }
 }
 
@@ -720,8 +768,7 @@ __global__ __launch_bounds__(256) void k_join_segments(ScanArgs a) {
     len = uniform(len);
     if (x >= size || (len <= a.seg && !R.final_state)) return;
     const double rate = a.rates[head];
-    const double gd = exp(-rate * (double)a.seg);
-    const float gs = (float)gd, gs_lo = (float)(gd - (double)gs);
+    const Decay gs = decay_of(-rate * (double)a.seg);
     const int64_t outside = ((int64_t)seq * a.heads + head) * size + (R.state_t ? x % R.v.dim * R.q.dim + x / R.v.dim : x);
     float s = R.state ? R.state[outside] : 0.0f;
     const int64_t slot0 = seq + t0 / a.seg;
@@ -743,7 +790,7 @@ __global__ __launch_bounds__(256) void k_join_segments(ScanArgs a) {
         load(next, j + N);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            s = fmaf(s, gs, fmaf(s, gs_lo, v[i]));
+            s = fmaf(s, gs.hi, fmaf(s, gs.lo, v[i]));
             p[(j + i) * step] = s;
         }
 #pragma unroll
@@ -752,12 +799,12 @@ __global__ __launch_bounds__(256) void k_join_segments(ScanArgs a) {
 #pragma unroll
     for (int i = 0; i < N; ++i)
         if (j + i < joins) {
-            s = fmaf(s, gs, fmaf(s, gs_lo, v[i]));
+            s = fmaf(s, gs.hi, fmaf(s, gs.lo, v[i]));
             p[(j + i) * step] = s;
         }
     if (R.final_state) {
         const float last = a.states[(((int64_t)blockIdx.z * a.heads + head) * a.slots + slot0 + joins) * size + x];
-        const double g = exp(-rate * (double)(len - joins * a.seg));
+        const double g = fmax(exp(-rate * (double)(len - joins * a.seg)), 0x1p-1074);  // not 0: s may be infinite
         R.final_state[outside] = len > 0 ? (float)(g * (double)s + (double)last) : s;
     }
 }

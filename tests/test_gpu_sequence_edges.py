@@ -120,3 +120,55 @@ def test_attention_refuses_its_other_outputs_as_inputs():
     for g in (dq, dk, dv):
         with pytest.raises(MdlstmError, match="overlaps grad_o"):
             op.backward(g)
+
+
+def _same_kind(name, got, want, tol):
+    """NaN and infinities where `want` has them, the rest within the tolerance."""
+    got = _np(got)
+    for what in (np.isnan, np.isposinf, np.isneginf):
+        assert np.array_equal(what(got), what(want)), (name, what.__name__, int(what(got).sum()), int(what(want).sum()))
+    f = np.isfinite(want)
+    _check(name, np.where(f, got, 0), np.where(f, want, 0), tol)
+
+
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), float("nan")])
+@pytest.mark.parametrize("where", ["q", "k", "v", "do", "state", "dstate"])
+@pytest.mark.parametrize("lengths,d,dtype", [([90, 45], 16, "f32"), ([90, 45], 32, "f32"), ([90, 45], 64, "bf16"),
+                                             ([90, 45], 128, "bf16"), ([1000], 64, "f32"), ([1000], 64, "bf16")])
+def test_infinite_values_give_what_the_recurrence_gives(lengths, d, dtype, where, bad):
+    """One value that is not finite, early in the first sequence: outputs, states and gradients are infinite or NaN
+    where the recurrence in 64 bits is, whole and in segments of 128."""
+    rng = np.random.default_rng(d + len(lengths))
+    T, n, heads = sum(lengths), len(lengths), 2
+    print(f"case: {bad} in {where}, {lengths}, {d} columns, {dtype}", flush=True)
+    t = {x: _rand(rng, T, heads, d, dtype=dtype) for x in ("q", "k", "v", "do")}
+    t["state"], t["dstate"] = _rand(rng, n, heads, d, d), _rand(rng, n, heads, d, d)
+    t[where][(0, 1, 3, 5) if "state" in where else (20, 1, 5)] = bad
+    a = torch.tensor([0.02, 0.05], device="cuda")
+    op = _seq().DecayAttention(lengths, heads, d, d, a, dtype=DT[dtype])
+    o, final = op.forward(t["q"], t["k"], t["v"], state=t["state"], final_state=True)
+    got = op.backward(t["do"], dstate=t["dstate"])
+    args = _np(t["q"]), _np(t["k"]), _np(t["v"]), lengths, _np(a), d ** -0.5
+    with np.errstate(invalid="ignore"):
+        wo, wf = orc.attention_forward(*args, _np(t["state"]))
+        want = orc.attention_backward(*args, _np(t["do"]), _np(t["state"]), _np(t["dstate"]))
+    _same_kind("o", o, wo, TOL[dtype])
+    _same_kind("final", final, wf, TOL32[dtype])
+    for name, g, w in zip(("dq", "dk", "dv", "dstate"), got, want):
+        _same_kind(name, g, w, TOL32[dtype] if name == "dstate" else TOL[dtype])
+
+
+@pytest.mark.parametrize("lengths,d,dtype", [([200, 33], 32, "f32"), ([200, 33], 64, "bf16"), ([1000], 64, "bf16"),
+                                             ([1000], 128, "f32")])
+def test_states_near_the_largest_number(lengths, d, dtype):
+    """States of some 2^124, of which fp32 holds 2^128, with outputs of ordinary size."""
+    rng = np.random.default_rng(d)
+    T, n, heads = sum(lengths), len(lengths), 2
+    q, k, v = (_rand(rng, T, heads, d, dtype=dtype) * s for s in (2.0 ** -120, 2.0 ** 61, 2.0 ** 61))
+    a, st = torch.tensor([0.05, 0.1], device="cuda"), _rand(rng, n, heads, d, d) * 2.0 ** 122
+    op = _seq().DecayAttention(lengths, heads, d, d, a, dtype=DT[dtype])
+    o, final = op.forward(q, k, v, state=st, final_state=True)
+    wo, wf = orc.attention_forward(_np(q), _np(k), _np(v), lengths, _np(a), d ** -0.5, _np(st))
+    assert np.abs(wf).max() < 2.0 ** 127
+    _check("o", o, wo, TOL[dtype])
+    _check("final", final, wf, TOL32[dtype])
