@@ -155,7 +155,7 @@ struct Unit {
 // False: no unit.
 __device__ __forceinline__ bool unit_of(const ScanArgs& a, Unit& u) {
     const int group = a.together, kv = a.heads / group, inner = a.n_roles * group;
-    const int64_t i = blockIdx.x >> 3, rest = i / inner * 8 + (blockIdx.x & 7);
+    const int64_t b = block_index(), i = b >> 3, rest = i / inner * 8 + (b & 7);
     const int in = (int)(i % inner);
     u.slot = rest / kv;
     if (u.slot >= a.slots) return false;
@@ -759,9 +759,12 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
 // zero and receives the state that segment j + 1 starts from; the last one's
 // goes to the final states.
 __global__ __launch_bounds__(256) void k_join_segments(ScanArgs a) {
-    const ScanRole& R = a.role[blockIdx.z];
-    const int seq = blockIdx.x / a.heads, head = blockIdx.x % a.heads, size = R.q.dim * R.v.dim;
-    const int x = blockIdx.y * 256 + threadIdx.x;
+    const int role = blockIdx.z % a.n_roles;
+    const ScanRole& R = a.role[role];
+    const int64_t unit = block_index();
+    if (unit >= (int64_t)a.n * a.heads) return;
+    const int seq = (int)(unit / a.heads), head = (int)(unit % a.heads), size = R.q.dim * R.v.dim;
+    const int x = blockIdx.z / a.n_roles * 256 + threadIdx.x;
     int64_t t0, len;
     sequence(a.offsets, seq, a.tokens, a.longest, t0, len);
     t0 = uniform(t0);
@@ -772,7 +775,7 @@ __global__ __launch_bounds__(256) void k_join_segments(ScanArgs a) {
     const int64_t outside = ((int64_t)seq * a.heads + head) * size + (R.state_t ? x % R.v.dim * R.q.dim + x / R.v.dim : x);
     float s = R.state ? R.state[outside] : 0.0f;
     const int64_t slot0 = seq + t0 / a.seg;
-    float* p = a.states + (((int64_t)blockIdx.z * a.heads + head) * a.slots + slot0) * size + x;
+    float* p = a.states + (((int64_t)role * a.heads + head) * a.slots + slot0) * size + x;
     const int64_t step = size;
     const int joins = len > 0 ? (int)((len - 1) / a.seg) : 0;
     // Latency bounds it: N loads are in flight while the N before are joined, and
@@ -803,7 +806,7 @@ __global__ __launch_bounds__(256) void k_join_segments(ScanArgs a) {
             p[(j + i) * step] = s;
         }
     if (R.final_state) {
-        const float last = a.states[(((int64_t)blockIdx.z * a.heads + head) * a.slots + slot0 + joins) * size + x];
+        const float last = a.states[(((int64_t)role * a.heads + head) * a.slots + slot0 + joins) * size + x];
         const double g = fmax(exp(-rate * (double)(len - joins * a.seg)), 0x1p-1074);  // not 0: s may be infinite
         R.final_state[outside] = len > 0 ? (float)(g * (double)s + (double)last) : s;
     }
@@ -811,7 +814,7 @@ __global__ __launch_bounds__(256) void k_join_segments(ScanArgs a) {
 
 template <typename T>
 __global__ __launch_bounds__(256) void k_sum_heads(int64_t n, int group, int dim, const float* src, T* dst) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;  // (token, kv head, element)
+    const int64_t i = block_index() * 256 + threadIdx.x;  // (token, kv head, element)
     if (i >= n) return;
     const int64_t th = i / dim;
     const float* p = src + th * group * dim + (i - th * dim);
@@ -836,10 +839,12 @@ template <typename T, int V, int CG>
 __global__ __launch_bounds__(256) void k_step(StepArgs a) {
     constexpr int RG = 256 / CG, N = (128 + RG - 1) / RG;  // rows at once, rows of a thread
     __shared__ float q[128], k[128], part[4][CG * V];
-    const int row = blockIdx.x, head = blockIdx.y, dk = a.q.dim, dv = a.v.dim;
+    const int64_t row = block_index();
+    if (row >= a.n) return;
+    const int head = blockIdx.z, dk = a.q.dim, dv = a.v.dim;
     const int c = threadIdx.x % CG * V, r0 = threadIdx.x / CG;
     const int64_t slot = a.slot ? a.slot[row] : row;
-    T* out = static_cast<T*>(a.out) + ((int64_t)row * a.heads + head) * dv;
+    T* out = static_cast<T*>(a.out) + (row * a.heads + head) * dv;
     if (slot < 0 || slot >= a.slots) {
         if ((int)threadIdx.x < dv) St<T>::st1(out + threadIdx.x, 0.0f);
         return;
@@ -934,17 +939,20 @@ template <typename T, int D, int NT, int TI, bool WIDE, int PIECES>
 static hipError_t scan(const ScanArgs& a, hipStream_t s) {
     const int inner = a.n_roles * a.together;
     const int64_t rest = (a.slots * (a.heads / a.together) + 7) / 8, blocks = rest * 8 * inner;
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+    dim3 grid;
     if (a.seg) {
-        k_scan<T, D, NT, 2, WIDE, 3, true><<<(unsigned)blocks, scan_threads<D, NT, 2>(), 0, s>>>(a);
+        if (!grid_of(blocks, scan_threads<D, NT, 2>(), grid)) return hipErrorInvalidValue;
+        k_scan<T, D, NT, 2, WIDE, 3, true><<<grid, scan_threads<D, NT, 2>(), 0, s>>>(a);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         const int size = a.role[0].q.dim * a.role[0].v.dim;
-        if ((int64_t)a.n * a.heads > 0x7fffffff) return hipErrorInvalidValue;
-        k_join_segments<<<dim3(a.n * a.heads, (size + 255) / 256, a.n_roles), 256, 0, s>>>(a);
+        if (!grid_of((int64_t)a.n * a.heads, 256, grid)) return hipErrorInvalidValue;
+        grid.z = (size + 255) / 256 * a.n_roles;
+        k_join_segments<<<grid, 256, 0, s>>>(a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    k_scan<T, D, NT, TI, WIDE, PIECES, false><<<(unsigned)blocks, scan_threads<D, NT, TI>(), 0, s>>>(a);
+    if (!grid_of(blocks, scan_threads<D, NT, TI>(), grid)) return hipErrorInvalidValue;
+    k_scan<T, D, NT, TI, WIDE, PIECES, false><<<grid, scan_threads<D, NT, TI>(), 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -994,18 +1002,21 @@ hipError_t launch_scan(const ScanArgs& in, hipStream_t s) {
 
 hipError_t launch_sum_heads(int64_t tokens, int kv_heads, int group, int dim, int dtype, const float* src, void* dst,
                             hipStream_t s) {
-    const int64_t n = tokens * kv_heads * dim, blocks = (n + 255) / 256;
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+    const int64_t n = tokens * kv_heads * dim;
+    dim3 grid;
+    if (!grid_of((n + 255) / 256, 256, grid)) return hipErrorInvalidValue;
     if (dtype)
-        k_sum_heads<<<(unsigned)blocks, 256, 0, s>>>(n, group, dim, src, static_cast<bf16_t*>(dst));
+        k_sum_heads<<<grid, 256, 0, s>>>(n, group, dim, src, static_cast<bf16_t*>(dst));
     else
-        k_sum_heads<<<(unsigned)blocks, 256, 0, s>>>(n, group, dim, src, static_cast<float*>(dst));
+        k_sum_heads<<<grid, 256, 0, s>>>(n, group, dim, src, static_cast<float*>(dst));
     return hipGetLastError();
 }
 
 template <typename T>
 static hipError_t step(const StepArgs& a, hipStream_t s) {
-    const dim3 grid(a.n, a.heads);
+    dim3 grid;
+    if (!grid_of(a.n, 256, grid)) return hipErrorInvalidValue;
+    grid.z = a.heads;
     const int dv = a.v.dim;
     if (dv % 4 == 0) {  // rows of the state are whole 16-byte vectors
         if (dv <= 16)

@@ -103,7 +103,7 @@ __device__ __forceinline__ void drop8(const Drop& d, uint64_t e, float (&v)[8]) 
 // ---------------------------------------------------------------------------
 template <typename T, bool WIDE>
 __global__ __launch_bounds__(256) void k_dropout(DropoutArgs a, int64_t vecs) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t i = block_index() * 256 + threadIdx.x;
     if (i >= a.rows * vecs) return;
     const int64_t row = i / vecs, c = (i - row * vecs) * 8;
     const int valid = (int)(a.cols - c < 8 ? a.cols - c : 8);
@@ -150,7 +150,7 @@ template <typename T, bool WIDE, int LANES, int NV, bool F8>
 __global__ __launch_bounds__(threads_of<LANES>()) void k_norm_fwd(NormArgs a) {
     __shared__ float lds[16];
     const int lanes = LANES ? LANES : blockDim.x;
-    const int64_t row = LANES ? (int64_t)blockIdx.x * (256 / lanes) + threadIdx.x / lanes : blockIdx.x;
+    const int64_t row = LANES ? block_index() * (256 / lanes) + threadIdx.x / lanes : block_index();
     if (row >= a.rows) return;
     const int lane = LANES ? threadIdx.x % lanes : threadIdx.x;
     const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
@@ -344,7 +344,8 @@ template <typename T, bool WIDE>
 hipError_t norm_fwd(const NormArgs& a, hipStream_t s) {
     return with_shape(a.cols, a.dtype, true, [&](auto L, auto N, int threads) {
         constexpr int rows = L() ? 256 / (L() ? L() : 1) : 1;
-        const dim3 grid((unsigned)((a.rows + rows - 1) / rows));
+        dim3 grid;
+        if (!grid_of((a.rows + rows - 1) / rows, threads, grid)) return hipErrorInvalidValue;
         if (a.y8)
             k_norm_fwd<T, WIDE, L(), N(), true><<<grid, threads, 0, s>>>(a);
         else
@@ -390,9 +391,9 @@ hipError_t launch_dropout(const DropoutArgs& in, hipStream_t s) {
     bool wide = aligned16(a.x) && aligned16(a.y) && (!a.residual || aligned16(a.residual));
     if (a.rows > 1)
         wide = wide && a.cols % 8 == 0 && a.x_stride * es % 16 == 0 && (!a.residual || a.r_stride * es % 16 == 0);
-    const int64_t vecs = (a.cols + 7) / 8, blocks = (a.rows * vecs + 255) / 256;
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks);
+    const int64_t vecs = (a.cols + 7) / 8;
+    dim3 grid;
+    if (!grid_of((a.rows * vecs + 255) / 256, 256, grid)) return hipErrorInvalidValue;
     if (a.dtype)
         wide ? k_dropout<bf16_t, true><<<grid, 256, 0, s>>>(a, vecs) : k_dropout<bf16_t, false><<<grid, 256, 0, s>>>(a, vecs);
     else

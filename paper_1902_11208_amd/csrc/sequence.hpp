@@ -9,6 +9,18 @@
 
 namespace mdl {
 
+// A grid of at least `blocks` workgroups. The runtime takes less than 2^32
+// threads along x, so more come as rows of a multiple of 8 workgroups, which
+// keeps a workgroup's XCD its index modulo 8. False beyond 65535 rows.
+inline bool grid_of(int64_t blocks, int threads, dim3& grid) {
+    const int64_t most = (0xffffffffll / threads) & ~7ll;
+    const int64_t rows = blocks > most ? (blocks + most - 1) / most : 1;
+    if (rows > 65535) return false;
+    grid = dim3((unsigned)(rows > 1 ? ((blocks + rows - 1) / rows + 7) & ~7ll : blocks), (unsigned)rows);
+    return true;
+}
+__device__ __forceinline__ int64_t block_index() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // A token tensor as a scan reads it: element (t, h, i) at
 // p[t * token_stride + (h / group) * head_stride + i], i < dim.
 struct HeadView {

@@ -172,3 +172,99 @@ def test_states_near_the_largest_number(lengths, d, dtype):
     assert np.abs(wf).max() < 2.0 ** 127
     _check("o", o, wo, TOL[dtype])
     _check("final", final, wf, TOL32[dtype])
+
+
+# --- more than 2^32 threads along one dimension of a grid, which the runtime does not take ---------------------
+def _room(gigabytes):
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < gigabytes << 30:
+        pytest.skip(f"needs {gigabytes} GiB of device memory")
+
+
+def _randn(*shape, seed=1):
+    return torch.randn(shape, generator=torch.Generator("cuda").manual_seed(seed), device="cuda", dtype=torch.bfloat16)
+
+
+def test_dropout_of_more_rows_than_threads():
+    """2^32 + 3 rows of one element, a thread each: rows two apart, so they are not one long row."""
+    _room(40)
+    rows, p, seed, call = (1 << 32) + 3, 0.5, 7, 9
+    x = torch.ones(rows, 2, dtype=torch.bfloat16, device="cuda")[:, :1]
+    y = _seq().dropout(x, p, seed, call)[:, 0]
+    kept = int((y[:1 << 31] == 2).sum()), int((y[1 << 31:] == 2).sum())
+    assert all(abs(k - (1 << 30)) < 5 * 2 ** 15.5 for k in kept), kept
+    for e in (0, 1 << 31, 1 << 32):  # element e = 8 b + j has half j of block b's words
+        w = [h for x in orc.philox(e >> 3, call, seed) for h in (x & 0xFFFF, x >> 16)]
+        assert [float(v) for v in y[e:e + 3]] == [2.0 if u >= 1 << 15 else 0.0 for u in w[:3]], e
+    del x, y
+    torch.cuda.empty_cache()
+
+
+def test_norm_of_more_rows_than_workgroups():
+    """2^29 + 1 rows of one element, eight threads each."""
+    _room(16)
+    rows = (1 << 29) + 1
+    x = _randn(rows, 1)
+    y, _ = _seq().ResidualNorm(torch.ones(1, device="cuda"), rows, eps=1.0).forward(x)
+    for at in range(0, rows, 1 << 27):
+        a = x[at:at + (1 << 27)].float()
+        assert float((y[at:at + (1 << 27)].float() - a * torch.rsqrt(a * a + 1)).abs().max()) <= 2.0 ** -8
+    del x, y
+    torch.cuda.empty_cache()
+
+
+def test_attention_of_more_examples_than_workgroups():
+    """16400 examples of one token with 1024 heads, a workgroup of 256 threads each."""
+    _room(16)
+    n, heads, d = 16400, 1024, 33
+    q, k, v = (_randn(n, heads, d, seed=s) for s in (1, 2, 3))
+    op = _seq().DecayAttention(np.ones(n, np.int64), heads, d, d, torch.zeros(heads, device="cuda"), scale=1.0)
+    o = op.forward(q, k, v)
+    for at in range(0, n, 4100):
+        s = slice(at, at + 4100)
+        want = (q[s].float() * k[s].float()).sum(2, keepdim=True) * v[s].float()
+        assert float((o[s].float() - want).norm() / want.norm()) <= TOL["bf16"]
+    del q, k, v, o, op
+    torch.cuda.empty_cache()
+
+
+def test_states_of_more_examples_than_workgroups():
+    """One example of 1500 tokens in segments among 65600 empty ones of 256 heads, which keep their states; steps of
+    2^24 rows, the most of one call."""
+    _room(16)
+    rng = np.random.default_rng(31)
+    n, heads, d, T = 65601, 256, 4, 1500
+    lengths = np.zeros(n, np.int64)
+    lengths[n - 1] = T
+    q, k, v = (_rand(rng, T, heads, d) for _ in range(3))
+    a = torch.from_numpy(rng.uniform(0, 0.1, heads).astype(np.float32)).cuda()
+    st = torch.randn(n, heads, d, d, device="cuda")
+    o, final = _seq().DecayAttention(lengths, heads, d, d, a, dtype=torch.float32).forward(q, k, v, state=st, final_state=True)
+    wo, wf = orc.attention_forward(_np(q), _np(k), _np(v), [T], _np(a), d ** -0.5, _np(st[-1:]))
+    _check("o", o, wo, 1e-5)
+    _check("final", final[-1:], wf, 1e-5)
+    assert torch.equal(final[:-1], st[:-1])
+    n = 1 << 24
+    q, k, v, st = (torch.randn(n, 1, 1, device="cuda") for _ in range(4))
+    st = st.unsqueeze(3)
+    want = st * 0.5 + (k * v).unsqueeze(3)
+    o = _seq().decay_attention_step(q, k, v, st, torch.tensor([np.log(2.0)], dtype=torch.float32, device="cuda"), scale=1.0)
+    assert float((st - want).abs().max()) <= 1e-5 and float((o - q * want[:, :, 0]).abs().max()) <= 1e-4
+
+
+def test_gradients_of_shared_heads_beyond_32_bits():
+    """2^32 elements of dk, each summed over the two heads that share it. A rate of 200 leaves nothing of the token
+    before, so dk = scale (q_0 (do_0 . v) + q_1 (do_1 . v)) of the token itself."""
+    _room(120)
+    T, kv, dk = 65544, 512, 128
+    q, do, k, v = _randn(T, 2 * kv, dk), _randn(T, 2 * kv, 1, seed=2), _randn(T, kv, dk, seed=3), _randn(T, kv, 1, seed=4)
+    op = _seq().DecayAttention([4096] * 16 + [8], 2 * kv, dk, 1, torch.full((2 * kv,), 200.0, device="cuda"), kv_heads=kv, scale=1.0)
+    op.forward(q, k, v)
+    got = op.backward(do)[1]
+    for at in (0, 32768, T - 64):
+        s = slice(at, at + 64)
+        want = (q[s].float() * do[s].float()).unflatten(1, (kv, 2)).sum(2) * v[s].float()
+        assert float((got[s].float() - want).norm() / want.norm()) <= TOL["bf16"]
+        assert torch.isfinite(got[s]).all()
+    del q, do, k, v, op, got
+    torch.cuda.empty_cache()
