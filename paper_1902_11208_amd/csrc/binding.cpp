@@ -4,6 +4,7 @@
 // kernels (a step 8.4 us of host time).
 #include <torch/extension.h>
 
+#include <c10/hip/HIPGuard.h>
 #include <c10/hip/HIPStream.h>
 
 #include <sstream>
@@ -79,6 +80,13 @@ void on_gpu(const at::Tensor& t, const char* name) {
 
 void* stream_of(const MaybeStream& s, at::Device device) {
     return s ? reinterpret_cast<void*>(*s) : static_cast<void*>(c10::hip::getCurrentHIPStream(device.index()).stream());
+}
+
+// Memory for work on `s`: what the current stream freed may still be in use there.
+at::Tensor empty(at::IntArrayRef shape, const at::Tensor& like, const MaybeStream& s) {
+    c10::hip::OptionalHIPStreamGuard on;
+    if (s) on.reset_stream(c10::hip::getStreamFromExternal(reinterpret_cast<hipStream_t>(*s), like.device().index()));
+    return at::empty(shape, like.options().memory_format(at::MemoryFormat::Contiguous));
 }
 
 // ---------------------------------------------------------------------------
@@ -162,7 +170,7 @@ at::Tensor step(const at::Tensor& q, const at::Tensor& k, const at::Tensor& v, c
     const int32_t* at_slot = static_cast<int32_t*>(full(slots, "slots", {n}, at::kInt, dev));
     const void* given = full(out, "out", {n, h, dv}, dt, dev);
     on_gpu(q, "q");
-    const at::Tensor o = out ? *out : at::empty({n, h, dv}, q.options().memory_format(at::MemoryFormat::Contiguous));
+    const at::Tensor o = out ? *out : empty({n, h, dv}, q, stream);
     (void)given;
     mdlstm_status st;
     {
@@ -244,7 +252,7 @@ at::Tensor dropout(const at::Tensor& x, double p, uint64_t seed, uint64_t call, 
     }
     full(out, "out", x.sizes(), dt, dev);
     on_gpu(x, "x");
-    const at::Tensor y = out ? *out : at::empty(x.sizes(), x.options().memory_format(at::MemoryFormat::Contiguous));
+    const at::Tensor y = out ? *out : empty(x.sizes(), x, stream);
     mdlstm_status st;
     {
         py::gil_scoped_release none;

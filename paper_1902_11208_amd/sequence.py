@@ -7,11 +7,14 @@ do. Every step of the computation runs in libmdlstm.so's HIP kernels; this
 module and its native part (_binding: tensor checks, pointers and strides) own
 buffers and marshal arguments. Objects own their output buffers: a call
 overwrites what the call before returned. Calls run on `stream` (default: the
-current stream); an object, its tensors and what it returned have to outlive the
-work enqueued on any other stream.
+current stream), and buffers are allocated for the stream of the call that first
+needs them; an object, its tensors and what it returned have to outlive the work
+enqueued on any other stream. An object's calls share its buffers and workspace,
+so calls on several streams have to be put in order by the caller.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 
 import numpy as np
@@ -30,6 +33,12 @@ FP8 = torch.float8_e4m3fn
 
 def _stream(stream):
     return None if stream is None else stream.cuda_stream
+
+
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    """Memory for work on `stream`: what the current stream freed may still be in use there."""
+    with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def _u64(v, name: str) -> int:
@@ -90,26 +99,26 @@ class DecayAttention:
         self._o = self._grads = self._saved = None
         self._finals, self._dstates = [], []
 
-    def _spare(self, buffers: list, *used) -> torch.Tensor:
+    def _spare(self, buffers: list, stream, *used) -> torch.Tensor:
         """The first of the buffers of states that none of `used` lies in."""
         for b in buffers:
             if all(_apart(b, u) for u in used):
                 return b
-        buffers.append(torch.empty(self._state_shape, dtype=torch.float32, device=self.device))
+        buffers.append(_empty(self._state_shape, torch.float32, self.device, stream))
         return buffers[-1]
 
-    def _workspace(self, backward: int) -> torch.Tensor:
+    def _workspace(self, backward: int, stream) -> torch.Tensor:
         if self._ws[backward] is None:
-            self._ws[backward] = torch.empty(self._bytes[backward], dtype=torch.uint8, device=self.device)
+            self._ws[backward] = _empty(self._bytes[backward], torch.uint8, self.device, stream)
         return self._ws[backward]
 
     def forward(self, q, k, v, state=None, final_state: bool = False, stream=None):
         """o [tokens, heads, dim_v]; with final_state also the states the sequences leave [n, heads, dim_k, dim_v].
         state: the states they start from (None: zero). q, k, v may be views of one projection's output."""
         if self._o is None:
-            self._o = torch.empty((self.tokens, self.heads, self.dim_v), dtype=self.dtype, device=self.device)
-        final = self._spare(self._finals, state) if final_state else None
-        self._op.forward(q, k, v, state, self._o, final, self._workspace(0), _stream(stream))
+            self._o = _empty((self.tokens, self.heads, self.dim_v), self.dtype, self.device, stream)
+        final = self._spare(self._finals, stream, state) if final_state else None
+        self._op.forward(q, k, v, state, self._o, final, self._workspace(0, stream), _stream(stream))
         self._saved = (q, k, v, state)
         return (self._o, final) if final_state else self._o
 
@@ -120,10 +129,10 @@ class DecayAttention:
             raise ValueError("backward needs a forward call on this layer first")
         q, k, v, state = self._saved
         if self._grads is None:
-            self._grads = tuple(torch.empty((self.tokens, h, d), dtype=self.dtype, device=self.device) for h, d in (
+            self._grads = tuple(_empty((self.tokens, h, d), self.dtype, self.device, stream) for h, d in (
                 (self.heads, self.dim_k), (self.kv_heads, self.dim_k), (self.kv_heads, self.dim_v)))
-        out = None if state is None else self._spare(self._dstates, state, dstate)
-        self._op.backward(q, k, v, state, do, dstate, *self._grads, out, self._workspace(1), _stream(stream))
+        out = None if state is None else self._spare(self._dstates, stream, state, dstate)
+        self._op.backward(q, k, v, state, do, dstate, *self._grads, out, self._workspace(1, stream), _stream(stream))
         return self._grads if state is None else self._grads + (out,)
 
 
@@ -161,24 +170,19 @@ class ResidualNorm:
             raise ValueError(lib().mdlstm_last_error().decode(errors="replace"))
         self._op = _binding.Norm(cols, desc.dtype, desc.eps, desc.p, self.rows, weight)
         self._drops = round(float(dropout) * 65536) > 0
-        shape = (self.rows, cols)
         self._ws_bytes, self._ws = nbytes, None
-        self._h = self._dx = self._dres = self._dw = self._saved = None
-        if self.fp8:
-            self._y = torch.empty(shape, dtype=FP8, device=self.device)
-            self._scale = torch.empty(self.rows, dtype=torch.float32, device=self.device)
-            self._rstd = None
-        else:
-            self._y = torch.empty(shape, dtype=dtype, device=self.device)
-            self._scale = None
-            self._rstd = torch.empty(self.rows, dtype=torch.float32, device=self.device)
+        self._y = self._scale = self._rstd = self._h = self._dx = self._dres = self._dw = self._saved = None
 
     def forward(self, x, residual=None, seed: int = 0, call: int = 0, stream=None):
         """(y, h), or with out "fp8" (y, scale, h): y[i, j] stands for float(y[i, j]) * scale[i]. h is the new residual;
         without residual and dropout it is x itself. x and residual: [rows, cols], contiguous along their rows."""
         plain = residual is None and not self._drops
+        if self._y is None:
+            self._y = _empty((self.rows, self.cols), FP8 if self.fp8 else self.dtype, self.device, stream)
+            per_row = _empty(self.rows, torch.float32, self.device, stream)
+            self._scale, self._rstd = (per_row, None) if self.fp8 else (None, per_row)
         if not plain and self._h is None:
-            self._h = torch.empty((self.rows, self.cols), dtype=self.dtype, device=self.device)
+            self._h = _empty((self.rows, self.cols), self.dtype, self.device, stream)
         seed, call = _u64(seed, "seed"), _u64(call, "call")
         self._op.forward(x, residual, None if plain else self._h, self._y, self._scale, self._rstd, seed, call,
                          _stream(stream))
@@ -195,12 +199,12 @@ class ResidualNorm:
             raise ValueError("backward needs a forward call on this norm first (and no 8-bit output)")
         h, seed, call, residual = self._saved
         if self._dx is None:
-            self._dx = torch.empty((self.rows, self.cols), dtype=self.dtype, device=self.device)
-            self._dw = torch.empty(self.cols, dtype=torch.float32, device=self.device)
-            self._ws = torch.empty(self._ws_bytes, dtype=torch.uint8, device=self.device)
+            self._dx = _empty((self.rows, self.cols), self.dtype, self.device, stream)
+            self._dw = _empty(self.cols, torch.float32, self.device, stream)
+            self._ws = _empty(self._ws_bytes, torch.uint8, self.device, stream)
         both = residual and self._drops
         if both and self._dres is None:
-            self._dres = torch.empty((self.rows, self.cols), dtype=self.dtype, device=self.device)
+            self._dres = _empty((self.rows, self.cols), self.dtype, self.device, stream)
         self._op.backward(h, self._rstd, dy, dh, seed, call, self._dx, self._dres if both else None, self._dw, self._ws,
                           _stream(stream))
         return self._dx, (self._dres if both else self._dx) if residual else None, self._dw

@@ -268,3 +268,43 @@ def test_gradients_of_shared_heads_beyond_32_bits():
         assert torch.isfinite(got[s]).all()
     del q, do, k, v, op, got
     torch.cuda.empty_cache()
+
+
+# --- streams -----------------------------------------------------------------------------------------------------
+def test_buffers_of_another_stream():
+    """Fresh objects called with stream=: memory that the current stream has freed, but still writes, must not become
+    their buffers. Blocks of the buffers' sizes are freed while fills of them wait behind a long kernel."""
+    rng = np.random.default_rng(37)
+    T, heads, d = 300, 2, 64
+    sq, side = _seq(), torch.cuda.Stream()
+    q, k, v, do = (_rand(rng, T, heads, d) for _ in range(4))
+    st, ds, a = _rand(rng, 1, heads, d, d), _rand(rng, 1, heads, d, d), torch.tensor([0.05, 0.1], device="cuda")
+    x, res, dy, w = _rand(rng, T, 128), _rand(rng, T, 128), _rand(rng, T, 128), torch.ones(128, device="cuda")
+
+    def calls(stream):
+        op = sq.DecayAttention([T], heads, d, d, a, dtype=torch.float32)
+        norm = sq.ResidualNorm(w, T, dtype=torch.float32, dropout=0.2)
+        norm8 = sq.ResidualNorm(w, T, dtype=torch.float32, out="fp8")
+        state = st.clone()
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream())
+            torch.cuda._sleep(100_000_000)  # some 50 ms
+            for n in (T * heads * d, heads * d * d, T * 128, T, 128, T * 32, T * 128 // 4, 64, 4096, 1 << 16):
+                blocks = [torch.empty(n, device="cuda") for _ in range(8)]
+                for b in blocks:
+                    b.fill_(float("nan"))
+                del blocks, b
+        y, h = norm.forward(x, res, seed=1, call=2, stream=stream)
+        y8, scale, _ = norm8.forward(x, res, stream=stream)
+        got = [*op.forward(q, k, v, state=st, final_state=True, stream=stream), *op.backward(do, dstate=ds, stream=stream),
+               y, h, *norm.backward(dy, dy, stream=stream), y8.view(torch.uint8), scale,
+               sq.dropout(x, 0.5, 3, 4, stream=stream),
+               sq.decay_attention_step(q[:1], k[:1], v[:1], state, a, stream=stream)]
+        return got, (op, norm, norm8, state)
+
+    want, keep = calls(None)
+    torch.cuda.synchronize()
+    got, keep2 = calls(side)
+    torch.cuda.synchronize()
+    for i, (g, w_) in enumerate(zip(got, want)):
+        assert torch.equal(g, w_), i
