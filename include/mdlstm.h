@@ -553,7 +553,7 @@ typedef struct {
  * h is x itself. Output, one of the two, the other NULL:
  *   d_y  (out) [rows][cols], storage type;
  *   d_y8 (out) [rows][cols], float8 e4m3, and d_scale (out) [rows], fp32:
- *        y / scale rounded to nearest even, scale = max(max_row |y| / 448,
+ *        the fp32 quotient y / scale rounded to nearest even, scale = max(max_row |y| / 448,
  *        2^-126) (NaN where the row has one, infinite where |y| is).
  * d_rstd (out, may be NULL) [rows]: rsqrt(mean(h^2) + eps), for the backward.
  */

