@@ -175,8 +175,9 @@ class ResidualNorm:
 
     def forward(self, x, residual=None, seed: int = 0, call: int = 0, stream=None):
         """(y, h), or with out "fp8" (y, scale, h): y[i, j] stands for float(y[i, j]) * scale[i]. h is the new residual;
-        without residual and dropout it is x itself. x and residual: [rows, cols], contiguous along their rows."""
-        plain = residual is None and not self._drops
+        without residual and dropout it is x itself (a copy where x is this object's y, which the call overwrites).
+        x and residual: [rows, cols], contiguous along their rows."""
+        plain = residual is None and not self._drops and (self._y is None or _apart(self._y, x))
         if self._y is None:
             self._y = _empty((self.rows, self.cols), FP8 if self.fp8 else self.dtype, self.device, stream)
             per_row = _empty(self.rows, torch.float32, self.device, stream)

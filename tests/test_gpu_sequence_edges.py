@@ -311,6 +311,24 @@ def test_buffers_of_another_stream():
 
 
 # --- norm ----------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("cols,dtype", [(64, "f32"), (512, "bf16"), (3000, "bf16")])
+def test_norm_of_its_own_output(cols, dtype):
+    """A norm's y as its next x, without residual and dropout, where h is x: the gradients need what x was."""
+    rng = np.random.default_rng(cols)
+    x, dy = _rand(rng, 5, cols, dtype=dtype), _rand(rng, 5, cols, dtype=dtype)
+    w = 1 + 0.3 * _rand(rng, cols)
+    op = _seq().ResidualNorm(w, 5, dtype=DT[dtype], eps=1e-5)
+    y, _ = op.forward(x)
+    h = y.clone()
+    y, got_h = op.forward(y)
+    dx, _, dw = op.backward(dy)
+    _check("y", y, orc.norm_forward(_np(h), _np(w), 1e-5)[0], TOL[dtype])
+    wx, _, ww = orc.norm_backward(_np(h), _np(w), 1e-5, _np(dy))
+    assert torch.equal(got_h, h)
+    _check("dx", dx, wx, TOL[dtype])
+    _check("dw", dw, ww, TOL32[dtype])
+
+
 @pytest.mark.parametrize("t", [13, 19, 26, 31, 38, 51, 62, 95, 125, 3001])
 def test_fp8_codes_are_those_of_the_quotient(t):
     """h = 1/2 everywhere and eps = 3/4 make the norm's factor 1 and y = w / 2, exactly. Quotients y / scale lie at
