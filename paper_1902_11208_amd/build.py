@@ -8,7 +8,6 @@ Usage: python -m paper_1902_11208_amd.build [--verbose]
 from __future__ import annotations
 
 import concurrent.futures as cf
-import importlib.util
 import os
 import subprocess
 import sys
@@ -63,15 +62,14 @@ def _compile(src: str, verbose: bool) -> str:
     return obj
 
 
-def _torch() -> str:
-    return os.path.dirname(importlib.util.find_spec("torch").origin)  # found, not imported: that takes longer
-
-
 def _compile_binding() -> str:
-    obj, t = os.path.join(BUILD, "binding.o"), _torch()
+    import torch
+
+    obj, t = os.path.join(BUILD, "binding.o"), os.path.dirname(torch.__file__)
+    abi = int(torch.compiled_with_cxx11_abi())  # std::string as torch's own libraries have it
     includes = [os.path.join(t, "include"), os.path.join(t, "include", "torch", "csrc", "api", "include"),
                 sysconfig.get_paths()["include"], os.path.join(ROCM, "include")]
-    cmd = [CXX, "-O2", "-fPIC", "-std=c++17", "-DTORCH_EXTENSION_NAME=_binding", "-D_GLIBCXX_USE_CXX11_ABI=1", "-DUSE_ROCM",
+    cmd = [CXX, "-O2", "-fPIC", "-std=c++17", "-DTORCH_EXTENSION_NAME=_binding", f"-D_GLIBCXX_USE_CXX11_ABI={abi}", "-DUSE_ROCM",
            "-D__HIP_PLATFORM_AMD__", "-I", INCLUDE, *[x for i in includes for x in ("-isystem", i)], "-c",
            os.path.join(CSRC, "binding.cpp"), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -80,27 +78,38 @@ def _compile_binding() -> str:
     return obj
 
 
+def _link_binding(obj: str) -> None:
+    import torch
+
+    tmp = BINDING + ".tmp"
+    cmd = [CXX, "-shared", obj, "-o", tmp, "-L", os.path.join(os.path.dirname(torch.__file__), "lib"), "-ltorch_python",
+           "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_hip", "-L", PKG, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"link of the binding failed:\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, BINDING)
+
+
 def build(verbose: bool = False) -> str:
+    """The library, then the binding: the error of a binding that does not build is raised when the library is in
+    place, with no binding of an earlier build beside it."""
     os.makedirs(BUILD, exist_ok=True)
     jobs = min(len(SOURCES) + 1, max(1, min(16, os.cpu_count() or 1)))
     with cf.ThreadPoolExecutor(jobs) as ex:
         binding = ex.submit(_compile_binding)
         objs = list(ex.map(lambda s: _compile(s, verbose), SOURCES))
-        binding = binding.result()
     tmp = LIB + ".tmp"
     cmd = [HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-Wl,--no-undefined", *objs, "-o", tmp]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, LIB)
-    lib = os.path.join(_torch(), "lib")
-    tmp = BINDING + ".tmp"
-    cmd = [CXX, "-shared", binding, "-o", tmp, "-L", lib, "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_hip",
-           "-L", PKG, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN"]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"link of the binding failed:\n{r.stdout}\n{r.stderr}")
-    os.replace(tmp, BINDING)
+    try:
+        _link_binding(binding.result())
+    except Exception as e:
+        if os.path.exists(BINDING):
+            os.remove(BINDING)
+        raise RuntimeError("libmdlstm.so is built, the sequence operators' binding is not") from e
     return LIB
 
 

@@ -22,12 +22,10 @@ def read_fixture(name):
 
 @pytest.fixture(scope="session")
 def built_lib():
-    """Path of libmdlstm.so; built in-tree only if nothing is built yet."""
-    from paper_1902_11208_amd import _lib
+    """Path of libmdlstm.so; it and the sequence operators' binding are built in-tree only if one is missing."""
+    from paper_1902_11208_amd import _lib, build
 
-    if not os.path.exists(_lib.LIB_PATH):
-        from paper_1902_11208_amd import build
-
+    if not os.path.exists(_lib.LIB_PATH) or not os.path.exists(build.BINDING):
         build.build()
     return _lib.LIB_PATH
 
