@@ -192,13 +192,13 @@ __device__ __forceinline__ int row_offset(int row, int stride) { return stride <
 // and a chunk spans less than 2^31 bytes.
 template <typename T, int D, int THREADS, bool WIDE>
 struct Stage {
-    // (32 columns of bf16 in four waves: half of the threads suffice)
-    static constexpr int EPV = 16 / sizeof(T), VPR = D / EPV, ALL = C * VPR, N = (ALL + THREADS - 1) / THREADS, STEP = THREADS / VPR;
+    static constexpr int EPV = 16 / sizeof(T), VPR = D / EPV, N = C * VPR / THREADS, STEP = THREADS / VPR;
+    static_assert(N * THREADS == C * VPR, "every thread has the same number of vectors");
     u32x4 v[N];
     int offset;  // of the first vector
     __device__ __forceinline__ void init(int64_t stride, int dim) {
         const int first = threadIdx.x / VPR, col = threadIdx.x % VPR * EPV;
-        offset = col < dim && (int)threadIdx.x < ALL ? row_offset(first, (int)stride) + col * (int)sizeof(T) : OUT;
+        offset = col < dim ? row_offset(first, (int)stride) + col * (int)sizeof(T) : OUT;
     }
     __device__ __forceinline__ void load(const char* base, int64_t stride, int dim, int row0) {
         const int first = threadIdx.x / VPR, col = threadIdx.x % VPR * EPV;
@@ -212,7 +212,7 @@ struct Stage {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 v[i] = u32x4{0, 0, 0, 0};
-                if (first + i * STEP >= row0 && (int)threadIdx.x < ALL) {
+                if (first + i * STEP >= row0) {
                     const T* p = reinterpret_cast<const T*>(base + (first + i * STEP) * stride) + col;
                     T e[EPV];
 #pragma unroll
@@ -224,7 +224,6 @@ struct Stage {
     }
     template <bool IS_Q>
     __device__ __forceinline__ void store(T* tile, int pitch) const {
-        if (ALL < THREADS && (int)threadIdx.x >= ALL) return;
         T* p = tile + threadIdx.x / VPR * pitch;
         const int col = threadIdx.x % VPR * EPV;
 #pragma unroll
