@@ -913,16 +913,30 @@ __global__ __launch_bounds__(256) void k_step(StepArgs a) {
 }  // namespace
 
 // Tokens of a segment, 0: sequences are scanned whole. Segments cost a second
-// pass over k and v, the states between them and two more launches, so they are
-// taken only where the longest sequence would keep half of the chip or more idle
-// (64 sequences of 200 to 600 tokens, 4 heads of 32 fp32: 28 us whole, 37 us in
-// segments; one of 2048, 8 heads of 64: 21 us in segments, 63 whole). They
-// are as long as fills the chip once: four workgroups a CU, two above 64
+// pass over k and v, the states between them and two more launches, so the
+// longest sequence has to leave most of the chip idle for long: `idle` is how
+// many times the chip could run all workgroups while it runs. Equal sequences,
+// us whole and in segments, forward (gradients):
+//     tokens  heads          idle       whole          segments
+//      512    4 x 32 fp32    256 (85)   21.5 (21.6)    21.0 (18.2)
+//                            32 (10.7)  21.5 (21.7)    18.7 (22.8)
+//                            16 (5.3)   21.9 (23.0)    22.4 (30.0)
+//     1024    8 x 64 bf16    32 (10.7)  34.8 (34.9)    22.2 (33.4)
+//                            8 (2.7)    35.5 (45.5)    39.5 (76.2)
+//     2048    8 x 64 bf16    8 (2.7)    65.4 (83.4)    55.1 (119)
+//                            4 (1.3)    66.0 (113)     84.3 (223)
+//     2048    4 x 128 bf16   16 (5.3)   117 (118)      50.0 (95.9)
+//                            8 (2.7)    117 (121)      67.2 (178)
+// One sequence of 384 tokens gains nothing (8 x 64 bf16: 16.1 and 18.1; 4 x 128
+// 26.8 and 27.5; 4 x 64 fp32 29.7 and 24.1).
+// They are as long as fills the chip once: four workgroups a CU, two above 64
 // columns (one sequence of 32768, 8 heads of 128 bf16: 105 us with two, 127 with
 // four; of 65536, 8 heads of 64: 88 us with four, 103 with one and a half).
 static int64_t segment_of(const ScanArgs& a) {
     const int64_t resident = std::max(a.role[0].q.dim, a.role[0].v.dim) > 64 ? 512 : 1024, lanes = (int64_t)a.heads * a.n_roles;
-    if (a.longest <= 768 || a.longest * resident <= 2 * a.tokens * lanes) return 0;
+    if (a.longest <= 384) return 0;
+    const double idle = (double)a.longest * resident / ((double)a.tokens * lanes);
+    if (idle < 6.0 || (double)a.longest * idle <= 8192.0) return 0;
     const int64_t want = resident / lanes + 1;  // slots
     return std::max<int64_t>((a.tokens / want + C - 1) / C * C, 128);
 }

@@ -81,3 +81,18 @@ def test_attention_accepts_buffers_that_touch(backward):
     """Buffers one right after the other pass the checks (and the call then finds no device)."""
     st, says = _call(_apart(), backward)
     assert st not in (OK, INVALID, WORKSPACE, UNSUPPORTED) and "overlap" not in says, (st, says)
+
+
+# --- where sequences are cut into segments: the workspace then holds states -----------------------------------
+@pytest.mark.parametrize("n,tokens,heads,dim,dtype,forward,backward", [
+    (1, 384, 4, 32, 0, False, False), (1, 512, 4, 32, 0, True, True), (1, 512, 8, 64, 1, True, True),
+    (8, 512, 4, 32, 0, True, False), (16, 512, 4, 32, 0, False, False), (4, 1024, 8, 64, 1, True, True),
+    (16, 1024, 8, 64, 1, False, False), (16, 2048, 8, 64, 1, True, False), (32, 2048, 8, 64, 1, False, False),
+    (8, 2048, 4, 128, 1, True, False), (16, 2048, 4, 128, 1, True, False), (64, 2048, 4, 128, 1, False, False),
+    (1, 65536, 8, 64, 1, True, True)])
+def test_segments_only_where_they_are_faster(n, tokens, heads, dim, dtype, forward, backward):
+    L = _L()
+    d = L.AttentionDesc(heads, heads, dim, dim, dtype, 1.0)
+    for b, want in ((0, forward), (1, backward)):
+        size = L.lib().mdlstm_attention_workspace_bytes(d, n, n * tokens, tokens, b)
+        assert (size > 256) == want, (b, size)
