@@ -82,7 +82,12 @@ struct Mx<float> {
         for (int r = 0; r < 4; ++r) f[r] = tile[(row0 + 4 * g + r) * pitch + col0 + n];
         return f;
     }
-    static __device__ __forceinline__ Frag from(const floatx4* t) { return t[0]; }
+    // fp32 numbers as operands of a product
+    static constexpr int OPERANDS = 1;
+    template <int N>
+    static __device__ __forceinline__ void split(const floatx4* t, Frag (&f)[N]) {
+        f[0] = t[0];
+    }
 };
 template <>
 struct Mx<bf16_t> {
@@ -120,6 +125,21 @@ struct Mx<bf16_t> {
     static __device__ __forceinline__ Frag from(const floatx4* t) {
         return as_bf16x8(make_uint4(f2bf2(t[0][0], t[0][1]), f2bf2(t[0][2], t[0][3]), f2bf2(t[1][0], t[1][1]),
                                     f2bf2(t[1][2], t[1][3])));
+    }
+    // fp32 numbers as N bf16 operands: rounded, what that leaves out rounded, ...
+    static constexpr int OPERANDS = 2;
+    template <int N>
+    static __device__ __forceinline__ void split(const floatx4* t, Frag (&f)[N]) {
+        floatx4 x[2] = {t[0], t[1]};
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+            f[c] = from(x);
+            if (c + 1 < N)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[h][r] -= (float)f[c][4 * h + r];
+        }
     }
 };
 
@@ -358,7 +378,7 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
     constexpr int KT = SPLIT ? 1 : D / 16, OT = SPLIT ? 2 : TI;  // state tiles of a column tile, token tiles they meet
     static_assert(!SPLIT || (TPF == 1 && NT == 1), "a split state is built for fp32");
     constexpr int PQ = D + M::PAD_Q, PK = D + M::PAD;
-    constexpr int NP = sizeof(T) == 4 ? 1 : PIECES;
+    constexpr int NP = sizeof(T) == 4 ? 1 : PIECES, NO = M::OPERANDS;
     constexpr bool SHARE = SPLIT || (TI == 2 && !LOCAL && THREADS >= 192);
     constexpr int AT_K = LOCAL ? 0 : C * PQ, AT_V = AT_K + C * PK, BUF = AT_V + C * PK;
     constexpr int BUFS = 2 * BUF * sizeof(T) <= 60 * 1024 ? 2 : 1;
@@ -369,7 +389,7 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
     constexpr int PO = D + 8, OUT_PIECES = C * D / 8, OBUFS = SHARE ? 1 : 2;
     __shared__ __align__(16) T out_rows[ROWS_OUT ? OBUFS * C * PO : 8];
     typedef T Tile[64][4];  // P^T tile, four values of a lane together
-    __shared__ __align__(16) Tile shared_p[SHARE ? 3 : 1];
+    __shared__ __align__(16) Tile shared_p[NO][SHARE ? 3 : 1];
     __shared__ __align__(16) float passed[SPLIT ? 4 : 1][64][4];
     Unit u;
     if (!unit_of(a, u)) return;
@@ -514,7 +534,11 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
 #pragma unroll
                     for (int r = 0; r < 4; ++r) p[0][r] = 4 * g + r <= n ? p[0][r] * same[r] : 0.0f;
                 }
-                St<T>::st4(shared_p[wave][l], p[0]);
+                const floatx4 t[2] = {p[0], zero};
+                Frag f[NO];
+                M::split(t, f);
+#pragma unroll
+                for (int c = 0; c < NO; ++c) __builtin_memcpy(shared_p[c][wave][l], &f[c], sizeof(shared_p[c][wave][l]));
             }
 #pragma unroll
             for (int m = 0; m < NT; ++m)
@@ -544,9 +568,12 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
                     floatx4 t[TPF];
 #pragma unroll
                     for (int x = 0; x < TPF; ++x) t[x] = S[k * TPF + x][m];
-                    const Frag s = M::from(t);
+                    Frag s[NO];
+                    M::split(t, s);
 #pragma unroll
-                    for (int h = 0; h < OT; ++h) o[m][h] = M::mma(s, q[h], o[m][h]);
+                    for (int c = 0; c < NO; ++c)
+#pragma unroll
+                        for (int h = 0; h < OT; ++h) o[m][h] = M::mma(s[c], q[h], o[m][h]);
                 }
             }
 #pragma unroll
@@ -566,18 +593,22 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
                 out += (int64_t)C * os;
                 flush0 = 0;
             }
-            Frag f0[2 / TPF], f1[2 / TPF];  // P^T for the token tiles 0 and 1
+            Frag f0[2 / TPF][NO], f1[2 / TPF][NO];  // P^T for the token tiles 0 and 1
             if (SHARE) {
                 lds_barrier();
                 if constexpr (sizeof(T) == 2) {
-                    const uint2 x = *reinterpret_cast<const uint2*>(shared_p[0][l]), y = *reinterpret_cast<const uint2*>(shared_p[1][l]),
-                                z = *reinterpret_cast<const uint2*>(shared_p[2][l]);
-                    f0[0] = as_bf16x8(make_uint4(x.x, x.y, 0, 0));
-                    f1[0] = as_bf16x8(make_uint4(y.x, y.y, z.x, z.y));
+#pragma unroll
+                    for (int c = 0; c < NO; ++c) {
+                        const uint2 x = *reinterpret_cast<const uint2*>(shared_p[c][0][l]),
+                                    y = *reinterpret_cast<const uint2*>(shared_p[c][1][l]),
+                                    z = *reinterpret_cast<const uint2*>(shared_p[c][2][l]);
+                        f0[0][c] = as_bf16x8(make_uint4(x.x, x.y, 0, 0));
+                        f1[0][c] = as_bf16x8(make_uint4(y.x, y.y, z.x, z.y));
+                    }
                 } else {
-                    f0[0] = St<T>::ld4(shared_p[0][l]);
-                    f1[0] = St<T>::ld4(shared_p[1][l]);
-                    f1[1] = St<T>::ld4(shared_p[2][l]);
+                    f0[0][0] = St<T>::ld4(shared_p[0][0][l]);
+                    f1[0][0] = St<T>::ld4(shared_p[0][1][l]);
+                    f1[1][0] = St<T>::ld4(shared_p[0][2][l]);
                     if (SPLIT) o[0][0] = (i0 == 0 ? o[0][0] : o[0][OT - 1]) + St<float>::ld4(passed[wave ^ COLS][l]);
                 }
             } else {
@@ -590,18 +621,20 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
                 const floatx4 b0[2] = {p[0], zero}, b1[2] = {p[1], p[2]};
 #pragma unroll
                 for (int h = 0; h < 2 / TPF; ++h) {
-                    f0[h] = M::from(b0 + h);
-                    f1[h] = M::from(b1 + h);
+                    M::split(b0 + h, f0[h]);
+                    M::split(b1 + h, f1[h]);
                 }
             }
 #pragma unroll
-            for (int m = 0; m < NT; ++m) {
-                if (TI == 2 || i0 == 0) o[m][0] = M::mma(vf[m][0], f0[0], o[m][0]);
-                if (TI == 2 || i0 == 1) {
+            for (int m = 0; m < NT; ++m)
 #pragma unroll
-                    for (int h = 0; h < 2 / TPF; ++h) o[m][TI - 1] = M::mma(vf[m][h], f1[h], o[m][TI - 1]);
+                for (int c = 0; c < NO; ++c) {
+                    if (TI == 2 || i0 == 0) o[m][0] = M::mma(vf[m][0], f0[0][c], o[m][0]);
+                    if (TI == 2 || i0 == 1) {
+#pragma unroll
+                        for (int h = 0; h < 2 / TPF; ++h) o[m][TI - 1] = M::mma(vf[m][h], f1[h][c], o[m][TI - 1]);
+                    }
                 }
-            }
         } else {
 #pragma unroll
             for (int m = 0; m < NT; ++m)
@@ -637,15 +670,7 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) x[h][r] = (float)vf[m][0][4 * h + r] * (w[h][r] * fresh);
-#pragma unroll
-                for (int c = 0; c < NP; ++c) {
-                    wv[m][0][c] = M::from(x);
-                    if (c + 1 < NP)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h)
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) x[h][r] -= (float)wv[m][0][c][4 * h + r];
-                }
+                M::split(x, wv[m][0]);
             }
         }
 #pragma unroll

@@ -343,3 +343,29 @@ def test_fp8_codes_are_those_of_the_quotient(t):
     want = (y / s).to(torch.float8_e4m3fn)
     got = y8.cpu()
     assert torch.equal(got.view(torch.uint8), want.view(torch.uint8).expand(3, -1)), (got.float()[0] - want.float()).nonzero()
+
+
+# --- bf16 --------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("lengths,heads,kv,dk,dv", [([300, 0, 131], 4, 4, 32, 32), ([300, 131], 4, 2, 64, 64),
+                                                    ([300, 131], 4, 1, 128, 128), ([200, 77], 2, 2, 24, 100), ([1500], 2, 2, 64, 64)])
+def test_bf16_outputs_are_rounded_once(lengths, heads, kv, dk, dv):
+    """Scores and states enter the products as fp32 numbers, so outputs and gradients carry the error of their own
+    rounding only: uniform in half a step of 8 bits either way, that is 2^-7 / sqrt(12) of the binade's lower edge or
+    less, in the mean over many outputs. Shared heads' sums and states see fp32 sums too."""
+    rng = np.random.default_rng(dk + dv)
+    T, n, once = sum(lengths), len(lengths), 2.0 ** -7 / 12 ** 0.5
+    print(f"case: bf16 {lengths} heads {heads}/{kv} dims {dk}x{dv}", flush=True)
+    q, k = _rand(rng, T, heads, dk, dtype="bf16"), _rand(rng, T, kv, dk, dtype="bf16")
+    v, do = _rand(rng, T, kv, dv, dtype="bf16"), _rand(rng, T, heads, dv, dtype="bf16")
+    st, ds = _rand(rng, n, heads, dk, dv), _rand(rng, n, heads, dk, dv)
+    a = torch.from_numpy(rng.uniform(0.004, 0.3, heads).astype(np.float32)).cuda()
+    op = _seq().DecayAttention(lengths, heads, dk, dv, a, kv_heads=kv)
+    o, final = op.forward(q, k, v, state=st, final_state=True)
+    dq, dk_, dv_, dst = op.backward(do, dstate=ds)
+    args = _np(q), _np(k), _np(v), lengths, _np(a), dk ** -0.5
+    wo, wf = orc.attention_forward(*args, _np(st))
+    want = orc.attention_backward(*args, _np(do), _np(st), _np(ds))
+    for name, g, w in zip(("o", "dq", "dk", "dv"), (o, dq, dk_, dv_), (wo, *want[:3])):
+        assert rel_err(_np(g), w) <= once, (name, rel_err(_np(g), w))
+    for name, g, w in (("final", final, wf), ("dstate", dst, want[3])):
+        assert rel_err(_np(g), w) <= 1e-5, (name, rel_err(_np(g), w))
