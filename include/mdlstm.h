@@ -448,7 +448,10 @@ typedef struct {
  * The state restarts at every example's edge (S_{-1} = 0, or d_state), so the
  * packed result equals each example computed alone. Query heads h share the
  * key and value head h / (heads / kv_heads).
- * dtype: storage of q, k, v, o and their gradients; states and sums are fp32.
+ * dtype: storage of q, k, v, o and their gradients; states and sums are fp32 (in
+ * bf16 they enter the matrix products as two bf16 pieces, 2^-17 off at most), and
+ * an output is rounded once, to its storage. A value that is not finite gives
+ * what the recurrence gives, in its own example and head.
  * 1 <= dim_k, dim_v <= 128, 1 <= kv_heads <= heads <= 1024, heads a multiple of
  * kv_heads.
  */
@@ -472,7 +475,8 @@ size_t mdlstm_attention_workspace_bytes(const mdlstm_attention_desc* desc, int32
  * d_order [n] (device; may be NULL: as numbered): the examples in the order in
  * which they are started, which changes no result but the time: longest first
  * keeps the chip busy to the end. An entry outside [0, n) is skipped; an example
- * that is not listed is not computed.
+ * that is not listed need not be computed (where long examples are cut into
+ * segments the order is not read and all are).
  * d_rates [heads]: a_h, fp32.
  * d_state [n][heads][dim_k][dim_v] (may be NULL: zero): the state each example
  * starts from; d_final (out, may be NULL): the state it leaves (an empty

@@ -38,20 +38,23 @@ __device__ __forceinline__ void sequence(const int64_t* offsets, int i, int64_t 
 // as they stand, with the reduction slots of lane group g taken as rows 4 g + r
 // (and 16 + 4 g + r). The state never passes through LDS.
 //
-// bf16: P and S are rounded to bf16 as operands, one rounding of each on its
-// way to an output that is rounded to bf16 itself (measured 2.3e-3 of the
-// output, 1.7e-3 for fp32 sums rounded once). The state's own sum takes
-// g^(C-1-j) v_j in PIECES bf16 pieces (2: 2^-17 of a term is left out, 3: 2^-25,
-// where the state is a result of the call), so it is as good as its fp32
-// accumulators; one piece would add a third rounding to every output.
+// bf16: q, k and v are operands as they are stored; P and S, fp32 sums, enter as
+// two bf16 pieces each, the rounded number and what that leaves out (2^-17 of it
+// is dropped), so an output carries the error of its own rounding only: 1.66e-3
+// of the outputs. One piece each would leave 2.35e-3 and take 103 instead of
+// 127 us for the wide batch's forward pass, 212 instead of 266 for its gradients.
+// The state's sum takes g^(C-1-j) v_j in PIECES pieces (2, or 3 where the state is
+// a result of the call: 2^-25 of a term is left out).
 //
-// What bounds it: memory where the heads are 64 and more wide and units are many
-// (1024 units of 1024 tokens, 128 columns bf16, 1.07 GB: 240 us, 4.5 TB/s; 64
-// columns 115 us, 4.7 TB/s, where a copy reaches 5.5), the latency of a chunk
-// where they are few (a unit alone: 0.9 us a chunk at 64 bf16 columns, 1.7 at 128,
-// 1.1 at 32 fp32), and the fp32 MFMA at 128 fp32 columns (3.1 TB/s). C = 32 and not
-// 64: the products inside a chunk grow with C, the state's do not, and a chunk of
-// 64 rows would leave one workgroup a CU at 128 columns.
+// What bounds it: memory at 64 columns where units are many (1024 units of 1024
+// tokens, bf16, 0.54 GB: 115 us, 4.7 TB/s, where a copy reaches 5.5); at 128 bf16
+// columns the waits between a chunk's products, which two workgroups a CU cannot
+// fill (1024 units of 1024 tokens, 1.07 GB: 294 us, 3.7 TB/s; matrix instructions
+// take 19% of the time, vector instructions 30%); the fp32 MFMA at 128 fp32 columns
+// (694 us, 3.1 TB/s); the latency of a chunk where units are few (a unit alone: 1.0
+// us a chunk at 64 bf16 columns, 2.1 at 128, 1.05 at 32 fp32). C = 32 and not 64: the
+// products inside a chunk grow with C, the state's do not, and a chunk of 64 rows
+// would leave one workgroup a CU at 128 columns.
 // ---------------------------------------------------------------------------
 constexpr int C = 32;
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -171,7 +174,7 @@ struct Unit {
 // Units in launch order: workgroup b runs on XCD b % 8, which takes the roles
 // and `together` heads of one slot one after the other: they read the same
 // tokens, and the heads of a token share cache lines where they are narrow (1024
-// units of 32 bf16 columns, 32 chunks each: 76 us by (slot, key head), 50 by slot).
+// units of 32 bf16 columns, 32 chunks each: 78 us by (slot, key head), 49 by slot).
 // False: no unit.
 __device__ __forceinline__ bool unit_of(const ScanArgs& a, Unit& u) {
     const int group = a.together, kv = a.heads / group, inner = a.n_roles * group;
@@ -183,7 +186,7 @@ __device__ __forceinline__ bool unit_of(const ScanArgs& a, Unit& u) {
     u.head = (int)(rest % kv) * group + in / a.n_roles;
     u.j = 0;
     u.seq = (int)u.slot;
-    if (!a.seg && a.order) {  // longest first: the wide batch's gradients 255 -> 229 us
+    if (!a.seg && a.order) {  // longest first: the wide batch's gradients 269 us, 295 as numbered
         u.seq = __builtin_amdgcn_readfirstlane(a.order[u.slot]);
         if (u.seq < 0 || u.seq >= a.n) return false;
     }
@@ -384,7 +387,7 @@ __global__ __launch_bounds__((scan_threads<D, NT, TI>()), 2) void k_scan(ScanArg
     constexpr int BUFS = 2 * BUF * sizeof(T) <= 60 * 1024 ? 2 : 1;
     __shared__ __align__(16) T lds[BUFS * BUF];
     // bf16 outputs pass through LDS, to leave as whole rows a chunk later: a wave's
-    // own stores are 32 bytes of a row (wide batch forward 117 -> 104 us)
+    // own stores are 32 bytes of a row (wide batch forward 128 us, 171 with those)
     constexpr bool ROWS_OUT = sizeof(T) == 2 && WIDE && !LOCAL;
     constexpr int PO = D + 8, OUT_PIECES = C * D / 8, OBUFS = SHARE ? 1 : 2;
     __shared__ __align__(16) T out_rows[ROWS_OUT ? OBUFS * C * PO : 8];
@@ -852,7 +855,11 @@ __global__ __launch_bounds__(256) void k_sum_heads(int64_t n, int group, int dim
 // workgroup per (row, head) issues all its loads of the state at once. CG
 // threads share a row of it, V columns each; the workgroup's other threads take
 // other rows, and their sums for o meet by shuffles and in LDS. 509 rows of 16 heads
-// of 128 x 128: 204 us for 1.07 GB, 5.3 TB/s; few rows: the launch (3.2 us).
+// of 128 x 128: 204 us for 1.07 GB, 5.3 TB/s; few rows: the launch (3.2 us). 4 heads of
+// 32 x 32 fp32, 16384 rows: 4.6 TB/s. Narrower states leave most of the 256 threads
+// without one (16 x 16 and 65536 rows: 427 us, 1.4 TB/s, 1.6 ns a workgroup), and
+// states whose rows are not 16-byte vectors move by 4 bytes a lane (61 x 61, 4096
+// rows: 143 us, 3.5 TB/s).
 // ---------------------------------------------------------------------------
 template <int V>
 struct Cols {
@@ -943,20 +950,21 @@ __global__ __launch_bounds__(256) void k_step(StepArgs a) {
 // many times the chip could run all workgroups while it runs. Equal sequences,
 // us whole and in segments, forward (gradients):
 //     tokens  heads          idle       whole          segments
-//      512    4 x 32 fp32    256 (85)   21.5 (21.6)    21.0 (18.2)
-//                            32 (10.7)  21.5 (21.7)    18.7 (22.8)
-//                            16 (5.3)   21.9 (23.0)    22.4 (30.0)
-//     1024    8 x 64 bf16    32 (10.7)  34.8 (34.9)    22.2 (33.4)
-//                            8 (2.7)    35.5 (45.5)    39.5 (76.2)
-//     2048    8 x 64 bf16    8 (2.7)    65.4 (83.4)    55.1 (119)
-//                            4 (1.3)    66.0 (113)     84.3 (223)
-//     2048    4 x 128 bf16   16 (5.3)   117 (118)      50.0 (95.9)
-//                            8 (2.7)    117 (121)      67.2 (178)
-// One sequence of 384 tokens gains nothing (8 x 64 bf16: 16.1 and 18.1; 4 x 128
-// 26.8 and 27.5; 4 x 64 fp32 29.7 and 24.1).
+//      512    4 x 32 fp32    256 (85)   21.4 (21.5)    17.9 (18.0)
+//                            32 (10.7)  21.6 (22.2)    18.8 (23.2)
+//                            16 (5.3)   21.7 (22.6)    22.4 (30.1)
+//     1024    8 x 64 bf16    32 (10.7)  37.3 (38.1)    23.0 (34.5)
+//                            8 (2.7)    37.9 (51.3)    39.9 (81.0)
+//     2048    8 x 64 bf16    8 (2.7)    70.3 (97.1)    55.4 (128)
+//                            4 (1.3)    73.2 (141)     85.2 (245)
+//     2048    4 x 128 bf16   16 (5.3)   146 (146)      51.9 (105)
+//                            8 (2.7)    147 (148)      71.8 (205)
+// One sequence of 384 tokens gains little (8 x 64 bf16: 17.1 and 18.6; 4 x 128
+// 31.7 and 29.0; 4 x 64 fp32 29.3 and 23.9).
 // They are as long as fills the chip once: four workgroups a CU, two above 64
-// columns (one sequence of 32768, 8 heads of 128 bf16: 105 us with two, 127 with
-// four; of 65536, 8 heads of 64: 88 us with four, 103 with one and a half).
+// columns (one sequence of 32768, 8 heads of 128 bf16: 109 us with two, 144 with
+// four, 157 with one; of 65536, 8 heads of 64: 78 us with four, 91 with eight, 95
+// with one and a half).
 static int64_t segment_of(const ScanArgs& a) {
     const int64_t resident = std::max(a.role[0].q.dim, a.role[0].v.dim) > 64 ? 512 : 1024, lanes = (int64_t)a.heads * a.n_roles;
     if (a.longest <= 384) return 0;
@@ -1029,8 +1037,7 @@ hipError_t launch_scan(const ScanArgs& in, hipStream_t s) {
     // states and both tiles; 256 units 24 and 29), at 16 only up to a unit a SIMD
     // (32 units 18 us against 22; 1024 units of 8 to 400 tokens, log-normal about 100,
     // 16.4 against 19.0, of 200 each 13.7 against 13.8; gradients as 1536 units of 50
-    // tokens 11.1 against 8.6). bf16 gains nothing from it (32 units 15 us both ways,
-    // 2048 units 61 against 57).
+    // tokens 11.1 against 8.6). bf16 gained nothing from it (2048 units 61 against 57).
     if (d <= 16)
         return a.slots * a.heads * a.n_roles <= 1024 ? scan_any<float, 16, 1, 1>(a, s) : scan_any<float, 16, 1, 2>(a, s);
     if (d <= 32) return scan_any<float, 32, 1, 1>(a, s);

@@ -7,7 +7,7 @@
 // dropout with a residual, 48000 x 2048 bf16, 99 us (590 MB, 6.0 TB/s); norm with
 // residual and dropout, 96000 x 512 bf16, 66 us forward (6.0 TB/s) and 100 us
 // backward (4.9 TB/s) with 4 us for dw's shares; 8-bit output, 16383 x 5000 bf16,
-// 116 us (4.9 TB/s). A block of the generator (ten rounds of two 32-bit products)
+// 117 us (4.9 TB/s). A block of the generator (ten rounds of two 32-bit products)
 // serves eight elements, 16 bits each, so it stays below the memory's time.
 #include <algorithm>
 #include <type_traits>
@@ -332,9 +332,12 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 
 // lane holds and the threads of a workgroup. Measured at 60 million elements:
 // two bytes an element leave a lane 16 bytes of a tensor a vector, and then two
 // vectors in one wave beat two waves (rows of 1000: backward 125 against 143 us;
-// four bytes: forward 113 against 92), and a forward pass wants at most about
-// four waves on a row's barriers (8-bit output, rows of 4096: 78 against 86 us, of
-// 5000: 87 with three vectors, 116 with ten waves; backward 4096: 184 against 133).
+// four bytes: forward 113 against 92), and a forward pass wants few waves on a
+// row's barriers: four up to 2048 elements, then two vectors (8-bit output, rows of
+// 4096: 79 against 86 us; backward 4096: 184 against 133), from 4097 to 6144 three in
+// four waves (5000: 89 with them, 116 with ten waves), and beyond again two, in
+// seven or eight waves (8192: 81, with four vectors in four waves 86; 7168: 86
+// against 90).
 template <typename F>
 hipError_t with_shape(int cols, int dtype, bool forward, F&& f) {
     const int v = (cols + 7) / 8, waves = (v + 63) / 64;

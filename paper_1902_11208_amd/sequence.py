@@ -64,7 +64,8 @@ class DecayAttention:
     every sequence's edge. lengths: tokens of each sequence (host), e.g. the
     widths of an output layer's rectangles; zero is allowed. rates: [heads] fp32
     device tensor, >= 0. kv_heads: heads of k and v, shared by heads / kv_heads
-    query heads each. scale: 1 / sqrt(dim_k) unless given.
+    query heads each. scale: 1 / sqrt(dim_k) unless given. dtype: storage of q, k, v,
+    o and their gradients; sums and states are fp32, and outputs are rounded once.
 
     States that a call returned may be given back to the object, to go through
     sequences piece by piece: a call writes to a buffer that neither its
