@@ -37,6 +37,8 @@ def _stream(stream):
 
 def _empty(shape, dtype, device, stream) -> torch.Tensor:
     """Memory for work on `stream`: what the current stream freed may still be in use there."""
+    if stream is not None and not isinstance(stream, torch.cuda.Stream):  # another holder of a stream handle
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
     with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
         return torch.empty(shape, dtype=dtype, device=device)
 

@@ -369,3 +369,21 @@ def test_bf16_outputs_are_rounded_once(lengths, heads, kv, dk, dv):
         assert rel_err(_np(g), w) <= once, (name, rel_err(_np(g), w))
     for name, g, w in (("final", final, wf), ("dstate", dst, want[3])):
         assert rel_err(_np(g), w) <= 1e-5, (name, rel_err(_np(g), w))
+
+
+def test_streams_by_their_handle():
+    """stream= takes whatever holds a stream's handle (the default stream's is 0)."""
+    import types
+
+    side = torch.cuda.Stream()
+    x = torch.ones(40, 64, device="cuda")
+    w = torch.ones(64, device="cuda")
+    want = _seq().ResidualNorm(w, 40, dtype=torch.float32).forward(x)[0]
+    drop = _seq().dropout(x, 0.5, 1)
+    torch.cuda.synchronize()
+    for s in (torch.cuda.default_stream(), side, types.SimpleNamespace(cuda_stream=side.cuda_stream),
+              torch.cuda.ExternalStream(side.cuda_stream)):
+        y = _seq().ResidualNorm(w, 40, dtype=torch.float32).forward(x, stream=s)[0]
+        d = _seq().dropout(x, 0.5, 1, stream=s)
+        torch.cuda.synchronize()
+        assert torch.equal(y, want) and torch.equal(d, drop)
