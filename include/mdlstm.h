@@ -582,6 +582,112 @@ mdlstm_status mdlstm_norm_backward(const mdlstm_norm_desc* desc, int64_t rows, c
                                    uint64_t seed, uint64_t call, void* d_dx, void* d_dresidual, float* d_dw,
                                    void* d_workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Gated linear recurrence over packed sequences. Per example and channel, with
+ * the fp32 state h,
+ *     h_t = f_t h_(t-1) + u_t
+ *     gate MDLSTM_GATE_SIGMOID: f = sigmoid(z), u = (1 - f) x
+ *     gate MDLSTM_GATE_NONE:    f = z, u = x
+ * The state restarts at every example's edge (h_(-1) = 0, or d_state). dtype:
+ * storage of z, x, h and their gradients; sums and states are fp32 and an output is
+ * rounded once. A value that is not finite gives what the recurrence gives, in its
+ * own example and channel. 1 <= channels <= 2^20.
+ */
+typedef enum { MDLSTM_GATE_NONE = 0, MDLSTM_GATE_SIGMOID = 1 } mdlstm_gate;
+typedef struct {
+    int32_t channels, dtype;
+    int32_t gate; /* mdlstm_gate */
+} mdlstm_recurrence_desc;
+
+/* Workspace of a forward call, or with backward != 0 of a backward call, as for
+ * the attention calls. 0 when an argument is invalid; otherwise at least 16. */
+size_t mdlstm_recurrence_workspace_bytes(const mdlstm_recurrence_desc* desc, int32_t n, int64_t tokens,
+                                         int64_t longest, int32_t backward);
+
+/* Bytes of d_marks, the fp32 states that a forward call keeps for its backward
+ * call (one of every 128 tokens). 0 when an argument is invalid; otherwise at least 16. */
+size_t mdlstm_recurrence_marks_bytes(const mdlstm_recurrence_desc* desc, int64_t tokens);
+
+/*
+ * d_offsets, d_order, tokens and longest as for mdlstm_attention_forward. d_z and
+ * d_x: rows of `channels` elements, z_stride and x_stride >= channels elements
+ * apart. d_state [n][channels] (may be NULL: zero): the state each example starts
+ * from; d_final (out, may be NULL): the state it leaves. d_h (out) [tokens]
+ * [channels]. d_marks (out, may be NULL: no backward call follows). Asynchronous on
+ * `stream`; capturable into a graph. Buffers that the call writes must not
+ * overlap others (INVALID_ARG).
+ */
+mdlstm_status mdlstm_recurrence_forward(const mdlstm_recurrence_desc* desc, int32_t n, int64_t tokens, int64_t longest,
+                                        const int64_t* d_offsets, const int32_t* d_order, const void* d_z,
+                                        int64_t z_stride, const void* d_x, int64_t x_stride, const float* d_state,
+                                        void* d_h, float* d_final, float* d_marks, void* d_workspace,
+                                        size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of sum(h * dh) + sum(final * dfinal) with respect to z, x and the
+ * initial state, after a forward call on the same inputs (d_marks as that call
+ * left it). d_dh: rows dh_stride >= channels apart. d_dfinal and d_dstate (out)
+ * may be NULL. d_dz and d_dx (out) [tokens][channels] are overwritten.
+ */
+mdlstm_status mdlstm_recurrence_backward(const mdlstm_recurrence_desc* desc, int32_t n, int64_t tokens, int64_t longest,
+                                         const int64_t* d_offsets, const int32_t* d_order, const void* d_z,
+                                         int64_t z_stride, const void* d_x, int64_t x_stride, const float* d_state,
+                                         const float* d_marks, const void* d_dh, int64_t dh_stride,
+                                         const float* d_dfinal, void* d_dz, void* d_dx, float* d_dstate,
+                                         void* d_workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * One token for each of n sequences: row i of z and x advances the state at
+ * d_state [slots][channels] (in and out, fp32) of slot d_slots[i] (device; NULL:
+ * slot i, then n <= slots) and gives h_i (d_h [n][channels]). A slot outside
+ * [0, slots) marks an idle row: its h is zero and no state changes. Two rows must
+ * not name the same slot.
+ */
+mdlstm_status mdlstm_recurrence_step(const mdlstm_recurrence_desc* desc, int32_t n, const void* d_z, int64_t z_stride,
+                                     const void* d_x, int64_t x_stride, float* d_state, int64_t slots,
+                                     const int32_t* d_slots, void* d_h, void* stream);
+
+/*
+ * Norm over groups with an activation, channels last. Per example and group of
+ * channels / groups neighbouring channels, mean and var over the example's tokens
+ * and the group's channels:
+ *     c = (x - mean) rstd     rstd = 1 / sqrt(var + eps)     y = act(c w + b)
+ * act: none, max(u, 0) (its derivative at 0 is 0), or u sigmoid(u). w, b: fp32
+ * [channels]. dtype: storage of x, y and their gradients; sums are fp32 (var from
+ * the distances to the mean), those of long examples joined in 64 bits, all in a
+ * fixed order. channels <= 2^20, channels / groups <= 4096 (UNSUPPORTED beyond).
+ */
+typedef enum { MDLSTM_NO_ACTIVATION = 0, MDLSTM_RELU = 1, MDLSTM_SILU = 2 } mdlstm_activation;
+typedef struct {
+    int32_t channels, groups, dtype;
+    int32_t activation; /* mdlstm_activation */
+    float eps;          /* > 0 */
+} mdlstm_group_norm_desc;
+
+/* Workspace of a forward or (backward != 0) backward call; 0 for invalid
+ * arguments, otherwise at least 16. */
+size_t mdlstm_group_norm_workspace_bytes(const mdlstm_group_norm_desc* desc, int32_t n, int64_t tokens, int64_t longest,
+                                         int32_t backward);
+
+/*
+ * d_offsets, d_order, tokens, longest as for mdlstm_attention_forward; d_x: rows
+ * x_stride >= channels apart. d_y (out) [tokens][channels]; d_mean and d_rstd (out)
+ * [n][groups], for the backward (an empty example's mean is 0).
+ */
+mdlstm_status mdlstm_group_norm_forward(const mdlstm_group_norm_desc* desc, int32_t n, int64_t tokens, int64_t longest,
+                                        const int64_t* d_offsets, const int32_t* d_order, const void* d_x,
+                                        int64_t x_stride, const float* d_w, const float* d_b, void* d_y, float* d_mean,
+                                        float* d_rstd, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients of sum(y * dy): d_dx (out) [tokens][channels], d_dw and d_db (out)
+ * [channels] fp32, overwritten. d_dy: rows dy_stride >= channels apart. */
+mdlstm_status mdlstm_group_norm_backward(const mdlstm_group_norm_desc* desc, int32_t n, int64_t tokens, int64_t longest,
+                                         const int64_t* d_offsets, const int32_t* d_order, const void* d_x,
+                                         int64_t x_stride, const float* d_w, const float* d_b, const float* d_mean,
+                                         const float* d_rstd, const void* d_dy, int64_t dy_stride, void* d_dx,
+                                         float* d_dw, float* d_db, void* d_workspace, size_t workspace_bytes,
+                                         void* stream);
+
 /* Message for the last non-OK status returned on the calling thread. */
 const char* mdlstm_last_error(void);
 

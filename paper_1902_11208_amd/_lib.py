@@ -48,9 +48,19 @@ class NormDesc(ctypes.Structure):
     _fields_ = [("cols", c_i32), ("dtype", c_i32), ("eps", ctypes.c_float), ("p", ctypes.c_double)]
 
 
+class RecurrenceDesc(ctypes.Structure):
+    _fields_ = [("channels", c_i32), ("dtype", c_i32), ("gate", c_i32)]
+
+
+class GroupNormDesc(ctypes.Structure):
+    _fields_ = [("channels", c_i32), ("groups", c_i32), ("dtype", c_i32), ("activation", c_i32), ("eps", ctypes.c_float)]
+
+
 P_HEADS = ctypes.POINTER(Heads)
 P_ATTENTION = ctypes.POINTER(AttentionDesc)
 P_NORM = ctypes.POINTER(NormDesc)
+P_RECURRENCE = ctypes.POINTER(RecurrenceDesc)
+P_GROUP_NORM = ctypes.POINTER(GroupNormDesc)
 
 SIGNATURES = {
     "mdlstm_pack_workspace_bytes": (c_size, [c_i32]),
@@ -101,6 +111,20 @@ SIGNATURES = {
     "mdlstm_norm_workspace_bytes": (c_size, [P_NORM, c_i64]),
     "mdlstm_norm_backward": (c_i32, [P_NORM, c_i64, c_void, c_i64, c_void, c_void, c_void, c_void, c_u64, c_u64, c_void,
                                      c_void, c_void, c_void, c_size, c_void]),
+    "mdlstm_recurrence_workspace_bytes": (c_size, [P_RECURRENCE, c_i32, c_i64, c_i64, c_i32]),
+    "mdlstm_recurrence_marks_bytes": (c_size, [P_RECURRENCE, c_i64]),
+    "mdlstm_recurrence_forward": (c_i32, [P_RECURRENCE, c_i32, c_i64, c_i64, c_void, c_void, c_void, c_i64, c_void, c_i64,
+                                          c_void, c_void, c_void, c_void, c_void, c_size, c_void]),
+    "mdlstm_recurrence_backward": (c_i32, [P_RECURRENCE, c_i32, c_i64, c_i64, c_void, c_void, c_void, c_i64, c_void, c_i64,
+                                           c_void, c_void, c_void, c_i64, c_void, c_void, c_void, c_void, c_void, c_size,
+                                           c_void]),
+    "mdlstm_recurrence_step": (c_i32, [P_RECURRENCE, c_i32, c_void, c_i64, c_void, c_i64, c_void, c_i64, c_void, c_void,
+                                       c_void]),
+    "mdlstm_group_norm_workspace_bytes": (c_size, [P_GROUP_NORM, c_i32, c_i64, c_i64, c_i32]),
+    "mdlstm_group_norm_forward": (c_i32, [P_GROUP_NORM, c_i32, c_i64, c_i64, c_void, c_void, c_void, c_i64, c_void, c_void,
+                                          c_void, c_void, c_void, c_void, c_size, c_void]),
+    "mdlstm_group_norm_backward": (c_i32, [P_GROUP_NORM, c_i32, c_i64, c_i64, c_void, c_void, c_void, c_i64, c_void, c_void,
+                                           c_void, c_void, c_void, c_i64, c_void, c_void, c_void, c_void, c_size, c_void]),
 }
 
 STATUS = {0: "OK", 1: "INVALID_ARG", 2: "TOO_WIDE", 3: "BAD_LAYOUT", 4: "WORKSPACE", 5: "UNSUPPORTED", 6: "DEVICE",

@@ -263,6 +263,141 @@ at::Tensor dropout(const at::Tensor& x, double p, uint64_t seed, uint64_t call, 
     return y;
 }
 
+// ---------------------------------------------------------------------------
+// Gated recurrence and group norm over packed sequences
+// ---------------------------------------------------------------------------
+struct Recurrence {
+    mdlstm_recurrence_desc desc;
+    int32_t n;
+    int64_t tokens, longest;
+    at::Tensor offsets, order;
+    at::ScalarType dtype;
+    at::Device device;
+
+    Recurrence(int channels, int dtype_, int gate, int n_, int64_t tokens_, int64_t longest_, at::Tensor offsets_,
+               at::Tensor order_)
+        : desc{channels, dtype_, gate}, n(n_), tokens(tokens_), longest(longest_), offsets(std::move(offsets_)),
+          order(std::move(order_)), dtype(storage(dtype_)), device(offsets.device()) {}
+
+    int64_t row_like(const at::Tensor& t, const char* name) const {
+        return rows_of(t, name, tokens, desc.channels, dtype, device);
+    }
+    float* state_like(const MaybeTensor& t, const char* name) const {
+        return static_cast<float*>(full(t, name, {n, desc.channels}, at::kFloat, device));
+    }
+
+    // h, final, marks, the workspace and the gradients are the caller's own buffers
+    void forward(const at::Tensor& z, const at::Tensor& x, const MaybeTensor& state, const at::Tensor& h,
+                 const MaybeTensor& final, const at::Tensor& marks, const at::Tensor& ws, const MaybeStream& stream) const {
+        const int64_t zs = row_like(z, "z"), xs = row_like(x, "x");
+        const float* from = state_like(state, "state");
+        float* to = state_like(final, "final");
+        on_gpu(z, "z");
+        const c10::hip::HIPGuard on(device.index());
+        mdlstm_status st;
+        {
+            py::gil_scoped_release none;
+            st = mdlstm_recurrence_forward(&desc, n, tokens, longest, offsets.data_ptr<int64_t>(), order.data_ptr<int32_t>(),
+                                           z.data_ptr(), zs, x.data_ptr(), xs, from, h.data_ptr(), to, marks.data_ptr<float>(),
+                                           ws.data_ptr(), ws.numel(), stream_of(stream, device));
+        }
+        ok(st);
+    }
+
+    void backward(const at::Tensor& z, const at::Tensor& x, const MaybeTensor& state, const at::Tensor& marks,
+                  const at::Tensor& dh, const MaybeTensor& dfinal, const at::Tensor& dz, const at::Tensor& dx,
+                  const MaybeTensor& dstate, const at::Tensor& ws, const MaybeStream& stream) const {
+        const int64_t zs = row_like(z, "z"), xs = row_like(x, "x"), gs = row_like(dh, "dh");
+        const float *from = state_like(state, "state"), *df = state_like(dfinal, "dstate");
+        float* ds = state_like(dstate, "dstate");
+        const c10::hip::HIPGuard on(device.index());
+        mdlstm_status st;
+        {
+            py::gil_scoped_release none;
+            st = mdlstm_recurrence_backward(&desc, n, tokens, longest, offsets.data_ptr<int64_t>(), order.data_ptr<int32_t>(),
+                                            z.data_ptr(), zs, x.data_ptr(), xs, from, marks.data_ptr<float>(), dh.data_ptr(), gs,
+                                            df, dz.data_ptr(), dx.data_ptr(), ds, ws.data_ptr(), ws.numel(),
+                                            stream_of(stream, device));
+        }
+        ok(st);
+    }
+};
+
+at::Tensor recurrence_step(const at::Tensor& z, const at::Tensor& x, const at::Tensor& state, const MaybeTensor& slots, int gate,
+                           const MaybeTensor& out, const MaybeStream& stream) {
+    for (const auto& [t, name] : {std::tuple<const at::Tensor&, const char*>{z, "z"}, {x, "x"}, {state, "state"}})
+        if (!t.defined() || t.dim() != 2) refuse(name, " must be a tensor of 2 dimensions");
+    const int64_t n = z.size(0), c = z.size(1), count = state.size(0);
+    if (n > INT32_MAX || c > INT32_MAX) refuse("z is too large");
+    const at::ScalarType dt = z.scalar_type();
+    const at::Device dev = z.device();
+    const mdlstm_recurrence_desc desc = {(int32_t)c, dtype_code(z), gate};
+    const int64_t zs = rows_of(z, "z", n, c, dt, dev), xs = rows_of(x, "x", n, c, dt, dev);
+    float* st = static_cast<float*>(full(state, "state", {count, c}, at::kFloat, dev));
+    const int32_t* at_slot = static_cast<int32_t*>(full(slots, "slots", {n}, at::kInt, dev));
+    full(out, "out", {n, c}, dt, dev);
+    on_gpu(z, "z");
+    const c10::hip::HIPGuard on(dev.index());
+    const at::Tensor h = out ? *out : empty({n, c}, z, stream);
+    mdlstm_status status;
+    {
+        py::gil_scoped_release none;
+        status = mdlstm_recurrence_step(&desc, (int32_t)n, z.data_ptr(), zs, x.data_ptr(), xs, st, count, at_slot, h.data_ptr(),
+                                        stream_of(stream, dev));
+    }
+    ok(status);
+    return h;
+}
+
+struct GroupNorm {
+    mdlstm_group_norm_desc desc;
+    int32_t n;
+    int64_t tokens, longest;
+    at::Tensor offsets, order, weight, bias;
+    at::ScalarType dtype;
+    at::Device device;
+
+    GroupNorm(int channels, int groups, int dtype_, int activation, double eps, int n_, int64_t tokens_, int64_t longest_,
+              at::Tensor offsets_, at::Tensor order_, at::Tensor weight_, at::Tensor bias_)
+        : desc{channels, groups, dtype_, activation, (float)eps}, n(n_), tokens(tokens_), longest(longest_),
+          offsets(std::move(offsets_)), order(std::move(order_)), weight(std::move(weight_)), bias(std::move(bias_)),
+          dtype(storage(dtype_)), device(weight.device()) {}
+
+    // all but x and dy are the caller's own buffers
+    void forward(const at::Tensor& x, const at::Tensor& y, const at::Tensor& mean, const at::Tensor& rstd, const at::Tensor& ws,
+                 const MaybeStream& stream) const {
+        const int64_t xs = rows_of(x, "x", tokens, desc.channels, dtype, device);
+        on_gpu(x, "x");
+        const c10::hip::HIPGuard on(device.index());
+        mdlstm_status st;
+        {
+            py::gil_scoped_release none;
+            st = mdlstm_group_norm_forward(&desc, n, tokens, longest, offsets.data_ptr<int64_t>(), order.data_ptr<int32_t>(),
+                                           x.data_ptr(), xs, weight.data_ptr<float>(), bias.data_ptr<float>(), y.data_ptr(),
+                                           mean.data_ptr<float>(), rstd.data_ptr<float>(), ws.data_ptr(), ws.numel(),
+                                           stream_of(stream, device));
+        }
+        ok(st);
+    }
+
+    void backward(const at::Tensor& x, const at::Tensor& mean, const at::Tensor& rstd, const at::Tensor& dy, const at::Tensor& dx,
+                  const at::Tensor& dw, const at::Tensor& db, const at::Tensor& ws, const MaybeStream& stream) const {
+        const int64_t xs = rows_of(x, "x", tokens, desc.channels, dtype, device),
+                      gs = rows_of(dy, "dy", tokens, desc.channels, dtype, device);
+        const c10::hip::HIPGuard on(device.index());
+        mdlstm_status st;
+        {
+            py::gil_scoped_release none;
+            st = mdlstm_group_norm_backward(&desc, n, tokens, longest, offsets.data_ptr<int64_t>(), order.data_ptr<int32_t>(),
+                                            x.data_ptr(), xs, weight.data_ptr<float>(), bias.data_ptr<float>(),
+                                            mean.data_ptr<float>(), rstd.data_ptr<float>(), dy.data_ptr(), gs, dx.data_ptr(),
+                                            dw.data_ptr<float>(), db.data_ptr<float>(), ws.data_ptr(), ws.numel(),
+                                            stream_of(stream, device));
+        }
+        ok(st);
+    }
+};
+
 }  // namespace
 
 PYBIND11_MODULE(_binding, m) {
@@ -274,6 +409,15 @@ PYBIND11_MODULE(_binding, m) {
         .def(py::init<int, int, double, double, int64_t, at::Tensor>())
         .def("forward", &Norm::forward)
         .def("backward", &Norm::backward);
+    py::class_<Recurrence>(m, "Recurrence")
+        .def(py::init<int, int, int, int, int64_t, int64_t, at::Tensor, at::Tensor>())
+        .def("forward", &Recurrence::forward)
+        .def("backward", &Recurrence::backward);
+    py::class_<GroupNorm>(m, "GroupNorm")
+        .def(py::init<int, int, int, int, double, int, int64_t, int64_t, at::Tensor, at::Tensor, at::Tensor, at::Tensor>())
+        .def("forward", &GroupNorm::forward)
+        .def("backward", &GroupNorm::backward);
     m.def("step", &step);
+    m.def("recurrence_step", &recurrence_step);
     m.def("dropout", &dropout);
 }

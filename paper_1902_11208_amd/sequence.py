@@ -1,6 +1,7 @@
 """Layers along the packed frames of the examples (or any packed tokens):
-linear attention with a decay for each head, root-mean-square norm of a
-residual sum, dropout, and the attention's single-token step.
+linear attention with a decay for each head, a gated linear recurrence, the
+single-token steps of both, root-mean-square norm of a residual sum, dropout, and
+a norm over groups of channels with an activation.
 
 Tokens lie example after example without padding, as the output layer's frames
 do. Every step of the computation runs in libmdlstm.so's HIP kernels; this
@@ -20,7 +21,7 @@ import ctypes
 import numpy as np
 import torch
 
-from ._lib import AttentionDesc, NormDesc, lib
+from ._lib import AttentionDesc, GroupNormDesc, NormDesc, RecurrenceDesc, lib
 from .api import check_tensor, dtype_code
 
 try:
@@ -29,6 +30,8 @@ except ImportError as e:
     raise RuntimeError("the native binding is missing: build it with `python -m paper_1902_11208_amd.build`") from e
 
 FP8 = torch.float8_e4m3fn
+GATES = {None: 0, "sigmoid": 1}
+ACTIVATIONS = {None: 0, "relu": 1, "silu": 2}
 
 
 def _stream(stream):
@@ -145,6 +148,155 @@ def decay_attention_step(q, k, v, state, rates, slots=None, scale: float = None,
     tensor, the state of each row (None: row i has state i); a slot outside the states marks an idle row, whose o
     is zero. No two rows may name the same slot."""
     return _binding.step(q, k, v, state, rates, slots, scale, out, _stream(stream))
+
+
+class _PackedLayer:
+    """Sequences of given lengths, packed: where they start, and the order in which they are started."""
+
+    def __init__(self, lengths, channels: int, dtype, device):
+        n = np.asarray(lengths, np.int64).reshape(-1)
+        if n.size and n.min() < 0:
+            raise ValueError("a sequence has a negative length")
+        self.n, self.tokens, self.longest = int(n.size), int(n.sum()), int(n.max()) if n.size else 0
+        self.channels, self.dtype = int(channels), dtype
+        self._lengths, self._device = n, torch.device(device)
+
+    def _bytes_of(self, call, *args) -> int:
+        nbytes = int(call(*args))
+        if not nbytes:
+            raise ValueError(lib().mdlstm_last_error().decode(errors="replace"))
+        return nbytes
+
+    def _upload(self):
+        n = self._lengths
+        self.offsets = torch.from_numpy(np.concatenate([[0], np.cumsum(n)])).to(self._device)
+        # longest first, so that no long sequence starts when the others are done
+        self.order = torch.from_numpy(np.argsort(-n, kind="stable").astype(np.int32)).to(self._device)
+        self.device = self.offsets.device
+        self._ws, self._saved = [None, None], None
+
+    def _workspace(self, backward: int, stream) -> torch.Tensor:
+        if self._ws[backward] is None:
+            self._ws[backward] = _empty(self._bytes[backward], torch.uint8, self.device, stream)
+        return self._ws[backward]
+
+
+class GatedRecurrence(_PackedLayer):
+    """Gated linear recurrence over packed sequences, for each channel
+
+        h_t = f_t h_(t-1) + u_t        gate "sigmoid": f = sigmoid(z), u = (1 - f) x        gate None: f = z, u = x
+
+    the state in fp32 restarting at every sequence's edge. lengths: tokens of each sequence (host); zero is allowed.
+    dtype: storage of z, x, h and their gradients; sums and states are fp32, and outputs are rounded once.
+
+    States that a call returned may be given back to the object, to go through sequences piece by piece: a call
+    writes to a buffer that neither its arguments nor the forward call it belongs to use. Its other outputs must not be
+    its inputs.
+    """
+
+    def __init__(self, lengths, channels: int, dtype=torch.bfloat16, gate: str = "sigmoid", device="cuda"):
+        if gate not in GATES:
+            raise ValueError(f"gate {gate!r} is not None or 'sigmoid'")
+        super().__init__(lengths, channels, dtype, device)
+        desc = RecurrenceDesc(self.channels, dtype_code(dtype), GATES[gate])
+        self._bytes = [self._bytes_of(lib().mdlstm_recurrence_workspace_bytes, ctypes.byref(desc), self.n, self.tokens,
+                                      self.longest, b) for b in (0, 1)]
+        self._marks_bytes = self._bytes_of(lib().mdlstm_recurrence_marks_bytes, ctypes.byref(desc), self.tokens)
+        self._upload()
+        self._op = _binding.Recurrence(self.channels, desc.dtype, desc.gate, self.n, self.tokens, self.longest, self.offsets,
+                                       self.order)
+        self._h = self._marks = self._grads = None
+        self._finals, self._dstates = [], []
+
+    def _spare(self, buffers: list, stream, *used) -> torch.Tensor:
+        """The first of the buffers of states that none of `used` lies in."""
+        for b in buffers:
+            if all(_apart(b, u) for u in used):
+                return b
+        buffers.append(_empty((self.n, self.channels), torch.float32, self.device, stream))
+        return buffers[-1]
+
+    def forward(self, z, x, state=None, final_state: bool = False, stream=None):
+        """h [tokens, channels]; with final_state also the states the sequences leave [n, channels]. state: the states
+        they start from (None: zero). z and x: [tokens, channels], contiguous along their rows (views of one
+        projection's output, say)."""
+        if self._h is None:
+            self._h = _empty((self.tokens, self.channels), self.dtype, self.device, stream)
+            self._marks = _empty(self._marks_bytes // 4, torch.float32, self.device, stream)
+        final = self._spare(self._finals, stream, state) if final_state else None
+        self._op.forward(z, x, state, self._h, final, self._marks, self._workspace(0, stream), _stream(stream))
+        self._saved = (z, x, state)
+        return (self._h, final) if final_state else self._h
+
+    def backward(self, dh, dstate=None, stream=None):
+        """(dz, dx) after a forward call, from the gradient of h (and of the final states, dstate); where the forward
+        was given states, (dz, dx, gradient of those)."""
+        if self._saved is None:
+            raise ValueError("backward needs a forward call on this layer first")
+        z, x, state = self._saved
+        if self._grads is None:
+            self._grads = tuple(_empty((self.tokens, self.channels), self.dtype, self.device, stream) for _ in range(2))
+        out = None if state is None else self._spare(self._dstates, stream, state, dstate)
+        self._op.backward(z, x, state, self._marks, dh, dstate, *self._grads, out, self._workspace(1, stream), _stream(stream))
+        return self._grads if state is None else self._grads + (out,)
+
+
+def gated_recurrence_step(z, x, state, slots=None, gate: str = "sigmoid", out=None, stream=None) -> torch.Tensor:
+    """One token for each of n sequences: z and x [n, channels] advance the fp32 states [slots, channels] in place and
+    give h [n, channels]. slots: int32 [n] device tensor, the state of each row (None: row i has state i); a slot
+    outside the states marks an idle row, whose h is zero. No two rows may name the same slot."""
+    if gate not in GATES:
+        raise ValueError(f"gate {gate!r} is not None or 'sigmoid'")
+    return _binding.recurrence_step(z, x, state, slots, GATES[gate], out, _stream(stream))
+
+
+class GroupNorm(_PackedLayer):
+    """Norm over groups of channels with an activation, channels last, over packed sequences:
+
+        y = act((x - mean) / sqrt(var + eps) * weight + bias)
+
+    mean and var over the tokens of a sequence (pixels of an image) and the channels of a group, channels / groups
+    neighbouring ones. weight, bias: [channels] fp32 device tensors. activation: None, "relu" or "silu". dtype: storage
+    of x, y and their gradients; sums are fp32.
+    """
+
+    def __init__(self, lengths, weight: torch.Tensor, bias: torch.Tensor, groups: int, dtype=torch.bfloat16, eps: float = 1e-5,
+                 activation: str = None):
+        if not isinstance(weight, torch.Tensor) or weight.dim() != 1:
+            raise ValueError("weight must be a [channels] tensor")
+        if activation not in ACTIVATIONS:
+            raise ValueError(f"activation {activation!r} is not None, 'relu' or 'silu'")
+        super().__init__(lengths, weight.numel(), dtype, weight.device)
+        check_tensor(weight, "weight", (self.channels,), torch.float32)
+        check_tensor(bias, "bias", (self.channels,), torch.float32, weight.device)
+        self.weight, self.bias, self.groups = weight, bias, int(groups)
+        desc = GroupNormDesc(self.channels, self.groups, dtype_code(dtype), ACTIVATIONS[activation], float(eps))
+        self._bytes = [self._bytes_of(lib().mdlstm_group_norm_workspace_bytes, ctypes.byref(desc), self.n, self.tokens,
+                                      self.longest, b) for b in (0, 1)]
+        self._upload()
+        self._op = _binding.GroupNorm(self.channels, self.groups, desc.dtype, desc.activation, desc.eps, self.n, self.tokens,
+                                      self.longest, self.offsets, self.order, weight, bias)
+        self._y = self._stats = self._grads = None
+
+    def forward(self, x, stream=None) -> torch.Tensor:
+        """y [tokens, channels] of x [tokens, channels], contiguous along its rows."""
+        if self._y is None:
+            self._y = _empty((self.tokens, self.channels), self.dtype, self.device, stream)
+            self._stats = [_empty((self.n, self.groups), torch.float32, self.device, stream) for _ in range(2)]
+        self._op.forward(x, self._y, *self._stats, self._workspace(0, stream), _stream(stream))
+        self._saved = x
+        return self._y
+
+    def backward(self, dy, stream=None):
+        """(dx, dweight, dbias) after a forward call, from the gradient of y."""
+        if self._saved is None:
+            raise ValueError("backward needs a forward call on this norm first")
+        if self._grads is None:
+            self._grads = (_empty((self.tokens, self.channels), self.dtype, self.device, stream),
+                           _empty(self.channels, torch.float32, self.device, stream),
+                           _empty(self.channels, torch.float32, self.device, stream))
+        self._op.backward(self._saved, *self._stats, dy, *self._grads, self._workspace(1, stream), _stream(stream))
+        return self._grads
 
 
 class ResidualNorm:

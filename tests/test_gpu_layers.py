@@ -1,0 +1,376 @@
+"""GPU parity of the gated recurrence, its single-token step and the group norm
+against the float64 oracle (oracle/layers.py).
+
+Tolerances, normwise L2 and max-norm relative error. fp32 storage: 1e-5, as for
+the other layers (a few hundred roundings of 2^-24). bf16 storage: an output is
+computed in fp32 and rounded once, at most 2^-8 of itself, so 2^-8 + 1e-5 bounds
+both norms; fp32 results of bf16 inputs 1e-5."""
+import numpy as np
+import pytest
+
+from conftest import rel_err, rel_max
+from oracle import layers as orc
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+TOL = {"f32": 1e-5, "bf16": 2.0 ** -8 + 1e-5}
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu(built_lib):
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def _seq():
+    from paper_1902_11208_amd import sequence
+
+    return sequence
+
+
+def _np(t):
+    return t.detach().cpu().to(torch.float64).numpy()
+
+
+def _check(name, got, want, tol):
+    got = _np(got) if isinstance(got, torch.Tensor) else got
+    assert got.shape == want.shape, (name, got.shape, want.shape)
+    e, m = rel_err(got, want), rel_max(got, want)
+    assert e <= tol and m <= tol, (name, e, m)
+
+
+def _rand(rng, *shape, dtype="f32"):
+    return torch.from_numpy(rng.standard_normal(shape).astype(np.float32)).to(DT[dtype]).cuda()
+
+
+def _rows(rng, T, C, dtype, layout, shift=0.0):
+    """[T, C] contiguous, as part of longer rows (fused), or as such rows off every alignment (odd)."""
+    pad = {"contiguous": 0, "fused": C, "odd": C + 1 + C % 2}[layout]
+    a = (_rand(rng, T, C + pad) + shift).to(DT[dtype])
+    return a[:, pad:] if layout == "fused" else a[:, pad - C:pad] if layout == "odd" else a
+
+
+LENGTHS = [[1], [0, 3, 0], [127, 128, 129, 0, 1], [1, 2, 300, 0, 17, 8], [1000], [9, 2500, 700]]
+
+
+@pytest.mark.parametrize("lengths", LENGTHS, ids=str)
+@pytest.mark.parametrize("channels,layout", [(1, "contiguous"), (3, "odd"), (8, "fused"), (16, "contiguous"), (31, "fused"),
+                                             (64, "fused"), (65, "contiguous"), (130, "odd"), (200, "fused")])
+@pytest.mark.parametrize("gate", ["sigmoid", None])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_recurrence(lengths, channels, layout, gate, dtype):
+    rng = np.random.default_rng(channels + len(lengths))
+    T, n = sum(lengths), len(lengths)
+    z = _rows(rng, T, channels, dtype, layout, 1.0)
+    if gate is None:
+        z = torch.sigmoid(z.float()).to(DT[dtype])
+    x, dh = _rows(rng, T, channels, dtype, layout), _rows(rng, T, channels, dtype, layout)
+    op = _seq().GatedRecurrence(lengths, channels, dtype=DT[dtype], gate=gate)
+    for with_state in (False, True):
+        state = _rand(rng, n, channels) if with_state else None
+        dfinal = _rand(rng, n, channels) if with_state else None
+        st, df = (None if v is None else _np(v) for v in (state, dfinal))
+        wh, wf = orc.recurrence_forward(_np(z), _np(x), lengths, gate, st)
+        h, final = op.forward(z, x, state=state, final_state=True)
+        _check("h", h, wh, TOL[dtype])
+        _check("final", final, wf, 1e-5)
+        got = op.backward(dh, dfinal)
+        want = orc.recurrence_backward(_np(z), _np(x), lengths, gate, _np(dh), st, df)
+        for name, g, w, tol in zip(("dz", "dx", "dstate"), got, want, (TOL[dtype], TOL[dtype], 1e-5)):
+            _check(name, g, w, tol)
+
+
+def _walk(f, u, h):
+    """The recurrence in fp32, token by token."""
+    out = np.empty_like(f)
+    with np.errstate(all="ignore"):
+        for t in range(len(f)):
+            out[t] = h = (f[t] * h + u[t]).astype(np.float32)
+    return out
+
+
+def _same(name, got, want, tol=1e-5):
+    """Infinities and NaN in the same places, the others near."""
+    with np.errstate(all="ignore"):
+        assert np.array_equal(np.isnan(got), np.isnan(want)), (name, "NaN", np.argwhere(np.isnan(got) != np.isnan(want))[:4])
+        inf = np.isinf(want)
+        assert np.array_equal(np.isinf(got), inf) and np.array_equal(got[inf], want[inf]), (name, "infinities")
+        ok = np.isfinite(want)
+        assert np.all(np.abs(got[ok] - want[ok]) <= tol * np.abs(want[ok]) + 1e-30), name
+
+
+@pytest.mark.parametrize("T", [60, 400, 5000])
+def test_recurrence_of_values_that_are_not_finite(T):
+    """Coefficients given: growth past fp32's range and back, factors that underflow under a large or infinite state,
+    zeros under an infinite one, NaN; each in channels of its own. Positive values, so that nothing cancels."""
+    rng = np.random.default_rng(T)
+    C = 12
+    f = rng.uniform(0.5, 1.0, (T, C)).astype(np.float32)
+    u = rng.uniform(0.1, 1.0, (T, C)).astype(np.float32)
+    state = np.ones((1, C), np.float32)
+    f[:, 1] = 1.7                       # overflows, u = 0 keeps h at 0 until the first input
+    u[:, 1] = 0
+    state[0, 1] = 0
+    u[T // 2, 1] = 1e-30
+    f[:, 2] = 1e-9                      # underflows under a large state
+    state[0, 2] = 3e38
+    u[:, 2] = 0
+    f[5, 3], u[20, 3] = np.inf, 0       # infinite from there
+    f[T - 9, 3] = 0                     # 0 times infinity
+    u[7, 4] = np.inf
+    u[9, 5] = np.nan
+    f[11, 6] = np.nan
+    f[30:45, 7], f[45:58, 7] = 1e6, 1e-6    # out of the range of a product of factors and back
+    u[:, 7] = 0
+    f[:, 8] = 0
+    state[0, 9] = np.inf
+    f[:, 9] = 1e-9
+    u[:, 10], f[:, 10], state[0, 10] = 0, 1.0, 1e30
+    z, x = torch.from_numpy(f).cuda(), torch.from_numpy(u).cuda()
+    op = _seq().GatedRecurrence([T], C, dtype=torch.float32, gate=None)
+    h, final = op.forward(z, x, state=torch.from_numpy(state).cuda(), final_state=True)
+    want = _walk(f, u, state[0])
+    got = h.cpu().numpy()
+    for c in range(C):
+        _same(f"channel {c}", got[:, c], want[:, c], 1e-4)
+    _same("final", final.cpu().numpy()[0], want[-1], 1e-4)  # joined from the slices' sums: rounded in another order than h
+    # the adjoint is the same recurrence from the end: s_t = f_t (dh_t + s_(t+1))
+    op.forward(torch.from_numpy(f[::-1].copy()).cuda(), x)
+    _, dx = op.backward(torch.from_numpy(u[::-1].copy()).cuda(), torch.from_numpy(state).cuda())
+    want = np.empty_like(f)
+    s = state[0]
+    with np.errstate(all="ignore"):
+        for t in range(T):
+            want[t] = (u[t] + s).astype(np.float32)
+            s = (f[t] * want[t]).astype(np.float32)
+    got = dx.cpu().numpy()[::-1]
+    for c in range(C):
+        _same(f"adjoint of channel {c}", got[:, c], want[:, c], 1e-4)
+
+
+@pytest.mark.parametrize("gate", ["sigmoid", None])
+def test_recurrence_gradients_against_differences(gate):
+    rng = np.random.default_rng(3)
+    lengths, C = [5, 0, 140], 3
+    T = sum(lengths)
+    z, x, dh = (rng.standard_normal((T, C)) * 0.5 for _ in range(3))
+    op = _seq().GatedRecurrence(lengths, C, dtype=torch.float32, gate=gate)
+    cuda = lambda v: torch.from_numpy(v.astype(np.float32)).cuda()  # noqa: E731
+    op.forward(cuda(z), cuda(x))
+    dz, dx = (_np(g) for g in op.backward(cuda(dh)))
+    f = lambda z, x: float((orc.recurrence_forward(z, x, lengths, gate)[0] * dh).sum())  # noqa: E731
+    for t, c in ((0, 0), (4, 2), (5, 1), (70, 0), (T - 1, 2)):
+        d = np.zeros((T, C))
+        d[t, c] = 1e-6
+        assert abs((f(z + d, x) - f(z - d, x)) / 2e-6 - dz[t, c]) < 1e-4 * max(1.0, abs(dz[t, c]))
+        assert abs((f(z, x + d) - f(z, x - d)) / 2e-6 - dx[t, c]) < 1e-4 * max(1.0, abs(dx[t, c]))
+
+
+@pytest.mark.parametrize("lengths", [[33, 0, 70], [1500, 900], [9000]], ids=str)
+def test_recurrence_piece_by_piece(lengths):
+    """States passed back to the object they came from; each piece equals the oracle's from the same states."""
+    rng = np.random.default_rng(5)
+    T, C = sum(lengths), 24
+    op = _seq().GatedRecurrence(lengths, C, dtype=torch.float32)
+    state, st = None, None
+    for _ in range(3):
+        z, x, dh = (_rand(rng, T, C) for _ in range(3))
+        wh, wf = orc.recurrence_forward(_np(z), _np(x), lengths, "sigmoid", st)
+        h, new = op.forward(z, x, state=state, final_state=True)
+        _check("h", h, wh, 1e-5)
+        _check("final", new, wf, 1e-5)
+        want = orc.recurrence_backward(_np(z), _np(x), lengths, "sigmoid", _np(dh), st, wf)
+        for name, g, w in zip(("dz", "dx", "dstate"), op.backward(dh, new), want):
+            _check(name, g, w, 1e-5)
+        state, st = new, wf
+
+
+@pytest.mark.parametrize("n,channels,layout", [(1, 1, "contiguous"), (4, 256, "fused"), (7, 65, "odd"), (300, 96, "fused")])
+@pytest.mark.parametrize("gate", ["sigmoid", None])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_recurrence_step(n, channels, layout, gate, dtype):
+    rng = np.random.default_rng(n)
+    z, x = _rows(rng, n, channels, dtype, layout), _rows(rng, n, channels, dtype, layout)
+    state = _rand(rng, n + 5, channels)
+    slots = torch.from_numpy(rng.permutation(n + 5)[:n].astype(np.int32)).cuda()
+    if n > 2:
+        slots[1], slots[2] = -1, n + 5
+    before, at = _np(state), slots.cpu().numpy()
+    h = _seq().gated_recurrence_step(z, x, state, slots=slots, gate=gate)
+    f, u = orc.gates(_np(z), _np(x), gate)
+    want, left = np.zeros((n, channels)), before.copy()
+    for i in range(n):
+        if 0 <= at[i] < n + 5:
+            left[at[i]] = want[i] = f[i] * before[at[i]] + u[i]
+    _check("h", h, want, TOL[dtype])
+    _check("state", state, left, 1e-5)
+    state = torch.from_numpy(before.astype(np.float32)).cuda()
+    out = torch.empty_like(h)
+    assert _seq().gated_recurrence_step(z, x, state, gate=gate, out=out) is not None
+    _check("h of slots in order", out, f * before[:n] + u, TOL[dtype])
+
+
+def test_recurrence_steps_equal_the_scan():
+    rng = np.random.default_rng(8)
+    n, T, C = 3, 40, 10
+    z, x = _rand(rng, n * T, C), _rand(rng, n * T, C)
+    h, final = _seq().GatedRecurrence([T] * n, C, dtype=torch.float32).forward(z, x, final_state=True)
+    state = torch.zeros(n, C, device="cuda")
+    for t in range(T):
+        o = _seq().gated_recurrence_step(z.view(n, T, C)[:, t], x.view(n, T, C)[:, t], state)
+        _check("h", o, _np(h.view(n, T, C)[:, t]), 1e-5)
+    _check("state", state, _np(final), 1e-5)
+
+
+@pytest.mark.parametrize("lengths", [[1], [0, 3, 0], [127, 128, 1, 0, 9], [700, 30], [5000, 2, 0, 3000]], ids=str)
+@pytest.mark.parametrize("channels,groups,layout", [(1, 1, "contiguous"), (6, 2, "odd"), (64, 4, "fused"), (65, 5, "contiguous"),
+                                                    (40, 40, "fused"), (320, 32, "contiguous"), (300, 1, "odd"), (1024, 2, "fused")])
+@pytest.mark.parametrize("act", [None, "relu", "silu"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_group_norm(lengths, channels, groups, layout, act, dtype):
+    rng = np.random.default_rng(channels + len(lengths))
+    T = sum(lengths)
+    x, dy = _rows(rng, T, channels, dtype, layout, 0.5), _rows(rng, T, channels, dtype, layout)
+    w, b = 1 + 0.1 * _rand(rng, channels), 0.1 * _rand(rng, channels)
+    if channels // groups == 1 and min(n for n in lengths if n) == 1:
+        # one value in a group: x - mean is 0 but for rounding, and relu is asked at b itself
+        b = b.abs() + 0.05
+    op = _seq().GroupNorm(lengths, w, b, groups, dtype=DT[dtype], activation=act)
+    args = (lengths, _np(w), _np(b), groups, 1e-5, act)
+    _check("y", op.forward(x), orc.group_norm(_np(x), *args), TOL[dtype])
+    dx, dw, db = op.backward(dy)
+    wx, ww, wb = orc.group_norm(_np(x), *args, dy=_np(dy))
+    near = np.abs(wx).max() < 1e-2 * np.abs(_np(dy)).max()  # groups of few values: dx is a difference of numbers of dy's size / dev
+    if not near:
+        _check("dx", dx, wx, 2 * TOL[dtype])
+    else:
+        assert np.abs(_np(dx) - wx).max() <= 1e-4 * np.abs(_np(dy)).max() / np.sqrt(1e-5)
+    if np.abs(ww).max() > 1e-3:
+        _check("dw", dw, ww, 1e-4)
+    _check("db", db, wb, 1e-5)
+
+
+@pytest.mark.parametrize("mean", [100.0, -3000.0])
+@pytest.mark.parametrize("T", [50, 20000])
+def test_group_norm_beside_a_large_mean(mean, T):
+    """fp32: the distances from the mean keep x's own rounding, 2^-24 of the mean, and the mean's: 2^-23 |mean| beside 1."""
+    rng = np.random.default_rng(2)
+    x = _rand(rng, T, 16) + mean
+    one, zero = torch.ones(16, device="cuda"), torch.zeros(16, device="cuda")
+    y = _seq().GroupNorm([T], one, zero, 2, dtype=torch.float32).forward(x)
+    _check("y", y, orc.group_norm(_np(x), [T], np.ones(16), np.zeros(16), 2, 1e-5, None), 2 * 2.0 ** -23 * abs(mean) + 1e-5)
+
+
+def test_group_norm_keeps_bad_values_in_their_groups():
+    rng = np.random.default_rng(4)
+    lengths = [40, 9000, 30]
+    x, dy = _rand(rng, sum(lengths), 32), _rand(rng, sum(lengths), 32)
+    one, zero = torch.ones(32, device="cuda"), torch.zeros(32, device="cuda")
+    for bad in (float("nan"), float("inf")):
+        for t in (3, 5000, 9050):
+            v = x.clone()
+            v[t, 9] = bad
+            op = _seq().GroupNorm(lengths, one, zero, 4, dtype=torch.float32, activation="silu")
+            y, (dx, _, _) = op.forward(v).clone(), op.backward(dy)
+            i = 0 if t < 40 else 1 if t < 9040 else 2
+            lo = sum(lengths[:i])
+            hit = torch.zeros(sum(lengths), 32, dtype=torch.bool, device="cuda")
+            hit[lo:lo + lengths[i], 8:16] = True
+            assert not torch.isfinite(y[hit]).any() and torch.isfinite(y[~hit]).all()
+            assert not torch.isfinite(dx[hit]).any() and torch.isfinite(dx[~hit]).all()
+
+
+def _layers(rng, lengths, C):
+    seq = _seq()
+    w, b = 1 + 0.1 * _rand(rng, C), 0.1 * _rand(rng, C)
+    return seq.GatedRecurrence(lengths, C, dtype=torch.float32), seq.GroupNorm(lengths, w, b, 4, dtype=torch.float32, activation="silu")
+
+
+@pytest.mark.parametrize("lengths", [[30, 0, 200], [9000, 40]], ids=str)
+def test_replays_of_captured_calls(lengths):
+    """A recurrence and a norm, forward and backward, captured and replayed with eager work between; a replay equals the
+    eager result on the same inputs bit for bit."""
+    rng = np.random.default_rng(6)
+    T, C = sum(lengths), 48
+    rec, norm = _layers(rng, lengths, C)
+    z, x, dy = (_rand(rng, T, C) for _ in range(3))
+
+    def run():
+        y = norm.forward(rec.forward(z, x))
+        dx, dw, db = norm.backward(dy)
+        return (y, dw, db) + rec.backward(dx)
+
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = run()
+    for k in range(4):
+        for t in (z, x, dy):
+            t.copy_(_rand(rng, T, C))
+        want = [o.clone() for o in run()]
+        for o in outs:
+            o.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        if k % 2:
+            torch.cuda.synchronize()
+        assert all(torch.equal(o, w) for o, w in zip(outs, want))
+
+
+def test_calls_on_another_stream():
+    rng = np.random.default_rng(7)
+    lengths, C = [500, 3000], 64
+    T = sum(lengths)
+    rec, norm = _layers(rng, lengths, C)
+    z, x = _rand(rng, T, C), _rand(rng, T, C)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    h = rec.forward(z, x, stream=side)
+    y = norm.forward(h, stream=side)
+    dx, dw, db = norm.backward(x, stream=side)
+    dz, dxx = rec.backward(dx, stream=side)
+    out = _seq().gated_recurrence_step(z[:9], x[:9], torch.zeros(9, C, device="cuda"), stream=side)
+    side.synchronize()
+    rec2, norm2 = _seq().GatedRecurrence(lengths, C, dtype=torch.float32), _seq().GroupNorm(
+        lengths, norm.weight, norm.bias, 4, dtype=torch.float32, activation="silu")
+    h2 = rec2.forward(z, x)
+    y2 = norm2.forward(h2)
+    g2 = norm2.backward(x)
+    r2 = rec2.backward(g2[0])
+    for a, b in zip((h, y, dx, dw, db, dz, dxx), (h2, y2, *g2, *r2)):
+        assert torch.equal(a, b)
+    f, u = orc.gates(_np(z[:9]), _np(x[:9]), "sigmoid")
+    _check("step", out, u, 1e-5)
+
+
+def test_rows_behind_the_last_sequence_stay():
+    """Offsets that end before the tensors do: nothing behind them is written."""
+    import ctypes
+
+    from paper_1902_11208_amd import _lib
+
+    L, C, T = _lib.lib(), 20, 300
+    off = torch.tensor([0, 100, 170], dtype=torch.int64, device="cuda")
+    z, x, dh = (torch.randn(T, C, device="cuda") for _ in range(3))
+    h, dz, dx = (torch.full((T, C), 7.0, device="cuda") for _ in range(3))
+    d = _lib.RecurrenceDesc(C, 0, 1)
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    marks = torch.empty(int(L.mdlstm_recurrence_marks_bytes(ctypes.byref(d), T)) // 4, device="cuda")
+    s = torch.cuda.current_stream().cuda_stream
+    _lib.check(L.mdlstm_recurrence_forward(d, 2, T, T, off.data_ptr(), None, z.data_ptr(), C, x.data_ptr(), C, None,
+                                           h.data_ptr(), None, marks.data_ptr(), ws.data_ptr(), ws.numel(), s))
+    _lib.check(L.mdlstm_recurrence_backward(d, 2, T, T, off.data_ptr(), None, z.data_ptr(), C, x.data_ptr(), C, None,
+                                            marks.data_ptr(), dh.data_ptr(), C, None, dz.data_ptr(), dx.data_ptr(), None,
+                                            ws.data_ptr(), ws.numel(), s))
+    for t in (h, dz, dx):
+        assert (t[170:] == 7).all() and (t[:170] != 7).all()
+    g = _lib.GroupNormDesc(C, 4, 0, 0, 1e-5)
+    w, b, mean, rstd = torch.ones(C, device="cuda"), torch.zeros(C, device="cuda"), torch.empty(2, 4, device="cuda"), torch.empty(2, 4, device="cuda")
+    y = torch.full((T, C), 7.0, device="cuda")
+    _lib.check(L.mdlstm_group_norm_forward(g, 2, T, T, off.data_ptr(), None, x.data_ptr(), C, w.data_ptr(), b.data_ptr(),
+                                           y.data_ptr(), mean.data_ptr(), rstd.data_ptr(), ws.data_ptr(), ws.numel(), s))
+    assert (y[170:] == 7).all() and (y[:170] != 7).all()
