@@ -688,6 +688,45 @@ mdlstm_status mdlstm_group_norm_backward(const mdlstm_group_norm_desc* desc, int
                                          float* d_dw, float* d_db, void* d_workspace, size_t workspace_bytes,
                                          void* stream);
 
+/*
+ * Softmax cross entropy over a vocabulary, from rows x [rows][dim] and the
+ * vocabulary's weights W [vocab][dim], without stored logits. With l = x W^T,
+ *     loss_i = log(sum_v exp(l_iv)) - l_i,target
+ * A row whose target lies outside [0, vocab) has loss 0 and takes no part in the
+ * gradients, whatever it holds. dtype: storage of x, W and their gradients. In bf16
+ * the logits are products of bf16 numbers summed in fp32, and the softmax enters
+ * the gradients' products rounded to bf16 once (its target's share of dx is not
+ * rounded); in fp32 operands are three bf16 numbers each, 2^-24 together, for
+ * magnitudes up to 3.38e38. Sums are fp32 in a fixed order. rows <= 2^22,
+ * dim <= 65536, vocab <= 2^24 (UNSUPPORTED beyond).
+ */
+typedef struct {
+    int32_t dim, vocab, dtype;
+} mdlstm_vocabulary_desc;
+
+/* Workspace of a forward or (backward != 0) backward call; 0 for invalid
+ * arguments, otherwise at least 16. */
+size_t mdlstm_vocabulary_workspace_bytes(const mdlstm_vocabulary_desc* desc, int64_t rows, int32_t backward);
+
+/*
+ * d_x and d_w: rows x_stride and w_stride >= dim elements apart. d_targets [rows]
+ * (int64). d_losses (out) [rows] fp32; d_stats (out) [2][rows] fp32, for the
+ * backward: log of the sum over the tokens but the target, and the target's logit.
+ * Asynchronous on `stream`; capturable into a graph. Buffers that the call writes
+ * must not overlap others (INVALID_ARG).
+ */
+mdlstm_status mdlstm_vocabulary_forward(const mdlstm_vocabulary_desc* desc, int64_t rows, const void* d_x, int64_t x_stride,
+                                        const void* d_w, int64_t w_stride, const int64_t* d_targets, float* d_losses,
+                                        float* d_stats, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients of sum(losses * dlosses), after a forward call on the same inputs
+ * (d_stats as that call left it). d_dlosses [rows] fp32. d_dx (out) [rows][dim] and
+ * d_dw (out) [vocab][dim] in the storage type, overwritten. */
+mdlstm_status mdlstm_vocabulary_backward(const mdlstm_vocabulary_desc* desc, int64_t rows, const void* d_x, int64_t x_stride,
+                                         const void* d_w, int64_t w_stride, const int64_t* d_targets, const float* d_stats,
+                                         const float* d_dlosses, void* d_dx, void* d_dw, void* d_workspace,
+                                         size_t workspace_bytes, void* stream);
+
 /* Message for the last non-OK status returned on the calling thread. */
 const char* mdlstm_last_error(void);
 

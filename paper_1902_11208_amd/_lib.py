@@ -56,11 +56,16 @@ class GroupNormDesc(ctypes.Structure):
     _fields_ = [("channels", c_i32), ("groups", c_i32), ("dtype", c_i32), ("activation", c_i32), ("eps", ctypes.c_float)]
 
 
+class VocabularyDesc(ctypes.Structure):
+    _fields_ = [("dim", c_i32), ("vocab", c_i32), ("dtype", c_i32)]
+
+
 P_HEADS = ctypes.POINTER(Heads)
 P_ATTENTION = ctypes.POINTER(AttentionDesc)
 P_NORM = ctypes.POINTER(NormDesc)
 P_RECURRENCE = ctypes.POINTER(RecurrenceDesc)
 P_GROUP_NORM = ctypes.POINTER(GroupNormDesc)
+P_VOCABULARY = ctypes.POINTER(VocabularyDesc)
 
 SIGNATURES = {
     "mdlstm_pack_workspace_bytes": (c_size, [c_i32]),
@@ -125,6 +130,11 @@ SIGNATURES = {
                                           c_void, c_void, c_void, c_void, c_size, c_void]),
     "mdlstm_group_norm_backward": (c_i32, [P_GROUP_NORM, c_i32, c_i64, c_i64, c_void, c_void, c_void, c_i64, c_void, c_void,
                                            c_void, c_void, c_void, c_i64, c_void, c_void, c_void, c_void, c_size, c_void]),
+    "mdlstm_vocabulary_workspace_bytes": (c_size, [P_VOCABULARY, c_i64, c_i32]),
+    "mdlstm_vocabulary_forward": (c_i32, [P_VOCABULARY, c_i64, c_void, c_i64, c_void, c_i64, c_void, c_void, c_void, c_void,
+                                          c_size, c_void]),
+    "mdlstm_vocabulary_backward": (c_i32, [P_VOCABULARY, c_i64, c_void, c_i64, c_void, c_i64, c_void, c_void, c_void, c_void,
+                                           c_void, c_void, c_size, c_void]),
 }
 
 STATUS = {0: "OK", 1: "INVALID_ARG", 2: "TOO_WIDE", 3: "BAD_LAYOUT", 4: "WORKSPACE", 5: "UNSUPPORTED", 6: "DEVICE",

@@ -398,6 +398,54 @@ struct GroupNorm {
     }
 };
 
+// ---------------------------------------------------------------------------
+// Loss over a vocabulary
+// ---------------------------------------------------------------------------
+struct Vocabulary {
+    mdlstm_vocabulary_desc desc;
+    int64_t rows;
+    at::Tensor weight;
+    at::ScalarType dtype;
+    at::Device device;
+
+    Vocabulary(int dim, int vocab, int dtype_, int64_t rows_, at::Tensor weight_)
+        : desc{dim, vocab, dtype_}, rows(rows_), weight(std::move(weight_)), dtype(storage(dtype_)), device(weight.device()) {}
+
+    int64_t x_like(const at::Tensor& t, const char* name) const { return rows_of(t, name, rows, desc.dim, dtype, device); }
+    int64_t* labels(const at::Tensor& t) const { return static_cast<int64_t*>(full(t, "targets", {rows}, at::kLong, device)); }
+
+    // all but x, targets and dlosses are the caller's own buffers
+    void forward(const at::Tensor& x, const at::Tensor& targets, const at::Tensor& losses, const at::Tensor& stats,
+                 const at::Tensor& ws, const MaybeStream& stream) const {
+        const int64_t xs = x_like(x, "x");
+        const int64_t* t = labels(targets);
+        on_gpu(x, "x");
+        const c10::hip::HIPGuard on(device.index());
+        mdlstm_status st;
+        {
+            py::gil_scoped_release none;
+            st = mdlstm_vocabulary_forward(&desc, rows, x.data_ptr(), xs, weight.data_ptr(), desc.dim, t, losses.data_ptr<float>(),
+                                           stats.data_ptr<float>(), ws.data_ptr(), ws.numel(), stream_of(stream, device));
+        }
+        ok(st);
+    }
+
+    void backward(const at::Tensor& x, const at::Tensor& targets, const at::Tensor& stats, const at::Tensor& dlosses,
+                  const at::Tensor& dx, const at::Tensor& dw, const at::Tensor& ws, const MaybeStream& stream) const {
+        const int64_t xs = x_like(x, "x");
+        const int64_t* t = labels(targets);
+        const float* dl = static_cast<float*>(full(dlosses, "dlosses", {rows}, at::kFloat, device));
+        const c10::hip::HIPGuard on(device.index());
+        mdlstm_status st;
+        {
+            py::gil_scoped_release none;
+            st = mdlstm_vocabulary_backward(&desc, rows, x.data_ptr(), xs, weight.data_ptr(), desc.dim, t, stats.data_ptr<float>(),
+                                            dl, dx.data_ptr(), dw.data_ptr(), ws.data_ptr(), ws.numel(), stream_of(stream, device));
+        }
+        ok(st);
+    }
+};
+
 }  // namespace
 
 PYBIND11_MODULE(_binding, m) {
@@ -417,6 +465,10 @@ PYBIND11_MODULE(_binding, m) {
         .def(py::init<int, int, int, int, double, int, int64_t, int64_t, at::Tensor, at::Tensor, at::Tensor, at::Tensor>())
         .def("forward", &GroupNorm::forward)
         .def("backward", &GroupNorm::backward);
+    py::class_<Vocabulary>(m, "Vocabulary")
+        .def(py::init<int, int, int, int64_t, at::Tensor>())
+        .def("forward", &Vocabulary::forward)
+        .def("backward", &Vocabulary::backward);
     m.def("step", &step);
     m.def("recurrence_step", &recurrence_step);
     m.def("dropout", &dropout);

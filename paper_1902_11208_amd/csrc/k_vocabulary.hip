@@ -1,0 +1,639 @@
+// Softmax cross entropy of rows over a vocabulary, from the rows x [rows][dim] and
+// the vocabulary's weights W [vocab][dim], without stored logits l = x W^T. With
+// the sum over the others, o = log(sum over v != target of exp(l_v)),
+//     loss = log(1 + exp(o - l_target))            1 - p_target = sigmoid(o - l_target)
+//     dl_v = c q_v,  c = dloss (1 - p_target),  q_v = exp(l_v - o),  q_target = -1
+//     dx = c (q W)        dW = (c q)^T x
+// Written so, neither the loss nor the gradient of a row whose target is nearly
+// certain is a difference of numbers near 1, and the target's share of dx enters its
+// product without rounding.
+//
+// Everything is a product of two operands whose rows run along the summed
+// dimension, C = A B^T on the matrix units (k_product): tiles of both operands go
+// straight to LDS in pieces of 64 of that dimension, two buffers in turn, and
+// products of 16 x 16 x 32 take them from there. The forward pass keeps of a tile of
+// logits each row's maximum and sum. The backward pass takes the vocabulary in
+// pieces: a piece's logits again, q in bf16 both ways round (q for dx, c q
+// transposed for dW), and two products with the transposed W and x.
+//
+// fp32 operands are three bf16 numbers each (split.hpp), the six largest products
+// kept. In bf16, q is rounded once to a matrix operand: a relative 2^-9 of each
+// of many terms beside the exact target.
+#include <algorithm>
+
+#include "common.hpp"
+#include "sequence.hpp"
+#include "split.hpp"
+#include "vocabulary.hpp"
+
+namespace mdl {
+namespace {
+
+constexpr int BK = 64;           // summed elements of a step
+constexpr float LOG2E = 1.4426950408889634f;
+
+// An operand: `pieces` planes of [rows][ld] bf16, ld a multiple of BK or enough elements for whole steps.
+struct Operand {
+    const bf16_t* p;
+    int64_t plane, ld;
+    int64_t rows;
+};
+
+// What of a row the epilogues need.
+struct RowInfo {
+    float others, scale;  // o and c
+    int target;           // -1: the row is left out
+    int pad;
+};
+
+enum { LOGSUM, GRADIENT, PLANES };
+
+struct Product {
+    Operand a, b;
+    int steps;          // steps of one pair of pieces
+    int pairs;          // 1, or 6 of the three pieces of each
+    int splits;         // PLANES: parts of the sum
+    int tiles_m, tiles_n;
+    // LOGSUM
+    const int64_t* targets;
+    float2* part;       // [tiles_n][a.rows] maximum and sum of exp(l - maximum) of the tile's columns but the target
+    float* logit;       // [a.rows] the target's logit
+    int64_t first;      // vocabulary index of b's first row
+    // GRADIENT
+    const RowInfo* info;
+    bf16_t* q;          // planes of [a.rows][ldq], columns b.rows to ldq are zeroed
+    bf16_t* qt;         // planes of [b.rows][ldt], columns a.rows to ldt are zeroed
+    int64_t ldq, ldt, q_plane, qt_plane;
+    // PLANES
+    float* out;         // [splits][a.rows][ldo]
+    int64_t ldo;
+    int add;            // to what is there
+};
+
+// A tile of a product: BM x BN, waves of WM x WN.
+template <int BM_, int BN_, int WM_, int WN_>
+struct Shape {
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, WAVES = BM / WM * (BN / WN), THREADS = WAVES * 64, MI = WM / 16,
+                         NI = WN / 16, LOADS = (BM + BN) / 8 / WAVES, A_LOADS = BM / 8 / WAVES;
+    static_assert(BM / 8 % WAVES == 0 && BN / 8 % WAVES == 0, "whole loads of a wave");
+};
+
+// Which pieces a pair multiplies, the smallest products first.
+__device__ __forceinline__ void pair_of(int pairs, int k, int& a, int& b) {
+    a = b = 0;
+    if (pairs == 1) return;
+    a = k == 0 ? 2 : k == 2 || k == 4 ? 1 : 0;  // (2,0) (0,2) (1,1) (0,1) (1,0) (0,0)
+    b = k == 1 ? 2 : k == 2 || k == 3 ? 1 : 0;
+}
+
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ __forceinline__ Buffer buffer_at(const void* p) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7ffffff0, 0x00027000);
+}
+
+// A tile's rows in LDS: 64 elements (128 bytes) each, their eight 16-byte chunks
+// exchanged by the row's index (chunk c of row r lies at c ^ (r & 7)), so that
+// the sixteen rows a matrix operand takes at once lie in different banks.
+template <class S>
+struct Tile {
+    bf16_t a[S::BM * BK], b[S::BN * BK];
+};
+
+template <class S>
+struct Loader {
+    uint32_t offset[S::LOADS];  // bytes from the tile's first row
+    __device__ __forceinline__ Loader(const Product& g, int64_t m0, int64_t n0) {
+        const int wave = threadIdx.x / 64, lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < S::LOADS; ++i) {
+            const bool a = i < S::A_LOADS;
+            const int r = (a ? i : i - S::A_LOADS) * S::WAVES * 8 + wave * 8 + lane / 8;
+            const Operand& o = a ? g.a : g.b;
+            const int64_t last = o.rows - 1 - (a ? m0 : n0);  // rows behind the last one repeat it
+            offset[i] = (uint32_t)((min((int64_t)r, last) * o.ld + ((lane & 7) ^ (lane / 8)) * 8) * 2);
+        }
+    }
+    __device__ __forceinline__ void load(Tile<S>& t, Buffer a, Buffer b) const {
+        const int wave = threadIdx.x / 64;
+#pragma unroll
+        for (int i = 0; i < S::LOADS; ++i) {
+            const bool is_a = i < S::A_LOADS;
+            bf16_t* to = (is_a ? t.a + i * S::WAVES * 8 * BK : t.b + (i - S::A_LOADS) * S::WAVES * 8 * BK) + wave * 8 * BK;
+#ifdef __HIP_DEVICE_COMPILE__  // the host's pass over this file has no such builtin
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(is_a ? a : b, (__attribute__((address_space(3))) void*)to, 16, offset[i], 0, 0, 0);
+#endif
+        }
+    }
+};
+
+template <class S>
+__device__ __forceinline__ void multiply(const Tile<S>& t, floatx4 (&acc)[S::MI][S::NI]) {
+    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, wm = wave / (S::BN / S::WN), wn = wave % (S::BN / S::WN);
+    const int row = lane & 15;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const int chunk = ((lane / 16 + half * 4) ^ (row & 7)) * 8;
+        bf16x8 a[S::MI], b[S::NI];
+#pragma unroll
+        for (int i = 0; i < S::MI; ++i) a[i] = *reinterpret_cast<const bf16x8*>(t.a + (wm * S::WM + i * 16 + row) * BK + chunk);
+#pragma unroll
+        for (int j = 0; j < S::NI; ++j) b[j] = *reinterpret_cast<const bf16x8*>(t.b + (wn * S::WN + j * 16 + row) * BK + chunk);
+#pragma unroll
+        for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+            for (int j = 0; j < S::NI; ++j) acc[i][j] = mfma_bf16(a[i], b[j], acc[i][j]);
+        __builtin_amdgcn_sched_barrier(0);  // both halves' operands at once do not fit the registers
+    }
+}
+
+// Tiles in an order that keeps those of an XCD (workgroups 8 apart) near each
+// other: runs of the list per XCD, the list in blocks of 8 rows of tiles.
+__device__ __forceinline__ void place(const Product& g, int index, int& tm, int& tn) {
+    const int total = g.tiles_m * g.tiles_n, each = total / 8, more = total % 8, xcd = index % 8, at = index / 8;
+    const int k = xcd * each + min(xcd, more) + at;
+    const int band = 8 * g.tiles_n, first = k / band * 8, high = min(8, g.tiles_m - first), in = k % band;
+    tm = first + in % high;
+    tn = in / high;
+}
+
+__device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * LOG2E); }
+
+template <class S, int WHAT, int PIECES>
+__global__ __launch_bounds__(S::THREADS) void k_product(Product g) {
+    __shared__ Tile<S> t0;
+    __shared__ Tile<S> t1;
+    int tm, tn;
+    place(g, blockIdx.x, tm, tn);
+    tm = __builtin_amdgcn_readfirstlane(tm);
+    tn = __builtin_amdgcn_readfirstlane(tn);
+    const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
+    const int all = g.steps * g.pairs, split = blockIdx.y;
+    const int from = __builtin_amdgcn_readfirstlane((int)((int64_t)all * split / g.splits)),
+              to = __builtin_amdgcn_readfirstlane((int)((int64_t)all * (split + 1) / g.splits));
+    const Loader<S> load(g, m0, n0);
+    const bf16_t *pa = g.a.p + m0 * g.a.ld, *pb = g.b.p + n0 * g.b.ld;
+    int pair = __builtin_amdgcn_readfirstlane(g.steps ? from / g.steps : 0), step = from - pair * g.steps;  // of the next fetch
+    auto fetch = [&](Tile<S>& t) {
+        int a, b;
+        pair_of(g.pairs, pair, a, b);
+        load.load(t, buffer_at(pa + a * g.a.plane + (int64_t)step * BK), buffer_at(pb + b * g.b.plane + (int64_t)step * BK));
+        if (++step == g.steps) step = 0, ++pair;
+    };
+    floatx4 acc[S::MI][S::NI];
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+        for (int j = 0; j < S::NI; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    int k = from;
+    if (k < to) fetch(t0);
+    __syncthreads();
+    for (; k + 2 <= to; k += 2) {
+        fetch(t1);
+        multiply<S>(t0, acc);
+        __syncthreads();  // t1 has arrived, t0 has been read
+        if (k + 2 < to) fetch(t0);
+        multiply<S>(t1, acc);
+        __syncthreads();
+    }
+    if (k < to) multiply<S>(t0, acc);
+    __syncthreads();
+    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, wm = wave / (S::BN / S::WN), wn = wave % (S::BN / S::WN);
+    const int quad = lane / 16, col = lane & 15;
+    const int64_t rows = g.a.rows, cols = g.b.rows;
+    if constexpr (WHAT == PLANES) {
+        float* out = g.out + (int64_t)split * rows * g.ldo;
+#pragma unroll
+        for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int64_t m = m0 + wm * S::WM + i * 16 + quad * 4 + r;
+#pragma unroll
+                for (int j = 0; j < S::NI; ++j) {
+                    const int64_t n = n0 + wn * S::WN + j * 16 + col;
+                    if (m < rows && n < cols) {
+                        float* p = out + m * g.ldo + n;
+                        *p = g.add ? *p + acc[i][j][r] : acc[i][j][r];
+                    }
+                }
+            }
+    } else if constexpr (WHAT == LOGSUM) {
+        int* target = reinterpret_cast<int*>(t0.a);  // of the tile's rows, counted from the tile's first column
+        float2* sums = reinterpret_cast<float2*>(t1.a);  // [BN / WN][BM]
+        for (int r = threadIdx.x; r < S::BM; r += S::THREADS) {
+            const int64_t t = m0 + r < rows ? g.targets[m0 + r] - g.first - n0 : -1;
+            target[r] = t >= 0 && t < S::BN && t < cols - n0 ? (int)t : -1;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int row = wm * S::WM + i * 16 + quad * 4 + r, t = target[row];
+                float v[S::NI], top = -__builtin_huge_valf(), sum = 0.0f;
+#pragma unroll
+                for (int j = 0; j < S::NI; ++j) {
+                    const int n = wn * S::WN + j * 16 + col;
+                    v[j] = acc[i][j][r];
+                    if (n == t) g.logit[m0 + row] = v[j];
+                    if (n == t || n0 + n >= cols) v[j] = -__builtin_huge_valf();
+                    top = fmaxf(top, v[j]);
+                }
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+                const float base = top == -__builtin_huge_valf() ? 0.0f : top;
+#pragma unroll
+                for (int j = 0; j < S::NI; ++j) sum += exp_of(v[j] - base);
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+                if (col == 0) sums[wn * S::BM + row] = make_float2(top, sum);
+            }
+        __syncthreads();
+        for (int r = threadIdx.x; r < S::BM; r += S::THREADS) {
+            if (m0 + r >= rows) break;
+            float2 s = sums[r];
+#pragma unroll
+            for (int w = 1; w < S::BN / S::WN; ++w) {
+                const float2 n = sums[w * S::BM + r];
+                const float top = fmaxf(s.x, n.x), base = top == -__builtin_huge_valf() ? 0.0f : top;
+                s = make_float2(top, s.y * exp_of(s.x - base) + n.y * exp_of(n.x - base));
+            }
+            g.part[(int64_t)tn * rows + m0 + r] = s;
+        }
+    } else {
+        RowInfo* info = reinterpret_cast<RowInfo*>(t0.a);
+        for (int r = threadIdx.x; r < S::BM; r += S::THREADS) {
+            info[r] = g.info[min(m0 + r, rows - 1)];
+            if (m0 + r >= rows) info[r].target = -1;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+            for (int j = 0; j < S::NI; ++j) {
+                const int64_t n = n0 + wn * S::WN + j * 16 + col, m = m0 + wm * S::WM + i * 16 + quad * 4;
+                float v[4], c[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const RowInfo f = info[wm * S::WM + i * 16 + quad * 4 + r];
+                    float e = f.target == g.first + n ? -1.0f : exp_of(acc[i][j][r] - f.others);
+                    if (f.target < 0 || n >= cols) e = 0.0f;
+                    v[r] = e;
+                    c[r] = f.target < 0 || n >= cols ? 0.0f : e * f.scale;
+                }
+#pragma unroll
+                for (int k = 0; k < PIECES; ++k) {
+                    const uint32_t v01 = f2bf2(v[0], v[1]), v23 = f2bf2(v[2], v[3]), c01 = f2bf2(c[0], c[1]), c23 = f2bf2(c[2], c[3]);
+                    if (n < g.ldq) {
+                        bf16_t* p = g.q + k * g.q_plane + m * g.ldq + n;
+                        if (m < rows) p[0] = (bf16_t)v01;
+                        if (m + 1 < rows) p[g.ldq] = (bf16_t)(v01 >> 16);
+                        if (m + 2 < rows) p[2 * g.ldq] = (bf16_t)v23;
+                        if (m + 3 < rows) p[3 * g.ldq] = (bf16_t)(v23 >> 16);
+                    }
+                    if (n < cols && m < g.ldt) *reinterpret_cast<uint2*>(g.qt + k * g.qt_plane + n * g.ldt + m) = make_uint2(c01, c23);
+                    v[0] -= __uint_as_float(v01 << 16);
+                    v[1] -= __uint_as_float(v01 & 0xffff0000u);
+                    v[2] -= __uint_as_float(v23 << 16);
+                    v[3] -= __uint_as_float(v23 & 0xffff0000u);
+                    c[0] -= __uint_as_float(c01 << 16);
+                    c[1] -= __uint_as_float(c01 & 0xffff0000u);
+                    c[2] -= __uint_as_float(c23 << 16);
+                    c[3] -= __uint_as_float(c23 & 0xffff0000u);
+                }
+            }
+    }
+}
+
+// A row's parts together, in order: o, the target's logit and the loss.
+__global__ __launch_bounds__(256) void k_losses(VocabularyArgs a, const float2* part, int64_t parts) {
+    const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (r >= a.rows) return;
+    float2 s = make_float2(-__builtin_huge_valf(), 0.0f);
+    for (int64_t k = 0; k < parts; ++k) {
+        const float2 n = part[k * a.rows + r];
+        const float top = fmaxf(s.x, n.x), base = top == -__builtin_huge_valf() ? 0.0f : top;
+        s = make_float2(top, s.y * exp_of(s.x - base) + n.y * exp_of(n.x - base));
+    }
+    const int64_t t = a.targets[r];
+    const bool counts = t >= 0 && t < a.vocab;
+    const float others = s.x + logf(s.y);  // no others: -infinity
+    const float d = others - a.stats[a.rows + r];
+    a.stats[r] = others;
+    if (!counts) a.stats[a.rows + r] = 0.0f;
+    a.losses[r] = !counts ? 0.0f : d > 0.0f ? d + log1pf(expf(-d)) : log1pf(expf(d));
+}
+
+__global__ __launch_bounds__(256) void k_row_info(VocabularyArgs a, RowInfo* info) {
+    const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (r >= a.rows) return;
+    const int64_t t = a.targets[r];
+    RowInfo v = {0.0f, 0.0f, -1, 0};
+    if (t >= 0 && t < a.vocab) {
+        const float others = a.stats[r], d = others - a.stats[a.rows + r];
+        v.others = others == -__builtin_huge_valf() ? 0.0f : others;  // then there is no q
+        v.scale = a.dloss[r] * (d < 0.0f ? expf(d) / (1.0f + expf(d)) : 1.0f / (1.0f + expf(-d)));
+        v.target = (int)t;
+    }
+    info[r] = v;
+}
+
+// pieces of v at p, p + plane, ...
+template <typename T>
+__device__ __forceinline__ void put(bf16_t* p, int64_t plane, float v) {
+    if constexpr (sizeof(T) == 2) {
+        *p = f2bf(v);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            const bf16_t b = f2bf(v);
+            p[k * plane] = b;
+            v -= bf2f(b);
+        }
+    }
+}
+
+// Rows as an operand: padded with zeros to ld, fp32 in three pieces.
+template <typename T>
+__global__ __launch_bounds__(256) void k_pack(RowView src, int64_t rows, int cols, bf16_t* dst, int64_t plane, int64_t ld) {
+    const int64_t i = block_index() * 256 + threadIdx.x, r = i / ld, c = i - r * ld;
+    if (r >= rows) return;
+    put<T>(dst + i, plane, c < cols ? St<T>::ld1(static_cast<const T*>(src.p) + r * src.stride + c) : 0.0f);
+}
+
+// The same transposed: dst [cols][ld], ld >= rows; rows that `targets` leaves out are zero.
+template <typename T>
+__global__ __launch_bounds__(256) void k_pack_transposed(RowView src, int64_t rows, int cols, const int64_t* targets, int64_t vocab,
+                                                         bf16_t* dst, int64_t plane, int64_t ld, int blocks) {
+    __shared__ float lds[64][65];
+    const int64_t index = block_index(), r0 = index / blocks * 64;
+    const int c0 = (int)(index % blocks) * 64;
+    if (r0 >= ld) return;
+    for (int k = threadIdx.x; k < 64 * 64; k += 256) {
+        const int64_t r = r0 + k / 64;
+        const int c = c0 + k % 64;
+        bool there = r < rows && c < cols;
+        if (there && targets) there = targets[r] >= 0 && targets[r] < vocab;
+        lds[k / 64][k % 64] = there ? St<T>::ld1(static_cast<const T*>(src.p) + r * src.stride + c) : 0.0f;
+    }
+    __syncthreads();
+    for (int k = threadIdx.x; k < 64 * 64; k += 256) {
+        const int64_t r = r0 + k % 64;
+        const int c = c0 + k / 64;
+        if (r < ld && c < cols) put<T>(dst + c * ld + r, plane, lds[k % 64][k / 64]);
+    }
+}
+
+// The planes of a product together, in order, times the row's scale, as stored.
+template <typename T>
+__global__ __launch_bounds__(256) void k_finish(const float* planes, int splits, int64_t rows, int cols, int64_t ld, const RowInfo* info, T* out) {
+    const int64_t i = block_index() * 256 + threadIdx.x, r = i / cols, c = i - r * cols;
+    if (r >= rows) return;
+    float s = 0.0f;
+    for (int k = 0; k < splits; ++k) s += planes[(k * rows + r) * ld + c];
+    if (info) s = info[r].target < 0 ? 0.0f : s * info[r].scale;
+    St<T>::st1(out + i, s);
+}
+
+// ---------------------------------------------------------------------------
+// Host
+// ---------------------------------------------------------------------------
+int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+typedef Shape<256, 256, 128, 64> Large;
+typedef Shape<128, 128, 64, 64> Middle;
+typedef Shape<64, 128, 64, 32> Low;
+
+template <typename F>
+auto with_shape(int64_t m, int64_t n, F&& f) {
+    if (m <= 64) return f(Low());
+    if ((m + 255) / 256 * ((n + 255) / 256) >= 192) return f(Large());
+    return f(Middle());
+}
+
+// Parts of the sum of a product whose tiles alone leave the chip idle.
+int splits_of(int64_t m, int64_t n, int64_t steps) {
+    return with_shape(m, n, [&](auto shape) {
+        typedef decltype(shape) S;
+        const int64_t tiles = std::max<int64_t>(1, (m + S::BM - 1) / S::BM * ((n + S::BN - 1) / S::BN)), want = S::THREADS == 512 ? 256 : 512;
+        return (int)std::max<int64_t>(1, std::min<int64_t>(want / tiles, steps / 8));
+    });
+}
+
+template <int WHAT, int PIECES = 1>
+hipError_t product(Product g, hipStream_t s) {
+    return with_shape(g.a.rows, g.b.rows, [&](auto shape) {
+        typedef decltype(shape) S;
+        g.tiles_m = (int)((g.a.rows + S::BM - 1) / S::BM);
+        g.tiles_n = (int)((g.b.rows + S::BN - 1) / S::BN);
+        if (WHAT != PLANES) g.splits = 1;
+        k_product<S, WHAT, PIECES><<<dim3((unsigned)(g.tiles_m * g.tiles_n), (unsigned)g.splits), S::THREADS, 0, s>>>(g);
+        return hipGetLastError();
+    });
+}
+
+int64_t column_tile(int64_t m, int64_t n) {
+    return with_shape(m, n, [](auto shape) { return (int64_t)decltype(shape)::BN; });
+}
+
+// Where everything lies in a call's workspace, and how the vocabulary is cut.
+struct Plan {
+    int64_t piece, dimp, rowsp;   // vocabulary rows of a piece, dim and rows in whole steps
+    int pieces;                   // of an operand's numbers
+    bool pack_x, pack_w;
+    int splits_dx, splits_dw;
+    int64_t x, w, part, info, xt, wt, q, qt, dx, dw, total;  // offsets
+};
+
+bool direct(const VocabularyArgs& a, const RowView& v) {
+    return a.dtype && a.dim % BK == 0 && v.stride % 8 == 0 && v.stride < (1 << 22) && (reinterpret_cast<uintptr_t>(v.p) & 15) == 0;
+}
+
+Plan plan_of(const VocabularyArgs& a, bool backward) {
+    Plan p{};
+    p.pieces = a.dtype ? 1 : 3;
+    p.dimp = up(a.dim, BK);
+    p.rowsp = up(std::max<int64_t>(a.rows, 1), BK);
+    // pieces of at most 2^28 logits, and of 2^16 weights at a time
+    const int64_t most = std::max<int64_t>(256, std::min<int64_t>(65536, ((int64_t)1 << 28) / p.rowsp / 256 * 256));
+    const int64_t count = (a.vocab + most - 1) / most;
+    p.piece = std::min<int64_t>(up(a.vocab, BK), up((a.vocab + count - 1) / count, 256));
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const int64_t from = at;
+        at += up(bytes, 256);
+        return from;
+    };
+    // whether the operands lie as products want them is known at the call only
+    p.x = take(p.rowsp * p.dimp * 2 * p.pieces);
+    p.w = take(p.piece * p.dimp * 2 * p.pieces);
+    if (!backward) {
+        p.part = take((a.vocab / 128 + 2 + (a.vocab + p.piece - 1) / p.piece) * a.rows * 8);
+    } else {
+        p.info = take(a.rows * (int64_t)sizeof(RowInfo));
+        p.xt = take(a.dim * p.rowsp * 2 * p.pieces);
+        p.wt = take(a.dim * p.piece * 2 * p.pieces);
+        p.q = take(p.rowsp * p.piece * 2 * p.pieces);
+        p.qt = take(p.rowsp * p.piece * 2 * p.pieces);
+        const int pairs = p.pieces == 1 ? 1 : 6;
+        p.splits_dx = splits_of(a.rows, a.dim, p.piece / BK * pairs);
+        p.splits_dw = splits_of(p.piece, a.dim, p.rowsp / BK * pairs);
+        p.dx = take(p.splits_dx * a.rows * a.dim * 4);
+        p.dw = take(p.splits_dw * p.piece * a.dim * 4);
+    }
+    p.total = std::max<int64_t>(at, 16);
+    return p;
+}
+
+#define OK_OR_RETURN(expr)                     \
+    do {                                       \
+        const hipError_t _e = (expr);          \
+        if (_e != hipSuccess) return _e;       \
+    } while (0)
+
+template <typename T>
+hipError_t pack(const RowView& v, int64_t rows, int cols, bf16_t* dst, int64_t plane, int64_t ld, hipStream_t s) {
+    dim3 grid;
+    if (!grid_of((rows * ld + 255) / 256, 256, grid)) return hipErrorInvalidValue;
+    k_pack<T><<<grid, 256, 0, s>>>(v, rows, cols, dst, plane, ld);
+    return hipGetLastError();
+}
+template <typename T>
+hipError_t pack_transposed(const RowView& v, int64_t rows, int cols, const int64_t* targets, int64_t vocab, bf16_t* dst, int64_t plane,
+                           int64_t ld, hipStream_t s) {
+    const int blocks = (cols + 63) / 64;
+    dim3 grid;
+    if (!grid_of((ld + 63) / 64 * blocks, 256, grid)) return hipErrorInvalidValue;
+    k_pack_transposed<T><<<grid, 256, 0, s>>>(v, rows, cols, targets, vocab, dst, plane, ld, blocks);
+    return hipGetLastError();
+}
+
+// x, and vocabulary rows first .. first + n - 1, as operands of the logits.
+template <typename T>
+hipError_t x_operand(const VocabularyArgs& a, const Plan& p, Operand& o, hipStream_t s) {
+    if (direct(a, a.x)) {
+        o = Operand{static_cast<const bf16_t*>(a.x.p), 0, a.x.stride, a.rows};
+        return hipSuccess;
+    }
+    bf16_t* to = reinterpret_cast<bf16_t*>(static_cast<char*>(a.ws) + p.x);
+    o = Operand{to, p.rowsp * p.dimp, p.dimp, a.rows};
+    return pack<T>(a.x, a.rows, a.dim, to, o.plane, o.ld, s);
+}
+template <typename T>
+hipError_t w_operand(const VocabularyArgs& a, const Plan& p, int64_t first, int64_t n, Operand& o, hipStream_t s) {
+    const RowView w = {static_cast<const T*>(a.w.p) + first * a.w.stride, a.w.stride};
+    if (direct(a, a.w)) {
+        o = Operand{static_cast<const bf16_t*>(w.p), 0, w.stride, n};
+        return hipSuccess;
+    }
+    bf16_t* to = reinterpret_cast<bf16_t*>(static_cast<char*>(a.ws) + p.w);
+    o = Operand{to, p.piece * p.dimp, p.dimp, n};
+    return pack<T>(w, n, a.dim, to, o.plane, o.ld, s);
+}
+
+template <typename T>
+hipError_t forward(const VocabularyArgs& a, hipStream_t s) {
+    const Plan p = plan_of(a, false);
+    char* ws = static_cast<char*>(a.ws);
+    Product g{};
+    OK_OR_RETURN(x_operand<T>(a, p, g.a, s));
+    g.steps = (int)(p.dimp / BK);
+    g.pairs = p.pieces == 1 ? 1 : 6;
+    g.targets = a.targets;
+    g.logit = a.stats + a.rows;
+    float2* part = reinterpret_cast<float2*>(ws + p.part);
+    // without a copy nothing cuts the vocabulary but the size of a launch
+    const int64_t piece = direct(a, a.w) ? std::max(p.piece, ((int64_t)1 << 22) / ((a.rows + 63) / 64) * 128) : p.piece;
+    int64_t parts = 0;
+    for (int64_t first = 0; first < a.vocab; first += piece) {
+        const int64_t n = std::min<int64_t>(piece, a.vocab - first);
+        OK_OR_RETURN(w_operand<T>(a, p, first, n, g.b, s));
+        g.first = first;
+        g.part = part + parts * a.rows;
+        OK_OR_RETURN(product<LOGSUM>(g, s));
+        const int64_t tile = column_tile(a.rows, n);
+        parts += (n + tile - 1) / tile;
+    }
+    k_losses<<<(unsigned)((a.rows + 255) / 256), 256, 0, s>>>(a, part, parts);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t backward(const VocabularyArgs& a, hipStream_t s) {
+    const Plan p = plan_of(a, true);
+    char* ws = static_cast<char*>(a.ws);
+    auto bf = [&](int64_t at) { return reinterpret_cast<bf16_t*>(ws + at); };
+    auto f32 = [&](int64_t at) { return reinterpret_cast<float*>(ws + at); };
+    RowInfo* info = reinterpret_cast<RowInfo*>(ws + p.info);
+    const int pairs = p.pieces == 1 ? 1 : 6;
+    T *dx = static_cast<T*>(a.dx), *dw = static_cast<T*>(a.dw);
+    if (a.rows > 0) {
+        k_row_info<<<(unsigned)((a.rows + 255) / 256), 256, 0, s>>>(a, info);
+        OK_OR_RETURN(hipGetLastError());
+    }
+    Product logits{};
+    if (a.rows > 0) OK_OR_RETURN(x_operand<T>(a, p, logits.a, s));
+    const int64_t xt_plane = a.dim * p.rowsp;
+    OK_OR_RETURN(pack_transposed<T>(a.x, a.rows, a.dim, a.targets, a.vocab, bf(p.xt), xt_plane, p.rowsp, s));
+    for (int64_t first = 0; first < a.vocab; first += p.piece) {
+        const int64_t n = std::min<int64_t>(p.piece, a.vocab - first), np = up(n, BK);
+        Product g = logits;
+        if (a.rows > 0) {
+            OK_OR_RETURN(w_operand<T>(a, p, first, n, g.b, s));
+            g.steps = (int)(p.dimp / BK);
+            g.pairs = pairs;
+            g.first = first;
+            g.info = info;
+            g.q = bf(p.q);
+            g.qt = bf(p.qt);
+            g.ldq = np;
+            g.ldt = p.rowsp;
+            g.q_plane = g.qt_plane = p.rowsp * p.piece;
+            OK_OR_RETURN((product<GRADIENT, sizeof(T) == 2 ? 1 : 3>(g, s)));
+            const int64_t wt_plane = a.dim * p.piece;
+            const RowView w = {static_cast<const T*>(a.w.p) + first * a.w.stride, a.w.stride};
+            OK_OR_RETURN(pack_transposed<T>(w, n, a.dim, nullptr, 0, bf(p.wt), wt_plane, np, s));
+            Product x{};
+            x.a = Operand{g.q, g.q_plane, np, a.rows};
+            x.b = Operand{bf(p.wt), wt_plane, np, a.dim};
+            x.steps = (int)(np / BK);
+            x.pairs = pairs;
+            x.splits = p.splits_dx;
+            x.out = f32(p.dx);
+            x.ldo = a.dim;
+            x.add = first > 0;
+            OK_OR_RETURN(product<PLANES>(x, s));
+        }
+        Product v{};
+        v.a = Operand{bf(p.qt), p.rowsp * p.piece, p.rowsp, n};
+        v.b = Operand{bf(p.xt), xt_plane, p.rowsp, a.dim};
+        v.steps = a.rows > 0 ? (int)(p.rowsp / BK) : 0;  // no rows: dW is zero
+        v.pairs = pairs;
+        v.splits = p.splits_dw;
+        v.out = f32(p.dw);
+        v.ldo = a.dim;
+        OK_OR_RETURN(product<PLANES>(v, s));
+        dim3 grid;
+        if (!grid_of((n * a.dim + 255) / 256, 256, grid)) return hipErrorInvalidValue;
+        k_finish<T><<<grid, 256, 0, s>>>(v.out, v.splits, n, a.dim, a.dim, nullptr, dw + first * a.dim);
+        OK_OR_RETURN(hipGetLastError());
+    }
+    if (a.rows == 0) return hipSuccess;
+    dim3 grid;
+    if (!grid_of((a.rows * a.dim + 255) / 256, 256, grid)) return hipErrorInvalidValue;
+    k_finish<T><<<grid, 256, 0, s>>>(f32(p.dx), p.splits_dx, a.rows, a.dim, a.dim, info, dx);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t vocabulary_workspace_bytes(const VocabularyArgs& a, bool backward) { return (size_t)plan_of(a, backward).total; }
+
+hipError_t launch_vocabulary_fwd(const VocabularyArgs& a, hipStream_t s) {
+    if (a.rows == 0) return hipSuccess;
+    return a.dtype ? forward<bf16_t>(a, s) : forward<float>(a, s);
+}
+hipError_t launch_vocabulary_bwd(const VocabularyArgs& a, hipStream_t s) {
+    return a.dtype ? backward<bf16_t>(a, s) : backward<float>(a, s);
+}
+
+}  // namespace mdl

@@ -1,5 +1,5 @@
-// Host side of the gated recurrence and the group norm of include/mdlstm.h:
-// argument validation (always before the first HIP call), workspace planning and
+// Host side of the gated recurrence, the group norm and the loss over a vocabulary
+// of include/mdlstm.h: argument validation (always before the first HIP call), workspace planning and
 // dispatch.
 #include <algorithm>
 #include <cmath>
@@ -7,6 +7,7 @@
 #include "checks.hpp"
 #include "groupnorm.hpp"
 #include "recurrence.hpp"
+#include "vocabulary.hpp"
 
 namespace {
 
@@ -67,6 +68,28 @@ mdl::GroupNormArgs group_norm_args(const mdlstm_group_norm_desc* d, const mdl::P
     a.dtype = d->dtype;
     a.act = d->activation;
     a.eps = d->eps;
+    return a;
+}
+
+mdlstm_status check_vocabulary(const mdlstm_vocabulary_desc* d, int64_t rows) {
+    if (!d) return fail(MDLSTM_ERR_INVALID_ARG, "desc is NULL");
+    OK_OR_RETURN(check_dtype(d->dtype));
+    if (d->dim < 1 || d->vocab < 1) return fail(MDLSTM_ERR_INVALID_ARG, "dim %d and vocab %d must be positive", d->dim, d->vocab);
+    if (d->dim > mdl::kMaxVocabularyDim || d->vocab > mdl::kMaxVocabulary)
+        return fail(MDLSTM_ERR_UNSUPPORTED, "dim %d, vocab %d: at most %d and %d", d->dim, d->vocab, mdl::kMaxVocabularyDim,
+                    mdl::kMaxVocabulary);
+    if (rows < 0) return fail(MDLSTM_ERR_INVALID_ARG, "%lld rows", (long long)rows);
+    if (rows > mdl::kMaxVocabularyRows)
+        return fail(MDLSTM_ERR_UNSUPPORTED, "%lld rows: at most %lld", (long long)rows, (long long)mdl::kMaxVocabularyRows);
+    return MDLSTM_OK;
+}
+
+mdl::VocabularyArgs vocabulary_args(const mdlstm_vocabulary_desc* d, int64_t rows) {
+    mdl::VocabularyArgs a{};
+    a.dtype = d->dtype;
+    a.dim = d->dim;
+    a.vocab = d->vocab;
+    a.rows = rows;
     return a;
 }
 
@@ -276,6 +299,76 @@ mdlstm_status mdlstm_group_norm_backward(const mdlstm_group_norm_desc* desc, int
     a.db = d_db;
     a.ws = d_workspace;
     HIP_OR_FAIL(mdl::launch_groupnorm_bwd(a, reinterpret_cast<hipStream_t>(stream)));
+    return MDLSTM_OK;
+}
+
+size_t mdlstm_vocabulary_workspace_bytes(const mdlstm_vocabulary_desc* desc, int64_t rows, int32_t backward) {
+    if (check_vocabulary(desc, rows) != MDLSTM_OK) return 0;
+    return mdl::vocabulary_workspace_bytes(vocabulary_args(desc, rows), backward != 0);
+}
+
+mdlstm_status mdlstm_vocabulary_forward(const mdlstm_vocabulary_desc* desc, int64_t rows, const void* d_x, int64_t x_stride,
+                                        const void* d_w, int64_t w_stride, const int64_t* d_targets, float* d_losses,
+                                        float* d_stats, void* d_workspace, size_t workspace_bytes, void* stream) {
+    OK_OR_RETURN(check_vocabulary(desc, rows));
+    const int64_t dim = desc->dim;
+    OK_OR_RETURN(check_rows(d_x, "x", rows, dim, x_stride, desc->dtype));
+    OK_OR_RETURN(check_rows(d_w, "w", desc->vocab, dim, w_stride, desc->dtype));
+    OK_OR_RETURN(check_out(d_targets, "targets", rows > 0, 8));
+    OK_OR_RETURN(check_out(d_losses, "losses", rows > 0, 4));
+    OK_OR_RETURN(check_out(d_stats, "stats", rows > 0, 4));
+    mdl::VocabularyArgs a = vocabulary_args(desc, rows);
+    const size_t need = mdl::vocabulary_workspace_bytes(a, false);
+    OK_OR_RETURN(check_workspace(d_workspace, workspace_bytes, need));
+    OK_OR_RETURN(check_apart({span("losses", d_losses, rows * 4, true), span("stats", d_stats, rows * 8, true),
+                              span("the workspace", d_workspace, (int64_t)need, true),
+                              span("x", d_x, rows_bytes(rows, dim, x_stride, desc->dtype), false),
+                              span("w", d_w, rows_bytes(desc->vocab, dim, w_stride, desc->dtype), false),
+                              span("targets", d_targets, rows * 8, false)}));
+    if (rows == 0) return MDLSTM_OK;
+    OK_OR_RETURN(mdl::poison_workspace(d_workspace, need, stream));
+    a.x = mdl::RowView{d_x, x_stride};
+    a.w = mdl::RowView{d_w, w_stride};
+    a.targets = d_targets;
+    a.losses = d_losses;
+    a.stats = d_stats;
+    a.ws = d_workspace;
+    HIP_OR_FAIL(mdl::launch_vocabulary_fwd(a, reinterpret_cast<hipStream_t>(stream)));
+    return MDLSTM_OK;
+}
+
+mdlstm_status mdlstm_vocabulary_backward(const mdlstm_vocabulary_desc* desc, int64_t rows, const void* d_x, int64_t x_stride,
+                                         const void* d_w, int64_t w_stride, const int64_t* d_targets, const float* d_stats,
+                                         const float* d_dlosses, void* d_dx, void* d_dw, void* d_workspace,
+                                         size_t workspace_bytes, void* stream) {
+    OK_OR_RETURN(check_vocabulary(desc, rows));
+    const int64_t dim = desc->dim, es = (int64_t)element(desc->dtype);
+    OK_OR_RETURN(check_rows(d_x, "x", rows, dim, x_stride, desc->dtype));
+    OK_OR_RETURN(check_rows(d_w, "w", desc->vocab, dim, w_stride, desc->dtype));
+    OK_OR_RETURN(check_out(d_targets, "targets", rows > 0, 8));
+    OK_OR_RETURN(check_out(d_stats, "stats", rows > 0, 4));
+    OK_OR_RETURN(check_out(d_dlosses, "dlosses", rows > 0, 4));
+    OK_OR_RETURN(check_out(d_dx, "dx", rows > 0, es));
+    OK_OR_RETURN(check_out(d_dw, "dw", true, es));
+    mdl::VocabularyArgs a = vocabulary_args(desc, rows);
+    const size_t need = mdl::vocabulary_workspace_bytes(a, true);
+    OK_OR_RETURN(check_workspace(d_workspace, workspace_bytes, need));
+    OK_OR_RETURN(check_apart({span("dx", d_dx, rows * dim * es, true), span("dw", d_dw, desc->vocab * dim * es, true),
+                              span("the workspace", d_workspace, (int64_t)need, true),
+                              span("x", d_x, rows_bytes(rows, dim, x_stride, desc->dtype), false),
+                              span("w", d_w, rows_bytes(desc->vocab, dim, w_stride, desc->dtype), false),
+                              span("targets", d_targets, rows * 8, false), span("stats", d_stats, rows * 8, false),
+                              span("dlosses", d_dlosses, rows * 4, false)}));
+    OK_OR_RETURN(mdl::poison_workspace(d_workspace, need, stream));
+    a.x = mdl::RowView{d_x, x_stride};
+    a.w = mdl::RowView{d_w, w_stride};
+    a.targets = d_targets;
+    a.stats = const_cast<float*>(d_stats);
+    a.dloss = d_dlosses;
+    a.dx = d_dx;
+    a.dw = d_dw;
+    a.ws = d_workspace;
+    HIP_OR_FAIL(mdl::launch_vocabulary_bwd(a, reinterpret_cast<hipStream_t>(stream)));
     return MDLSTM_OK;
 }
 

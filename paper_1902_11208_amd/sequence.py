@@ -1,7 +1,8 @@
 """Layers along the packed frames of the examples (or any packed tokens):
 linear attention with a decay for each head, a gated linear recurrence, the
-single-token steps of both, root-mean-square norm of a residual sum, dropout, and
-a norm over groups of channels with an activation.
+single-token steps of both, root-mean-square norm of a residual sum, dropout, a
+norm over groups of channels with an activation, and the softmax cross entropy over
+a vocabulary.
 
 Tokens lie example after example without padding, as the output layer's frames
 do. Every step of the computation runs in libmdlstm.so's HIP kernels; this
@@ -21,7 +22,7 @@ import ctypes
 import numpy as np
 import torch
 
-from ._lib import AttentionDesc, GroupNormDesc, NormDesc, RecurrenceDesc, lib
+from ._lib import AttentionDesc, GroupNormDesc, NormDesc, RecurrenceDesc, VocabularyDesc, lib
 from .api import check_tensor, dtype_code
 
 try:
@@ -364,6 +365,55 @@ class ResidualNorm:
         self._op.backward(h, self._rstd, dy, dh, seed, call, self._dx, self._dres if both else None, self._dw, self._ws,
                           _stream(stream))
         return self._dx, (self._dres if both else self._dx) if residual else None, self._dw
+
+
+class VocabularyLoss:
+    """Softmax cross entropy of `rows` rows over a vocabulary, without stored logits:
+
+        loss_i = log(sum_v exp(x_i . weight_v)) - x_i . weight_target_i
+
+    weight: [vocab, dim] device tensor, float32 or bfloat16, which x and the gradients share. A row whose target lies
+    outside [0, vocab) (-1, say) has loss 0 and takes no part in the gradients, whatever it holds. Sums are fp32.
+    """
+
+    def __init__(self, weight: torch.Tensor, rows: int):
+        if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
+            raise ValueError("weight must be a [vocab, dim] tensor")
+        desc = VocabularyDesc(weight.shape[1], weight.shape[0], dtype_code(weight.dtype))
+        check_tensor(weight, "weight", weight.shape, weight.dtype)
+        self.weight, self.rows, self.vocab, self.dim = weight, int(rows), weight.shape[0], weight.shape[1]
+        self.dtype, self.device = weight.dtype, weight.device
+        self._bytes = [int(lib().mdlstm_vocabulary_workspace_bytes(ctypes.byref(desc), self.rows, b)) for b in (0, 1)]
+        if not all(self._bytes):
+            raise ValueError(lib().mdlstm_last_error().decode(errors="replace"))
+        self._op = _binding.Vocabulary(self.dim, self.vocab, desc.dtype, self.rows, weight)
+        self._losses = self._stats = self._grads = self._saved = None
+        self._ws = [None, None]
+
+    def _workspace(self, backward: int, stream) -> torch.Tensor:
+        if self._ws[backward] is None:
+            self._ws[backward] = _empty(self._bytes[backward], torch.uint8, self.device, stream)
+        return self._ws[backward]
+
+    def forward(self, x, targets, stream=None) -> torch.Tensor:
+        """losses [rows] in fp32 of x [rows, dim], contiguous along its rows, and targets [rows] (int64)."""
+        if self._losses is None:
+            self._losses = _empty(self.rows, torch.float32, self.device, stream)
+            self._stats = _empty((2, self.rows), torch.float32, self.device, stream)
+        self._op.forward(x, targets, self._losses, self._stats, self._workspace(0, stream), _stream(stream))
+        self._saved = (x, targets)
+        return self._losses
+
+    def backward(self, dlosses, stream=None):
+        """(dx, dweight) in the storage type after a forward call, from the gradient of the losses [rows] (fp32). The
+        weights have to be as they were in the forward call."""
+        if self._saved is None:
+            raise ValueError("backward needs a forward call on this loss first")
+        if self._grads is None:
+            self._grads = (_empty((self.rows, self.dim), self.dtype, self.device, stream),
+                           _empty((self.vocab, self.dim), self.dtype, self.device, stream))
+        self._op.backward(*self._saved, self._stats, dlosses, *self._grads, self._workspace(1, stream), _stream(stream))
+        return self._grads
 
 
 def dropout(x, p: float, seed: int, call: int = 0, residual=None, out=None, stream=None) -> torch.Tensor:
