@@ -595,11 +595,16 @@ hipError_t with_lanes(int vecs, F&& f) {
 
 int vecs_of(int channels) { return (channels + V - 1) / V; }
 
-// Tokens of a segment; 0: whole sequences.
+// Tokens of a segment; 0: whole sequences. A workgroup's tiles follow each other,
+// so sequences are cut where the longest one would hold the chip up: where it is
+// longer than all tokens spread over the CUs. Segments then give a CU four units.
 int64_t segment_of(const RecurrenceArgs& a) {
-    (void)a;
-    return 0;
+    constexpr int64_t CUS = 256;
+    const int64_t blocks = (vecs_of(a.channels) + 31) / 32, share = a.seqs.tokens * blocks / CUS;
+    if (a.seqs.longest <= std::max<int64_t>(1024, 2 * share)) return 0;
+    return std::max<int64_t>(256, (share / 4 + kRecurrenceTile - 1) / kRecurrenceTile * kRecurrenceTile);
 }
+
 RecurrenceArgs plan(const RecurrenceArgs& in) {
     RecurrenceArgs a = in;
     a.seqs.seg = segment_of(a);
