@@ -611,7 +611,7 @@ size_t mdlstm_recurrence_marks_bytes(const mdlstm_recurrence_desc* desc, int64_t
 /*
  * d_offsets, d_order, tokens and longest as for mdlstm_attention_forward. d_z and
  * d_x: rows of `channels` elements, z_stride and x_stride >= channels elements
- * apart. d_state [n][channels] (may be NULL: zero): the state each example starts
+ * apart (at most 2^22: UNSUPPORTED beyond). d_state [n][channels] (may be NULL: zero): the state each example starts
  * from; d_final (out, may be NULL): the state it leaves. d_h (out) [tokens]
  * [channels]. d_marks (out, may be NULL: no backward call follows). Asynchronous on
  * `stream`; capturable into a graph. Buffers that the call writes must not

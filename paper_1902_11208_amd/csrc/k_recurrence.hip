@@ -17,6 +17,7 @@
 // rounded output: h - x is a difference, and a rounded h would leave it with
 // an error of 2^-9 of h.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.hpp"
 #include "recurrence.hpp"
@@ -93,22 +94,29 @@ __device__ __forceinline__ void store_f32(float* p, int valid, const float (&v)[
 
 // sigmoid(z) and 1 - sigmoid(z), both to a few ulp of themselves: the smaller one
 // is e / (1 + e) and not a difference. The reciprocal takes one Newton step: an
-// error of f is met again in every token that a state lives through.
+// error of f is met again in every token that a state lives through. EXACT: the
+// product with log2(e) keeps its low half, without which e is off by |z| 2^-24; for
+// bf16 inputs that is far below z's own rounding.
+template <bool EXACT>
 __device__ __forceinline__ void sigmoids(float z, float& f, float& rest) {
-    const float e = expf(-fabsf(z)), d = 1.0f + e;
+    constexpr float HIGH = -1.44269502162933349609375f, LOW = -1.925963033500011e-08f, LN2 = 0.693147180559945309f;
+    const float m = fabsf(z), t = m * HIGH;
+    float e = __builtin_amdgcn_exp2f(t);
+    if constexpr (EXACT) e = fmaf(e, LN2 * fmaf(m, LOW, fmaf(m, HIGH, -t)), e);
+    if (EXACT && t < -160.0f) e = 0.0f;  // below fp32's range, where m HIGH may be beyond it
+    const float d = 1.0f + e;
     float r = __builtin_amdgcn_rcpf(d);
     r = fmaf(fmaf(-d, r, 1.0f), r, r);
     const float small = e * r;
     f = z < 0.0f ? small : r;
     rest = z < 0.0f ? r : small;
-    if (z != z) f = rest = z;
 }
 
-template <bool SIG>
+template <typename T, bool SIG>
 __device__ __forceinline__ void coefficients(float z, float x, float& f, float& u) {
     if constexpr (SIG) {
         float rest;
-        sigmoids(z, f, rest);
+        sigmoids<sizeof(T) == 4>(z, f, rest);
         u = rest * x;
     } else {
         f = z;
@@ -116,115 +124,164 @@ __device__ __forceinline__ void coefficients(float z, float x, float& f, float& 
     }
 }
 
-// States beyond this, and sums that are not finite, are not joined by A h + B
-// (A may have fallen below fp32's range, 0 times infinity is no number, A and
-// B may have overflowed where the recurrence does not): the tokens are walked.
-constexpr float LARGE_STATE = 0x1p64f;
+// A h + B is what the tokens give unless something leaves fp32's range on the way:
+// A may have fallen below it under a large state, 0 times infinity is no number,
+// factors may have grown and shrunk. So slices whose factors multiply to more
+// than 4 or whose B is large are marked with NaN (sixteen of them then grow a state
+// by at most 2^32), and where a mark or a large state is met the tokens are walked
+// one by one.
+constexpr float LARGE = 0x1p40f;
 
-__device__ __forceinline__ bool finite(float v) { return fabsf(v) < __builtin_huge_valf(); }
-
-// (A, B) that a join can use, or NaN.
-__device__ __forceinline__ void mark_unusable(float& A, float& B) {
-    if (!(finite(A) && finite(B))) A = B = __builtin_nanf("");
+__device__ __forceinline__ void mark_factor(float& A, float most) {
+    if (!(fabsf(A) <= most)) A = __builtin_nanf("");
+}
+__device__ __forceinline__ void mark_rest(float& B) {
+    if (!(fabsf(B) <= LARGE)) B = __builtin_nanf("");
+}
+// The state from an unmarked run is not what the tokens give.
+__device__ __forceinline__ bool unsafe(float from, float joined) {
+    return from == from && (joined != joined || fabsf(from) > LARGE);
 }
 
+// Rows of a sequence as a thread reads them: a uniform base, and 32 bits of its own
+// offset (128 rows are less than 2^32 bytes apart by the caller's check).
+template <typename T, bool WIDE>
+struct Rows {
+    const char* base;
+    int64_t stride;  // bytes
+    uint32_t c;      // bytes
+    int valid;
+    __device__ __forceinline__ Rows(const RowView& v, int64_t t0, int c_, int valid_)
+        : base(static_cast<const char*>(v.p) + t0 * v.stride * (int64_t)sizeof(T)), stride(v.stride * (int64_t)sizeof(T)),
+          c((uint32_t)c_ * sizeof(T)), valid(valid_) {}
+    __device__ __forceinline__ Raw<T> at(const char* row, uint32_t offset) const {
+        return load_raw<T, WIDE>(reinterpret_cast<const T*>(row + offset), valid);
+    }
+    // a slice's eight tokens of the tile at `tile`, of which `n` tokens are real: behind them the last one again
+    __device__ __forceinline__ void load(int64_t tile, int64_t n, int slice, Raw<T> (&r)[L]) const {
+        const char* row = base + tile * stride;
+        if (n >= kRecurrenceTile) {
+            const uint32_t mine = (uint32_t)(slice * L) * (uint32_t)stride + c;
+#pragma unroll
+            for (int i = 0; i < L; ++i) r[i] = at(row + i * stride, mine);
+        } else {
+#pragma unroll
+            for (int i = 0; i < L; ++i) r[i] = at(row, (uint32_t)min(slice * L + i, (int)n - 1) * (uint32_t)stride + c);
+        }
+    }
+    __device__ __forceinline__ void token(int64_t t, float (&v)[V]) const { unpack(at(base + t * stride, c), v); }
+};
+
+// [tokens][channels] outputs of a slice, `n` tokens of the tile real.
+template <typename T, bool WIDE>
+struct Out {
+    char* base;
+    uint32_t stride, c;  // bytes
+    int valid;
+    __device__ __forceinline__ Out(void* p, int64_t t0, int channels, int c_, int valid_)
+        : base(static_cast<char*>(p) + t0 * channels * (int64_t)sizeof(T)), stride((uint32_t)channels * sizeof(T)),
+          c((uint32_t)c_ * sizeof(T)), valid(valid_) {}
+    __device__ __forceinline__ void store(int64_t tile, int slice, int l, const float (&v)[V]) const {
+        char* row = base + (tile + l) * (int64_t)stride;
+        if (valid > 0) store_vec<T, WIDE>(reinterpret_cast<T*>(row + ((uint32_t)(slice * L) * stride + c)), valid, v);
+    }
+};
+
 // What a thread is: a slice of a tile and two channels.
-template <typename T, int CL>
 struct Place {
     int slice, lane, c, valid;
-    __device__ __forceinline__ Place(const RecurrenceArgs& a, int block) {
-        slice = threadIdx.x / CL;
-        lane = threadIdx.x % CL;
-        c = (block * CL + lane) * V;
-        valid = max(0, min(V, a.channels - c));
+    __device__ __forceinline__ Place(int channels, int lanes, int block) {
+        slice = threadIdx.x / lanes;
+        lane = threadIdx.x % lanes;
+        c = (block * lanes + lane) * V;
+        valid = max(0, min(V, channels - c));
         if (valid == 0) c = 0;
     }
 };
 
-template <typename T, bool WIDE>
-struct Rows {
-    const T* p;
-    int64_t stride;
-    int valid;
-    __device__ __forceinline__ Rows(const RowView& v, int64_t t0, int c, int valid_)
-        : p(static_cast<const T*>(v.p) + t0 * v.stride + c), stride(v.stride), valid(valid_) {}
-    // eight tokens from t; those from `to` on repeat the last one (and are not used)
-    __device__ __forceinline__ void load(int64_t t, int64_t to, Raw<T> (&r)[L]) const {
-#pragma unroll
-        for (int i = 0; i < L; ++i) r[i] = load_raw<T, WIDE>(p + min(t + i, to - 1) * stride, valid);
-    }
-    __device__ __forceinline__ void at(int64_t t, float (&v)[V]) const { unpack(load_raw<T, WIDE>(p + t * stride, valid), v); }
-};
-
-// A slice's sums in LDS, of one of two tiles in turn (one barrier a tile).
-template <int CL, int N>
-struct Sums {
-    float v[2][N][SLICES][CL * V];
-};
-
-__device__ __forceinline__ void copy_in(float* to, const float (&v)[V]) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) to[i] = v[i];
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+    return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
-// The state that slice `mine` starts from and the one that the tile leaves, from
-// the state `h` it starts from (REVERSE: slices from the last to the first). True
-// where a channel's sums cannot be joined.
+// The workgroup's unit and block of channels; false where there is none.
+__device__ __forceinline__ bool find_unit(const RecurrenceArgs& a, int blocks, Unit& u, int& block) {
+    const int64_t index = block_index(), slot = uniform(index / blocks);
+    block = __builtin_amdgcn_readfirstlane((int)(index - slot * blocks));
+    if (slot >= a.seqs.slots || !unit_of(a.seqs, slot, u)) return false;
+    u.seq = __builtin_amdgcn_readfirstlane(u.seq);
+    u.t0 = uniform(u.t0);
+    u.len = uniform(u.len);
+    u.from = uniform(u.from);
+    u.to = uniform(u.to);
+    return true;
+}
+
+__device__ __forceinline__ int64_t mark_row(const Unit& u, int64_t tile) { return u.t0 / kRecurrenceTile + tile / kRecurrenceTile; }
+
+// What the slices of a tile tell each other, for one of two tiles in turn (one
+// barrier a tile): their sums, and the state (adjoint) that the tile before left.
+template <int CL, int N>
+struct Shared {
+    float2 sum[2][N][SLICES][CL];
+    float2 carry[2][CL];
+};
+__device__ __forceinline__ float2 pack(const float (&v)[V]) { return make_float2(v[0], v[1]); }
+
+// The state that meets slice `mine`, from `h` that meets the tile: the slices before
+// it (REVERSE: behind it) in order. A wave goes no further than its last one.
 template <int CL, bool REVERSE>
-__device__ __forceinline__ bool join_slices(const float (*A)[CL * V], const float (*B)[CL * V], int mine, int lane, float (&h)[V],
-                                            float (&start)[V]) {
-    float top[V], before[V];
+__device__ __forceinline__ void join_slices(const float2 (*A)[CL], const float2 (*B)[CL], int mine, int lane, float (&h)[V]) {
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+    const int n = REVERSE ? SLICES - 1 - wave * 64 / CL : min(SLICES - 1, (wave * 64 + 63) / CL);
+    for (int k0 = 0; k0 < n; k0 += 4) {
+        float2 pa[4], pb[4];
 #pragma unroll
-    for (int i = 0; i < V; ++i) before[i] = h[i], top[i] = fabsf(h[i]), start[i] = h[i];
+        for (int i = 0; i < 4; ++i) {
+            const int s = REVERSE ? SLICES - 1 - k0 - i : k0 + i;
+            pa[i] = A[s][lane];
+            pb[i] = B[s][lane];
+        }
 #pragma unroll
-    for (int k = 0; k < SLICES; ++k) {
-        const int s = REVERSE ? SLICES - 1 - k : k;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            if (s == mine) start[i] = h[i];
-            h[i] = fmaf(A[s][lane * V + i], h[i], B[s][lane * V + i]);
-            top[i] = fmaxf(top[i], fabsf(h[i]));
+        for (int i = 0; i < 4; ++i) {
+            const int s = REVERSE ? SLICES - 1 - k0 - i : k0 + i;
+            const bool before = REVERSE ? s > mine : s < mine;
+            const float h0 = fmaf(pa[i].x, h[0], pb[i].x), h1 = fmaf(pa[i].y, h[1], pb[i].y);
+            h[0] = before ? h0 : h[0];
+            h[1] = before ? h1 : h[1];
         }
     }
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < V; ++i) bad = bad || (before[i] == before[i] && (h[i] != h[i] || top[i] > LARGE_STATE));
-    return bad;
 }
 
-// h through the tokens from .. to - 1, one by one; `start`: the state in front of token `at`.
+// h through the tokens from .. to - 1, one by one.
 template <typename T, bool SIG, bool WIDE>
-__device__ __forceinline__ void walk_forward(Rows<T, WIDE> z, Rows<T, WIDE> x, int64_t from, int64_t to, int64_t at,
-                                             float (&h)[V], float (&start)[V]) {
+__device__ __forceinline__ void walk_forward(const Rows<T, WIDE>& z, const Rows<T, WIDE>& x, int64_t from, int64_t to, float (&h)[V]) {
 #pragma unroll 1
     for (int64_t t = from; t < to; ++t) {
         float vz[V], vx[V];
-        z.at(t, vz);
-        x.at(t, vx);
+        z.token(t, vz);
+        x.token(t, vx);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            if (t == at) start[i] = h[i];
             float f, u;
-            coefficients<SIG>(vz[i], vx[i], f, u);
+            coefficients<T, SIG>(vz[i], vx[i], f, u);
             h[i] = fmaf(f, h[i], u);
         }
     }
 }
 
-// The adjoint from token to - 1 down to `from`; `start`: the one that meets token at - 1.
+// The adjoint from token to - 1 down to `from`.
 template <typename T, bool SIG, bool WIDE>
-__device__ __forceinline__ void walk_reverse(Rows<T, WIDE> z, Rows<T, WIDE> dh, int64_t from, int64_t to, int64_t at,
-                                             float (&s)[V], float (&start)[V]) {
+__device__ __forceinline__ void walk_reverse(const Rows<T, WIDE>& z, const Rows<T, WIDE>& dh, int64_t from, int64_t to, float (&s)[V]) {
 #pragma unroll 1
     for (int64_t t = to - 1; t >= from; --t) {
         float vz[V], vg[V];
-        z.at(t, vz);
-        dh.at(t, vg);
+        z.token(t, vz);
+        dh.token(t, vg);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            if (t == at - 1) start[i] = s[i];
             float f, u;
-            coefficients<SIG>(vz[i], 0.0f, f, u);
+            coefficients<T, SIG>(vz[i], 0.0f, f, u);
             s[i] = f * (vg[i] + s[i]);
         }
     }
@@ -233,247 +290,281 @@ __device__ __forceinline__ void walk_reverse(Rows<T, WIDE> z, Rows<T, WIDE> dh, 
 template <int CL>
 constexpr int threads_of() { return CL * SLICES; }
 
+// A segment's A and B from its tiles', by the threads of the last slice to be joined.
+__device__ __forceinline__ void add_tile(const float (&tile_a)[V], const float (&tile_b)[V], float (&A)[V], float (&B)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        B[i] = fmaf(tile_a[i], B[i], tile_b[i]);
+        A[i] *= tile_a[i];
+        mark_factor(A[i], 0x1p32f);
+        mark_rest(B[i]);
+    }
+}
+
 // Forward pass of a sequence or segment. SUMS: only what it maps a state to, for the join.
 template <typename T, bool SIG, bool WIDE, int CL, bool SUMS>
 __global__ __launch_bounds__(threads_of<CL>()) void k_recurrence_fwd(RecurrenceArgs a, int blocks) {
-    __shared__ Sums<CL, 2> lds;
-    const int64_t index = block_index();
-    const int64_t slot = index / blocks;
+    __shared__ Shared<CL, 2> lds;
     Unit u;
-    if (slot >= a.seqs.slots || !unit_of(a.seqs, slot, u)) return;
-    const Place<T, CL> me(a, (int)(index - slot * blocks));
+    int block;
+    if (!find_unit(a, blocks, u, block)) return;
+    const Place me(a.channels, CL, block);
     const Rows<T, WIDE> z(a.z, u.t0, me.c, me.valid), x(a.x, u.t0, me.c, me.valid);
+    const Out<T, WIDE> out(a.h, u.t0, a.channels, me.c, me.valid);
     const int64_t row = (int64_t)u.seq * a.channels + me.c, slot_row = u.slot * a.channels + me.c;
-    float carry[V], A[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) carry[i] = 0.0f, A[i] = 1.0f;
-    if (!SUMS) {
-        if (u.from > 0)
-            load_f32(a.starts + slot_row, me.valid, carry);
-        else if (a.state)
-            load_f32(a.state + row, me.valid, carry);
+    const bool last = me.slice == SLICES - 1;
+    float h[V] = {}, A[V] = {1.0f, 1.0f}, B[V] = {};
+    if (!SUMS && last) {
+        if (u.from > 0) {
+            load_f32(a.starts + slot_row, me.valid, h);
+            if (a.marks && u.from < u.to) store_f32(a.marks + mark_row(u, u.from) * a.channels + me.c, me.valid, h);
+        } else if (a.state) {
+            load_f32(a.state + row, me.valid, h);
+        }
+        lds.carry[0][me.lane] = pack(h);
     }
     Raw<T> rz[L], rx[L];
-    int64_t t = u.from + me.slice * L;
-    if (u.from < u.to) z.load(t, u.to, rz), x.load(t, u.to, rx);
+    if (u.from < u.to) {
+        z.load(u.from, u.to - u.from, me.slice, rz);
+        x.load(u.from, u.to - u.from, me.slice, rx);
+    }
     int parity = 0;
-    for (int64_t tile = u.from; tile < u.to; tile += kRecurrenceTile, t += kRecurrenceTile, parity ^= 1) {
+    for (int64_t tile = u.from; tile < u.to; tile += kRecurrenceTile, parity ^= 1) {
+        const int n = (int)min(u.to - tile, (int64_t)kRecurrenceTile), mine = n - me.slice * L;  // real tokens of the tile, of the slice
         float f[L][V], in[L][V], pa[V], pb[V];
+        auto sums = [&](auto whole) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) pa[i] = 1.0f, pb[i] = 0.0f;
-#pragma unroll
-        for (int l = 0; l < L; ++l) {
-            float vz[V], vx[V];
-            unpack(rz[l], vz);
-            unpack(rx[l], vx);
-            const bool real = t + l < u.to;
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                coefficients<SIG>(vz[i], vx[i], f[l][i], in[l][i]);
-                if (!real) f[l][i] = 1.0f, in[l][i] = 0.0f;
-                pa[i] *= f[l][i];
-                pb[i] = fmaf(f[l][i], pb[i], in[l][i]);
-            }
-        }
-        if (tile + kRecurrenceTile < u.to) z.load(t + kRecurrenceTile, u.to, rz), x.load(t + kRecurrenceTile, u.to, rx);
-#pragma unroll
-        for (int i = 0; i < V; ++i) mark_unusable(pa[i], pb[i]);
-        copy_in(&lds.v[parity][0][me.slice][me.lane * V], pa);
-        copy_in(&lds.v[parity][1][me.slice][me.lane * V], pb);
-        lds_barrier();
-        float h[V];
-        if constexpr (SUMS) {
-#pragma unroll
-            for (int s = 0; s < SLICES; ++s)
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float fs = lds.v[parity][0][s][me.lane * V + i];
-                    A[i] *= fs;
-                    carry[i] = fmaf(fs, carry[i], lds.v[parity][1][s][me.lane * V + i]);
-                    if (fabsf(carry[i]) > LARGE_STATE) A[i] = __builtin_nanf("");
-                }
-        } else {
-            float before[V];
-#pragma unroll
-            for (int i = 0; i < V; ++i) before[i] = carry[i];
-            if (join_slices<CL, false>(lds.v[parity][0], lds.v[parity][1], me.slice, me.lane, carry, h)) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) carry[i] = before[i];
-                walk_forward<T, SIG, WIDE>(z, x, tile, min(tile + kRecurrenceTile, u.to), t, carry, h);
-            }
-            if (a.marks && tile > 0 && me.slice == 0)
-                store_f32(a.marks + (u.t0 / kRecurrenceTile + tile / kRecurrenceTile) * a.channels + me.c, me.valid, before);
-            T* out = static_cast<T*>(a.h) + (u.t0 + t) * a.channels + me.c;
+            for (int i = 0; i < V; ++i) pa[i] = 1.0f, pb[i] = 0.0f;
 #pragma unroll
             for (int l = 0; l < L; ++l) {
+                float vz[V], vx[V];
+                unpack(rz[l], vz);
+                unpack(rx[l], vx);
 #pragma unroll
-                for (int i = 0; i < V; ++i) h[i] = fmaf(f[l][i], h[i], in[l][i]);
-                if (t + l < u.to && me.valid) store_vec<T, WIDE>(out + (int64_t)l * a.channels, me.valid, h);
+                for (int i = 0; i < V; ++i) {
+                    coefficients<T, SIG>(vz[i], vx[i], f[l][i], in[l][i]);
+                    if (!whole() && l >= mine) f[l][i] = 1.0f, in[l][i] = 0.0f;
+                    pa[i] *= f[l][i];
+                    pb[i] = fmaf(f[l][i], pb[i], in[l][i]);
+                }
+            }
+        };
+        if (n == kRecurrenceTile)
+            sums(std::true_type());
+        else
+            sums(std::false_type());
+        const int64_t next = tile + kRecurrenceTile;
+        if (next < u.to) {
+            z.load(next, u.to - next, me.slice, rz);
+            x.load(next, u.to - next, me.slice, rx);
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            mark_factor(pa[i], 4.0f);
+            mark_rest(pb[i]);
+        }
+        lds.sum[parity][0][me.slice][me.lane] = pack(pa);
+        lds.sum[parity][1][me.slice][me.lane] = pack(pb);
+        lds_barrier();
+        if constexpr (SUMS) {
+            if (last) {
+                float ta[V] = {1.0f, 1.0f}, tb[V] = {};
+                for (int s = 0; s < SLICES; ++s) {
+                    const float2 sa = lds.sum[parity][0][s][me.lane], sb = lds.sum[parity][1][s][me.lane];
+                    ta[0] *= sa.x, ta[1] *= sa.y;
+                    tb[0] = fmaf(sa.x, tb[0], sb.x), tb[1] = fmaf(sa.y, tb[1], sb.y);
+                }
+                add_tile(ta, tb, A, B);
+            }
+        } else {
+            const float2 carry = lds.carry[parity][me.lane];
+            h[0] = carry.x, h[1] = carry.y;
+            join_slices<CL, false>(lds.sum[parity][0], lds.sum[parity][1], me.slice, me.lane, h);
+            if (unsafe(carry.x, h[0]) || unsafe(carry.y, h[1])) {
+                h[0] = carry.x, h[1] = carry.y;
+                walk_forward<T, SIG, WIDE>(z, x, tile, min(tile + me.slice * L, u.to), h);
+            }
+            auto go = [&](auto whole) {
+#pragma unroll
+                for (int l = 0; l < L; ++l) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) h[i] = fmaf(f[l][i], h[i], in[l][i]);
+                    if (whole() || l < mine) out.store(tile, me.slice, l, h);
+                }
+            };
+            if (n == kRecurrenceTile)
+                go(std::true_type());
+            else
+                go(std::false_type());
+            if (last) {
+                lds.carry[parity ^ 1][me.lane] = pack(h);
+                if (a.marks && next < u.to) store_f32(a.marks + mark_row(u, next) * a.channels + me.c, me.valid, h);
             }
         }
     }
-    if (me.slice != 0) return;
+    if (!last) return;
     if constexpr (SUMS) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) mark_unusable(A[i], carry[i]);
         store_f32(a.sums + slot_row, me.valid, A);
-        store_f32(a.sums + a.seqs.slots * a.channels + slot_row, me.valid, carry);
+        store_f32(a.sums + a.seqs.slots * a.channels + slot_row, me.valid, B);
     } else if (a.final_state && u.to == u.len) {
-        store_f32(a.final_state + row, me.valid, carry);
+        store_f32(a.final_state + row, me.valid, h);
     }
 }
 
 // Backward pass. SUMS: only what the unit maps the adjoint behind it to.
 template <typename T, bool SIG, bool WIDE, int CL, bool SUMS>
 __global__ __launch_bounds__(threads_of<CL>()) void k_recurrence_bwd(RecurrenceArgs a, int blocks) {
-    __shared__ Sums<CL, 3> lds;
-    const int64_t index = block_index();
-    const int64_t slot = index / blocks;
+    __shared__ Shared<CL, 3> lds;
     Unit u;
-    if (slot >= a.seqs.slots || !unit_of(a.seqs, slot, u)) return;
-    const Place<T, CL> me(a, (int)(index - slot * blocks));
+    int block;
+    if (!find_unit(a, blocks, u, block)) return;
+    const Place me(a.channels, CL, block);
     const Rows<T, WIDE> z(a.z, u.t0, me.c, me.valid), x(a.x, u.t0, me.c, me.valid), g(a.dh, u.t0, me.c, me.valid);
+    const Out<T, WIDE> out_z(a.dz, u.t0, a.channels, me.c, me.valid), out_x(a.dx, u.t0, a.channels, me.c, me.valid);
     const int64_t row = (int64_t)u.seq * a.channels + me.c, slot_row = u.slot * a.channels + me.c;
-    float carry[V], A[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) carry[i] = 0.0f, A[i] = 1.0f;
-    if (!SUMS) {
+    const bool first = me.slice == 0;
+    float s[V] = {}, A[V] = {1.0f, 1.0f}, B[V] = {}, mark[V] = {};
+    if (!SUMS && first) {
         if (u.to < u.len)
-            load_f32(a.starts + slot_row, me.valid, carry);
+            load_f32(a.starts + slot_row, me.valid, s);
         else if (a.dfinal)
-            load_f32(a.dfinal + row, me.valid, carry);
+            load_f32(a.dfinal + row, me.valid, s);
+        lds.carry[0][me.lane] = pack(s);
     }
-    auto load_mark = [&](int64_t tile, float (&m)[V]) {
+    auto load_mark = [&](int64_t tile) {
         if (tile > 0)
-            load_f32(a.marks + (u.t0 / kRecurrenceTile + tile / kRecurrenceTile) * a.channels + me.c, me.valid, m);
+            load_f32(a.marks + mark_row(u, tile) * a.channels + me.c, me.valid, mark);
         else if (a.state)
-            load_f32(a.state + row, me.valid, m);
+            load_f32(a.state + row, me.valid, mark);
         else
-#pragma unroll
-            for (int i = 0; i < V; ++i) m[i] = 0.0f;
+            mark[0] = mark[1] = 0.0f;
     };
     Raw<T> rz[L], rx[L], rg[L];
-    float mark[V];
-    int64_t tile = u.from + (u.to - u.from - 1) / kRecurrenceTile * kRecurrenceTile, t = tile + me.slice * L;
-    if (u.from < u.to) {
-        z.load(t, u.to, rz);
-        g.load(t, u.to, rg);
-        if (!SUMS) x.load(t, u.to, rx), load_mark(tile, mark);
-    }
-    int parity = 0;
-    for (; u.from < u.to && tile >= u.from; tile -= kRecurrenceTile, t -= kRecurrenceTile, parity ^= 1) {
-        // d: h_(t-1)'s share of dz without h, f (1 - f) (or 1), then dz without G
-        float f[L][V], in[L][V], d[L][V], dy[L][V], pa[V], pb[V], pr[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) pa[i] = 1.0f, pb[i] = 0.0f, pr[i] = 0.0f;
-#pragma unroll
-        for (int l = 0; l < L; ++l) {
-            float vz[V], vx[V];
-            unpack(rz[l], vz);
-            unpack(rg[l], dy[l]);
-            if (!SUMS) unpack(rx[l], vx);
-            const bool real = t + l < u.to;
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                if constexpr (SIG) {
-                    sigmoids(vz[i], f[l][i], d[l][i]);  // d: 1 - f
-                    in[l][i] = SUMS ? 0.0f : vx[i];     // x
-                } else {
-                    f[l][i] = vz[i];
-                    in[l][i] = SUMS ? 0.0f : vx[i];
-                    d[l][i] = 1.0f;
-                }
-                if (!real) f[l][i] = 1.0f, in[l][i] = d[l][i] = dy[l][i] = 0.0f;
-                pa[i] *= f[l][i];
-                if (!SUMS) pb[i] = fmaf(f[l][i], pb[i], d[l][i] * in[l][i]);
-            }
+    auto load = [&](int64_t tile) {
+        z.load(tile, u.to - tile, me.slice, rz);
+        g.load(tile, u.to - tile, me.slice, rg);
+        if constexpr (!SUMS) {
+            x.load(tile, u.to - tile, me.slice, rx);
+            load_mark(tile);
         }
+    };
+    int64_t tile = u.from + max(u.to - u.from - 1, (int64_t)0) / kRecurrenceTile * kRecurrenceTile;
+    if (u.from < u.to) load(tile);
+    int parity = 0;
+    for (; u.from < u.to && tile >= u.from; tile -= kRecurrenceTile, parity ^= 1) {
+        const int n = (int)min(u.to - tile, (int64_t)kRecurrenceTile), mine = n - me.slice * L;
+        // rest: 1 - f (or 1); in: x, then dz without G
+        float f[L][V], in[L][V], rest[L][V], dy[L][V], pa[V], pb[V], pr[V];
+        auto sums = [&](auto whole) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) pa[i] = 1.0f, pb[i] = 0.0f, pr[i] = 0.0f;
+#pragma unroll
+            for (int l = 0; l < L; ++l) {
+                float vz[V];
+                unpack(rz[l], vz);
+                unpack(rg[l], dy[l]);
+                if constexpr (!SUMS) unpack(rx[l], in[l]);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    if constexpr (SIG) {
+                        sigmoids<sizeof(T) == 4>(vz[i], f[l][i], rest[l][i]);
+                    } else {
+                        f[l][i] = vz[i];
+                        rest[l][i] = 1.0f;
+                    }
+                    if (!whole() && l >= mine) f[l][i] = 1.0f, in[l][i] = rest[l][i] = dy[l][i] = 0.0f;
+                    pa[i] *= f[l][i];
+                    if constexpr (!SUMS) pb[i] = fmaf(f[l][i], pb[i], SIG || !whole() ? rest[l][i] * in[l][i] : in[l][i]);
+                }
+            }
+        };
+        if (n == kRecurrenceTile)
+            sums(std::true_type());
+        else
+            sums(std::false_type());
 #pragma unroll
         for (int l = L - 1; l >= 0; --l)
 #pragma unroll
             for (int i = 0; i < V; ++i) pr[i] = f[l][i] * (dy[l][i] + pr[i]);
-        float now[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) now[i] = SUMS ? 0.0f : mark[i];
-        if (tile > u.from) {
-            z.load(t - kRecurrenceTile, u.to, rz);
-            g.load(t - kRecurrenceTile, u.to, rg);
-            if (!SUMS) x.load(t - kRecurrenceTile, u.to, rx), load_mark(tile - kRecurrenceTile, mark);
-        }
+        const float from[V] = {mark[0], mark[1]};
+        if (tile > u.from) load(tile - kRecurrenceTile);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            float pa2 = pa[i];
-            mark_unusable(pa2, pr[i]);
-            if (!SUMS) mark_unusable(pa[i], pb[i]);
-            if (pa2 != pa2) pa[i] = pa2;
+            mark_factor(pa[i], 4.0f);
+            mark_rest(pb[i]);
+            mark_rest(pr[i]);
         }
-        copy_in(&lds.v[parity][0][me.slice][me.lane * V], pa);
-        if (!SUMS) copy_in(&lds.v[parity][1][me.slice][me.lane * V], pb);
-        copy_in(&lds.v[parity][2][me.slice][me.lane * V], pr);
+        lds.sum[parity][0][me.slice][me.lane] = pack(pa);
+        if constexpr (!SUMS) lds.sum[parity][1][me.slice][me.lane] = pack(pb);
+        lds.sum[parity][2][me.slice][me.lane] = pack(pr);
         lds_barrier();
         if constexpr (SUMS) {
-#pragma unroll
-            for (int s = SLICES - 1; s >= 0; --s)
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float fs = lds.v[parity][0][s][me.lane * V + i];
-                    A[i] *= fs;
-                    carry[i] = fmaf(fs, carry[i], lds.v[parity][2][s][me.lane * V + i]);
-                    if (fabsf(carry[i]) > LARGE_STATE) A[i] = __builtin_nanf("");
+            if (first) {
+                float ta[V] = {1.0f, 1.0f}, tb[V] = {};
+                for (int k = SLICES - 1; k >= 0; --k) {
+                    const float2 sa = lds.sum[parity][0][k][me.lane], sb = lds.sum[parity][2][k][me.lane];
+                    ta[0] *= sa.x, ta[1] *= sa.y;
+                    tb[0] = fmaf(sa.x, tb[0], sb.x), tb[1] = fmaf(sa.y, tb[1], sb.y);
                 }
+                add_tile(ta, tb, A, B);
+            }
         } else {
-            float h[V], s[V], before[V];
-#pragma unroll
-            for (int i = 0; i < V; ++i) before[i] = now[i];
-            const int64_t end = min(tile + kRecurrenceTile, u.to);
-            if (join_slices<CL, false>(lds.v[parity][0], lds.v[parity][1], me.slice, me.lane, now, h))
-                walk_forward<T, SIG, WIDE>(z, x, tile, end, t, before, h);
-#pragma unroll
-            for (int i = 0; i < V; ++i) before[i] = carry[i];
-            if (join_slices<CL, true>(lds.v[parity][0], lds.v[parity][2], me.slice, me.lane, carry, s)) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) carry[i] = s[i] = before[i];
-                walk_reverse<T, SIG, WIDE>(z, g, tile, end, min(t + L, end), carry, s);
+            float h[V] = {from[0], from[1]};
+            join_slices<CL, false>(lds.sum[parity][0], lds.sum[parity][1], me.slice, me.lane, h);
+            if (unsafe(from[0], h[0]) || unsafe(from[1], h[1])) {
+                h[0] = from[0], h[1] = from[1];
+                walk_forward<T, SIG, WIDE>(z, x, tile, min(tile + me.slice * L, u.to), h);
+            }
+            const float2 carry = lds.carry[parity][me.lane];
+            s[0] = carry.x, s[1] = carry.y;
+            join_slices<CL, true>(lds.sum[parity][0], lds.sum[parity][2], me.slice, me.lane, s);
+            if (unsafe(carry.x, s[0]) || unsafe(carry.y, s[1])) {
+                s[0] = carry.x, s[1] = carry.y;
+                walk_reverse<T, SIG, WIDE>(z, g, min(tile + (me.slice + 1) * L, tile + n), tile + n, s);
             }
 #pragma unroll
             for (int l = 0; l < L; ++l)
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const float rest = d[l][i], xv = in[l][i];
+                    const float xv = in[l][i];
                     if constexpr (SIG) {
-                        in[l][i] = (h[i] - xv) * f[l][i] * rest;
-                        h[i] = fmaf(f[l][i], h[i], rest * xv);
+                        in[l][i] = (h[i] - xv) * (f[l][i] * rest[l][i]);
+                        h[i] = fmaf(f[l][i], h[i], rest[l][i] * xv);
                     } else {
                         in[l][i] = h[i];
                         h[i] = fmaf(f[l][i], h[i], xv);
                     }
                 }
-            const int64_t first = (u.t0 + t) * a.channels + me.c;
+            auto go = [&](auto whole) {
 #pragma unroll
-            for (int l = L - 1; l >= 0; --l) {
-                float oz[V], ox[V];
+                for (int l = L - 1; l >= 0; --l) {
+                    float oz[V], ox[V];
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float G = dy[l][i] + s[i];
-                    oz[i] = G * in[l][i];
-                    ox[i] = G * d[l][i];
-                    s[i] = f[l][i] * G;
+                    for (int i = 0; i < V; ++i) {
+                        const float G = dy[l][i] + s[i];
+                        oz[i] = G * in[l][i];
+                        ox[i] = SIG ? G * rest[l][i] : G;
+                        s[i] = f[l][i] * G;
+                    }
+                    if (whole() || l < mine) {
+                        out_z.store(tile, me.slice, l, oz);
+                        out_x.store(tile, me.slice, l, ox);
+                    }
                 }
-                if (t + l < u.to && me.valid) {
-                    store_vec<T, WIDE>(static_cast<T*>(a.dz) + first + (int64_t)l * a.channels, me.valid, oz);
-                    store_vec<T, WIDE>(static_cast<T*>(a.dx) + first + (int64_t)l * a.channels, me.valid, ox);
-                }
-            }
+            };
+            if (n == kRecurrenceTile)
+                go(std::true_type());
+            else
+                go(std::false_type());
+            if (first) lds.carry[parity ^ 1][me.lane] = pack(s);
         }
     }
-    if (me.slice != 0) return;
+    if (!first) return;
     if constexpr (SUMS) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) mark_unusable(A[i], carry[i]);
         store_f32(a.sums + slot_row, me.valid, A);
-        store_f32(a.sums + a.seqs.slots * a.channels + slot_row, me.valid, carry);
+        store_f32(a.sums + a.seqs.slots * a.channels + slot_row, me.valid, B);
     } else if (a.dstate && u.from == 0) {
-        store_f32(a.dstate + row, me.valid, carry);
+        store_f32(a.dstate + row, me.valid, s);
     }
 }
 
@@ -508,13 +599,13 @@ __global__ __launch_bounds__(64) void k_recurrence_join(RecurrenceArgs a, int bl
             const int64_t k = k0 + i, j = REVERSE ? count - 1 - k : k;
             if (k + 1 >= count) break;  // nothing starts behind the last one
             const float next = fmaf(A[i], h, B[i]);
-            if (h == h && (next != next || fabsf(h) > LARGE_STATE)) {
+            if (unsafe(h, next)) {
                 const int64_t lo = j * a.seqs.seg, hi = min(u.len, lo + a.seqs.seg);
                 for (int64_t s = lo; s < hi; ++s) {
                     const int64_t t = REVERSE ? lo + hi - 1 - s : s;
                     float f, in;
                     const float v = St<T>::ld1(x + t * other.stride);
-                    coefficients<SIG>(St<T>::ld1(z + t * a.z.stride), v, f, in);
+                    coefficients<T, SIG>(St<T>::ld1(z + t * a.z.stride), v, f, in);
                     h = REVERSE ? f * (v + h) : fmaf(f, h, in);
                 }
             } else {
@@ -555,7 +646,7 @@ __global__ __launch_bounds__(256) void k_advance(AdvanceArgs a, int vecs) {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             float f, u;
-            coefficients<SIG>(z[j], x[j], f, u);
+            coefficients<T, SIG>(z[j], x[j], f, u);
             h[j] = fmaf(f, h[j], u);
             o[j] = h[j];
         }

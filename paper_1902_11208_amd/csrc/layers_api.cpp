@@ -32,6 +32,14 @@ mdlstm_status check_recurrence(const mdlstm_recurrence_desc* d) {
     return MDLSTM_OK;
 }
 
+// Rows whose distance within a tile of tokens stays within 32 bits of bytes.
+mdlstm_status check_token_rows(const void* p, const char* name, int64_t tokens, int64_t cols, int64_t stride, int32_t dtype) {
+    OK_OR_RETURN(check_rows(p, name, tokens, cols, stride, dtype));
+    if (tokens > 1 && stride > (int64_t)1 << 22)
+        return fail(MDLSTM_ERR_UNSUPPORTED, "rows of %s are %lld elements apart: at most 2^22", name, (long long)stride);
+    return MDLSTM_OK;
+}
+
 mdl::RecurrenceArgs recurrence_args(const mdlstm_recurrence_desc* d, const mdl::Packed& seqs, bool backward) {
     mdl::RecurrenceArgs a{};
     a.seqs = seqs;
@@ -115,8 +123,8 @@ mdlstm_status mdlstm_recurrence_forward(const mdlstm_recurrence_desc* desc, int3
     OK_OR_RETURN(check_recurrence(desc));
     OK_OR_RETURN(check_sequences(n, tokens, longest));
     const int64_t cols = desc->channels, es = (int64_t)element(desc->dtype);
-    OK_OR_RETURN(check_rows(d_z, "z", tokens, cols, z_stride, desc->dtype));
-    OK_OR_RETURN(check_rows(d_x, "x", tokens, cols, x_stride, desc->dtype));
+    OK_OR_RETURN(check_token_rows(d_z, "z", tokens, cols, z_stride, desc->dtype));
+    OK_OR_RETURN(check_token_rows(d_x, "x", tokens, cols, x_stride, desc->dtype));
     OK_OR_RETURN(check_out(d_offsets, "offsets", n > 0, 8));
     OK_OR_RETURN(check_out(d_order, "order", false, 4));
     OK_OR_RETURN(check_out(d_state, "state", false, 4));
@@ -154,9 +162,9 @@ mdlstm_status mdlstm_recurrence_backward(const mdlstm_recurrence_desc* desc, int
     OK_OR_RETURN(check_recurrence(desc));
     OK_OR_RETURN(check_sequences(n, tokens, longest));
     const int64_t cols = desc->channels, es = (int64_t)element(desc->dtype);
-    OK_OR_RETURN(check_rows(d_z, "z", tokens, cols, z_stride, desc->dtype));
-    OK_OR_RETURN(check_rows(d_x, "x", tokens, cols, x_stride, desc->dtype));
-    OK_OR_RETURN(check_rows(d_dh, "dh", tokens, cols, dh_stride, desc->dtype));
+    OK_OR_RETURN(check_token_rows(d_z, "z", tokens, cols, z_stride, desc->dtype));
+    OK_OR_RETURN(check_token_rows(d_x, "x", tokens, cols, x_stride, desc->dtype));
+    OK_OR_RETURN(check_token_rows(d_dh, "dh", tokens, cols, dh_stride, desc->dtype));
     OK_OR_RETURN(check_out(d_offsets, "offsets", n > 0, 8));
     OK_OR_RETURN(check_out(d_order, "order", false, 4));
     OK_OR_RETURN(check_out(d_state, "state", false, 4));
