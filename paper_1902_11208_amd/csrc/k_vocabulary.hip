@@ -20,6 +20,7 @@
 // kept. In bf16, q is rounded once to a matrix operand: a relative 2^-9 of each
 // of many terms beside the exact target.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.hpp"
 #include "sequence.hpp"
@@ -78,13 +79,9 @@ struct Shape {
     static_assert(BM / 8 % WAVES == 0 && BN / 8 % WAVES == 0, "whole loads of a wave");
 };
 
-// Which pieces a pair multiplies, the smallest products first.
-__device__ __forceinline__ void pair_of(int pairs, int k, int& a, int& b) {
-    a = b = 0;
-    if (pairs == 1) return;
-    a = k == 0 ? 2 : k == 2 || k == 4 ? 1 : 0;  // (2,0) (0,2) (1,1) (0,1) (1,0) (0,0)
-    b = k == 1 ? 2 : k == 2 || k == 3 ? 1 : 0;
-}
+// Which pieces a pair of them multiplies, two bits each, the smallest products first:
+// (2, 0) (0, 2) (1, 1) (0, 1) (1, 0) (0, 0).
+constexpr uint32_t PIECES_A = 2 | 0 << 2 | 1 << 4 | 0 << 6 | 1 << 8, PIECES_B = 0 | 2 << 2 | 1 << 4 | 1 << 6 | 0 << 8;
 
 typedef __amdgpu_buffer_rsrc_t Buffer;
 __device__ __forceinline__ Buffer buffer_at(const void* p) {
@@ -114,7 +111,7 @@ struct Loader {
         }
     }
     __device__ __forceinline__ void load(Tile<S>& t, Buffer a, Buffer b) const {
-        const int wave = threadIdx.x / 64;
+        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
 #pragma unroll
         for (int i = 0; i < S::LOADS; ++i) {
             const bool is_a = i < S::A_LOADS;
@@ -126,24 +123,40 @@ struct Loader {
     }
 };
 
-template <class S>
-__device__ __forceinline__ void multiply(const Tile<S>& t, floatx4 (&acc)[S::MI][S::NI]) {
-    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, wm = wave / (S::BN / S::WN), wn = wave % (S::BN / S::WN);
-    const int row = lane & 15;
+// Operands of half a step (32 summed elements) from a tile: N sixteens of rows from the wave's `first`.
+template <int N>
+__device__ __forceinline__ void read_rows(const bf16_t* tile, int first, int half, bf16x8 (&v)[N]) {
+    const int lane = threadIdx.x & 63, row = lane & 15, chunk = ((lane / 16 + half * 4) ^ (row & 7)) * 8;
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const int chunk = ((lane / 16 + half * 4) ^ (row & 7)) * 8;
-        bf16x8 a[S::MI], b[S::NI];
+    for (int i = 0; i < N; ++i) v[i] = *reinterpret_cast<const bf16x8*>(tile + (first + i * 16 + row) * BK + chunk);
+}
+
+// Everything this wave asked of memory and LDS has come (vmcnt and lgkmcnt 0).
+__device__ __forceinline__ void all_arrived() { __builtin_amdgcn_s_waitcnt(0x0070); }
+
+// READS reads of LDS spread among PRODUCTS products, and nothing moved across.
+template <int READS, int PRODUCTS>
+__device__ __forceinline__ void interleave() {
 #pragma unroll
-        for (int i = 0; i < S::MI; ++i) a[i] = *reinterpret_cast<const bf16x8*>(t.a + (wm * S::WM + i * 16 + row) * BK + chunk);
-#pragma unroll
-        for (int j = 0; j < S::NI; ++j) b[j] = *reinterpret_cast<const bf16x8*>(t.b + (wn * S::WN + j * 16 + row) * BK + chunk);
-#pragma unroll
-        for (int i = 0; i < S::MI; ++i)
-#pragma unroll
-            for (int j = 0; j < S::NI; ++j) acc[i][j] = mfma_bf16(a[i], b[j], acc[i][j]);
-        __builtin_amdgcn_sched_barrier(0);  // both halves' operands at once do not fit the registers
+    for (int i = 0; i < READS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                  // a read of LDS
+        __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS / READS, 0);  // products
     }
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// over the sixteen lanes of a row of a matrix result
+template <bool MAX>
+__device__ __forceinline__ float over16(float v) {
+    auto with = [&](auto turn) {
+        const float o = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), turn(), 0xf, 0xf, false));
+        v = MAX ? fmaxf(v, o) : v + o;
+    };
+    with(std::integral_constant<int, 0x128>());
+    with(std::integral_constant<int, 0x124>());
+    with(std::integral_constant<int, 0x122>());
+    with(std::integral_constant<int, 0x121>());
+    return v;
 }
 
 // Tiles in an order that keeps those of an XCD (workgroups 8 apart) near each
@@ -157,6 +170,81 @@ __device__ __forceinline__ void place(const Product& g, int index, int& tm, int&
 }
 
 __device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * LOG2E); }
+
+// (maximum, sum of exp(l - maximum)) of two sets of columns together.
+__device__ __forceinline__ float2 join_sums(float2 s, float2 n) {
+    const float top = fmaxf(s.x, n.x), base = top == -__builtin_huge_valf() ? 0.0f : top;
+    return make_float2(top, s.y * exp_of(s.x - base) + n.y * exp_of(n.x - base));
+}
+
+// Piece k of a number.
+__device__ __forceinline__ float piece(float v, int k) {
+    for (int i = 0; i < k; ++i) v -= bf2f(f2bf(v));
+    return v;
+}
+
+// A tile's q as rows, and c q as columns, through LDS, so that whole lines leave.
+// A half of the tile lies in each of two buffers, in rows of whole 16-byte chunks that
+// are exchanged by the row's index, so that the lanes of a write meet different banks.
+template <class S>
+__device__ __forceinline__ void store_rows(const Product& g, bf16_t* b0, bf16_t* b1, const floatx4 (&acc)[S::MI][S::NI], int k, int64_t m0,
+                                           int64_t n0) {
+    constexpr int ROW = S::BN / 2, CHUNKS = S::BN / 8;
+    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, wm = wave / (S::BN / S::WN), wn = wave % (S::BN / S::WN);
+    const int quad = lane / 16, col = lane & 15;
+    bf16_t* to = wn * S::WN < ROW ? b0 : b1;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+        for (int j = 0; j < S::NI; ++j) {
+            const int n = wn * S::WN % ROW + j * 16 + col, m = wm * S::WM + i * 16 + quad * 4;
+            bf16_t* at = to + m * ROW + ((n / 8) ^ (quad << 1)) * 8 + n % 8;
+#pragma unroll
+            for (int r = 0; r < 4; r += 2) {
+                const uint32_t two = f2bf2(piece(acc[i][j][r], k), piece(acc[i][j][r + 1], k));
+                at[r * ROW] = (bf16_t)two;
+                at[(r + 1) * ROW] = (bf16_t)(two >> 16);
+            }
+        }
+    __syncthreads();
+    bf16_t* q = g.q + k * g.q_plane;
+    for (int x = threadIdx.x; x < S::BM * CHUNKS; x += S::THREADS) {
+        const int m = x / CHUNKS, c = x % CHUNKS;
+        const bf16_t* from = (c < CHUNKS / 2 ? b0 : b1) + m * ROW + ((c % (CHUNKS / 2)) ^ ((m / 4 & 3) << 1)) * 8;
+        const u32x4 v = *reinterpret_cast<const u32x4*>(from);
+        if (m0 + m < g.a.rows && n0 + c * 8 < g.ldq) *reinterpret_cast<u32x4*>(q + (m0 + m) * g.ldq + n0 + c * 8) = v;
+    }
+}
+
+template <class S>
+__device__ __forceinline__ void store_columns(const Product& g, bf16_t* b0, bf16_t* b1, const floatx4 (&acc)[S::MI][S::NI],
+                                              const float (&scale)[S::MI][4], int k, int64_t m0, int64_t n0) {
+    constexpr int ROW = S::BM, CHUNKS = S::BM / 8, HALF = S::BN / 2, MASK = S::BM / 16 - 1;
+    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, wm = wave / (S::BN / S::WN), wn = wave % (S::BN / S::WN);
+    const int quad = lane / 16, col = lane & 15;
+    bf16_t* to = wn * S::WN < HALF ? b0 : b1;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+        for (int j = 0; j < S::NI; ++j) {
+            const int n = wn * S::WN % HALF + j * 16 + col, m = wm * S::WM + i * 16 + quad * 4;
+            uint32_t two[2];
+#pragma unroll
+            for (int r = 0; r < 4; r += 2)
+                two[r / 2] = f2bf2(piece(acc[i][j][r] * scale[i][r], k), piece(acc[i][j][r + 1] * scale[i][r + 1], k));
+            *reinterpret_cast<uint2*>(to + n * ROW + ((m / 8) ^ ((n & MASK) << 1)) * 8 + m % 8) = make_uint2(two[0], two[1]);
+        }
+    __syncthreads();
+    bf16_t* qt = g.qt + k * g.qt_plane;
+    for (int x = threadIdx.x; x < S::BN * CHUNKS; x += S::THREADS) {
+        const int n = x / CHUNKS, c = x % CHUNKS;
+        const bf16_t* from = (n < HALF ? b0 : b1) + n % HALF * ROW + (c ^ ((n & MASK) << 1)) * 8;
+        const u32x4 v = *reinterpret_cast<const u32x4*>(from);
+        if (n0 + n < g.b.rows && m0 + c * 8 < g.ldt) *reinterpret_cast<u32x4*>(qt + (n0 + n) * g.ldt + m0 + c * 8) = v;
+    }
+}
 
 template <class S, int WHAT, int PIECES>
 __global__ __launch_bounds__(S::THREADS) void k_product(Product g) {
@@ -172,30 +260,68 @@ __global__ __launch_bounds__(S::THREADS) void k_product(Product g) {
               to = __builtin_amdgcn_readfirstlane((int)((int64_t)all * (split + 1) / g.splits));
     const Loader<S> load(g, m0, n0);
     const bf16_t *pa = g.a.p + m0 * g.a.ld, *pb = g.b.p + n0 * g.b.ld;
-    int pair = __builtin_amdgcn_readfirstlane(g.steps ? from / g.steps : 0), step = from - pair * g.steps;  // of the next fetch
-    auto fetch = [&](Tile<S>& t) {
-        int a, b;
-        pair_of(g.pairs, pair, a, b);
-        load.load(t, buffer_at(pa + a * g.a.plane + (int64_t)step * BK), buffer_at(pb + b * g.b.plane + (int64_t)step * BK));
-        if (++step == g.steps) step = 0, ++pair;
+    int pair = __builtin_amdgcn_readfirstlane(g.steps ? from / g.steps : 0), step = from - pair * g.steps, left = to - from;  // of the next fetch
+    const uint32_t pieces_a = g.pairs == 1 ? 0 : PIECES_A, pieces_b = g.pairs == 1 ? 0 : PIECES_B;
+    auto fetch = [&](Tile<S>& t) {  // behind the last step: that one again
+        const int64_t a = (pieces_a >> 2 * pair & 3) * g.a.plane, b = (pieces_b >> 2 * pair & 3) * g.b.plane;
+        load.load(t, buffer_at(pa + a + (int64_t)step * BK), buffer_at(pb + b + (int64_t)step * BK));
+        const int more = --left > 0, wrap = more & (step + 1 == g.steps);
+        pair += wrap;
+        step = wrap ? 0 : step + more;
     };
     floatx4 acc[S::MI][S::NI];
 #pragma unroll
     for (int i = 0; i < S::MI; ++i)
 #pragma unroll
         for (int j = 0; j < S::NI; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-    int k = from;
-    if (k < to) fetch(t0);
-    __syncthreads();
-    for (; k + 2 <= to; k += 2) {
+    // A step's tile is asked for a whole step before it is read, and a quarter step's
+    // operands are read while the quarter before multiplies. Before the last quarter,
+    // one barrier: the next tile has arrived, and all waves have read this one, whose
+    // place the tile after the next takes.
+    constexpr int MH = S::MI / 2, NI = S::NI;
+    const int wm0 = threadIdx.x / 64 / (S::BN / S::WN) * S::WM, wn0 = threadIdx.x / 64 % (S::BN / S::WN) * S::WN;
+    bf16x8 a0[MH], a1[MH], b0[NI], b1[NI];
+    auto multiply = [&](const bf16x8(&a)[MH], const bf16x8(&b)[NI], auto high) {
+#pragma unroll
+        for (int i = 0; i < MH; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) acc[high() * MH + i][j] = mfma_bf16(a[i], b[j], acc[high() * MH + i][j]);
+    };
+    const std::integral_constant<int, 0> low;
+    const std::integral_constant<int, 1> high;
+    auto one = [&](Tile<S>& now, Tile<S>& next) {
+        read_rows(now.a, wm0 + MH * 16, 0, a1);
+        multiply(a0, b0, low);
+        interleave<MH, MH * NI>();
+        read_rows(now.a, wm0 + MH * 16, 1, a0);
+        read_rows(now.b, wn0, 1, b1);
+        multiply(a1, b0, high);
+        interleave<MH + NI, MH * NI>();
+        read_rows(now.a, wm0, 1, a1);
+        multiply(a0, b1, high);
+        interleave<MH, MH * NI>();
+        all_arrived();
+        __builtin_amdgcn_s_barrier();
+        fetch(now);
+        read_rows(next.a, wm0, 0, a0);
+        read_rows(next.b, wn0, 0, b0);
+        multiply(a1, b1, low);
+        interleave<MH + NI, MH * NI>();
+    };
+    if (from < to) {
+        fetch(t0);
+        all_arrived();
+        __builtin_amdgcn_s_barrier();
         fetch(t1);
-        multiply<S>(t0, acc);
-        __syncthreads();  // t1 has arrived, t0 has been read
-        if (k + 2 < to) fetch(t0);
-        multiply<S>(t1, acc);
-        __syncthreads();
+        read_rows(t0.a, wm0, 0, a0);
+        read_rows(t0.b, wn0, 0, b0);
+        int k = from;
+        for (; k + 2 <= to; k += 2) {
+            one(t0, t1);
+            one(t1, t0);
+        }
+        if (k < to) one(t0, t1);
     }
-    if (k < to) multiply<S>(t0, acc);
     __syncthreads();
     const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, wm = wave / (S::BN / S::WN), wn = wave % (S::BN / S::WN);
     const int quad = lane / 16, col = lane & 15;
@@ -238,13 +364,11 @@ __global__ __launch_bounds__(S::THREADS) void k_product(Product g) {
                     if (n == t || n0 + n >= cols) v[j] = -__builtin_huge_valf();
                     top = fmaxf(top, v[j]);
                 }
-#pragma unroll
-                for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+                top = over16<true>(top);
                 const float base = top == -__builtin_huge_valf() ? 0.0f : top;
 #pragma unroll
                 for (int j = 0; j < S::NI; ++j) sum += exp_of(v[j] - base);
-#pragma unroll
-                for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+                sum = over16<false>(sum);
                 if (col == 0) sums[wn * S::BM + row] = make_float2(top, sum);
             }
         __syncthreads();
@@ -253,9 +377,7 @@ __global__ __launch_bounds__(S::THREADS) void k_product(Product g) {
             float2 s = sums[r];
 #pragma unroll
             for (int w = 1; w < S::BN / S::WN; ++w) {
-                const float2 n = sums[w * S::BM + r];
-                const float top = fmaxf(s.x, n.x), base = top == -__builtin_huge_valf() ? 0.0f : top;
-                s = make_float2(top, s.y * exp_of(s.x - base) + n.y * exp_of(n.x - base));
+                s = join_sums(s, sums[w * S::BM + r]);
             }
             g.part[(int64_t)tn * rows + m0 + r] = s;
         }
@@ -266,54 +388,51 @@ __global__ __launch_bounds__(S::THREADS) void k_product(Product g) {
             if (m0 + r >= rows) info[r].target = -1;
         }
         __syncthreads();
+        // q into the accumulators' place
 #pragma unroll
         for (int i = 0; i < S::MI; ++i)
 #pragma unroll
-            for (int j = 0; j < S::NI; ++j) {
-                const int64_t n = n0 + wn * S::WN + j * 16 + col, m = m0 + wm * S::WM + i * 16 + quad * 4;
-                float v[4], c[4];
+            for (int r = 0; r < 4; ++r) {
+                const RowInfo f = info[wm * S::WM + i * 16 + quad * 4 + r];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const RowInfo f = info[wm * S::WM + i * 16 + quad * 4 + r];
-                    float e = f.target == g.first + n ? -1.0f : exp_of(acc[i][j][r] - f.others);
-                    if (f.target < 0 || n >= cols) e = 0.0f;
-                    v[r] = e;
-                    c[r] = f.target < 0 || n >= cols ? 0.0f : e * f.scale;
-                }
-#pragma unroll
-                for (int k = 0; k < PIECES; ++k) {
-                    const uint32_t v01 = f2bf2(v[0], v[1]), v23 = f2bf2(v[2], v[3]), c01 = f2bf2(c[0], c[1]), c23 = f2bf2(c[2], c[3]);
-                    if (n < g.ldq) {
-                        bf16_t* p = g.q + k * g.q_plane + m * g.ldq + n;
-                        if (m < rows) p[0] = (bf16_t)v01;
-                        if (m + 1 < rows) p[g.ldq] = (bf16_t)(v01 >> 16);
-                        if (m + 2 < rows) p[2 * g.ldq] = (bf16_t)v23;
-                        if (m + 3 < rows) p[3 * g.ldq] = (bf16_t)(v23 >> 16);
-                    }
-                    if (n < cols && m < g.ldt) *reinterpret_cast<uint2*>(g.qt + k * g.qt_plane + n * g.ldt + m) = make_uint2(c01, c23);
-                    v[0] -= __uint_as_float(v01 << 16);
-                    v[1] -= __uint_as_float(v01 & 0xffff0000u);
-                    v[2] -= __uint_as_float(v23 << 16);
-                    v[3] -= __uint_as_float(v23 & 0xffff0000u);
-                    c[0] -= __uint_as_float(c01 << 16);
-                    c[1] -= __uint_as_float(c01 & 0xffff0000u);
-                    c[2] -= __uint_as_float(c23 << 16);
-                    c[3] -= __uint_as_float(c23 & 0xffff0000u);
+                for (int j = 0; j < S::NI; ++j) {
+                    const int64_t n = n0 + wn * S::WN + j * 16 + col;
+                    const float e = f.target == g.first + n ? -1.0f : exp_of(acc[i][j][r] - f.others);
+                    acc[i][j][r] = f.target < 0 || n >= cols ? 0.0f : e;
                 }
             }
+        float scale[S::MI][4];
+#pragma unroll
+        for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const RowInfo f = info[wm * S::WM + i * 16 + quad * 4 + r];
+                scale[i][r] = f.target < 0 ? 0.0f : f.scale;
+            }
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            store_rows<S>(g, t0.a, t1.a, acc, k, m0, n0);
+            store_columns<S>(g, t0.a, t1.a, acc, scale, k, m0, n0);
+        }
     }
 }
 
-// A row's parts together, in order: o, the target's logit and the loss.
-__global__ __launch_bounds__(256) void k_losses(VocabularyArgs a, const float2* part, int64_t parts) {
-    const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (r >= a.rows) return;
+// A row's parts together: o, the target's logit and the loss. Sixteen rows a
+// workgroup, 64 slices of the parts, joined in a fixed order.
+__global__ __launch_bounds__(1024) void k_losses(VocabularyArgs a, const float2* part, int64_t parts) {
+    __shared__ float2 lds[64][16];
+    const int in = threadIdx.x % 16, slice = threadIdx.x / 16;
+    const int64_t r = (int64_t)blockIdx.x * 16 + in;
     float2 s = make_float2(-__builtin_huge_valf(), 0.0f);
-    for (int64_t k = 0; k < parts; ++k) {
-        const float2 n = part[k * a.rows + r];
-        const float top = fmaxf(s.x, n.x), base = top == -__builtin_huge_valf() ? 0.0f : top;
-        s = make_float2(top, s.y * exp_of(s.x - base) + n.y * exp_of(n.x - base));
+    if (r < a.rows)
+        for (int64_t k = slice; k < parts; k += 64) s = join_sums(s, part[k * a.rows + r]);
+    lds[slice][in] = s;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        __syncthreads();
+        if (slice < o) lds[slice][in] = s = join_sums(s, lds[slice + o][in]);
     }
+    if (slice != 0 || r >= a.rows) return;
     const int64_t t = a.targets[r];
     const bool counts = t >= 0 && t < a.vocab;
     const float others = s.x + logf(s.y);  // no others: -infinity
@@ -414,7 +533,7 @@ auto with_shape(int64_t m, int64_t n, F&& f) {
 int splits_of(int64_t m, int64_t n, int64_t steps) {
     return with_shape(m, n, [&](auto shape) {
         typedef decltype(shape) S;
-        const int64_t tiles = std::max<int64_t>(1, (m + S::BM - 1) / S::BM * ((n + S::BN - 1) / S::BN)), want = S::THREADS == 512 ? 256 : 512;
+        const int64_t tiles = std::max<int64_t>(1, (m + S::BM - 1) / S::BM * ((n + S::BN - 1) / S::BN)), want = S::BM == 256 ? 256 : 512;
         return (int)std::max<int64_t>(1, std::min<int64_t>(want / tiles, steps / 8));
     });
 }
@@ -553,7 +672,7 @@ hipError_t forward(const VocabularyArgs& a, hipStream_t s) {
         const int64_t tile = column_tile(a.rows, n);
         parts += (n + tile - 1) / tile;
     }
-    k_losses<<<(unsigned)((a.rows + 255) / 256), 256, 0, s>>>(a, part, parts);
+    k_losses<<<(unsigned)((a.rows + 15) / 16), 1024, 0, s>>>(a, part, parts);
     return hipGetLastError();
 }
 
