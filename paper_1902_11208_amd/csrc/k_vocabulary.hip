@@ -42,7 +42,7 @@ struct Operand {
 
 // What of a row the epilogues need.
 struct RowInfo {
-    float others, scale;  // o and c
+    float others, scale;  // o log2(e) and c
     int target;           // -1: the row is left out
     int pad;
 };
@@ -57,7 +57,7 @@ struct Product {
     int tiles_m, tiles_n;
     // LOGSUM
     const int64_t* targets;
-    float2* part;       // [tiles_n][a.rows] maximum and sum of exp(l - maximum) of the tile's columns but the target
+    float2* part;       // [tiles_n][a.rows] of the tile's columns but the target (join_sums)
     float* logit;       // [a.rows] the target's logit
     int64_t first;      // vocabulary index of b's first row
     // GRADIENT
@@ -169,12 +169,15 @@ __device__ __forceinline__ void place(const Product& g, int index, int& tm, int&
     tn = in / high;
 }
 
-__device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * LOG2E); }
+__device__ __forceinline__ float exp2_of(float v) { return __builtin_amdgcn_exp2f(v); }
 
-// (maximum, sum of exp(l - maximum)) of two sets of columns together.
+// Sums of exponentials as (m, sum of 2^(l log2(e) - m)), m the rounded product of
+// the largest l with log2(e): the same m is taken from every term, so its rounding does
+// not matter. No columns: (-infinity, 0).
+__device__ __forceinline__ float finite_or_0(float m) { return m == -__builtin_huge_valf() ? 0.0f : m; }
 __device__ __forceinline__ float2 join_sums(float2 s, float2 n) {
-    const float top = fmaxf(s.x, n.x), base = top == -__builtin_huge_valf() ? 0.0f : top;
-    return make_float2(top, s.y * exp_of(s.x - base) + n.y * exp_of(n.x - base));
+    const float top = fmaxf(s.x, n.x), base = finite_or_0(top);
+    return make_float2(top, s.y * exp2_of(s.x - base) + n.y * exp2_of(n.x - base));
 }
 
 // Piece k of a number.
@@ -347,27 +350,32 @@ __global__ __launch_bounds__(S::THREADS) void k_product(Product g) {
         float2* sums = reinterpret_cast<float2*>(t1.a);  // [BN / WN][BM]
         for (int r = threadIdx.x; r < S::BM; r += S::THREADS) {
             const int64_t t = m0 + r < rows ? g.targets[m0 + r] - g.first - n0 : -1;
-            target[r] = t >= 0 && t < S::BN && t < cols - n0 ? (int)t : -1;
+            target[r] = t >= 0 && t < S::BN && t < cols - n0 ? (int)t : -(1 << 20);
         }
         __syncthreads();
+        const bool ragged = n0 + S::BN > cols;
 #pragma unroll
         for (int i = 0; i < S::MI; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int row = wm * S::WM + i * 16 + quad * 4 + r, t = target[row];
+                const int row = wm * S::WM + i * 16 + quad * 4 + r, t = target[row] - wn * S::WN - col;
                 float v[S::NI], top = -__builtin_huge_valf(), sum = 0.0f;
 #pragma unroll
-                for (int j = 0; j < S::NI; ++j) {
-                    const int n = wn * S::WN + j * 16 + col;
-                    v[j] = acc[i][j][r];
-                    if (n == t) g.logit[m0 + row] = v[j];
-                    if (n == t || n0 + n >= cols) v[j] = -__builtin_huge_valf();
-                    top = fmaxf(top, v[j]);
-                }
-                top = over16<true>(top);
-                const float base = top == -__builtin_huge_valf() ? 0.0f : top;
+                for (int j = 0; j < S::NI; ++j) v[j] = acc[i][j][r];
+                // rows whose target is in the wave's columns, and columns behind the last, are rare
+                if (ragged || __any(t > -16 && t < S::WN)) {
 #pragma unroll
-                for (int j = 0; j < S::NI; ++j) sum += exp_of(v[j] - base);
+                    for (int j = 0; j < S::NI; ++j) {
+                        if (t == j * 16) g.logit[m0 + row] = v[j];
+                        if (t == j * 16 || n0 + wn * S::WN + j * 16 + col >= cols) v[j] = -__builtin_huge_valf();
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < S::NI; ++j) top = fmaxf(top, v[j]);
+                top = over16<true>(top) * LOG2E;
+                const float base = finite_or_0(top);
+#pragma unroll
+                for (int j = 0; j < S::NI; ++j) sum += exp2_of(fmaf(v[j], LOG2E, -base));
                 sum = over16<false>(sum);
                 if (col == 0) sums[wn * S::BM + row] = make_float2(top, sum);
             }
@@ -389,16 +397,21 @@ __global__ __launch_bounds__(S::THREADS) void k_product(Product g) {
         }
         __syncthreads();
         // q into the accumulators' place
+        const bool ragged = n0 + S::BN > cols;
 #pragma unroll
         for (int i = 0; i < S::MI; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const RowInfo f = info[wm * S::WM + i * 16 + quad * 4 + r];
+                const int t = f.target < 0 ? -(1 << 20) : (int)min(max(f.target - g.first - n0 - wn * S::WN - col, (int64_t)-1024), (int64_t)1024);
 #pragma unroll
-                for (int j = 0; j < S::NI; ++j) {
-                    const int64_t n = n0 + wn * S::WN + j * 16 + col;
-                    const float e = f.target == g.first + n ? -1.0f : exp_of(acc[i][j][r] - f.others);
-                    acc[i][j][r] = f.target < 0 || n >= cols ? 0.0f : e;
+                for (int j = 0; j < S::NI; ++j) acc[i][j][r] = exp2_of(fmaf(acc[i][j][r], LOG2E, -f.others));
+                if (ragged || __any(t == -(1 << 20) || (t > -16 && t < S::WN))) {
+#pragma unroll
+                    for (int j = 0; j < S::NI; ++j) {
+                        if (t == j * 16) acc[i][j][r] = -1.0f;
+                        if (t == -(1 << 20) || n0 + wn * S::WN + j * 16 + col >= cols) acc[i][j][r] = 0.0f;
+                    }
                 }
             }
         float scale[S::MI][4];
@@ -416,6 +429,9 @@ __global__ __launch_bounds__(S::THREADS) void k_product(Product g) {
         }
     }
 }
+
+// o - l_target from log2 of the sum.
+__device__ __forceinline__ float sum_minus(float others, float logit) { return fmaf(others, 0.693147180559945309f, -logit); }
 
 // A row's parts together: o, the target's logit and the loss. Sixteen rows a
 // workgroup, 64 slices of the parts, joined in a fixed order.
@@ -435,9 +451,8 @@ __global__ __launch_bounds__(1024) void k_losses(VocabularyArgs a, const float2*
     if (slice != 0 || r >= a.rows) return;
     const int64_t t = a.targets[r];
     const bool counts = t >= 0 && t < a.vocab;
-    const float others = s.x + logf(s.y);  // no others: -infinity
-    const float d = others - a.stats[a.rows + r];
-    a.stats[r] = others;
+    const float d = sum_minus(s.x + log2f(s.y), a.stats[a.rows + r]);  // no others: -infinity
+    a.stats[r] = s.x + log2f(s.y);
     if (!counts) a.stats[a.rows + r] = 0.0f;
     a.losses[r] = !counts ? 0.0f : d > 0.0f ? d + log1pf(expf(-d)) : log1pf(expf(d));
 }
@@ -448,7 +463,7 @@ __global__ __launch_bounds__(256) void k_row_info(VocabularyArgs a, RowInfo* inf
     const int64_t t = a.targets[r];
     RowInfo v = {0.0f, 0.0f, -1, 0};
     if (t >= 0 && t < a.vocab) {
-        const float others = a.stats[r], d = others - a.stats[a.rows + r];
+        const float others = a.stats[r], d = sum_minus(others, a.stats[a.rows + r]);
         v.others = others == -__builtin_huge_valf() ? 0.0f : others;  // then there is no q
         v.scale = a.dloss[r] * (d < 0.0f ? expf(d) / (1.0f + expf(d)) : 1.0f / (1.0f + expf(-d)));
         v.target = (int)t;
@@ -479,7 +494,7 @@ __global__ __launch_bounds__(256) void k_pack(RowView src, int64_t rows, int col
     put<T>(dst + i, plane, c < cols ? St<T>::ld1(static_cast<const T*>(src.p) + r * src.stride + c) : 0.0f);
 }
 
-// The same transposed: dst [cols][ld], ld >= rows; rows that `targets` leaves out are zero.
+// The same transposed: dst [cols][ld], ld >= rows a multiple of 64; rows that `targets` leaves out are zero.
 template <typename T>
 __global__ __launch_bounds__(256) void k_pack_transposed(RowView src, int64_t rows, int cols, const int64_t* targets, int64_t vocab,
                                                          bf16_t* dst, int64_t plane, int64_t ld, int blocks) {
@@ -487,6 +502,7 @@ __global__ __launch_bounds__(256) void k_pack_transposed(RowView src, int64_t ro
     const int64_t index = block_index(), r0 = index / blocks * 64;
     const int c0 = (int)(index % blocks) * 64;
     if (r0 >= ld) return;
+#pragma unroll 4
     for (int k = threadIdx.x; k < 64 * 64; k += 256) {
         const int64_t r = r0 + k / 64;
         const int c = c0 + k % 64;
@@ -495,22 +511,58 @@ __global__ __launch_bounds__(256) void k_pack_transposed(RowView src, int64_t ro
         lds[k / 64][k % 64] = there ? St<T>::ld1(static_cast<const T*>(src.p) + r * src.stride + c) : 0.0f;
     }
     __syncthreads();
-    for (int k = threadIdx.x; k < 64 * 64; k += 256) {
-        const int64_t r = r0 + k % 64;
-        const int c = c0 + k / 64;
-        if (r < ld && c < cols) put<T>(dst + c * ld + r, plane, lds[k % 64][k / 64]);
+    for (int k = threadIdx.x; k < 64 * 8; k += 256) {  // eight rows of the source a chunk
+        const int r = k % 8 * 8, c = k / 8;
+        if (c0 + c >= cols) break;
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = lds[r + i][c];
+#pragma unroll
+        for (int n = 0; n < Pieces<T>::N; ++n) {
+            uint32_t two[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                two[i] = f2bf2(v[2 * i], v[2 * i + 1]);
+                v[2 * i] -= __uint_as_float(two[i] << 16);
+                v[2 * i + 1] -= __uint_as_float(two[i] & 0xffff0000u);
+            }
+            *reinterpret_cast<u32x4*>(dst + n * plane + (c0 + c) * ld + r0 + r) = u32x4{two[0], two[1], two[2], two[3]};
+        }
     }
 }
 
-// The planes of a product together, in order, times the row's scale, as stored.
-template <typename T>
-__global__ __launch_bounds__(256) void k_finish(const float* planes, int splits, int64_t rows, int cols, int64_t ld, const RowInfo* info, T* out) {
-    const int64_t i = block_index() * 256 + threadIdx.x, r = i / cols, c = i - r * cols;
-    if (r >= rows) return;
-    float s = 0.0f;
-    for (int k = 0; k < splits; ++k) s += planes[(k * rows + r) * ld + c];
-    if (info) s = info[r].target < 0 ? 0.0f : s * info[r].scale;
-    St<T>::st1(out + i, s);
+// The planes of a product together, in order, times the row's scale (info), as
+// stored. Rows without a scale come as one.
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void k_finish(const float* planes, int splits, int64_t rows, int64_t cols, int blocks, const RowInfo* info, T* out) {
+    const int64_t index = block_index(), r = index / blocks, c = ((index - r * blocks) * 256 + threadIdx.x) * 4;
+    if (r >= rows || c >= cols) return;
+    floatx4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int n = (int)min(cols - c, (int64_t)4);
+#pragma unroll 4
+    for (int k = 0; k < splits; ++k) {
+        const float* p = planes + (k * rows + r) * cols + c;
+        if (VEC) {
+            s += *reinterpret_cast<const floatx4*>(p);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < n) s[i] += p[i];
+        }
+    }
+    if (info) {
+        const RowInfo f = info[r];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = f.target < 0 ? 0.0f : s[i] * f.scale;
+    }
+    T* to = out + r * cols + c;
+    if (VEC) {
+        St<T>::st4(to, s);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < n) St<T>::st1(to + i, s[i]);
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -522,25 +574,38 @@ typedef Shape<256, 256, 128, 64> Large;
 typedef Shape<128, 128, 64, 64> Middle;
 typedef Shape<64, 128, 64, 32> Low;
 
-template <typename F>
+template <bool ANY = true, typename F>
 auto with_shape(int64_t m, int64_t n, F&& f) {
     if (m <= 64) return f(Low());
-    if ((m + 255) / 256 * ((n + 255) / 256) >= 192) return f(Large());
+    if constexpr (ANY)
+        if ((m + 255) / 256 * ((n + 255) / 256) >= 192) return f(Large());
     return f(Middle());
 }
 
-// Parts of the sum of a product whose tiles alone leave the chip idle.
+// Parts of the sum of a product, so that its tiles fill the chip: the number that
+// takes the least time by a model of it. A round of workgroups takes as long as
+// their steps (1.9 us of a large tile alone on its CU; 1.5 and 0.8 us of the others,
+// two on a CU) and two more to start and end; every part's plane is written and read
+// once, at 5 TB/s.
 int splits_of(int64_t m, int64_t n, int64_t steps) {
     return with_shape(m, n, [&](auto shape) {
         typedef decltype(shape) S;
-        const int64_t tiles = std::max<int64_t>(1, (m + S::BM - 1) / S::BM * ((n + S::BN - 1) / S::BN)), want = S::BM == 256 ? 256 : 512;
-        return (int)std::max<int64_t>(1, std::min<int64_t>(want / tiles, steps / 8));
+        const int64_t tiles = (m + S::BM - 1) / S::BM * ((n + S::BN - 1) / S::BN), slots = S::BM == 256 ? 256 : 512;
+        const double step = S::BM == 256 ? 1.9 : S::BM == 128 ? 1.5 : 0.8, plane = (double)m * n * 8 / 5e6;
+        int best = 1;
+        double least = 1e300;
+        for (int64_t k = 1; k <= std::max<int64_t>(1, std::min<int64_t>(64, steps / 4)); ++k) {
+            const double time = (double)((tiles * k + slots - 1) / slots) * ((steps + k - 1) / k + 2) * step + k * plane;
+            if (time < least) least = time, best = (int)k;
+        }
+        return best;
     });
 }
 
 template <int WHAT, int PIECES = 1>
 hipError_t product(Product g, hipStream_t s) {
-    return with_shape(g.a.rows, g.b.rows, [&](auto shape) {
+    // three pieces of q of a large tile do not fit the registers beside it
+    return with_shape<PIECES == 1>(g.a.rows, g.b.rows, [&](auto shape) {
         typedef decltype(shape) S;
         g.tiles_m = (int)((g.a.rows + S::BM - 1) / S::BM);
         g.tiles_n = (int)((g.b.rows + S::BN - 1) / S::BN);
@@ -559,8 +624,10 @@ struct Plan {
     int64_t piece, dimp, rowsp;   // vocabulary rows of a piece, dim and rows in whole steps
     int pieces;                   // of an operand's numbers
     bool pack_x, pack_w;
-    int splits_dx, splits_dw;
     int64_t x, w, part, info, xt, wt, q, qt, dx, dw, total;  // offsets
+    int pairs() const { return pieces == 1 ? 1 : 6; }
+    int splits_dx(const VocabularyArgs& a) const { return splits_of(a.rows, a.dim, piece / BK * pairs()); }
+    int splits_dw(const VocabularyArgs& a, int64_t n) const { return splits_of(n, a.dim, rowsp / BK * pairs()); }
 };
 
 bool direct(const VocabularyArgs& a, const RowView& v) {
@@ -572,10 +639,12 @@ Plan plan_of(const VocabularyArgs& a, bool backward) {
     p.pieces = a.dtype ? 1 : 3;
     p.dimp = up(a.dim, BK);
     p.rowsp = up(std::max<int64_t>(a.rows, 1), BK);
-    // pieces of at most 2^28 logits, and of 2^16 weights at a time
-    const int64_t most = std::max<int64_t>(256, std::min<int64_t>(65536, ((int64_t)1 << 28) / p.rowsp / 256 * 256));
-    const int64_t count = (a.vocab + most - 1) / most;
-    p.piece = std::min<int64_t>(up(a.vocab, BK), up((a.vocab + count - 1) / count, 256));
+    // Pieces of at most 2^28 logits and 2^16 weights; where there are several, with
+    // as many rows of large tiles as make dW's tiles a multiple of the 256 CUs.
+    int64_t most = std::max<int64_t>(256, std::min<int64_t>(65536, ((int64_t)1 << 28) / p.rowsp / 256 * 256)), even = 256;
+    while (even / 256 * ((a.dim + 255) / 256) % 256 && even < most) even *= 2;
+    if (even <= most) most = most / even * even;
+    p.piece = std::min<int64_t>(up(a.vocab, BK), most);
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
         const int64_t from = at;
@@ -593,11 +662,9 @@ Plan plan_of(const VocabularyArgs& a, bool backward) {
         p.wt = take(a.dim * p.piece * 2 * p.pieces);
         p.q = take(p.rowsp * p.piece * 2 * p.pieces);
         p.qt = take(p.rowsp * p.piece * 2 * p.pieces);
-        const int pairs = p.pieces == 1 ? 1 : 6;
-        p.splits_dx = splits_of(a.rows, a.dim, p.piece / BK * pairs);
-        p.splits_dw = splits_of(p.piece, a.dim, p.rowsp / BK * pairs);
-        p.dx = take(p.splits_dx * a.rows * a.dim * 4);
-        p.dw = take(p.splits_dw * p.piece * a.dim * 4);
+        const int64_t rest = a.vocab % p.piece;
+        p.dx = take(p.splits_dx(a) * a.rows * a.dim * 4);
+        p.dw = take(std::max(p.splits_dw(a, std::min<int64_t>(p.piece, a.vocab)) * p.piece, rest ? p.splits_dw(a, rest) * rest : 0) * a.dim * 4);
     }
     p.total = std::max<int64_t>(at, 16);
     return p;
@@ -623,6 +690,19 @@ hipError_t pack_transposed(const RowView& v, int64_t rows, int cols, const int64
     dim3 grid;
     if (!grid_of((ld + 63) / 64 * blocks, 256, grid)) return hipErrorInvalidValue;
     k_pack_transposed<T><<<grid, 256, 0, s>>>(v, rows, cols, targets, vocab, dst, plane, ld, blocks);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t finish(const float* planes, int splits, int64_t rows, int64_t cols, const RowInfo* info, T* out, hipStream_t s) {
+    const int64_t blocks = (cols + 1023) / 1024;
+    dim3 grid;
+    if (blocks > 0x7fffffff || !grid_of(rows * blocks, 256, grid)) return hipErrorInvalidValue;
+    // a piece's rows of dW start anywhere in dW where dim is odd
+    if (cols % 4 == 0 && (reinterpret_cast<uintptr_t>(out) & (4 * sizeof(T) - 1)) == 0)
+        k_finish<T, true><<<grid, 256, 0, s>>>(planes, splits, rows, cols, (int)blocks, info, out);
+    else
+        k_finish<T, false><<<grid, 256, 0, s>>>(planes, splits, rows, cols, (int)blocks, info, out);
     return hipGetLastError();
 }
 
@@ -656,7 +736,7 @@ hipError_t forward(const VocabularyArgs& a, hipStream_t s) {
     Product g{};
     OK_OR_RETURN(x_operand<T>(a, p, g.a, s));
     g.steps = (int)(p.dimp / BK);
-    g.pairs = p.pieces == 1 ? 1 : 6;
+    g.pairs = p.pairs();
     g.targets = a.targets;
     g.logit = a.stats + a.rows;
     float2* part = reinterpret_cast<float2*>(ws + p.part);
@@ -683,7 +763,7 @@ hipError_t backward(const VocabularyArgs& a, hipStream_t s) {
     auto bf = [&](int64_t at) { return reinterpret_cast<bf16_t*>(ws + at); };
     auto f32 = [&](int64_t at) { return reinterpret_cast<float*>(ws + at); };
     RowInfo* info = reinterpret_cast<RowInfo*>(ws + p.info);
-    const int pairs = p.pieces == 1 ? 1 : 6;
+    const int pairs = p.pairs();
     T *dx = static_cast<T*>(a.dx), *dw = static_cast<T*>(a.dw);
     if (a.rows > 0) {
         k_row_info<<<(unsigned)((a.rows + 255) / 256), 256, 0, s>>>(a, info);
@@ -716,7 +796,7 @@ hipError_t backward(const VocabularyArgs& a, hipStream_t s) {
             x.b = Operand{bf(p.wt), wt_plane, np, a.dim};
             x.steps = (int)(np / BK);
             x.pairs = pairs;
-            x.splits = p.splits_dx;
+            x.splits = p.splits_dx(a);
             x.out = f32(p.dx);
             x.ldo = a.dim;
             x.add = first > 0;
@@ -727,20 +807,14 @@ hipError_t backward(const VocabularyArgs& a, hipStream_t s) {
         v.b = Operand{bf(p.xt), xt_plane, p.rowsp, a.dim};
         v.steps = a.rows > 0 ? (int)(p.rowsp / BK) : 0;  // no rows: dW is zero
         v.pairs = pairs;
-        v.splits = p.splits_dw;
+        v.splits = p.splits_dw(a, n);
         v.out = f32(p.dw);
         v.ldo = a.dim;
         OK_OR_RETURN(product<PLANES>(v, s));
-        dim3 grid;
-        if (!grid_of((n * a.dim + 255) / 256, 256, grid)) return hipErrorInvalidValue;
-        k_finish<T><<<grid, 256, 0, s>>>(v.out, v.splits, n, a.dim, a.dim, nullptr, dw + first * a.dim);
-        OK_OR_RETURN(hipGetLastError());
+        OK_OR_RETURN(finish<T>(v.out, v.splits, 1, n * a.dim, nullptr, dw + first * a.dim, s));
     }
     if (a.rows == 0) return hipSuccess;
-    dim3 grid;
-    if (!grid_of((a.rows * a.dim + 255) / 256, 256, grid)) return hipErrorInvalidValue;
-    k_finish<T><<<grid, 256, 0, s>>>(f32(p.dx), p.splits_dx, a.rows, a.dim, a.dim, info, dx);
-    return hipGetLastError();
+    return finish<T>(f32(p.dx), p.splits_dx(a), a.rows, a.dim, info, dx, s);
 }
 
 }  // namespace
