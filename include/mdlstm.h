@@ -671,7 +671,7 @@ size_t mdlstm_group_norm_workspace_bytes(const mdlstm_group_norm_desc* desc, int
 
 /*
  * d_offsets, d_order, tokens, longest as for mdlstm_attention_forward; d_x: rows
- * x_stride >= channels apart. d_y (out) [tokens][channels]; d_mean and d_rstd (out)
+ * x_stride >= channels apart (at most 2^22: UNSUPPORTED beyond). d_y (out) [tokens][channels]; d_mean and d_rstd (out)
  * [n][groups], for the backward (an empty example's mean is 0).
  */
 mdlstm_status mdlstm_group_norm_forward(const mdlstm_group_norm_desc* desc, int32_t n, int64_t tokens, int64_t longest,

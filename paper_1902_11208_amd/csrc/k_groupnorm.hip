@@ -16,6 +16,7 @@
 // joined from their means and squared distances in 64 bits. Sums are taken in a
 // fixed order.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.hpp"
 #include "groupnorm.hpp"
@@ -84,24 +85,50 @@ __device__ __forceinline__ void store_vec(T* p, int valid, const float (&v)[V]) 
     }
 }
 
-// Vectors of a tensor that a thread holds: 128 bytes forward, two tensors of 64 bytes backward.
-template <typename T, bool BACKWARD>
-constexpr int Hold = (BACKWARD ? 64 : 128) / (V * sizeof(T));
+// How a pass holds a sequence: threads of a workgroup at most, and the vectors of x
+// that each holds (backward with the fp32 numbers e beside them).
+struct Forward {
+    static constexpr bool BACKWARD = false;
+    static constexpr int THREADS = 1024, BYTES = 160;
+};
+struct Backward {
+    static constexpr bool BACKWARD = true;
+    static constexpr int THREADS = 512, BYTES = 160;
+};
+struct BackwardOfWideRows {  // a row of a group needs more than 512 threads
+    static constexpr bool BACKWARD = true;
+    static constexpr int THREADS = 1024, BYTES = 64;
+};
+template <typename T, typename H>
+constexpr int Hold = H::BYTES / (V * sizeof(T));
 
-__device__ __forceinline__ float sigmoid(float u) { return 1.0f / (1.0f + expf(-u)); }
-
-__device__ __forceinline__ float activate(float u, int act) {
-    if (act == MDLSTM_SILU) return u * sigmoid(u);
-    if (act == MDLSTM_RELU) return u < 0.0f ? 0.0f : u;  // a NaN stays one
+// EXACT (fp32 storage): to an ulp or two; else the product with log2(e) is rounded,
+// |u| 2^-24 off, far below a bf16 u's own rounding.
+template <bool EXACT>
+__device__ __forceinline__ float sigmoid(float u) {
+    constexpr float HIGH = -1.44269502162933349609375f, LOW = -1.925963033500011e-08f, LN2 = 0.693147180559945309f;
+    const float t = u * HIGH;
+    float e = __builtin_amdgcn_exp2f(t);
+    if (EXACT && fabsf(t) < 120.0f) e = fmaf(e, LN2 * fmaf(u, LOW, fmaf(u, HIGH, -t)), e);
+    const float d = 1.0f + e;
+    float r = __builtin_amdgcn_rcpf(d);
+    if (EXACT && d < 0x1p120f) r = fmaf(fmaf(-d, r, 1.0f), r, r);
+    return r;
+}
+template <int ACT, bool EXACT>
+__device__ __forceinline__ float activate(float u) {
+    if (ACT == MDLSTM_SILU) return u * sigmoid<EXACT>(u);
+    if (ACT == MDLSTM_RELU) return u < 0.0f ? 0.0f : u;  // a NaN stays one
     return u;
 }
 // dy act'(u)
-__device__ __forceinline__ float activate_back(float dy, float u, int act) {
-    if (act == MDLSTM_SILU) {
-        const float s = sigmoid(u);
+template <int ACT, bool EXACT>
+__device__ __forceinline__ float activate_back(float dy, float u) {
+    if (ACT == MDLSTM_SILU) {
+        const float s = sigmoid<EXACT>(u);
         return dy * (s * fmaf(u, 1.0f - s, 1.0f));
     }
-    if (act == MDLSTM_RELU) return u > 0.0f ? dy : 0.0f;
+    if (ACT == MDLSTM_RELU) return u > 0.0f ? dy : 0.0f;
     return dy;
 }
 
@@ -113,7 +140,7 @@ struct Place {
         slice = threadIdx.x / a.lanes;
         lane = threadIdx.x % a.lanes;
         width = min(a.block, a.channels - block * a.block);
-        groups = width / (a.channels / a.groups);
+        groups = width / a.per;
         in_block = lane * V;
         valid = slice < slices ? max(0, min(V, width - in_block)) : 0;
         if (valid == 0) in_block = 0;
@@ -121,12 +148,46 @@ struct Place {
     }
 };
 
+// A segment's rows as a thread takes them: row slice + k slices is `k` steps behind
+// a uniform base, at 32 bits of the thread's own offset (slices * stride is less than 2^32
+// bytes by the caller's check).
+template <typename T, bool WIDE>
+struct Rows {
+    char* base;
+    int64_t step;  // bytes
+    uint32_t offset;
+    int valid;
+    __device__ __forceinline__ Rows(const void* p, int64_t stride, int64_t token, const Place& me)
+        : base(static_cast<char*>(const_cast<void*>(p)) + token * stride * (int64_t)sizeof(T)), step(me.slices * stride * (int64_t)sizeof(T)),
+          offset((uint32_t)me.slice * (uint32_t)stride * sizeof(T) + me.c * sizeof(T)), valid(me.valid) {}
+    __device__ __forceinline__ Raw<T> load(int k) const {
+        return load_raw<T, WIDE>(reinterpret_cast<const T*>(base + k * step + offset), valid);
+    }
+    __device__ __forceinline__ void store(int k, const float (&v)[V]) const {
+        store_vec<T, WIDE>(reinterpret_cast<T*>(base + k * step + offset), valid, v);
+    }
+};
+
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ bool find_unit(const GroupNormArgs& a, int64_t slot, Unit& u) {
+    if (slot >= a.seqs.slots || !unit_of(a.seqs, slot, u)) return false;
+    u.seq = __builtin_amdgcn_readfirstlane(u.seq);
+    u.t0 = uniform(u.t0);
+    u.len = uniform(u.len);
+    u.from = uniform(u.from);
+    u.to = uniform(u.to);
+    return true;
+}
+
 // Sums over the workgroup's tokens and a group's channels of K values a channel, for each of a thread's channels the
 // sum of its group. LDS: rows of `lanes` * V channels, a row a slice (or a wave, where waves hold whole rows), then the
-// groups' sums. Waves take the groups in turn.
+// groups' sums. Short groups are added up by a thread each, others by waves in turn.
 template <int K>
 __device__ __forceinline__ void group_sums(const GroupNormArgs& a, const Place& me, const float (&v)[K][V], float* lds, float (&out)[K][V]) {
-    const int per = a.channels / a.groups, row = a.lanes * V;
+    const int per = a.per, row = a.lanes * V;
     const bool whole = a.lanes <= 64 && 64 % a.lanes == 0;  // lanes of a wave that hold the same channels are added first
     const int rows = whole ? (int)blockDim.x / 64 : me.slices;
     float* total = lds + (K * rows) * row;
@@ -142,34 +203,46 @@ __device__ __forceinline__ void group_sums(const GroupNormArgs& a, const Place& 
 #pragma unroll
                 for (int i = 0; i < V; ++i) t[k][i] += __shfl_xor(t[k][i], o);
     }
-    __syncthreads();  // the sums of the call before have been read
+    lds_barrier();  // the sums of the call before have been read
     if (whole ? (threadIdx.x & 63) < a.lanes : me.slice < me.slices) {
         const int r = whole ? threadIdx.x / 64 : me.slice;
 #pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-            for (int i = 0; i < V; ++i) lds[(k * rows + r) * row + me.lane * V + i] = t[k][i];
+        for (int k = 0; k < K; ++k) *reinterpret_cast<floatx4*>(&lds[(k * rows + r) * row + me.lane * V]) = floatx4{t[k][0], t[k][1], t[k][2], t[k][3]};
     }
-    __syncthreads();
-    const int wave = threadIdx.x / 64, in_wave = threadIdx.x & 63, waves = blockDim.x / 64;
-    for (int g = wave; g < me.groups; g += waves) {
-        float s[K] = {};
-        for (int c = in_wave; c < per * rows; c += 64) {
-            const int r = c / per, at = r * row + g * per + (c - r * per);
-#pragma unroll
-            for (int k = 0; k < K; ++k) s[k] += lds[k * rows * row + at];
+    lds_barrier();
+    for (int c = threadIdx.x; c < K * me.width; c += blockDim.x) {  // the rows, in order, into the first
+        float* at = lds + (c < me.width ? c : rows * row + c - me.width);
+        float s = at[0];
+#pragma unroll 4
+        for (int r = 1; r < rows; ++r) s += at[r * row];
+        at[0] = s;
+    }
+    lds_barrier();
+    if (per <= 32) {
+        for (int x = threadIdx.x; x < K * me.groups; x += blockDim.x) {
+            const float* at = lds + (x < me.groups ? x * per : rows * row + (x - me.groups) * per);
+            float s = 0.0f;
+#pragma unroll 4
+            for (int c = 0; c < per; ++c) s += at[c];
+            total[x] = s;
         }
+    } else {
+        const int wave = threadIdx.x / 64, in_wave = threadIdx.x & 63, waves = blockDim.x / 64;
+        for (int x = wave; x < K * me.groups; x += waves) {
+            const float* at = lds + (x < me.groups ? x * per : rows * row + (x - me.groups) * per);
+            float s = 0.0f;
+            for (int c = in_wave; c < per; c += 64) s += at[c];
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) s[k] += __shfl_xor(s[k], o);
-            if (in_wave == 0) total[k * me.groups + g] = s[k];
+            for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+            if (in_wave == 0) total[x] = s;
         }
     }
-    __syncthreads();
+    lds_barrier();
+    int g = me.in_block / per, edge = (g + 1) * per;  // the channel behind the group
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const int g = min((me.in_block + i) / per, me.groups - 1);
+        if (me.in_block + i == edge) ++g, edge += per;
+        g = min(g, me.groups - 1);
 #pragma unroll
         for (int k = 0; k < K; ++k) out[k][i] = total[k * me.groups + g];
     }
@@ -177,66 +250,72 @@ __device__ __forceinline__ void group_sums(const GroupNormArgs& a, const Place& 
 
 // True for one thread and channel of each group of the block, to write what the group has.
 __device__ __forceinline__ bool speaks(const GroupNormArgs& a, const Place& me, int i) {
-    return me.slice == 0 && i < me.valid && (me.in_block + i) % (a.channels / a.groups) == 0;
+    return me.slice == 0 && i < me.valid && (me.in_block + i) % a.per == 0;
 }
 
 // Forward. AGAIN: a segment of a long sequence whose mean and rstd are known; else
 // a sequence that a workgroup holds, or a long one's segment for its sums alone.
-template <typename T, bool WIDE, bool AGAIN>
-__global__ __launch_bounds__(1024) void k_groupnorm_fwd(GroupNormArgs a) {
-    constexpr int N = Hold<T, false>;
-    extern __shared__ float lds[];
-    const int64_t index = block_index(), slot = index / a.blocks;
+template <typename T, int ACT, bool WIDE, bool AGAIN>
+__global__ __launch_bounds__(Forward::THREADS) void k_groupnorm_fwd(GroupNormArgs a) {
+    constexpr int N = Hold<T, Forward>;
+    extern __shared__ __attribute__((aligned(16))) float lds[];
+    const int64_t index = block_index(), slot = uniform(index / a.blocks);
     Unit u;
-    if (slot >= a.seqs.slots || !unit_of(a.seqs, slot, u)) return;
+    if (!find_unit(a, slot, u)) return;
     const bool part = u.from > 0 || u.to < u.len;
     if (AGAIN && !part) return;
-    const int block = (int)(index - slot * a.blocks), per = a.channels / a.groups;
+    const int block = __builtin_amdgcn_readfirstlane((int)(index - slot * a.blocks)), per = a.per, n = (int)(u.to - u.from);
     const Place me(a, block);
-    const T* x = static_cast<const T*>(a.x.p) + u.t0 * a.x.stride + me.c;
-    const int64_t t = u.from + me.slice, stat = (int64_t)u.seq * a.groups;
+    const Rows<T, WIDE> x(a.x.p, a.x.stride, u.t0 + u.from, me), y(a.y, a.channels, u.t0 + u.from, me);
+    const int64_t stat = (int64_t)u.seq * a.groups;
     const bool mine = me.valid > 0;
     float mean[1][V] = {}, rstd[V];
     Raw<T> raw[N];
-#pragma unroll
-    for (int k = 0; k < N; ++k)
-        if (mine && t + k * me.slices < u.to) raw[k] = load_raw<T, WIDE>(x + (t + (int64_t)k * me.slices) * a.x.stride, me.valid);
-    if constexpr (!AGAIN) {
-        const float count = (float)((u.to - u.from) * per);
-        float sum[1][V] = {};
+    // f(k) for the thread's vectors; what no thread of the workgroup has is skipped as a whole
+    auto each = [&](auto f) {
 #pragma unroll
         for (int k = 0; k < N; ++k)
-            if (mine && t + k * me.slices < u.to) {
-                float v[V];
-                unpack(raw[k], v);
+            if (k * me.slices < n)
+                if (mine && me.slice + k * me.slices < n) f(k);
+    };
+    each([&](int k) { raw[k] = x.load(k); });
+    float w[V], b[V];
 #pragma unroll
-                for (int i = 0; i < V; ++i) sum[0][i] += v[i];
-            }
+    for (int i = 0; i < V; ++i) {
+        w[i] = i < me.valid ? a.w[me.c + i] : 0.0f;
+        b[i] = i < me.valid ? a.b[me.c + i] : 0.0f;
+    }
+    if constexpr (!AGAIN) {
+        const float inv = n > 0 ? 1.0f / ((float)n * (float)per) : 0.0f;
+        float sum[1][V] = {};
+        each([&](int k) {
+            float v[V];
+            unpack(raw[k], v);
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum[0][i] += v[i];
+        });
         group_sums<1>(a, me, sum, lds, mean);
         float off[2][V] = {}, all[2][V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) mean[0][i] = count > 0.0f ? mean[0][i] / count : 0.0f;
+        for (int i = 0; i < V; ++i) mean[0][i] *= inv;
+        each([&](int k) {
+            float v[V];
+            unpack(raw[k], v);
 #pragma unroll
-        for (int k = 0; k < N; ++k)
-            if (mine && t + k * me.slices < u.to) {
-                float v[V];
-                unpack(raw[k], v);
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float d = v[i] - mean[0][i];
-                    off[0][i] += d;
-                    off[1][i] = fmaf(d, d, off[1][i]);
-                }
+            for (int i = 0; i < V; ++i) {
+                const float d = v[i] - mean[0][i];
+                off[0][i] += d;
+                off[1][i] = fmaf(d, d, off[1][i]);
             }
+        });
         group_sums<2>(a, me, off, lds, all);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float d = count > 0.0f ? all[0][i] / count : 0.0f;  // what rounding left of the mean
+            const float d = all[0][i] * inv;  // what rounding left of the mean
             mean[0][i] += d;
-            const float squares = fmaxf(all[1][i] - count * d * d, 0.0f);
+            const float squares = fmaxf(fmaf(-all[0][i], d, all[1][i]), 0.0f);
             if (all[1][i] != all[1][i]) mean[0][i] = all[1][i];
-            const float var = count > 0.0f ? squares / count : 0.0f;
-            rstd[i] = 1.0f / sqrtf(var + a.eps);
+            rstd[i] = 1.0f / sqrtf(fmaf(squares, inv, a.eps));
             if (speaks(a, me, i)) {
                 const int g = (me.c + i) / per;
                 if (part) {
@@ -258,23 +337,15 @@ __global__ __launch_bounds__(1024) void k_groupnorm_fwd(GroupNormArgs a) {
             rstd[i] = a.rstd[stat + g];
         }
     }
-    if (!mine) return;
-    float w[V], b[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        w[i] = i < me.valid ? a.w[me.c + i] : 0.0f;
-        b[i] = i < me.valid ? a.b[me.c + i] : 0.0f;
-    }
-    T* y = static_cast<T*>(a.y) + u.t0 * a.channels + me.c;
+    for (int i = 0; i < V; ++i) rstd[i] *= w[i];
+    each([&](int k) {
+        float v[V];
+        unpack(raw[k], v);
 #pragma unroll
-    for (int k = 0; k < N; ++k)
-        if (t + k * me.slices < u.to) {
-            float v[V];
-            unpack(raw[k], v);
-#pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = activate(fmaf((v[i] - mean[0][i]) * rstd[i], w[i], b[i]), a.act);
-            store_vec<T, WIDE>(y + (t + (int64_t)k * me.slices) * a.channels, me.valid, v);
-        }
+        for (int i = 0; i < V; ++i) v[i] = activate<ACT, sizeof(T) == 4>(fmaf(v[i] - mean[0][i], rstd[i], b[i]));
+        y.store(k, v);
+    });
 }
 
 // mean and rstd of the long sequences from their segments': a wave a group.
@@ -286,7 +357,7 @@ __global__ __launch_bounds__(64) void k_groupnorm_join(GroupNormArgs a) {
     sequence_of(a.seqs, seq, u);
     if (u.len <= a.seqs.seg) return;
     const int64_t count = (u.len + a.seqs.seg - 1) / a.seqs.seg, slot0 = u.t0 / a.seqs.seg + seq;
-    const int per = a.channels / a.groups;
+    const int per = a.per;
     auto sum = [&](auto f) {
         double s = 0.0;
         for (int64_t k = threadIdx.x; k < count; k += 64) {
@@ -306,12 +377,13 @@ __global__ __launch_bounds__(64) void k_groupnorm_join(GroupNormArgs a) {
 }
 
 // Backward, AGAIN as in the forward pass (the group means of g and g c are known).
-template <typename T, bool WIDE, bool AGAIN>
-__global__ __launch_bounds__(1024) void k_groupnorm_bwd(GroupNormArgs a) {
-    constexpr int N = Hold<T, true>;
-    extern __shared__ float lds[];
-    const int64_t index = block_index(), first = index / a.blocks;
-    const int block = (int)(index - first * a.blocks), per = a.channels / a.groups;
+template <typename T, typename H, int ACT, bool WIDE, bool AGAIN>
+__global__ __launch_bounds__(H::THREADS) void k_groupnorm_bwd(GroupNormArgs a) {
+    constexpr int N = Hold<T, H>;
+    extern __shared__ __attribute__((aligned(16))) float lds[];
+    const int64_t index = block_index(), first = uniform(index / a.blocks);
+    if (first >= a.parts) return;  // a launch has whole rows of workgroups
+    const int block = __builtin_amdgcn_readfirstlane((int)(index - first * a.blocks)), per = a.per;
     const Place me(a, block);
     const bool mine = me.valid > 0;
     float w[V], b[V], dw[V] = {}, db[V] = {};
@@ -322,49 +394,42 @@ __global__ __launch_bounds__(1024) void k_groupnorm_bwd(GroupNormArgs a) {
     }
     for (int64_t slot = first; slot < a.seqs.slots; slot += a.parts) {
         Unit u;
-        if (!unit_of(a.seqs, slot, u) || u.from >= u.to) continue;
+        if (!find_unit(a, slot, u) || u.from >= u.to) continue;
         const bool part = u.from > 0 || u.to < u.len;
         if (AGAIN && !part) continue;
-        const int64_t t = u.from + me.slice, stat = (int64_t)u.seq * a.groups;
-        const T* x = static_cast<const T*>(a.x.p) + u.t0 * a.x.stride + me.c;
-        const T* dy = static_cast<const T*>(a.dy.p) + u.t0 * a.dy.stride + me.c;
-        Raw<T> rx[N], rg[N];
+        const int n = (int)(u.to - u.from);
+        const int64_t stat = (int64_t)u.seq * a.groups, token = u.t0 + u.from;
+        const Rows<T, WIDE> x(a.x.p, a.x.stride, token, me), dy(a.dy.p, a.dy.stride, token, me), dx(a.dx, a.channels, token, me);
+        auto each = [&](auto f) {
 #pragma unroll
-        for (int k = 0; k < N; ++k)
-            if (mine && t + k * me.slices < u.to) {
-                rx[k] = load_raw<T, WIDE>(x + (t + (int64_t)k * me.slices) * a.x.stride, me.valid);
-                rg[k] = load_raw<T, WIDE>(dy + (t + (int64_t)k * me.slices) * a.dy.stride, me.valid);
-            }
-        float mean[V], rstd[V], m[2][V];
+            for (int k = 0; k < N; ++k)
+                if (k * me.slices < n)
+                    if (mine && me.slice + k * me.slices < n) f(k);
+        };
+        Raw<T> rx[N], rg[N];
+        each([&](int k) { rx[k] = x.load(k), rg[k] = dy.load(k); });
+        float mean[V], rstd[V], m[2][V], s[2][V] = {}, e[N][V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int g = min((me.c + i) / per, a.groups - 1);
             mean[i] = a.mean[stat + g];
             rstd[i] = a.rstd[stat + g];
         }
-        // a token's c and e
-        auto parts = [&](int k, float (&c)[V], float (&e)[V]) {
+        each([&](int k) {
+            float c[V];
             unpack(rx[k], c);
-            unpack(rg[k], e);
+            unpack(rg[k], e[k]);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 c[i] = (c[i] - mean[i]) * rstd[i];
-                e[i] = activate_back(e[i], fmaf(c[i], w[i], b[i]), a.act);
-            }
-        };
-        if constexpr (!AGAIN) {
-            float s[2][V] = {};
-#pragma unroll
-            for (int k = 0; k < N; ++k)
-                if (mine && t + k * me.slices < u.to) {
-                    float c[V], e[V];
-                    parts(k, c, e);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        s[0][i] += e[i];
-                        s[1][i] = fmaf(e[i], c[i], s[1][i]);
-                    }
+                e[k][i] = activate_back<ACT, sizeof(T) == 4>(e[k][i], fmaf(c[i], w[i], b[i]));
+                if constexpr (!AGAIN) {
+                    s[0][i] += e[k][i];
+                    s[1][i] = fmaf(e[k][i], c[i], s[1][i]);
                 }
+            }
+        });
+        if constexpr (!AGAIN) {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 db[i] += s[0][i];
@@ -383,9 +448,9 @@ __global__ __launch_bounds__(1024) void k_groupnorm_bwd(GroupNormArgs a) {
                     }
                 continue;
             }
-            const float count = (float)(u.len * per);
+            const float inv = 1.0f / ((float)n * (float)per);
 #pragma unroll
-            for (int i = 0; i < V; ++i) m[0][i] /= count, m[1][i] /= count;
+            for (int i = 0; i < V; ++i) m[0][i] *= inv, m[1][i] *= inv;
         } else {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
@@ -394,16 +459,16 @@ __global__ __launch_bounds__(1024) void k_groupnorm_bwd(GroupNormArgs a) {
                 m[1][i] = from[1];
             }
         }
-        T* dx = static_cast<T*>(a.dx) + u.t0 * a.channels + me.c;
+        each([&](int k) {
+            float c[V];
+            unpack(rx[k], c);
 #pragma unroll
-        for (int k = 0; k < N; ++k)
-            if (mine && t + k * me.slices < u.to) {
-                float c[V], e[V];
-                parts(k, c, e);
-#pragma unroll
-                for (int i = 0; i < V; ++i) e[i] = rstd[i] * (fmaf(e[i], w[i], -m[0][i]) - c[i] * m[1][i]);
-                store_vec<T, WIDE>(dx + (t + (int64_t)k * me.slices) * a.channels, me.valid, e);
+            for (int i = 0; i < V; ++i) {
+                c[i] = (c[i] - mean[i]) * rstd[i];
+                c[i] = rstd[i] * fmaf(-c[i], m[1][i], fmaf(e[k][i], w[i], -m[0][i]));
             }
+            dx.store(k, c);
+        });
     }
     if (AGAIN) return;
     // the workgroup's share of dw and db, its slices added in order
@@ -475,26 +540,35 @@ __global__ __launch_bounds__(1024) void k_groupnorm_dw(int channels, int64_t par
 
 bool aligned(const void* p, int to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
-// The shape of a pass: channels of a workgroup, its threads, the tokens it holds.
+// The shape of a pass: the threads of a workgroup and the tokens it holds.
 struct Shape {
     int threads, held;
 };
 
-Shape shape_of(GroupNormArgs& a, bool backward) {
-    const int per = a.channels / a.groups, es = a.dtype ? 2 : 4;
-    // whole groups of about 128 bytes of a row, in whole vectors where a few groups give them
+template <typename H>
+Shape shape_of(GroupNormArgs& a) {
+    const int per = a.channels / a.groups, es = a.dtype ? 2 : 4, hold = a.dtype ? Hold<bf16_t, H> : Hold<float, H>, most = H::THREADS;
+    a.per = per;
+    // whole groups, in whole vectors where a few groups give them
     int unit = per;
     while (unit % V && unit + per <= std::min(256, a.channels)) unit += per;
     if (unit % V) unit = per;
-    int block = unit;
-    while (block * es < 128 && block + unit <= a.channels) block += unit;
-    a.block = block;
-    a.blocks = (a.channels + block - 1) / block;
-    a.lanes = (block + V - 1) / V;
-    const int hold = (backward ? 64 : 128) / (V * es);
+    // about 128 bytes of a row; 64 where a workgroup then holds the longest sequence
+    auto with = [&](int bytes) {
+        int block = unit;
+        while (block * es < bytes && block + unit <= a.channels) block += unit;
+        a.block = block;
+        a.lanes = (block + V - 1) / V;
+    };
+    with(128);
+    if (most / a.lanes * hold < a.seqs.longest) {
+        with(64);
+        if (most / a.lanes * hold < a.seqs.longest) with(128);
+    }
+    a.blocks = (a.channels + a.block - 1) / a.block;
     Shape s;
     s.threads = 256;
-    while (s.threads < 1024 && (s.threads < a.lanes || (int64_t)s.threads / a.lanes * hold < a.seqs.longest)) s.threads *= 2;
+    while (s.threads < most && (s.threads < a.lanes || (int64_t)s.threads / a.lanes * hold < a.seqs.longest)) s.threads *= 2;
     s.held = s.threads / a.lanes * hold;
     a.seqs.seg = a.seqs.longest > s.held ? s.held : 0;
     a.seqs.slots = packed_slots(a.seqs, a.seqs.seg);
@@ -516,10 +590,11 @@ Plan plan_of(const GroupNormArgs& a, bool backward) {
     return p;
 }
 
-template <bool BACKWARD>
+template <typename H>
 hipError_t launch(const GroupNormArgs& in, hipStream_t s) {
     GroupNormArgs a = in;
-    const Shape shape = shape_of(a, BACKWARD);
+    constexpr bool BACKWARD = H::BACKWARD;
+    const Shape shape = shape_of<H>(a);
     const Plan p = plan_of(a, BACKWARD);
     char* ws = static_cast<char*>(a.ws);
     a.sums = reinterpret_cast<float*>(ws + p.sums);
@@ -539,15 +614,16 @@ hipError_t launch(const GroupNormArgs& in, hipStream_t s) {
     if (!grid_of((BACKWARD ? a.parts : a.seqs.slots) * a.blocks, shape.threads, grid) || !grid_of(a.seqs.slots * a.blocks, shape.threads, again) ||
         !grid_of((int64_t)a.seqs.n * a.groups, 64, join))
         return hipErrorInvalidValue;
-    auto run = [&](auto t, auto w) {
+    auto run = [&](auto t, auto act, auto w) {
         typedef decltype(t) T;
+        constexpr int ACT = act();
         constexpr bool W = w();
         hipError_t e = hipSuccess;
         if (a.seqs.n > 0) {
             if constexpr (BACKWARD)
-                k_groupnorm_bwd<T, W, false><<<grid, shape.threads, lds, s>>>(a);
+                k_groupnorm_bwd<T, H, ACT, W, false><<<grid, shape.threads, lds, s>>>(a);
             else
-                k_groupnorm_fwd<T, W, false><<<grid, shape.threads, lds, s>>>(a);
+                k_groupnorm_fwd<T, ACT, W, false><<<grid, shape.threads, lds, s>>>(a);
             e = hipGetLastError();
             if (e == hipSuccess && a.seqs.seg) {
                 if constexpr (BACKWARD)
@@ -557,9 +633,9 @@ hipError_t launch(const GroupNormArgs& in, hipStream_t s) {
                 e = hipGetLastError();
                 if (e != hipSuccess) return e;
                 if constexpr (BACKWARD)
-                    k_groupnorm_bwd<T, W, true><<<again, shape.threads, lds, s>>>(a);
+                    k_groupnorm_bwd<T, H, ACT, W, true><<<again, shape.threads, lds, s>>>(a);
                 else
-                    k_groupnorm_fwd<T, W, true><<<again, shape.threads, lds, s>>>(a);
+                    k_groupnorm_fwd<T, ACT, W, true><<<again, shape.threads, lds, s>>>(a);
                 e = hipGetLastError();
             }
         }
@@ -571,19 +647,30 @@ hipError_t launch(const GroupNormArgs& in, hipStream_t s) {
     };
     const std::true_type yes;
     const std::false_type no;
-    if (a.dtype) return wide ? run(bf16_t(), yes) : run(bf16_t(), no);
-    return wide ? run(float(), yes) : run(float(), no);
+    auto with_act = [&](auto t) {
+        const std::integral_constant<int, MDLSTM_NO_ACTIVATION> none;
+        const std::integral_constant<int, MDLSTM_RELU> relu;
+        const std::integral_constant<int, MDLSTM_SILU> silu;
+        if (a.act == MDLSTM_SILU) return wide ? run(t, silu, yes) : run(t, silu, no);
+        if (a.act == MDLSTM_RELU) return wide ? run(t, relu, yes) : run(t, relu, no);
+        return wide ? run(t, none, yes) : run(t, none, no);
+    };
+    return a.dtype ? with_act(bf16_t()) : with_act(float());
 }
+
+bool wide_rows(const GroupNormArgs& a) { return a.channels / a.groups > V * Backward::THREADS; }
 
 }  // namespace
 
 size_t groupnorm_workspace_bytes(const GroupNormArgs& in, bool backward) {
     GroupNormArgs a = in;
-    (void)shape_of(a, backward);
+    (void)(!backward ? shape_of<Forward>(a) : wide_rows(a) ? shape_of<BackwardOfWideRows>(a) : shape_of<Backward>(a));
     return (size_t)std::max<int64_t>(plan_of(a, backward).total, 16);
 }
 
-hipError_t launch_groupnorm_fwd(const GroupNormArgs& a, hipStream_t s) { return launch<false>(a, s); }
-hipError_t launch_groupnorm_bwd(const GroupNormArgs& a, hipStream_t s) { return launch<true>(a, s); }
+hipError_t launch_groupnorm_fwd(const GroupNormArgs& a, hipStream_t s) { return launch<Forward>(a, s); }
+hipError_t launch_groupnorm_bwd(const GroupNormArgs& a, hipStream_t s) {
+    return wide_rows(a) ? launch<BackwardOfWideRows>(a, s) : launch<Backward>(a, s);
+}
 
 }  // namespace mdl

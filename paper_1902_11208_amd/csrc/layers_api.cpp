@@ -237,7 +237,7 @@ mdlstm_status mdlstm_group_norm_forward(const mdlstm_group_norm_desc* desc, int3
     OK_OR_RETURN(check_group_norm(desc));
     OK_OR_RETURN(check_sequences(n, tokens, longest));
     const int64_t cols = desc->channels, es = (int64_t)element(desc->dtype), stats = (int64_t)n * desc->groups * 4;
-    OK_OR_RETURN(check_rows(d_x, "x", tokens, cols, x_stride, desc->dtype));
+    OK_OR_RETURN(check_token_rows(d_x, "x", tokens, cols, x_stride, desc->dtype));
     OK_OR_RETURN(check_out(d_offsets, "offsets", n > 0, 8));
     OK_OR_RETURN(check_out(d_order, "order", false, 4));
     OK_OR_RETURN(check_out(d_w, "w", n > 0, 4));
@@ -274,8 +274,8 @@ mdlstm_status mdlstm_group_norm_backward(const mdlstm_group_norm_desc* desc, int
     OK_OR_RETURN(check_group_norm(desc));
     OK_OR_RETURN(check_sequences(n, tokens, longest));
     const int64_t cols = desc->channels, es = (int64_t)element(desc->dtype), stats = (int64_t)n * desc->groups * 4;
-    OK_OR_RETURN(check_rows(d_x, "x", tokens, cols, x_stride, desc->dtype));
-    OK_OR_RETURN(check_rows(d_dy, "dy", tokens, cols, dy_stride, desc->dtype));
+    OK_OR_RETURN(check_token_rows(d_x, "x", tokens, cols, x_stride, desc->dtype));
+    OK_OR_RETURN(check_token_rows(d_dy, "dy", tokens, cols, dy_stride, desc->dtype));
     OK_OR_RETURN(check_out(d_offsets, "offsets", n > 0, 8));
     OK_OR_RETURN(check_out(d_order, "order", false, 4));
     OK_OR_RETURN(check_out(d_w, "w", n > 0, 4));

@@ -227,7 +227,7 @@ def test_recurrence_steps_equal_the_scan():
 
 @pytest.mark.parametrize("lengths", [[1], [0, 3, 0], [127, 128, 1, 0, 9], [700, 30], [5000, 2, 0, 3000]], ids=str)
 @pytest.mark.parametrize("channels,groups,layout", [(1, 1, "contiguous"), (6, 2, "odd"), (64, 4, "fused"), (65, 5, "contiguous"),
-                                                    (40, 40, "fused"), (320, 32, "contiguous"), (300, 1, "odd"), (1024, 2, "fused")])
+                                                    (40, 40, "fused"), (320, 32, "contiguous"), (300, 1, "odd"), (1024, 2, "fused"), (2502, 1, "contiguous"), (4096, 1, "odd")])
 @pytest.mark.parametrize("act", [None, "relu", "silu"])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_group_norm(lengths, channels, groups, layout, act, dtype):
@@ -250,7 +250,9 @@ def test_group_norm(lengths, channels, groups, layout, act, dtype):
         assert np.abs(_np(dx) - wx).max() <= 1e-4 * np.abs(_np(dy)).max() / np.sqrt(1e-5)
     if np.abs(ww).max() > 1e-3:
         _check("dw", dw, ww, 1e-4)
-    _check("db", db, wb, 1e-5)
+    # db is a sum of T numbers of at most 1.1 |dy|, each off by some eight roundings of 2^-24 of itself; where they cancel,
+    # that is what the sum may be off by
+    assert np.all(np.abs(_np(db) - wb) <= 1e-6 * (1.1 * np.abs(_np(dy)).sum(0)))
 
 
 @pytest.mark.parametrize("mean", [100.0, -3000.0])
