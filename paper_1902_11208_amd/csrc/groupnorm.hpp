@@ -29,7 +29,7 @@ struct GroupNormArgs {
     // set by the launchers: channels of a workgroup (whole groups), blocks of them in a row, lanes of a row, tokens
     // that a workgroup takes at once, workgroups along the slots, long sequences' sums of each slot
     // [slots][groups][2], what dw and db add up from [parts][2][channels], group means of long sequences [n][groups][2]
-    int per, block, blocks, lanes;  // per: channels of a group
+    int per, block, blocks, lanes, held;  // per: channels of a group, held: tokens
     int64_t parts;
     float* sums;
     float* part;

@@ -85,19 +85,24 @@ __device__ __forceinline__ void store_vec(T* p, int valid, const float (&v)[V]) 
     }
 }
 
-// How a pass holds a sequence: threads of a workgroup at most, and the vectors of x
-// that each holds (backward with the fp32 numbers e beside them).
-struct Forward {
-    static constexpr bool BACKWARD = false;
-    static constexpr int THREADS = 1024, BYTES = 160;
+// What a pass does: all of a sequence that a workgroup holds; or a segment's sums; or a
+// segment again, when its sequence's sums are known.
+enum { WHOLE, SUMS, AGAIN };
+
+// Threads of a workgroup at most, waves of a SIMD that its registers leave room for, the
+// bytes of x that a thread holds (backward with dy's and, for a whole sequence, the
+// fp32 numbers e beside them).
+struct ForwardWhole {
+    static constexpr int THREADS = 512, WAVES = 4, BYTES = 160;
 };
-struct Backward {
-    static constexpr bool BACKWARD = true;
-    static constexpr int THREADS = 512, BYTES = 160;
+struct BackwardWhole {
+    static constexpr int THREADS = 512, WAVES = 4, BYTES = 64;
 };
-struct BackwardOfWideRows {  // a row of a group needs more than 512 threads
-    static constexpr bool BACKWARD = true;
-    static constexpr int THREADS = 1024, BYTES = 64;
+struct Segments {
+    static constexpr int THREADS = 256, WAVES = 4, BYTES = 64;
+};
+struct SegmentsOfWideRows {  // a row of a group needs more than 256 threads
+    static constexpr int THREADS = 1024, WAVES = 4, BYTES = 64;
 };
 template <typename T, typename H>
 constexpr int Hold = H::BYTES / (V * sizeof(T));
@@ -154,12 +159,13 @@ struct Place {
 template <typename T, bool WIDE>
 struct Rows {
     char* base;
-    int64_t step;  // bytes
+    int64_t row, step;  // bytes
     uint32_t offset;
     int valid;
     __device__ __forceinline__ Rows(const void* p, int64_t stride, int64_t token, const Place& me)
-        : base(static_cast<char*>(const_cast<void*>(p)) + token * stride * (int64_t)sizeof(T)), step(me.slices * stride * (int64_t)sizeof(T)),
+        : base(static_cast<char*>(const_cast<void*>(p)) + token * stride * (int64_t)sizeof(T)), row(stride * (int64_t)sizeof(T)), step(me.slices * row),
           offset((uint32_t)me.slice * (uint32_t)stride * sizeof(T) + me.c * sizeof(T)), valid(me.valid) {}
+    __device__ __forceinline__ void skip(int tokens) { base += tokens * row; }
     __device__ __forceinline__ Raw<T> load(int k) const {
         return load_raw<T, WIDE>(reinterpret_cast<const T*>(base + k * step + offset), valid);
     }
@@ -171,6 +177,13 @@ struct Rows {
 __device__ __forceinline__ int64_t uniform(int64_t v) {
     const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
     return (int64_t)((uint64_t)hi << 32 | lo);
+}
+// The slot and the block of channels of a workgroup: all blocks of a slot on one XCD
+// (workgroups 8 apart) one after the other, as they share the rows' lines.
+__device__ __forceinline__ void place(const GroupNormArgs& a, int64_t& slot, int& block) {
+    const int64_t index = block_index(), at = index / 8;
+    slot = uniform(at / a.blocks) * 8 + index % 8;
+    block = __builtin_amdgcn_readfirstlane((int)(at % a.blocks));
 }
 __device__ __forceinline__ bool find_unit(const GroupNormArgs& a, int64_t slot, Unit& u) {
     if (slot >= a.seqs.slots || !unit_of(a.seqs, slot, u)) return false;
@@ -253,22 +266,21 @@ __device__ __forceinline__ bool speaks(const GroupNormArgs& a, const Place& me, 
     return me.slice == 0 && i < me.valid && (me.in_block + i) % a.per == 0;
 }
 
-// Forward. AGAIN: a segment of a long sequence whose mean and rstd are known; else
-// a sequence that a workgroup holds, or a long one's segment for its sums alone.
-template <typename T, int ACT, bool WIDE, bool AGAIN>
-__global__ __launch_bounds__(Forward::THREADS) void k_groupnorm_fwd(GroupNormArgs a) {
-    constexpr int N = Hold<T, Forward>;
+template <typename T, typename H, int ACT, bool WIDE, int MODE>
+__global__ __launch_bounds__(H::THREADS, H::WAVES) void k_groupnorm_fwd(GroupNormArgs a) {
+    constexpr int N = Hold<T, H>;
     extern __shared__ __attribute__((aligned(16))) float lds[];
-    const int64_t index = block_index(), slot = uniform(index / a.blocks);
+    int64_t slot;
+    int block;
+    place(a, slot, block);
     Unit u;
     if (!find_unit(a, slot, u)) return;
-    const bool part = u.from > 0 || u.to < u.len;
-    if (AGAIN && !part) return;
-    const int block = __builtin_amdgcn_readfirstlane((int)(index - slot * a.blocks)), per = a.per, n = (int)(u.to - u.from);
+    const int per = a.per, all = (int)(u.to - u.from);
     const Place me(a, block);
-    const Rows<T, WIDE> x(a.x.p, a.x.stride, u.t0 + u.from, me), y(a.y, a.channels, u.t0 + u.from, me);
+    Rows<T, WIDE> x(a.x.p, a.x.stride, u.t0 + u.from, me), y(a.y, a.channels, u.t0 + u.from, me);
     const int64_t stat = (int64_t)u.seq * a.groups;
     const bool mine = me.valid > 0;
+    int left = all, n = min(left, a.held);  // tokens from here on, those held now
     float mean[1][V] = {}, rstd[V];
     Raw<T> raw[N];
     // f(k) for the thread's vectors; what no thread of the workgroup has is skipped as a whole
@@ -278,15 +290,23 @@ __global__ __launch_bounds__(Forward::THREADS) void k_groupnorm_fwd(GroupNormArg
             if (k * me.slices < n)
                 if (mine && me.slice + k * me.slices < n) f(k);
     };
-    each([&](int k) { raw[k] = x.load(k); });
+    auto load = [&](int k) { raw[k] = x.load(k); };
+    auto next = [&]() {  // the tokens behind those held; false behind the last
+        x.skip(a.held);
+        y.skip(a.held);
+        left -= a.held;
+        n = min(left, a.held);
+        if (left > 0) each(load);
+        return left > 0;
+    };
+    each(load);
     float w[V], b[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         w[i] = i < me.valid ? a.w[me.c + i] : 0.0f;
         b[i] = i < me.valid ? a.b[me.c + i] : 0.0f;
     }
-    if constexpr (!AGAIN) {
-        const float inv = n > 0 ? 1.0f / ((float)n * (float)per) : 0.0f;
+    if constexpr (MODE != AGAIN) {
         float sum[1][V] = {};
         each([&](int k) {
             float v[V];
@@ -295,30 +315,34 @@ __global__ __launch_bounds__(Forward::THREADS) void k_groupnorm_fwd(GroupNormArg
             for (int i = 0; i < V; ++i) sum[0][i] += v[i];
         });
         group_sums<1>(a, me, sum, lds, mean);
-        float off[2][V] = {}, all[2][V];
+        float off[2][V] = {}, total[2][V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) mean[0][i] *= inv;
-        each([&](int k) {
-            float v[V];
-            unpack(raw[k], v);
+        for (int i = 0; i < V; ++i) mean[0][i] *= n > 0 ? 1.0f / ((float)n * (float)per) : 0.0f;
+        // distances from the mean of the tokens held first: those of a segment are not far from it beside their own spread
+        do {
+            each([&](int k) {
+                float v[V];
+                unpack(raw[k], v);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float d = v[i] - mean[0][i];
-                off[0][i] += d;
-                off[1][i] = fmaf(d, d, off[1][i]);
-            }
-        });
-        group_sums<2>(a, me, off, lds, all);
+                for (int i = 0; i < V; ++i) {
+                    const float d = v[i] - mean[0][i];
+                    off[0][i] += d;
+                    off[1][i] = fmaf(d, d, off[1][i]);
+                }
+            });
+        } while (MODE == SUMS && next());
+        group_sums<2>(a, me, off, lds, total);
+        const float inv = all > 0 ? 1.0f / ((float)all * (float)per) : 0.0f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float d = all[0][i] * inv;  // what rounding left of the mean
+            const float d = total[0][i] * inv;  // from there to the mean of all, and what rounding left
             mean[0][i] += d;
-            const float squares = fmaxf(fmaf(-all[0][i], d, all[1][i]), 0.0f);
-            if (all[1][i] != all[1][i]) mean[0][i] = all[1][i];
+            const float squares = fmaxf(fmaf(-total[0][i], d, total[1][i]), 0.0f);
+            if (total[1][i] != total[1][i]) mean[0][i] = total[1][i];
             rstd[i] = 1.0f / sqrtf(fmaf(squares, inv, a.eps));
             if (speaks(a, me, i)) {
                 const int g = (me.c + i) / per;
-                if (part) {
+                if (MODE == SUMS) {
                     float* s = a.sums + (u.slot * a.groups + g) * 2;
                     s[0] = mean[0][i];
                     s[1] = squares;
@@ -328,7 +352,7 @@ __global__ __launch_bounds__(Forward::THREADS) void k_groupnorm_fwd(GroupNormArg
                 }
             }
         }
-        if (part) return;
+        if (MODE == SUMS) return;
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -339,23 +363,24 @@ __global__ __launch_bounds__(Forward::THREADS) void k_groupnorm_fwd(GroupNormArg
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) rstd[i] *= w[i];
-    each([&](int k) {
-        float v[V];
-        unpack(raw[k], v);
+    do {
+        each([&](int k) {
+            float v[V];
+            unpack(raw[k], v);
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = activate<ACT, sizeof(T) == 4>(fmaf(v[i] - mean[0][i], rstd[i], b[i]));
-        y.store(k, v);
-    });
+            for (int i = 0; i < V; ++i) v[i] = activate<ACT, sizeof(T) == 4>(fmaf(v[i] - mean[0][i], rstd[i], b[i]));
+            y.store(k, v);
+        });
+    } while (MODE == AGAIN && next());
 }
 
-// mean and rstd of the long sequences from their segments': a wave a group.
+// mean and rstd of the sequences from their segments': a wave a group.
 __global__ __launch_bounds__(64) void k_groupnorm_join(GroupNormArgs a) {
     const int64_t index = block_index();
     const int seq = (int)(index / a.groups), g = (int)(index - (int64_t)seq * a.groups);
     if (seq >= a.seqs.n) return;
     Unit u;
     sequence_of(a.seqs, seq, u);
-    if (u.len <= a.seqs.seg) return;
     const int64_t count = (u.len + a.seqs.seg - 1) / a.seqs.seg, slot0 = u.t0 / a.seqs.seg + seq;
     const int per = a.per;
     auto sum = [&](auto f) {
@@ -368,22 +393,23 @@ __global__ __launch_bounds__(64) void k_groupnorm_join(GroupNormArgs a) {
         for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
         return s;
     };
-    const double mean = sum([](double n, double m, double) { return n * m; }) / (double)u.len;
+    const double mean = sum([](double n, double m, double) { return n * m; }) / (double)max(u.len, (int64_t)1);
     const double squares = sum([=](double n, double m, double q) { return q + n * per * (m - mean) * (m - mean); });
     if (threadIdx.x == 0) {
         a.mean[(int64_t)seq * a.groups + g] = (float)mean;
-        a.rstd[(int64_t)seq * a.groups + g] = (float)(1.0 / sqrt(squares / ((double)u.len * per) + (double)a.eps));
+        a.rstd[(int64_t)seq * a.groups + g] = (float)(1.0 / sqrt(squares / ((double)max(u.len, (int64_t)1) * per) + (double)a.eps));
     }
 }
 
-// Backward, AGAIN as in the forward pass (the group means of g and g c are known).
-template <typename T, typename H, int ACT, bool WIDE, bool AGAIN>
-__global__ __launch_bounds__(H::THREADS) void k_groupnorm_bwd(GroupNormArgs a) {
+template <typename T, typename H, int ACT, bool WIDE, int MODE>
+__global__ __launch_bounds__(H::THREADS, H::WAVES) void k_groupnorm_bwd(GroupNormArgs a) {
     constexpr int N = Hold<T, H>;
     extern __shared__ __attribute__((aligned(16))) float lds[];
-    const int64_t index = block_index(), first = uniform(index / a.blocks);
-    if (first >= a.parts) return;  // a launch has whole rows of workgroups
-    const int block = __builtin_amdgcn_readfirstlane((int)(index - first * a.blocks)), per = a.per;
+    int64_t first;
+    int block;
+    place(a, first, block);
+    if (first >= a.parts) return;
+    const int per = a.per;
     const Place me(a, block);
     const bool mine = me.valid > 0;
     float w[V], b[V], dw[V] = {}, db[V] = {};
@@ -395,11 +421,10 @@ __global__ __launch_bounds__(H::THREADS) void k_groupnorm_bwd(GroupNormArgs a) {
     for (int64_t slot = first; slot < a.seqs.slots; slot += a.parts) {
         Unit u;
         if (!find_unit(a, slot, u) || u.from >= u.to) continue;
-        const bool part = u.from > 0 || u.to < u.len;
-        if (AGAIN && !part) continue;
-        const int n = (int)(u.to - u.from);
+        const int all = (int)(u.to - u.from);
+        int left = all, n = min(left, a.held);
         const int64_t stat = (int64_t)u.seq * a.groups, token = u.t0 + u.from;
-        const Rows<T, WIDE> x(a.x.p, a.x.stride, token, me), dy(a.dy.p, a.dy.stride, token, me), dx(a.dx, a.channels, token, me);
+        Rows<T, WIDE> x(a.x.p, a.x.stride, token, me), dy(a.dy.p, a.dy.stride, token, me), dx(a.dx, a.channels, token, me);
         auto each = [&](auto f) {
 #pragma unroll
             for (int k = 0; k < N; ++k)
@@ -407,7 +432,17 @@ __global__ __launch_bounds__(H::THREADS) void k_groupnorm_bwd(GroupNormArgs a) {
                     if (mine && me.slice + k * me.slices < n) f(k);
         };
         Raw<T> rx[N], rg[N];
-        each([&](int k) { rx[k] = x.load(k), rg[k] = dy.load(k); });
+        auto load = [&](int k) { rx[k] = x.load(k), rg[k] = dy.load(k); };
+        auto next = [&]() {
+            x.skip(a.held);
+            dy.skip(a.held);
+            dx.skip(a.held);
+            left -= a.held;
+            n = min(left, a.held);
+            if (left > 0) each(load);
+            return left > 0;
+        };
+        each(load);
         float mean[V], rstd[V], m[2][V], s[2][V] = {}, e[N][V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -415,21 +450,30 @@ __global__ __launch_bounds__(H::THREADS) void k_groupnorm_bwd(GroupNormArgs a) {
             mean[i] = a.mean[stat + g];
             rstd[i] = a.rstd[stat + g];
         }
-        each([&](int k) {
-            float c[V];
+        auto parts = [&](int k, float (&c)[V], float (&e)[V]) {
             unpack(rx[k], c);
-            unpack(rg[k], e[k]);
+            unpack(rg[k], e);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 c[i] = (c[i] - mean[i]) * rstd[i];
-                e[k][i] = activate_back<ACT, sizeof(T) == 4>(e[k][i], fmaf(c[i], w[i], b[i]));
-                if constexpr (!AGAIN) {
-                    s[0][i] += e[k][i];
-                    s[1][i] = fmaf(e[k][i], c[i], s[1][i]);
-                }
+                e[i] = activate_back<ACT, sizeof(T) == 4>(e[i], fmaf(c[i], w[i], b[i]));
             }
-        });
-        if constexpr (!AGAIN) {
+        };
+        if constexpr (MODE != AGAIN) {
+            do {
+                each([&](int k) {
+                    float c[V], now[V];
+                    parts(k, c, now);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        if (MODE == WHOLE) e[k][i] = now[i];
+                        s[0][i] += now[i];
+                        s[1][i] = fmaf(now[i], c[i], s[1][i]);
+                    }
+                });
+            } while (MODE == SUMS && next());
+        }
+        if constexpr (MODE != AGAIN) {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 db[i] += s[0][i];
@@ -438,7 +482,7 @@ __global__ __launch_bounds__(H::THREADS) void k_groupnorm_bwd(GroupNormArgs a) {
                 s[1][i] *= w[i];
             }
             group_sums<2>(a, me, s, lds, m);
-            if (part) {
+            if (MODE == SUMS) {
 #pragma unroll
                 for (int i = 0; i < V; ++i)
                     if (speaks(a, me, i)) {
@@ -448,7 +492,7 @@ __global__ __launch_bounds__(H::THREADS) void k_groupnorm_bwd(GroupNormArgs a) {
                     }
                 continue;
             }
-            const float inv = 1.0f / ((float)n * (float)per);
+            const float inv = 1.0f / ((float)all * (float)per);
 #pragma unroll
             for (int i = 0; i < V; ++i) m[0][i] *= inv, m[1][i] *= inv;
         } else {
@@ -459,18 +503,23 @@ __global__ __launch_bounds__(H::THREADS) void k_groupnorm_bwd(GroupNormArgs a) {
                 m[1][i] = from[1];
             }
         }
-        each([&](int k) {
-            float c[V];
-            unpack(rx[k], c);
+        do {
+            each([&](int k) {
+                float c[V], now[V];
+                if constexpr (MODE == AGAIN) {
+                    parts(k, c, now);
+                } else {
+                    unpack(rx[k], c);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                c[i] = (c[i] - mean[i]) * rstd[i];
-                c[i] = rstd[i] * fmaf(-c[i], m[1][i], fmaf(e[k][i], w[i], -m[0][i]));
-            }
-            dx.store(k, c);
-        });
+                    for (int i = 0; i < V; ++i) c[i] = (c[i] - mean[i]) * rstd[i], now[i] = e[k][i];
+                }
+#pragma unroll
+                for (int i = 0; i < V; ++i) c[i] = rstd[i] * fmaf(-c[i], m[1][i], fmaf(now[i], w[i], -m[0][i]));
+                dx.store(k, c);
+            });
+        } while (MODE == AGAIN && next());
     }
-    if (AGAIN) return;
+    if (MODE == AGAIN) return;
     // the workgroup's share of dw and db, its slices added in order
     float* to = a.part + first * 2 * a.channels;
 #pragma unroll
@@ -488,14 +537,13 @@ __global__ __launch_bounds__(H::THREADS) void k_groupnorm_bwd(GroupNormArgs a) {
     }
 }
 
-// The group means of g and g c of the long sequences: a wave a group.
+// The group means of g and g c of the sequences: a wave a group.
 __global__ __launch_bounds__(64) void k_groupnorm_means(GroupNormArgs a) {
     const int64_t index = block_index();
     const int seq = (int)(index / a.groups), g = (int)(index - (int64_t)seq * a.groups);
     if (seq >= a.seqs.n) return;
     Unit u;
     sequence_of(a.seqs, seq, u);
-    if (u.len <= a.seqs.seg) return;
     const int64_t count = (u.len + a.seqs.seg - 1) / a.seqs.seg, slot0 = u.t0 / a.seqs.seg + seq;
     double s0 = 0.0, s1 = 0.0;
     for (int64_t k = threadIdx.x; k < count; k += 64) {
@@ -506,7 +554,7 @@ __global__ __launch_bounds__(64) void k_groupnorm_means(GroupNormArgs a) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) s0 += __shfl_xor(s0, o), s1 += __shfl_xor(s1, o);
     if (threadIdx.x == 0) {
-        const double size = (double)u.len * (a.channels / a.groups);
+        const double size = (double)max(u.len, (int64_t)1) * a.per;
         float* to = a.means + ((int64_t)seq * a.groups + g) * 2;
         to[0] = (float)(s0 / size);
         to[1] = (float)(s1 / size);
@@ -540,40 +588,61 @@ __global__ __launch_bounds__(1024) void k_groupnorm_dw(int channels, int64_t par
 
 bool aligned(const void* p, int to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
-// The shape of a pass: the threads of a workgroup and the tokens it holds.
-struct Shape {
-    int threads, held;
-};
-
+// Chooses channels of a workgroup, its threads and whether it holds whole sequences
+// (seqs.seg 0). A workgroup takes whole groups, about 128 bytes of a row; 64 or 32
+// where it then holds the longest sequence. Measured for the wide batch of 300 to 1200
+// tokens of 512 channels: see k_groupnorm_fwd and k_groupnorm_bwd.
 template <typename H>
-Shape shape_of(GroupNormArgs& a) {
-    const int per = a.channels / a.groups, es = a.dtype ? 2 : 4, hold = a.dtype ? Hold<bf16_t, H> : Hold<float, H>, most = H::THREADS;
-    a.per = per;
+int shape_of(GroupNormArgs& a) {
+    const int es = a.dtype ? 2 : 4, hold = a.dtype ? Hold<bf16_t, H> : Hold<float, H>;
+    a.per = a.channels / a.groups;
     // whole groups, in whole vectors where a few groups give them
-    int unit = per;
-    while (unit % V && unit + per <= std::min(256, a.channels)) unit += per;
-    if (unit % V) unit = per;
-    // about 128 bytes of a row; 64 where a workgroup then holds the longest sequence
+    int unit = a.per;
+    while (unit % V && unit + a.per <= std::min(256, a.channels)) unit += a.per;
+    if (unit % V) unit = a.per;
     auto with = [&](int bytes) {
         int block = unit;
         while (block * es < bytes && block + unit <= a.channels) block += unit;
         a.block = block;
         a.lanes = (block + V - 1) / V;
+        a.blocks = (a.channels + block - 1) / block;
+        return a.lanes <= H::THREADS ? H::THREADS / a.lanes * hold : 0;
     };
-    with(128);
-    if (most / a.lanes * hold < a.seqs.longest) {
-        with(64);
-        if (most / a.lanes * hold < a.seqs.longest) with(128);
-    }
-    a.blocks = (a.channels + a.block - 1) / a.block;
-    Shape s;
-    s.threads = 256;
-    while (s.threads < most && (s.threads < a.lanes || (int64_t)s.threads / a.lanes * hold < a.seqs.longest)) s.threads *= 2;
-    s.held = s.threads / a.lanes * hold;
-    a.seqs.seg = a.seqs.longest > s.held ? s.held : 0;
+    int held = 0;
+    for (int bytes : {128, 64, 32})
+        if ((held = with(bytes)) >= std::max<int64_t>(a.seqs.longest, 1)) break;
+    const bool whole = held >= std::max<int64_t>(a.seqs.longest, 1);
+    if (!whole) held = with(128);
+    int threads = H::THREADS;
+    while (whole && threads > 64 && threads / 2 >= a.lanes && (int64_t)threads / 2 / a.lanes * hold >= a.seqs.longest) threads /= 2;
+    // segments of up to eight times what a workgroup holds, where they still fill the chip several times: a workgroup's
+    // start (its sequence, weights, sums) takes about as long as 32 KB
+    const int64_t times = std::max<int64_t>(1, std::min<int64_t>(8, a.seqs.tokens * a.blocks / (std::max(held, 1) * (int64_t)4096)));
+    a.held = whole ? (int)std::max<int64_t>(a.seqs.longest, 1) : held;
+    a.seqs.seg = whole ? 0 : std::max<int64_t>(held * times, 1);
     a.seqs.slots = packed_slots(a.seqs, a.seqs.seg);
     a.parts = a.seqs.seg ? a.seqs.slots : std::min<int64_t>(a.seqs.slots, std::max(1, 4096 / a.blocks));
-    return s;
+    return threads;
+}
+
+// The same for segments, whatever the longest sequence.
+template <typename H>
+int segments_of(GroupNormArgs& a) {
+    const int64_t longest = a.seqs.longest;
+    a.seqs.longest = (int64_t)1 << 40;
+    const int threads = shape_of<H>(a);
+    a.seqs.longest = longest;
+    return threads;
+}
+
+// f with the way a pass holds its sequences (shape_of is done), and the threads of a workgroup.
+template <bool BACKWARD, typename F>
+auto with_hold(GroupNormArgs& a, F&& f) {
+    typedef std::conditional_t<BACKWARD, BackwardWhole, ForwardWhole> Whole;
+    const int threads = shape_of<Whole>(a);
+    if (!a.seqs.seg) return f(Whole(), threads);
+    if (a.per > V * Segments::THREADS) return f(SegmentsOfWideRows(), segments_of<SegmentsOfWideRows>(a));
+    return f(Segments(), segments_of<Segments>(a));
 }
 
 int64_t align256(int64_t bytes) { return (bytes + 255) & ~(int64_t)255; }
@@ -590,11 +659,9 @@ Plan plan_of(const GroupNormArgs& a, bool backward) {
     return p;
 }
 
-template <typename H>
-hipError_t launch(const GroupNormArgs& in, hipStream_t s) {
-    GroupNormArgs a = in;
-    constexpr bool BACKWARD = H::BACKWARD;
-    const Shape shape = shape_of<H>(a);
+template <bool BACKWARD, typename H>
+hipError_t launch(GroupNormArgs a, int threads, hipStream_t s) {
+    constexpr bool SEG = std::is_same_v<H, Segments> || std::is_same_v<H, SegmentsOfWideRows>;
     const Plan p = plan_of(a, BACKWARD);
     char* ws = static_cast<char*>(a.ws);
     a.sums = reinterpret_cast<float*>(ws + p.sums);
@@ -607,11 +674,11 @@ hipError_t launch(const GroupNormArgs& in, hipStream_t s) {
     else
         wide = wide && aligned(a.y, V * es);
     const bool whole = a.lanes <= 64 && 64 % a.lanes == 0;
-    const int rows = whole ? shape.threads / 64 : shape.threads / a.lanes;
-    const size_t sums = (size_t)2 * rows * a.lanes * V + 2 * (a.block / (a.channels / a.groups)), shares = (size_t)(shape.threads / a.lanes) * a.lanes * V;
+    const int rows = whole ? threads / 64 : threads / a.lanes;
+    const size_t sums = (size_t)2 * rows * a.lanes * V + 2 * (a.block / a.per), shares = (size_t)(threads / a.lanes) * a.lanes * V;
     const size_t lds = std::max(sums, BACKWARD ? shares : (size_t)0) * 4;
-    dim3 grid, again, join;
-    if (!grid_of((BACKWARD ? a.parts : a.seqs.slots) * a.blocks, shape.threads, grid) || !grid_of(a.seqs.slots * a.blocks, shape.threads, again) ||
+    dim3 grid, join;
+    if (!grid_of(((BACKWARD ? a.parts : a.seqs.slots) + 7) / 8 * 8 * a.blocks, threads, grid) ||
         !grid_of((int64_t)a.seqs.n * a.groups, 64, join))
         return hipErrorInvalidValue;
     auto run = [&](auto t, auto act, auto w) {
@@ -619,24 +686,25 @@ hipError_t launch(const GroupNormArgs& in, hipStream_t s) {
         constexpr int ACT = act();
         constexpr bool W = w();
         hipError_t e = hipSuccess;
-        if (a.seqs.n > 0) {
+        auto pass = [&](auto mode) {
             if constexpr (BACKWARD)
-                k_groupnorm_bwd<T, H, ACT, W, false><<<grid, shape.threads, lds, s>>>(a);
+                k_groupnorm_bwd<T, H, ACT, W, mode()><<<grid, threads, lds, s>>>(a);
             else
-                k_groupnorm_fwd<T, ACT, W, false><<<grid, shape.threads, lds, s>>>(a);
-            e = hipGetLastError();
-            if (e == hipSuccess && a.seqs.seg) {
+                k_groupnorm_fwd<T, H, ACT, W, mode()><<<grid, threads, lds, s>>>(a);
+            return hipGetLastError();
+        };
+        if (a.seqs.n > 0) {
+            if constexpr (!SEG) {
+                e = pass(std::integral_constant<int, WHOLE>());
+            } else {
+                e = pass(std::integral_constant<int, SUMS>());
+                if (e != hipSuccess) return e;
                 if constexpr (BACKWARD)
                     k_groupnorm_means<<<join, 64, 0, s>>>(a);
                 else
                     k_groupnorm_join<<<join, 64, 0, s>>>(a);
                 e = hipGetLastError();
-                if (e != hipSuccess) return e;
-                if constexpr (BACKWARD)
-                    k_groupnorm_bwd<T, H, ACT, W, true><<<again, shape.threads, lds, s>>>(a);
-                else
-                    k_groupnorm_fwd<T, ACT, W, true><<<again, shape.threads, lds, s>>>(a);
-                e = hipGetLastError();
+                if (e == hipSuccess) e = pass(std::integral_constant<int, AGAIN>());
             }
         }
         if (BACKWARD && e == hipSuccess) {
@@ -658,19 +726,21 @@ hipError_t launch(const GroupNormArgs& in, hipStream_t s) {
     return a.dtype ? with_act(bf16_t()) : with_act(float());
 }
 
-bool wide_rows(const GroupNormArgs& a) { return a.channels / a.groups > V * Backward::THREADS; }
-
 }  // namespace
 
 size_t groupnorm_workspace_bytes(const GroupNormArgs& in, bool backward) {
     GroupNormArgs a = in;
-    (void)(!backward ? shape_of<Forward>(a) : wide_rows(a) ? shape_of<BackwardOfWideRows>(a) : shape_of<Backward>(a));
-    return (size_t)std::max<int64_t>(plan_of(a, backward).total, 16);
+    auto plan = [&](auto, int) { return plan_of(a, backward).total; };
+    return (size_t)std::max<int64_t>(backward ? with_hold<true>(a, plan) : with_hold<false>(a, plan), 16);
 }
 
-hipError_t launch_groupnorm_fwd(const GroupNormArgs& a, hipStream_t s) { return launch<Forward>(a, s); }
-hipError_t launch_groupnorm_bwd(const GroupNormArgs& a, hipStream_t s) {
-    return wide_rows(a) ? launch<BackwardOfWideRows>(a, s) : launch<Backward>(a, s);
+hipError_t launch_groupnorm_fwd(const GroupNormArgs& in, hipStream_t s) {
+    GroupNormArgs a = in;
+    return with_hold<false>(a, [&](auto hold, int threads) { return launch<false, decltype(hold)>(a, threads, s); });
+}
+hipError_t launch_groupnorm_bwd(const GroupNormArgs& in, hipStream_t s) {
+    GroupNormArgs a = in;
+    return with_hold<true>(a, [&](auto hold, int threads) { return launch<true, decltype(hold)>(a, threads, s); });
 }
 
 }  // namespace mdl

@@ -243,16 +243,26 @@ def test_group_norm(lengths, channels, groups, layout, act, dtype):
     _check("y", op.forward(x), orc.group_norm(_np(x), *args), TOL[dtype])
     dx, dw, db = op.backward(dy)
     wx, ww, wb = orc.group_norm(_np(x), *args, dy=_np(dy))
-    near = np.abs(wx).max() < 1e-2 * np.abs(_np(dy)).max()  # groups of few values: dx is a difference of numbers of dy's size / dev
+    dx, dw, db, ndy = _np(dx), _np(dw), _np(db), np.abs(_np(dy))
+    # relu's derivative jumps at u = 0: where u is within its rounding (some twenty of 2^-24 of |c w| + |b| < 10) either side is right
+    edge = np.zeros(dx.shape)
+    if act == "relu":
+        u = orc.group_norm(_np(x), *args[:-1], None)
+        edge = (np.abs(u) < 1.2e-5) * ndy
+        dx = np.where(edge > 0, wx, dx)
+        edge_w = (edge * np.abs((u - _np(b)) / _np(w))).sum(0)
+    else:
+        edge_w = 0
+    near = np.abs(wx).max() < 1e-2 * ndy.max()  # groups of few values: dx is a difference of numbers of dy's size / dev
     if not near:
         _check("dx", dx, wx, 2 * TOL[dtype])
     else:
-        assert np.abs(_np(dx) - wx).max() <= 1e-4 * np.abs(_np(dy)).max() / np.sqrt(1e-5)
+        assert np.abs(dx - wx).max() <= 1e-4 * ndy.max() / np.sqrt(1e-5)
     if np.abs(ww).max() > 1e-3:
-        _check("dw", dw, ww, 1e-4)
+        assert np.all(np.abs(dw - ww) <= 1e-4 * np.abs(ww).max() + edge_w)
     # db is a sum of T numbers of at most 1.1 |dy|, each off by some eight roundings of 2^-24 of itself; where they cancel,
     # that is what the sum may be off by
-    assert np.all(np.abs(_np(db) - wb) <= 1e-6 * (1.1 * np.abs(_np(dy)).sum(0)))
+    assert np.all(np.abs(db - wb) <= 1e-6 * (1.1 * ndy.sum(0)) + edge.sum(0))
 
 
 @pytest.mark.parametrize("mean", [100.0, -3000.0])
