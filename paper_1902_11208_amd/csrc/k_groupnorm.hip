@@ -93,19 +93,19 @@ enum { WHOLE, SUMS, AGAIN };
 // bytes of x that a thread holds (backward with dy's and, for a whole sequence, the
 // fp32 numbers e beside them).
 struct ForwardWhole {
-    static constexpr int THREADS = 512, WAVES = 4, BYTES = 160;
+    static constexpr int THREADS = 512, WAVES = 4, BYTES[2] = {160, 160}, LEAST = 64;  // bytes of fp32 and bf16; of a row at least
 };
 struct BackwardWhole {
-    static constexpr int THREADS = 512, WAVES = 4, BYTES = 64;
+    static constexpr int THREADS = 256, WAVES = 2, BYTES[2] = {160, 96}, LEAST = 64;
 };
 struct Segments {
-    static constexpr int THREADS = 256, WAVES = 4, BYTES = 64;
+    static constexpr int THREADS = 256, WAVES = 4, BYTES[2] = {64, 64}, LEAST = 128;
 };
 struct SegmentsOfWideRows {  // a row of a group needs more than 256 threads
-    static constexpr int THREADS = 1024, WAVES = 4, BYTES = 64;
+    static constexpr int THREADS = 1024, WAVES = 4, BYTES[2] = {64, 64}, LEAST = 128;
 };
 template <typename T, typename H>
-constexpr int Hold = H::BYTES / (V * sizeof(T));
+constexpr int Hold = H::BYTES[sizeof(T) == 2] / (V * sizeof(T));
 
 // EXACT (fp32 storage): to an ulp or two; else the product with log2(e) is rounded,
 // |u| 2^-24 off, far below a bf16 u's own rounding.
@@ -589,8 +589,8 @@ __global__ __launch_bounds__(1024) void k_groupnorm_dw(int channels, int64_t par
 bool aligned(const void* p, int to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
 // Chooses channels of a workgroup, its threads and whether it holds whole sequences
-// (seqs.seg 0). A workgroup takes whole groups, about 128 bytes of a row; 64 or 32
-// where it then holds the longest sequence. Measured for the wide batch of 300 to 1200
+// (seqs.seg 0). A workgroup takes whole groups, about 128 bytes of a row; 64 where
+// it then holds the longest sequence. Measured for the wide batch of 300 to 1200
 // tokens of 512 channels: see k_groupnorm_fwd and k_groupnorm_bwd.
 template <typename H>
 int shape_of(GroupNormArgs& a) {
@@ -609,7 +609,7 @@ int shape_of(GroupNormArgs& a) {
         return a.lanes <= H::THREADS ? H::THREADS / a.lanes * hold : 0;
     };
     int held = 0;
-    for (int bytes : {128, 64, 32})
+    for (int bytes = 128; bytes >= H::LEAST; bytes /= 2)
         if ((held = with(bytes)) >= std::max<int64_t>(a.seqs.longest, 1)) break;
     const bool whole = held >= std::max<int64_t>(a.seqs.longest, 1);
     if (!whole) held = with(128);
@@ -617,7 +617,7 @@ int shape_of(GroupNormArgs& a) {
     while (whole && threads > 64 && threads / 2 >= a.lanes && (int64_t)threads / 2 / a.lanes * hold >= a.seqs.longest) threads /= 2;
     // segments of up to eight times what a workgroup holds, where they still fill the chip several times: a workgroup's
     // start (its sequence, weights, sums) takes about as long as 32 KB
-    const int64_t times = std::max<int64_t>(1, std::min<int64_t>(8, a.seqs.tokens * a.blocks / (std::max(held, 1) * (int64_t)4096)));
+    const int64_t times = std::max<int64_t>(1, std::min<int64_t>(8, a.seqs.tokens * a.blocks / (std::max(held, 1) * (int64_t)2048)));
     a.held = whole ? (int)std::max<int64_t>(a.seqs.longest, 1) : held;
     a.seqs.seg = whole ? 0 : std::max<int64_t>(held * times, 1);
     a.seqs.slots = packed_slots(a.seqs, a.seqs.seg);
@@ -676,6 +676,7 @@ hipError_t launch(GroupNormArgs a, int threads, hipStream_t s) {
     const bool whole = a.lanes <= 64 && 64 % a.lanes == 0;
     const int rows = whole ? threads / 64 : threads / a.lanes;
     const size_t sums = (size_t)2 * rows * a.lanes * V + 2 * (a.block / a.per), shares = (size_t)(threads / a.lanes) * a.lanes * V;
+    if (a.seqs.slots * a.blocks <= 512) a.seqs.order = nullptr;  // all start at once: the order's load would only be waited for
     const size_t lds = std::max(sums, BACKWARD ? shares : (size_t)0) * 4;
     dim3 grid, join;
     if (!grid_of(((BACKWARD ? a.parts : a.seqs.slots) + 7) / 8 * 8 * a.blocks, threads, grid) ||

@@ -205,10 +205,13 @@ __device__ __forceinline__ int64_t uniform(int64_t v) {
 }
 
 // The workgroup's unit and block of channels; false where there is none.
+template <bool SUMS>
 __device__ __forceinline__ bool find_unit(const RecurrenceArgs& a, int blocks, Unit& u, int& block) {
-    const int64_t index = block_index(), slot = uniform(index / blocks);
+    const int64_t index = block_index();
+    int64_t slot = uniform(index / blocks);
     block = __builtin_amdgcn_readfirstlane((int)(index - slot * blocks));
-    if (slot >= a.seqs.slots || !unit_of(a.seqs, slot, u)) return false;
+    if (!SUMS && a.seqs.seg) slot = a.seqs.slots - 1 - slot;  // what the pass for the sums read last is still in the caches
+    if (slot < 0 || slot >= a.seqs.slots || !unit_of(a.seqs, slot, u)) return false;
     u.seq = __builtin_amdgcn_readfirstlane(u.seq);
     u.t0 = uniform(u.t0);
     u.len = uniform(u.len);
@@ -307,7 +310,7 @@ __global__ __launch_bounds__(threads_of<CL>()) void k_recurrence_fwd(RecurrenceA
     __shared__ Shared<CL, 2> lds;
     Unit u;
     int block;
-    if (!find_unit(a, blocks, u, block)) return;
+    if (!find_unit<SUMS>(a, blocks, u, block)) return;
     const Place me(a.channels, CL, block);
     const Rows<T, WIDE> z(a.z, u.t0, me.c, me.valid), x(a.x, u.t0, me.c, me.valid);
     const Out<T, WIDE> out(a.h, u.t0, a.channels, me.c, me.valid);
@@ -417,7 +420,7 @@ __global__ __launch_bounds__(threads_of<CL>()) void k_recurrence_bwd(RecurrenceA
     __shared__ Shared<CL, 3> lds;
     Unit u;
     int block;
-    if (!find_unit(a, blocks, u, block)) return;
+    if (!find_unit<SUMS>(a, blocks, u, block)) return;
     const Place me(a.channels, CL, block);
     const Rows<T, WIDE> z(a.z, u.t0, me.c, me.valid), x(a.x, u.t0, me.c, me.valid), g(a.dh, u.t0, me.c, me.valid);
     const Out<T, WIDE> out_z(a.dz, u.t0, a.channels, me.c, me.valid), out_x(a.dx, u.t0, a.channels, me.c, me.valid);
@@ -584,21 +587,39 @@ __global__ __launch_bounds__(64) void k_recurrence_join(RecurrenceArgs a, int bl
     const T* z = static_cast<const T*>(a.z.p) + u.t0 * a.z.stride + c;
     const RowView& other = REVERSE ? a.dh : a.x;
     const T* x = static_cast<const T*>(other.p) + u.t0 * other.stride + c;
-    constexpr int AHEAD = 8;  // segments whose sums are loaded together
+    constexpr int AHEAD = 16;  // segments together: loaded ahead, and joined without a branch where none is unsafe
+    float next_a[AHEAD], next_b[AHEAD];
+    auto load = [&](int64_t k0) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int64_t k = min(k0 + i, count - 1), at = (slot0 + (REVERSE ? count - 1 - k : k)) * a.channels + c;
+            next_a[i] = a.sums[at];
+            next_b[i] = a.sums[all + at];
+        }
+    };
+    auto start_of = [&](int64_t k) -> float& { return a.starts[(slot0 + (REVERSE ? count - 2 - k : k + 1)) * a.channels + c]; };  // behind segment k
+    if (count > 1) load(0);
     for (int64_t k0 = 0; k0 + 1 < count; k0 += AHEAD) {
+        const int n = (int)min(count - 1 - k0, (int64_t)AHEAD);  // nothing starts behind the last one
         float A[AHEAD], B[AHEAD];
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            const int64_t k = min(k0 + i, count - 1);
-            const int64_t at = (slot0 + (REVERSE ? count - 1 - k : k)) * a.channels + c;
-            A[i] = a.sums[at];
-            B[i] = a.sums[all + at];
-        }
+        for (int i = 0; i < AHEAD; ++i) A[i] = next_a[i], B[i] = next_b[i];
+        if (k0 + AHEAD + 1 < count) load(k0 + AHEAD);
+        const float from = h;
+        bool walk = false;
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            const int64_t k = k0 + i, j = REVERSE ? count - 1 - k : k;
-            if (k + 1 >= count) break;  // nothing starts behind the last one
-            const float next = fmaf(A[i], h, B[i]);
+        for (int i = 0; i < AHEAD; ++i)
+            if (i < n) {
+                const float next = fmaf(A[i], h, B[i]);
+                walk = walk || unsafe(h, next);
+                h = next;
+                start_of(k0 + i) = h;
+            }
+        if (!walk) continue;
+        h = from;
+        for (int i = 0; i < n; ++i) {  // each from its sums if that is safe, else token by token
+            const int64_t j = REVERSE ? count - 1 - k0 - i : k0 + i, at = (slot0 + j) * a.channels + c;
+            const float next = fmaf(a.sums[at], h, a.sums[all + at]);
             if (unsafe(h, next)) {
                 const int64_t lo = j * a.seqs.seg, hi = min(u.len, lo + a.seqs.seg);
                 for (int64_t s = lo; s < hi; ++s) {
@@ -611,7 +632,7 @@ __global__ __launch_bounds__(64) void k_recurrence_join(RecurrenceArgs a, int bl
             } else {
                 h = next;
             }
-            a.starts[(slot0 + (REVERSE ? j - 1 : j + 1)) * a.channels + c] = h;
+            start_of(k0 + i) = h;
         }
     }
 }
@@ -709,7 +730,7 @@ RecurrenceArgs plan(const RecurrenceArgs& in) {
 
 template <bool BACKWARD>
 hipError_t launch(const RecurrenceArgs& in, hipStream_t s) {
-    const RecurrenceArgs a = plan(in);
+    RecurrenceArgs a = plan(in);
     if (a.seqs.n == 0) return hipSuccess;
     const int es = a.dtype ? 2 : 4;
     bool wide = a.channels % V == 0 && wide_rows(a.z, es) && wide_rows(a.x, es);
@@ -724,6 +745,7 @@ hipError_t launch(const RecurrenceArgs& in, hipStream_t s) {
             constexpr int CL = lanes();
             constexpr bool SIG = sig(), W = w();
             const int blocks = (vecs + CL - 1) / CL;
+            if (a.seqs.slots * blocks <= 512) a.seqs.order = nullptr;  // all start at once: the order's load would only be waited for
             dim3 grid;
             if (!grid_of(a.seqs.slots * blocks, threads_of<CL>(), grid)) return hipErrorInvalidValue;
             if (a.seqs.seg) {

@@ -44,7 +44,7 @@ struct Operand {
 struct RowInfo {
     float others, scale;  // o log2(e) and c
     int target;           // -1: the row is left out
-    int pad;
+    float rest;           // what rounding -c to bf16 left of it
 };
 
 enum { LOGSUM, GRADIENT, PLANES };
@@ -461,14 +461,69 @@ __global__ __launch_bounds__(256) void k_row_info(VocabularyArgs a, RowInfo* inf
     const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (r >= a.rows) return;
     const int64_t t = a.targets[r];
-    RowInfo v = {0.0f, 0.0f, -1, 0};
+    RowInfo v = {0.0f, 0.0f, -1, 0.0f};
     if (t >= 0 && t < a.vocab) {
         const float others = a.stats[r], d = sum_minus(others, a.stats[a.rows + r]);
         v.others = others == -__builtin_huge_valf() ? 0.0f : others;  // then there is no q
         v.scale = a.dloss[r] * (d < 0.0f ? expf(d) / (1.0f + expf(d)) : 1.0f / (1.0f + expf(-d)));
         v.target = (int)t;
+        v.rest = bf2f(f2bf(v.scale)) - v.scale;
     }
     info[r] = v;
+}
+
+// The targets' shares of dW, -c x, enter its product with c rounded to bf16. Where all
+// losses have one gradient, c is nearly one number and its rounding, up to 2^-8 of it,
+// would be a bias of all of dW; so what it left is added, sum over the rows of a
+// target of rest x. It is small beside the share, so 32-bit fixed-point numbers hold it
+// (rows of at most the largest rest |x|, 2^30 for all rows together: 2^-16 of the
+// largest one's rest with 16384 rows), and their sums do not depend on the atomics' order.
+__global__ __launch_bounds__(256) void k_largest_rest(RowView x, int64_t rows, int dim, const RowInfo* info, uint32_t* most) {
+    __shared__ float lds[4];
+    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63;
+    float top = 0.0f;
+    for (int64_t r = (int64_t)blockIdx.x * 4 + wave; r < rows; r += (int64_t)gridDim.x * 4) {
+        const RowInfo f = info[r];
+        if (f.target < 0) continue;
+        float row = 0.0f;
+        for (int c = lane; c < dim; c += 64) row = fmaxf(row, fabsf(St<bf16_t>::ld1(static_cast<const bf16_t*>(x.p) + r * x.stride + c)));
+        row *= fabsf(f.rest);
+        if (row < __builtin_huge_valf()) top = fmaxf(top, row);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    if (lane == 0) lds[wave] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
+    if (threadIdx.x == 0 && top > 0.0f) atomicMax(most, __float_as_uint(top));  // positive floats are ordered as their bits
+}
+
+// The power of two that takes the rests to fixed point.
+__device__ __forceinline__ float fixed_point(uint32_t most, int64_t rows) {
+    const float all = __uint_as_float(most) * (float)rows;
+    if (!(all > 0x1p-90f && all < 0x1p90f)) return 0.0f;  // none, or beyond what this is for
+    int e;
+    (void)frexpf(all, &e);
+    return ldexpf(1.0f, 30 - e);
+}
+
+__global__ __launch_bounds__(256) void k_clear(u32x4* p, int64_t n) {
+    const int64_t i = block_index() * 256 + threadIdx.x;
+    if (i < n) p[i] = u32x4{0, 0, 0, 0};
+}
+
+__global__ __launch_bounds__(256) void k_add_rests(RowView x, int64_t rows, int dim, const RowInfo* info, const uint32_t* most, int64_t first,
+                                                   int64_t n, int* rests) {
+    const int64_t r = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+    if (r >= rows) return;
+    const RowInfo f = info[r];
+    const float scale = fixed_point(*most, rows);
+    if (f.target < first || f.target >= first + n || scale == 0.0f) return;
+    int* to = rests + (f.target - first) * dim;
+    for (int c = threadIdx.x & 63; c < dim; c += 64) {
+        const float v = f.rest * St<bf16_t>::ld1(static_cast<const bf16_t*>(x.p) + r * x.stride + c) * scale;
+        if (fabsf(v) < 0x1p30f) atomicAdd(to + c, (int)rintf(v));
+    }
 }
 
 // pieces of v at p, p + plane, ...
@@ -531,10 +586,11 @@ __global__ __launch_bounds__(256) void k_pack_transposed(RowView src, int64_t ro
     }
 }
 
-// The planes of a product together, in order, times the row's scale (info), as
-// stored. Rows without a scale come as one.
+// The planes of a product together, in order, with the rests (above) and times the
+// row's scale (info), as stored. Rows without a scale come as one.
 template <typename T, bool VEC>
-__global__ __launch_bounds__(256) void k_finish(const float* planes, int splits, int64_t rows, int64_t cols, int blocks, const RowInfo* info, T* out) {
+__global__ __launch_bounds__(256) void k_finish(const float* planes, int splits, int64_t rows, int64_t cols, int blocks, const RowInfo* info,
+                                                const int* rests, const uint32_t* most, int64_t all_rows, T* out) {
     const int64_t index = block_index(), r = index / blocks, c = ((index - r * blocks) * 256 + threadIdx.x) * 4;
     if (r >= rows || c >= cols) return;
     floatx4 s = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -549,6 +605,12 @@ __global__ __launch_bounds__(256) void k_finish(const float* planes, int splits,
             for (int i = 0; i < 4; ++i)
                 if (i < n) s[i] += p[i];
         }
+    }
+    if (rests) {
+        const float scale = fixed_point(*most, all_rows), back = scale > 0.0f ? 1.0f / scale : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < n) s[i] += (float)rests[r * cols + c + i] * back;
     }
     if (info) {
         const RowInfo f = info[r];
@@ -624,7 +686,7 @@ struct Plan {
     int64_t piece, dimp, rowsp;   // vocabulary rows of a piece, dim and rows in whole steps
     int pieces;                   // of an operand's numbers
     bool pack_x, pack_w;
-    int64_t x, w, part, info, xt, wt, q, qt, dx, dw, total;  // offsets
+    int64_t x, w, part, info, most, rests, xt, wt, q, qt, dx, dw, total;  // offsets
     int pairs() const { return pieces == 1 ? 1 : 6; }
     int splits_dx(const VocabularyArgs& a) const { return splits_of(a.rows, a.dim, piece / BK * pairs()); }
     int splits_dw(const VocabularyArgs& a, int64_t n) const { return splits_of(n, a.dim, rowsp / BK * pairs()); }
@@ -658,6 +720,8 @@ Plan plan_of(const VocabularyArgs& a, bool backward) {
         p.part = take((a.vocab / 128 + 2 + (a.vocab + p.piece - 1) / p.piece) * a.rows * 8);
     } else {
         p.info = take(a.rows * (int64_t)sizeof(RowInfo));
+        p.most = take(16);
+        if (p.pieces == 1) p.rests = take(std::min<int64_t>(p.piece, a.vocab) * a.dim * 4);
         p.xt = take(a.dim * p.rowsp * 2 * p.pieces);
         p.wt = take(a.dim * p.piece * 2 * p.pieces);
         p.q = take(p.rowsp * p.piece * 2 * p.pieces);
@@ -694,15 +758,24 @@ hipError_t pack_transposed(const RowView& v, int64_t rows, int cols, const int64
 }
 
 template <typename T>
-hipError_t finish(const float* planes, int splits, int64_t rows, int64_t cols, const RowInfo* info, T* out, hipStream_t s) {
+hipError_t finish(const float* planes, int splits, int64_t rows, int64_t cols, const RowInfo* info, const int* rests, const uint32_t* most,
+                  int64_t all_rows, T* out, hipStream_t s) {
     const int64_t blocks = (cols + 1023) / 1024;
     dim3 grid;
     if (blocks > 0x7fffffff || !grid_of(rows * blocks, 256, grid)) return hipErrorInvalidValue;
     // a piece's rows of dW start anywhere in dW where dim is odd
     if (cols % 4 == 0 && (reinterpret_cast<uintptr_t>(out) & (4 * sizeof(T) - 1)) == 0)
-        k_finish<T, true><<<grid, 256, 0, s>>>(planes, splits, rows, cols, (int)blocks, info, out);
+        k_finish<T, true><<<grid, 256, 0, s>>>(planes, splits, rows, cols, (int)blocks, info, rests, most, all_rows, out);
     else
-        k_finish<T, false><<<grid, 256, 0, s>>>(planes, splits, rows, cols, (int)blocks, info, out);
+        k_finish<T, false><<<grid, 256, 0, s>>>(planes, splits, rows, cols, (int)blocks, info, rests, most, all_rows, out);
+    return hipGetLastError();
+}
+
+hipError_t clear(void* p, int64_t bytes, hipStream_t s) {
+    const int64_t n = (bytes + 15) / 16;
+    dim3 grid;
+    if (!grid_of((n + 255) / 256, 256, grid)) return hipErrorInvalidValue;
+    k_clear<<<grid, 256, 0, s>>>(static_cast<u32x4*>(p), n);
     return hipGetLastError();
 }
 
@@ -769,6 +842,14 @@ hipError_t backward(const VocabularyArgs& a, hipStream_t s) {
         k_row_info<<<(unsigned)((a.rows + 255) / 256), 256, 0, s>>>(a, info);
         OK_OR_RETURN(hipGetLastError());
     }
+    uint32_t* most = reinterpret_cast<uint32_t*>(ws + p.most);
+    const bool exact_c = sizeof(T) == 2 && a.rows > 0;
+    const unsigned row_waves = (unsigned)((a.rows + 3) / 4);
+    if (exact_c) {
+        OK_OR_RETURN(clear(most, 16, s));
+        k_largest_rest<<<std::min(row_waves, 512u), 256, 0, s>>>(a.x, a.rows, a.dim, info, most);
+        OK_OR_RETURN(hipGetLastError());
+    }
     Product logits{};
     if (a.rows > 0) OK_OR_RETURN(x_operand<T>(a, p, logits.a, s));
     const int64_t xt_plane = a.dim * p.rowsp;
@@ -811,10 +892,17 @@ hipError_t backward(const VocabularyArgs& a, hipStream_t s) {
         v.out = f32(p.dw);
         v.ldo = a.dim;
         OK_OR_RETURN(product<PLANES>(v, s));
-        OK_OR_RETURN(finish<T>(v.out, v.splits, 1, n * a.dim, nullptr, dw + first * a.dim, s));
+        int* rests = nullptr;
+        if (exact_c) {
+            rests = reinterpret_cast<int*>(ws + p.rests);
+            OK_OR_RETURN(clear(rests, n * a.dim * 4, s));
+            k_add_rests<<<row_waves, 256, 0, s>>>(a.x, a.rows, a.dim, info, most, first, n, rests);
+            OK_OR_RETURN(hipGetLastError());
+        }
+        OK_OR_RETURN(finish<T>(v.out, v.splits, 1, n * a.dim, nullptr, rests, most, a.rows, dw + first * a.dim, s));
     }
     if (a.rows == 0) return hipSuccess;
-    return finish<T>(f32(p.dx), p.splits_dx(a), a.rows, a.dim, info, dx, s);
+    return finish<T>(f32(p.dx), p.splits_dx(a), a.rows, a.dim, info, nullptr, nullptr, 0, dx, s);
 }
 
 }  // namespace

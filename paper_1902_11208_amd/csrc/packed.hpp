@@ -50,13 +50,15 @@ __device__ __forceinline__ bool unit_of(const Packed& p, int64_t slot, Unit& u) 
         sequence_of(p, seq, u);
         return true;
     }
-    int lo = 0, hi = p.n - 1;  // the last sequence whose first slot is not behind `slot`
+    // The last sequence whose first slot is not behind `slot`: a wave looks at 64 places at once, as a load
+    // depends on the one before (128 sequences: two loads, not seven). Called by whole waves.
+    int lo = 0, hi = p.n - 1;
     while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (min(max(p.offsets[mid], (int64_t)0), p.tokens) / p.seg + mid <= slot)
-            lo = mid;
-        else
-            hi = mid - 1;
+        const int step = (hi - lo + 63) / 64, at = lo + ((int)(threadIdx.x & 63) + 1) * step;
+        const bool before = at <= hi && at > lo && min(max(p.offsets[at], (int64_t)0), p.tokens) / p.seg + at <= slot;
+        const int steps = __popcll(__ballot(before));
+        hi = min(hi, lo + (steps + 1) * step - 1);
+        lo += steps * step;
     }
     sequence_of(p, lo, u);
     u.from = (slot - lo - u.t0 / p.seg) * p.seg;
