@@ -416,7 +416,7 @@ __global__ __launch_bounds__(threads_of<CL>()) void k_recurrence_fwd(RecurrenceA
 
 // Backward pass. SUMS: only what the unit maps the adjoint behind it to.
 template <typename T, bool SIG, bool WIDE, int CL, bool SUMS>
-__global__ __launch_bounds__(threads_of<CL>()) void k_recurrence_bwd(RecurrenceArgs a, int blocks) {
+__global__ __launch_bounds__(threads_of<CL>(), sizeof(T) == 2 ? 4 : 2) void k_recurrence_bwd(RecurrenceArgs a, int blocks) {
     __shared__ Shared<CL, 3> lds;
     Unit u;
     int block;
@@ -456,17 +456,22 @@ __global__ __launch_bounds__(threads_of<CL>()) void k_recurrence_bwd(RecurrenceA
     int parity = 0;
     for (; u.from < u.to && tile >= u.from; tile -= kRecurrenceTile, parity ^= 1) {
         const int n = (int)min(u.to - tile, (int64_t)kRecurrenceTile), mine = n - me.slice * L;
-        // rest: 1 - f (or 1); in: x, then dz without G
-        float f[L][V], in[L][V], rest[L][V], dy[L][V], pa[V], pb[V], pr[V];
+        // rest: 1 - f (or 1); cx, cg: x and dh as loaded, the registers of the fp32 numbers would halve the waves of bf16
+        float f[L][V], rest[L][V], pa[V], pb[V], pr[V];
+        Raw<T> cx[L], cg[L];
         auto sums = [&](auto whole) {
 #pragma unroll
             for (int i = 0; i < V; ++i) pa[i] = 1.0f, pb[i] = 0.0f, pr[i] = 0.0f;
 #pragma unroll
             for (int l = 0; l < L; ++l) {
-                float vz[V];
+                float vz[V], vx[V];
+                const bool real = whole() || l < mine;
                 unpack(rz[l], vz);
-                unpack(rg[l], dy[l]);
-                if constexpr (!SUMS) unpack(rx[l], in[l]);
+                cg[l] = real ? rg[l] : Raw<T>{};
+                if constexpr (!SUMS) {
+                    cx[l] = real ? rx[l] : Raw<T>{};
+                    unpack(cx[l], vx);
+                }
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     if constexpr (SIG) {
@@ -475,9 +480,9 @@ __global__ __launch_bounds__(threads_of<CL>()) void k_recurrence_bwd(RecurrenceA
                         f[l][i] = vz[i];
                         rest[l][i] = 1.0f;
                     }
-                    if (!whole() && l >= mine) f[l][i] = 1.0f, in[l][i] = rest[l][i] = dy[l][i] = 0.0f;
+                    if (!real) f[l][i] = 1.0f, rest[l][i] = 0.0f;
                     pa[i] *= f[l][i];
-                    if constexpr (!SUMS) pb[i] = fmaf(f[l][i], pb[i], SIG || !whole() ? rest[l][i] * in[l][i] : in[l][i]);
+                    if constexpr (!SUMS) pb[i] = fmaf(f[l][i], pb[i], SIG ? rest[l][i] * vx[i] : vx[i]);
                 }
             }
         };
@@ -486,9 +491,12 @@ __global__ __launch_bounds__(threads_of<CL>()) void k_recurrence_bwd(RecurrenceA
         else
             sums(std::false_type());
 #pragma unroll
-        for (int l = L - 1; l >= 0; --l)
+        for (int l = L - 1; l >= 0; --l) {
+            float dy[V];
+            unpack(cg[l], dy);
 #pragma unroll
-            for (int i = 0; i < V; ++i) pr[i] = f[l][i] * (dy[l][i] + pr[i]);
+            for (int i = 0; i < V; ++i) pr[i] = f[l][i] * (dy[i] + pr[i]);
+        }
         const float from[V] = {mark[0], mark[1]};
         if (tile > u.from) load(tile - kRecurrenceTile);
 #pragma unroll
@@ -525,26 +533,30 @@ __global__ __launch_bounds__(threads_of<CL>()) void k_recurrence_bwd(RecurrenceA
                 s[0] = carry.x, s[1] = carry.y;
                 walk_reverse<T, SIG, WIDE>(z, g, min(tile + (me.slice + 1) * L, tile + n), tile + n, s);
             }
+            float in[L][V];  // dz without G
 #pragma unroll
-            for (int l = 0; l < L; ++l)
+            for (int l = 0; l < L; ++l) {
+                float vx[V];
+                unpack(cx[l], vx);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const float xv = in[l][i];
                     if constexpr (SIG) {
-                        in[l][i] = (h[i] - xv) * (f[l][i] * rest[l][i]);
-                        h[i] = fmaf(f[l][i], h[i], rest[l][i] * xv);
+                        in[l][i] = (h[i] - vx[i]) * (f[l][i] * rest[l][i]);
+                        h[i] = fmaf(f[l][i], h[i], rest[l][i] * vx[i]);
                     } else {
                         in[l][i] = h[i];
-                        h[i] = fmaf(f[l][i], h[i], xv);
+                        h[i] = fmaf(f[l][i], h[i], vx[i]);
                     }
                 }
+            }
             auto go = [&](auto whole) {
 #pragma unroll
                 for (int l = L - 1; l >= 0; --l) {
-                    float oz[V], ox[V];
+                    float oz[V], ox[V], dy[V];
+                    unpack(cg[l], dy);
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        const float G = dy[l][i] + s[i];
+                        const float G = dy[i] + s[i];
                         oz[i] = G * in[l][i];
                         ox[i] = SIG ? G * rest[l][i] : G;
                         s[i] = f[l][i] * G;

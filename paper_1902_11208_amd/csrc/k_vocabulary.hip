@@ -349,8 +349,8 @@ __global__ __launch_bounds__(S::THREADS) void k_product(Product g) {
         int* target = reinterpret_cast<int*>(t0.a);  // of the tile's rows, counted from the tile's first column
         float2* sums = reinterpret_cast<float2*>(t1.a);  // [BN / WN][BM]
         for (int r = threadIdx.x; r < S::BM; r += S::THREADS) {
-            const int64_t t = m0 + r < rows ? g.targets[m0 + r] - g.first - n0 : -1;
-            target[r] = t >= 0 && t < S::BN && t < cols - n0 ? (int)t : -(1 << 20);
+            const int64_t t = m0 + r < rows ? g.targets[m0 + r] : -1, at = t < 0 ? -1 : t - g.first - n0;
+            target[r] = at >= 0 && at < S::BN && at < cols - n0 ? (int)at : -(1 << 20);
         }
         __syncthreads();
         const bool ragged = n0 + S::BN > cols;
