@@ -47,7 +47,7 @@ struct RowInfo {
     float rest;           // what rounding -c to bf16 left of it
 };
 
-enum { LOGSUM, GRADIENT, PLANES };
+enum { LOGSUM, GRADIENT, PLANES, RESULT };
 
 struct Product {
     Operand a, b;
@@ -69,6 +69,12 @@ struct Product {
     float* out;         // [splits][a.rows][ldo]
     int64_t ldo;
     int add;            // to what is there
+    // RESULT: [a.rows][ldo] as stored, with the rests and times the rows' scale (k_finish)
+    void* result;
+    const RowInfo* rows;
+    const int* rests;
+    const uint32_t* most;
+    int64_t all_rows;
 };
 
 // A tile of a product: BM x BN, waves of WM x WN.
@@ -178,6 +184,15 @@ __device__ __forceinline__ float finite_or_0(float m) { return m == -__builtin_h
 __device__ __forceinline__ float2 join_sums(float2 s, float2 n) {
     const float top = fmaxf(s.x, n.x), base = finite_or_0(top);
     return make_float2(top, s.y * exp2_of(s.x - base) + n.y * exp2_of(n.x - base));
+}
+
+// The power of two that takes the rests to fixed point.
+__device__ __forceinline__ float fixed_point(uint32_t most, int64_t rows) {
+    const float all = __uint_as_float(most) * (float)rows;
+    if (!(all > 0x1p-90f && all < 0x1p90f)) return 0.0f;  // none, or beyond what this is for
+    int e;
+    (void)frexpf(all, &e);
+    return ldexpf(1.0f, 30 - e);
 }
 
 // Piece k of a number.
@@ -345,6 +360,27 @@ __global__ __launch_bounds__(S::THREADS) void k_product(Product g) {
                     }
                 }
             }
+    } else if constexpr (WHAT == RESULT) {
+        typedef std::conditional_t<PIECES == 1, bf16_t, float> T;
+        const float scale = g.rests ? fixed_point(*g.most, g.all_rows) : 0.0f, back = scale > 0.0f ? 1.0f / scale : 0.0f;
+#pragma unroll
+        for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int64_t m = m0 + wm * S::WM + i * 16 + quad * 4 + r;
+                if (m >= rows) continue;
+                RowInfo f = {0.0f, 1.0f, 0, 0.0f};
+                if (g.rows) f = g.rows[m];
+#pragma unroll
+                for (int j = 0; j < S::NI; ++j) {
+                    const int64_t n = n0 + wn * S::WN + j * 16 + col;
+                    if (n >= cols) continue;
+                    float v = acc[i][j][r];
+                    if (g.rests) v += (float)g.rests[m * g.ldo + n] * back;
+                    if (g.rows) v = f.target < 0 ? 0.0f : v * f.scale;
+                    St<T>::st1(static_cast<T*>(g.result) + m * g.ldo + n, v);
+                }
+            }
     } else if constexpr (WHAT == LOGSUM) {
         int* target = reinterpret_cast<int*>(t0.a);  // of the tile's rows, counted from the tile's first column
         float2* sums = reinterpret_cast<float2*>(t1.a);  // [BN / WN][BM]
@@ -457,19 +493,17 @@ __global__ __launch_bounds__(1024) void k_losses(VocabularyArgs a, const float2*
     a.losses[r] = !counts ? 0.0f : d > 0.0f ? d + log1pf(expf(-d)) : log1pf(expf(d));
 }
 
-__global__ __launch_bounds__(256) void k_row_info(VocabularyArgs a, RowInfo* info) {
-    const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (r >= a.rows) return;
+__device__ __forceinline__ RowInfo row_info(const VocabularyArgs& a, int64_t r) {
     const int64_t t = a.targets[r];
     RowInfo v = {0.0f, 0.0f, -1, 0.0f};
     if (t >= 0 && t < a.vocab) {
         const float others = a.stats[r], d = sum_minus(others, a.stats[a.rows + r]);
-        v.others = others == -__builtin_huge_valf() ? 0.0f : others;  // then there is no q
+        v.others = finite_or_0(others);  // no others: there is no q
         v.scale = a.dloss[r] * (d < 0.0f ? expf(d) / (1.0f + expf(d)) : 1.0f / (1.0f + expf(-d)));
         v.target = (int)t;
         v.rest = bf2f(f2bf(v.scale)) - v.scale;
     }
-    info[r] = v;
+    return v;
 }
 
 // The targets' shares of dW, -c x, enter its product with c rounded to bf16. Where all
@@ -498,20 +532,6 @@ __global__ __launch_bounds__(256) void k_largest_rest(RowView x, int64_t rows, i
     if (threadIdx.x == 0 && top > 0.0f) atomicMax(most, __float_as_uint(top));  // positive floats are ordered as their bits
 }
 
-// The power of two that takes the rests to fixed point.
-__device__ __forceinline__ float fixed_point(uint32_t most, int64_t rows) {
-    const float all = __uint_as_float(most) * (float)rows;
-    if (!(all > 0x1p-90f && all < 0x1p90f)) return 0.0f;  // none, or beyond what this is for
-    int e;
-    (void)frexpf(all, &e);
-    return ldexpf(1.0f, 30 - e);
-}
-
-__global__ __launch_bounds__(256) void k_clear(u32x4* p, int64_t n) {
-    const int64_t i = block_index() * 256 + threadIdx.x;
-    if (i < n) p[i] = u32x4{0, 0, 0, 0};
-}
-
 __global__ __launch_bounds__(256) void k_add_rests(RowView x, int64_t rows, int dim, const RowInfo* info, const uint32_t* most, int64_t first,
                                                    int64_t n, int* rests) {
     const int64_t r = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
@@ -526,63 +546,103 @@ __global__ __launch_bounds__(256) void k_add_rests(RowView x, int64_t rows, int 
     }
 }
 
-// pieces of v at p, p + plane, ...
+// The pieces of eight numbers at p, p + plane, ..., 16-byte aligned.
 template <typename T>
-__device__ __forceinline__ void put(bf16_t* p, int64_t plane, float v) {
-    if constexpr (sizeof(T) == 2) {
-        *p = f2bf(v);
-    } else {
+__device__ __forceinline__ void put(bf16_t* p, int64_t plane, float (&v)[8]) {
 #pragma unroll
-        for (int k = 0; k < 3; ++k) {
-            const bf16_t b = f2bf(v);
-            p[k * plane] = b;
-            v -= bf2f(b);
+    for (int n = 0; n < Pieces<T>::N; ++n) {
+        uint32_t two[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            two[i] = f2bf2(v[2 * i], v[2 * i + 1]);
+            v[2 * i] -= __uint_as_float(two[i] << 16);
+            v[2 * i + 1] -= __uint_as_float(two[i] & 0xffff0000u);
         }
+        *reinterpret_cast<u32x4*>(p + n * plane) = u32x4{two[0], two[1], two[2], two[3]};
     }
 }
 
-// Rows as an operand: padded with zeros to ld, fp32 in three pieces.
+// Rows as an operand: fp32 in three pieces, [rows][ld] padded with zeros (NULL: not
+// wanted); and transposed, [cols][ldt], ldt >= rows a multiple of 64, where rows that
+// `targets` leaves out are zero (NULL: not wanted).
+struct Copy {
+    RowView src;
+    int64_t rows;
+    int cols;
+    bf16_t* dst;
+    int64_t plane, ld;
+    bf16_t* dst_t;
+    int64_t plane_t, ldt;
+    const int64_t* targets;
+    int vocab;
+};
+
 template <typename T>
-__global__ __launch_bounds__(256) void k_pack(RowView src, int64_t rows, int cols, bf16_t* dst, int64_t plane, int64_t ld) {
-    const int64_t i = block_index() * 256 + threadIdx.x, r = i / ld, c = i - r * ld;
-    if (r >= rows) return;
-    put<T>(dst + i, plane, c < cols ? St<T>::ld1(static_cast<const T*>(src.p) + r * src.stride + c) : 0.0f);
+__device__ __forceinline__ void pack(const Copy& p, int64_t chunk) {  // eight elements
+    const int64_t r = chunk * 8 / p.ld, c = chunk * 8 - r * p.ld;
+    if (r >= p.rows) return;
+    const T* from = static_cast<const T*>(p.src.p) + r * p.src.stride + c;
+    float v[8];
+    if (c + 8 <= p.cols && (reinterpret_cast<uintptr_t>(from) & (4 * sizeof(T) - 1)) == 0) {
+        const floatx4 a = St<T>::ld4(from), b = St<T>::ld4(from + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = c + i < p.cols ? St<T>::ld1(from + i) : 0.0f;
+    }
+    put<T>(p.dst + chunk * 8, p.plane, v);
 }
 
-// The same transposed: dst [cols][ld], ld >= rows a multiple of 64; rows that `targets` leaves out are zero.
 template <typename T>
-__global__ __launch_bounds__(256) void k_pack_transposed(RowView src, int64_t rows, int cols, const int64_t* targets, int64_t vocab,
-                                                         bf16_t* dst, int64_t plane, int64_t ld, int blocks) {
-    __shared__ float lds[64][65];
-    const int64_t index = block_index(), r0 = index / blocks * 64;
-    const int c0 = (int)(index % blocks) * 64;
-    if (r0 >= ld) return;
+__device__ __forceinline__ void pack_transposed(const Copy& p, int64_t index, float (*lds)[65]) {  // 64 rows of 64 columns
+    const int blocks = (p.cols + 63) / 64, c0 = (int)(index % blocks) * 64;
+    const int64_t r0 = index / blocks * 64;
 #pragma unroll 4
     for (int k = threadIdx.x; k < 64 * 64; k += 256) {
         const int64_t r = r0 + k / 64;
         const int c = c0 + k % 64;
-        bool there = r < rows && c < cols;
-        if (there && targets) there = targets[r] >= 0 && targets[r] < vocab;
-        lds[k / 64][k % 64] = there ? St<T>::ld1(static_cast<const T*>(src.p) + r * src.stride + c) : 0.0f;
+        bool there = r < p.rows && c < p.cols;
+        if (there && p.targets) there = p.targets[r] >= 0 && p.targets[r] < p.vocab;
+        lds[k / 64][k % 64] = there ? St<T>::ld1(static_cast<const T*>(p.src.p) + r * p.src.stride + c) : 0.0f;
     }
     __syncthreads();
     for (int k = threadIdx.x; k < 64 * 8; k += 256) {  // eight rows of the source a chunk
         const int r = k % 8 * 8, c = k / 8;
-        if (c0 + c >= cols) break;
+        if (c0 + c >= p.cols) break;
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = lds[r + i][c];
-#pragma unroll
-        for (int n = 0; n < Pieces<T>::N; ++n) {
-            uint32_t two[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                two[i] = f2bf2(v[2 * i], v[2 * i + 1]);
-                v[2 * i] -= __uint_as_float(two[i] << 16);
-                v[2 * i + 1] -= __uint_as_float(two[i] & 0xffff0000u);
-            }
-            *reinterpret_cast<u32x4*>(dst + n * plane + (c0 + c) * ld + r0 + r) = u32x4{two[0], two[1], two[2], two[3]};
-        }
+        put<T>(p.dst_t + (c0 + c) * p.ldt + r0 + r, p.plane_t, v);
+    }
+}
+
+// What a product needs first, side by side in one launch: x and W as operands, the rows'
+// info, cleared memory.
+struct Prepare {
+    Copy copy[2];
+    VocabularyArgs a;
+    RowInfo* info;          // or NULL
+    u32x4* zero[2];         // of `zeros` 16-byte pieces
+    int64_t zeros[2];
+    int64_t end[7];         // workgroups up to the end of each part
+};
+template <typename T>
+__global__ __launch_bounds__(256) void k_prepare(Prepare p) {
+    __shared__ float lds[64][65];
+    const int64_t block = block_index();
+    int part = 0;
+    while (part < 7 && block >= p.end[part]) ++part;
+    if (part == 7) return;
+    const int64_t index = block - (part ? p.end[part - 1] : 0), i = index * 256 + threadIdx.x;
+    if (part < 2) {
+        pack_transposed<T>(p.copy[part], index, lds);
+    } else if (part < 4) {
+        pack<T>(p.copy[part - 2], i);
+    } else if (part == 4) {
+        if (i < p.a.rows) p.info[i] = row_info(p.a, i);
+    } else {
+        if (i < p.zeros[part - 5]) p.zero[part - 5][i] = u32x4{0, 0, 0, 0};
     }
 }
 
@@ -667,11 +727,11 @@ int splits_of(int64_t m, int64_t n, int64_t steps) {
 template <int WHAT, int PIECES = 1>
 hipError_t product(Product g, hipStream_t s) {
     // three pieces of q of a large tile do not fit the registers beside it
-    return with_shape<PIECES == 1>(g.a.rows, g.b.rows, [&](auto shape) {
+    return with_shape<WHAT != GRADIENT || PIECES == 1>(g.a.rows, g.b.rows, [&](auto shape) {
         typedef decltype(shape) S;
         g.tiles_m = (int)((g.a.rows + S::BM - 1) / S::BM);
         g.tiles_n = (int)((g.b.rows + S::BN - 1) / S::BN);
-        if (WHAT != PLANES) g.splits = 1;
+        if (WHAT != PLANES) g.splits = 1;  // PLANES: the caller's
         k_product<S, WHAT, PIECES><<<dim3((unsigned)(g.tiles_m * g.tiles_n), (unsigned)g.splits), S::THREADS, 0, s>>>(g);
         return hipGetLastError();
     });
@@ -741,23 +801,6 @@ Plan plan_of(const VocabularyArgs& a, bool backward) {
     } while (0)
 
 template <typename T>
-hipError_t pack(const RowView& v, int64_t rows, int cols, bf16_t* dst, int64_t plane, int64_t ld, hipStream_t s) {
-    dim3 grid;
-    if (!grid_of((rows * ld + 255) / 256, 256, grid)) return hipErrorInvalidValue;
-    k_pack<T><<<grid, 256, 0, s>>>(v, rows, cols, dst, plane, ld);
-    return hipGetLastError();
-}
-template <typename T>
-hipError_t pack_transposed(const RowView& v, int64_t rows, int cols, const int64_t* targets, int64_t vocab, bf16_t* dst, int64_t plane,
-                           int64_t ld, hipStream_t s) {
-    const int blocks = (cols + 63) / 64;
-    dim3 grid;
-    if (!grid_of((ld + 63) / 64 * blocks, 256, grid)) return hipErrorInvalidValue;
-    k_pack_transposed<T><<<grid, 256, 0, s>>>(v, rows, cols, targets, vocab, dst, plane, ld, blocks);
-    return hipGetLastError();
-}
-
-template <typename T>
 hipError_t finish(const float* planes, int splits, int64_t rows, int64_t cols, const RowInfo* info, const int* rests, const uint32_t* most,
                   int64_t all_rows, T* out, hipStream_t s) {
     const int64_t blocks = (cols + 1023) / 1024;
@@ -771,43 +814,60 @@ hipError_t finish(const float* planes, int splits, int64_t rows, int64_t cols, c
     return hipGetLastError();
 }
 
-hipError_t clear(void* p, int64_t bytes, hipStream_t s) {
-    const int64_t n = (bytes + 15) / 16;
+template <typename T>
+hipError_t prepare(Prepare p, hipStream_t s) {
+    int64_t at = 0;
+    for (int k = 0; k < 2; ++k) {
+        const Copy& c = p.copy[k];
+        if (c.dst_t) at += c.ldt / 64 * ((c.cols + 63) / 64);
+        p.end[k] = at;
+    }
+    for (int k = 0; k < 2; ++k) {
+        const Copy& c = p.copy[k];
+        if (c.dst) at += (c.rows * c.ld / 8 + 255) / 256;
+        p.end[2 + k] = at;
+    }
+    if (p.info) at += (p.a.rows + 255) / 256;
+    p.end[4] = at;
+    for (int k = 0; k < 2; ++k) p.end[5 + k] = at += (p.zeros[k] + 255) / 256;
+    if (at == 0) return hipSuccess;
     dim3 grid;
-    if (!grid_of((n + 255) / 256, 256, grid)) return hipErrorInvalidValue;
-    k_clear<<<grid, 256, 0, s>>>(static_cast<u32x4*>(p), n);
+    if (!grid_of(at, 256, grid)) return hipErrorInvalidValue;
+    k_prepare<T><<<grid, 256, 0, s>>>(p);
     return hipGetLastError();
 }
 
-// x, and vocabulary rows first .. first + n - 1, as operands of the logits.
+// x, and vocabulary rows first .. first + n - 1, as operands of the logits: as they are, or a copy in the workspace.
 template <typename T>
-hipError_t x_operand(const VocabularyArgs& a, const Plan& p, Operand& o, hipStream_t s) {
-    if (direct(a, a.x)) {
-        o = Operand{static_cast<const bf16_t*>(a.x.p), 0, a.x.stride, a.rows};
-        return hipSuccess;
-    }
-    bf16_t* to = reinterpret_cast<bf16_t*>(static_cast<char*>(a.ws) + p.x);
-    o = Operand{to, p.rowsp * p.dimp, p.dimp, a.rows};
-    return pack<T>(a.x, a.rows, a.dim, to, o.plane, o.ld, s);
+Operand x_operand(const VocabularyArgs& a, const Plan& p, Copy& c) {
+    c.src = a.x;
+    c.rows = a.rows;
+    c.cols = a.dim;
+    if (direct(a, a.x)) return Operand{static_cast<const bf16_t*>(a.x.p), 0, a.x.stride, a.rows};
+    c.dst = reinterpret_cast<bf16_t*>(static_cast<char*>(a.ws) + p.x);
+    c.plane = p.rowsp * p.dimp;
+    c.ld = p.dimp;
+    return Operand{c.dst, c.plane, c.ld, a.rows};
 }
 template <typename T>
-hipError_t w_operand(const VocabularyArgs& a, const Plan& p, int64_t first, int64_t n, Operand& o, hipStream_t s) {
-    const RowView w = {static_cast<const T*>(a.w.p) + first * a.w.stride, a.w.stride};
-    if (direct(a, a.w)) {
-        o = Operand{static_cast<const bf16_t*>(w.p), 0, w.stride, n};
-        return hipSuccess;
-    }
-    bf16_t* to = reinterpret_cast<bf16_t*>(static_cast<char*>(a.ws) + p.w);
-    o = Operand{to, p.piece * p.dimp, p.dimp, n};
-    return pack<T>(w, n, a.dim, to, o.plane, o.ld, s);
+Operand w_operand(const VocabularyArgs& a, const Plan& p, int64_t first, int64_t n, Copy& c) {
+    c.src = RowView{static_cast<const T*>(a.w.p) + first * a.w.stride, a.w.stride};
+    c.rows = n;
+    c.cols = a.dim;
+    if (direct(a, a.w)) return Operand{static_cast<const bf16_t*>(c.src.p), 0, a.w.stride, n};
+    c.dst = reinterpret_cast<bf16_t*>(static_cast<char*>(a.ws) + p.w);
+    c.plane = p.piece * p.dimp;
+    c.ld = p.dimp;
+    return Operand{c.dst, c.plane, c.ld, n};
 }
 
 template <typename T>
 hipError_t forward(const VocabularyArgs& a, hipStream_t s) {
     const Plan p = plan_of(a, false);
     char* ws = static_cast<char*>(a.ws);
+    Prepare prep{};
     Product g{};
-    OK_OR_RETURN(x_operand<T>(a, p, g.a, s));
+    g.a = x_operand<T>(a, p, prep.copy[0]);
     g.steps = (int)(p.dimp / BK);
     g.pairs = p.pairs();
     g.targets = a.targets;
@@ -818,7 +878,9 @@ hipError_t forward(const VocabularyArgs& a, hipStream_t s) {
     int64_t parts = 0;
     for (int64_t first = 0; first < a.vocab; first += piece) {
         const int64_t n = std::min<int64_t>(piece, a.vocab - first);
-        OK_OR_RETURN(w_operand<T>(a, p, first, n, g.b, s));
+        g.b = w_operand<T>(a, p, first, n, prep.copy[1]);
+        OK_OR_RETURN(prepare<T>(prep, s));
+        prep = Prepare{};
         g.first = first;
         g.part = part + parts * a.rows;
         OK_OR_RETURN(product<LOGSUM>(g, s));
@@ -838,27 +900,48 @@ hipError_t backward(const VocabularyArgs& a, hipStream_t s) {
     RowInfo* info = reinterpret_cast<RowInfo*>(ws + p.info);
     const int pairs = p.pairs();
     T *dx = static_cast<T*>(a.dx), *dw = static_cast<T*>(a.dw);
-    if (a.rows > 0) {
-        k_row_info<<<(unsigned)((a.rows + 255) / 256), 256, 0, s>>>(a, info);
-        OK_OR_RETURN(hipGetLastError());
-    }
     uint32_t* most = reinterpret_cast<uint32_t*>(ws + p.most);
-    const bool exact_c = sizeof(T) == 2 && a.rows > 0;
+    int* rests = sizeof(T) == 2 && a.rows > 0 ? reinterpret_cast<int*>(ws + p.rests) : nullptr;
     const unsigned row_waves = (unsigned)((a.rows + 3) / 4);
-    if (exact_c) {
-        OK_OR_RETURN(clear(most, 16, s));
-        k_largest_rest<<<std::min(row_waves, 512u), 256, 0, s>>>(a.x, a.rows, a.dim, info, most);
-        OK_OR_RETURN(hipGetLastError());
-    }
-    Product logits{};
-    if (a.rows > 0) OK_OR_RETURN(x_operand<T>(a, p, logits.a, s));
-    const int64_t xt_plane = a.dim * p.rowsp;
-    OK_OR_RETURN(pack_transposed<T>(a.x, a.rows, a.dim, a.targets, a.vocab, bf(p.xt), xt_plane, p.rowsp, s));
+    const int64_t xt_plane = a.dim * p.rowsp, wt_plane = a.dim * p.piece;
     for (int64_t first = 0; first < a.vocab; first += p.piece) {
         const int64_t n = std::min<int64_t>(p.piece, a.vocab - first), np = up(n, BK);
-        Product g = logits;
+        Prepare prep{};
+        Product g{};
+        g.a = x_operand<T>(a, p, prep.copy[0]);
+        g.b = w_operand<T>(a, p, first, n, prep.copy[1]);
+        if (first == 0) {
+            Copy& c = prep.copy[0];
+            c.dst_t = bf(p.xt);
+            c.plane_t = xt_plane;
+            c.ldt = p.rowsp;
+            c.targets = a.targets;
+            c.vocab = a.vocab;
+            prep.a = a;
+            prep.info = a.rows > 0 ? info : nullptr;
+            prep.zero[1] = reinterpret_cast<u32x4*>(most);
+            prep.zeros[1] = 1;
+        } else {
+            prep.copy[0] = Copy{};  // is there
+        }
         if (a.rows > 0) {
-            OK_OR_RETURN(w_operand<T>(a, p, first, n, g.b, s));
+            Copy& c = prep.copy[1];
+            c.dst_t = bf(p.wt);
+            c.plane_t = wt_plane;
+            c.ldt = np;
+        } else {
+            prep.copy[1] = Copy{};
+        }
+        if (rests) {
+            prep.zero[0] = reinterpret_cast<u32x4*>(rests);
+            prep.zeros[0] = (n * a.dim + 3) / 4;
+        }
+        OK_OR_RETURN(prepare<T>(prep, s));
+        if (rests && first == 0) {
+            k_largest_rest<<<std::min(row_waves, 512u), 256, 0, s>>>(a.x, a.rows, a.dim, info, most);
+            OK_OR_RETURN(hipGetLastError());
+        }
+        if (a.rows > 0) {
             g.steps = (int)(p.dimp / BK);
             g.pairs = pairs;
             g.first = first;
@@ -869,9 +952,6 @@ hipError_t backward(const VocabularyArgs& a, hipStream_t s) {
             g.ldt = p.rowsp;
             g.q_plane = g.qt_plane = p.rowsp * p.piece;
             OK_OR_RETURN((product<GRADIENT, sizeof(T) == 2 ? 1 : 3>(g, s)));
-            const int64_t wt_plane = a.dim * p.piece;
-            const RowView w = {static_cast<const T*>(a.w.p) + first * a.w.stride, a.w.stride};
-            OK_OR_RETURN(pack_transposed<T>(w, n, a.dim, nullptr, 0, bf(p.wt), wt_plane, np, s));
             Product x{};
             x.a = Operand{g.q, g.q_plane, np, a.rows};
             x.b = Operand{bf(p.wt), wt_plane, np, a.dim};
@@ -881,7 +961,14 @@ hipError_t backward(const VocabularyArgs& a, hipStream_t s) {
             x.out = f32(p.dx);
             x.ldo = a.dim;
             x.add = first > 0;
-            OK_OR_RETURN(product<PLANES>(x, s));
+            if (x.splits == 1 && p.piece >= a.vocab) {
+                x.result = dx;
+                x.rows = info;
+                OK_OR_RETURN((product<RESULT, Pieces<T>::N>(x, s)));
+                dx = nullptr;
+            } else {
+                OK_OR_RETURN(product<PLANES>(x, s));
+            }
         }
         Product v{};
         v.a = Operand{bf(p.qt), p.rowsp * p.piece, p.rowsp, n};
@@ -891,17 +978,24 @@ hipError_t backward(const VocabularyArgs& a, hipStream_t s) {
         v.splits = p.splits_dw(a, n);
         v.out = f32(p.dw);
         v.ldo = a.dim;
-        OK_OR_RETURN(product<PLANES>(v, s));
-        int* rests = nullptr;
-        if (exact_c) {
-            rests = reinterpret_cast<int*>(ws + p.rests);
-            OK_OR_RETURN(clear(rests, n * a.dim * 4, s));
+        if (rests) {
             k_add_rests<<<row_waves, 256, 0, s>>>(a.x, a.rows, a.dim, info, most, first, n, rests);
             OK_OR_RETURN(hipGetLastError());
         }
-        OK_OR_RETURN(finish<T>(v.out, v.splits, 1, n * a.dim, nullptr, rests, most, a.rows, dw + first * a.dim, s));
+        // stored by the product where a launch more is what costs; of 16384 x 1024 numbers, planes stored and read
+        // again take 415 us with their product, two-byte stores beside the rests' loads 455
+        if (v.splits == 1 && n * a.dim < 1 << 22) {
+            v.result = dw + first * a.dim;
+            v.rests = rests;
+            v.most = most;
+            v.all_rows = a.rows;
+            OK_OR_RETURN((product<RESULT, Pieces<T>::N>(v, s)));
+        } else {
+            OK_OR_RETURN(product<PLANES>(v, s));
+            OK_OR_RETURN(finish<T>(v.out, v.splits, 1, n * a.dim, nullptr, rests, most, a.rows, dw + first * a.dim, s));
+        }
     }
-    if (a.rows == 0) return hipSuccess;
+    if (a.rows == 0 || !dx) return hipSuccess;  // no rows, or stored by the product
     return finish<T>(f32(p.dx), p.splits_dx(a), a.rows, a.dim, info, nullptr, nullptr, 0, dx, s);
 }
 
