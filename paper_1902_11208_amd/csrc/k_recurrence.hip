@@ -10,7 +10,12 @@
 // its tokens' f and u in registers, the slices' sums meet in LDS, every thread
 // finds the state its slice starts from and goes through its tokens once more.
 // So each input is read once and each output written once, and HBM bounds it. The
-// next tile is loaded while one is computed.
+// next tile is loaded while one is computed. Measured: 128 sequences of 300 to 1200
+// tokens of 512 bf16 channels, forward 67 us (290 MB, 4.3 TB/s), backward 128 us (490
+// MB, 3.8 TB/s); one sequence of 65536 tokens of 1024, in segments, 50 us for their
+// sums, 11 to join them, 77 for the pass itself. Its vector instructions (some thirty a
+// number with a sigmoid, the reciprocal and exponential four times one) come near the
+// memory's time in bf16: with 64-bit row addresses and masks in every tile it was 123 us.
 //
 // The forward pass keeps the fp32 state at every tile's start (1/64 of bf16
 // inputs), and the backward pass finds h again from it instead of from the
