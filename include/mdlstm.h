@@ -611,7 +611,7 @@ size_t mdlstm_recurrence_marks_bytes(const mdlstm_recurrence_desc* desc, int64_t
 /*
  * d_offsets, d_order, tokens and longest as for mdlstm_attention_forward. d_z and
  * d_x: rows of `channels` elements, z_stride and x_stride >= channels elements
- * apart (at most 2^22: UNSUPPORTED beyond). d_state [n][channels] (may be NULL: zero): the state each example starts
+ * apart (at most 2^20: UNSUPPORTED beyond). d_state [n][channels] (may be NULL: zero): the state each example starts
  * from; d_final (out, may be NULL): the state it leaves. d_h (out) [tokens]
  * [channels]. d_marks (out, may be NULL: no backward call follows). Asynchronous on
  * `stream`; capturable into a graph. Buffers that the call writes must not
@@ -671,7 +671,7 @@ size_t mdlstm_group_norm_workspace_bytes(const mdlstm_group_norm_desc* desc, int
 
 /*
  * d_offsets, d_order, tokens, longest as for mdlstm_attention_forward; d_x: rows
- * x_stride >= channels apart (at most 2^22: UNSUPPORTED beyond). d_y (out) [tokens][channels]; d_mean and d_rstd (out)
+ * x_stride >= channels apart (at most 2^20: UNSUPPORTED beyond). d_y (out) [tokens][channels]; d_mean and d_rstd (out)
  * [n][groups], for the backward (an empty example's mean is 0).
  */
 mdlstm_status mdlstm_group_norm_forward(const mdlstm_group_norm_desc* desc, int32_t n, int64_t tokens, int64_t longest,
@@ -695,8 +695,8 @@ mdlstm_status mdlstm_group_norm_backward(const mdlstm_group_norm_desc* desc, int
  * A row whose target lies outside [0, vocab) has loss 0 and takes no part in the
  * gradients, whatever it holds. dtype: storage of x, W and their gradients. In bf16
  * the logits are products of bf16 numbers summed in fp32, and the softmax enters
- * the gradients' products rounded to bf16 once (its target's share of dx is not
- * rounded); in fp32 operands are three bf16 numbers each, 2^-24 together, for
+ * the gradients' products rounded to bf16 once, the targets' shares without that
+ * rounding; in fp32 operands are three bf16 numbers each, 2^-24 together, for
  * magnitudes up to 3.38e38. Sums are fp32 in a fixed order. rows <= 2^22,
  * dim <= 65536, vocab <= 2^24 (UNSUPPORTED beyond).
  */

@@ -32,11 +32,12 @@ mdlstm_status check_recurrence(const mdlstm_recurrence_desc* d) {
     return MDLSTM_OK;
 }
 
-// Rows whose distance within a tile of tokens stays within 32 bits of bytes.
+// Rows whose distance within a workgroup's tokens (128 in the recurrence, up to 512 between
+// a thread's in the group norm) stays within 32 bits of bytes.
 mdlstm_status check_token_rows(const void* p, const char* name, int64_t tokens, int64_t cols, int64_t stride, int32_t dtype) {
     OK_OR_RETURN(check_rows(p, name, tokens, cols, stride, dtype));
-    if (tokens > 1 && stride > (int64_t)1 << 22)
-        return fail(MDLSTM_ERR_UNSUPPORTED, "rows of %s are %lld elements apart: at most 2^22", name, (long long)stride);
+    if (tokens > 1 && stride > kMaxChannels)
+        return fail(MDLSTM_ERR_UNSUPPORTED, "rows of %s are %lld elements apart: at most %d", name, (long long)stride, kMaxChannels);
     return MDLSTM_OK;
 }
 

@@ -26,7 +26,7 @@ def _L():
 SEQUENCES_BAD = [(dict(n=-1), INVALID), (dict(n=1 << 25), INVALID), (dict(tokens=-1), INVALID), (dict(longest=-1), INVALID),
                  (dict(longest=101), INVALID), (dict(n=0), INVALID), (dict(tokens=1 << 50, longest=1), INVALID)]
 CALL_BAD = [(dict(offsets=None), INVALID), (dict(offsets=FAKE + 4), INVALID), (dict(order=FAKE + 2), INVALID),
-            (dict(x=None), INVALID), (dict(x=FAKE + 2), INVALID), (dict(xs=23), INVALID), (dict(xs=(1 << 22) + 1), UNSUPPORTED),
+            (dict(x=None), INVALID), (dict(x=FAKE + 2), INVALID), (dict(xs=23), INVALID), (dict(xs=(1 << 20) + 1), UNSUPPORTED),
             (dict(xs=1 << 60), INVALID), (dict(ws=None), WORKSPACE), (dict(short=True), WORKSPACE), (dict(ws=_at(9) + 4), INVALID)]
 RECURRENCE_BAD = [(dict(desc=None), INVALID), (dict(channels=0), INVALID), (dict(channels=(1 << 20) + 1), UNSUPPORTED),
                   (dict(dtype=2), INVALID), (dict(gate=2), INVALID), (dict(gate=-1), INVALID)] + SEQUENCES_BAD
