@@ -229,7 +229,7 @@ __device__ __forceinline__ void group_sums(const GroupNormArgs& a, const Place& 
         for (int k = 0; k < K; ++k) *reinterpret_cast<floatx4*>(&lds[(k * rows + r) * row + me.lane * V]) = floatx4{t[k][0], t[k][1], t[k][2], t[k][3]};
     }
     lds_barrier();
-    for (int c = threadIdx.x; c < K * me.width; c += blockDim.x) {  // the rows, in order, into the first
+    for (int c = threadIdx.x; c < K * me.width; c += (int)blockDim.x) {  // the rows, in order, into the first
         float* at = lds + (c < me.width ? c : rows * row + c - me.width);
         float s = at[0];
 #pragma unroll 4
@@ -641,7 +641,9 @@ int segments_of(GroupNormArgs& a) {
     return threads;
 }
 
-// f with the way a pass holds its sequences (shape_of is done), and the threads of a workgroup.
+// f with the way a pass holds its sequences (shape_of is done), and the threads of a workgroup. Whole where the
+// longest fits: 512 sequences of 60 tokens of 256 channels in bf16 14 us forward and 30 backward, in segments 40
+// and 62; of 200 tokens 32 and 81 against 61 and 106.
 template <bool BACKWARD, typename F>
 auto with_hold(GroupNormArgs& a, F&& f) {
     typedef std::conditional_t<BACKWARD, BackwardWhole, ForwardWhole> Whole;

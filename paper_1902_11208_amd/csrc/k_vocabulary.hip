@@ -704,6 +704,11 @@ typedef Shape<256, 256, 128, 64> Large;
 typedef Shape<128, 128, 64, 64> Middle;
 typedef Shape<64, 128, 64, 32> Low;
 
+// Low tiles where the rows fill half a middle one at most, Large ones where they
+// still give most CUs a tile. Forward at 64 rows, 1024 channels and 50000 words:
+// Low 26 us, Middle 31, Large 44. Forward and backward at 4000 rows: 4000 words of
+// 1024 channels (256 large tiles) Large 45 / 183, Middle 49 / 186 us; at 2000 rows
+// and 5000 words of 512 channels (160) Middle 31 / 117, Large 33 / 124.
 template <bool ANY = true, typename F>
 auto with_shape(int64_t m, int64_t n, F&& f) {
     if (m <= 64) return f(Low());

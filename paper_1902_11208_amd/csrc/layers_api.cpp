@@ -41,13 +41,12 @@ mdlstm_status check_token_rows(const void* p, const char* name, int64_t tokens, 
     return MDLSTM_OK;
 }
 
-mdl::RecurrenceArgs recurrence_args(const mdlstm_recurrence_desc* d, const mdl::Packed& seqs, bool backward) {
+mdl::RecurrenceArgs recurrence_args(const mdlstm_recurrence_desc* d, const mdl::Packed& seqs) {
     mdl::RecurrenceArgs a{};
     a.seqs = seqs;
     a.channels = d->channels;
     a.dtype = d->dtype;
     a.sigmoid = d->gate == MDLSTM_GATE_SIGMOID;
-    a.backward = backward;
     return a;
 }
 
@@ -107,9 +106,9 @@ mdl::VocabularyArgs vocabulary_args(const mdlstm_vocabulary_desc* d, int64_t row
 extern "C" {
 
 size_t mdlstm_recurrence_workspace_bytes(const mdlstm_recurrence_desc* desc, int32_t n, int64_t tokens, int64_t longest,
-                                         int32_t backward) {
+                                         int32_t) {  // both directions cut the same segments
     if (check_recurrence(desc) != MDLSTM_OK || check_sequences(n, tokens, longest) != MDLSTM_OK) return 0;
-    return mdl::recurrence_workspace_bytes(recurrence_args(desc, packed(n, tokens, longest, nullptr, nullptr), backward != 0));
+    return mdl::recurrence_workspace_bytes(recurrence_args(desc, packed(n, tokens, longest, nullptr, nullptr)));
 }
 
 size_t mdlstm_recurrence_marks_bytes(const mdlstm_recurrence_desc* desc, int64_t tokens) {
@@ -132,7 +131,7 @@ mdlstm_status mdlstm_recurrence_forward(const mdlstm_recurrence_desc* desc, int3
     OK_OR_RETURN(check_out(d_h, "h", tokens > 0, es));
     OK_OR_RETURN(check_out(d_final, "final", false, 4));
     OK_OR_RETURN(check_out(d_marks, "marks", false, 4));
-    mdl::RecurrenceArgs a = recurrence_args(desc, packed(n, tokens, longest, d_offsets, d_order), false);
+    mdl::RecurrenceArgs a = recurrence_args(desc, packed(n, tokens, longest, d_offsets, d_order));
     const size_t need = mdl::recurrence_workspace_bytes(a);
     OK_OR_RETURN(check_workspace(d_workspace, workspace_bytes, need));
     OK_OR_RETURN(check_apart({span("h", d_h, tokens * cols * es, true), span("final", d_final, n * cols * 4, true),
@@ -174,7 +173,7 @@ mdlstm_status mdlstm_recurrence_backward(const mdlstm_recurrence_desc* desc, int
     OK_OR_RETURN(check_out(d_dz, "dz", tokens > 0, es));
     OK_OR_RETURN(check_out(d_dx, "dx", tokens > 0, es));
     OK_OR_RETURN(check_out(d_dstate, "dstate", false, 4));
-    mdl::RecurrenceArgs a = recurrence_args(desc, packed(n, tokens, longest, d_offsets, d_order), true);
+    mdl::RecurrenceArgs a = recurrence_args(desc, packed(n, tokens, longest, d_offsets, d_order));
     const size_t need = mdl::recurrence_workspace_bytes(a);
     OK_OR_RETURN(check_workspace(d_workspace, workspace_bytes, need));
     OK_OR_RETURN(check_apart({span("dz", d_dz, tokens * cols * es, true), span("dx", d_dx, tokens * cols * es, true),

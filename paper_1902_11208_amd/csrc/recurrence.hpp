@@ -14,7 +14,7 @@ constexpr int kRecurrenceTile = 128;  // tokens of a tile; a state is kept at ev
 
 struct RecurrenceArgs {
     Packed seqs;
-    int channels, dtype, sigmoid, backward;
+    int channels, dtype, sigmoid;
     RowView z, x, dh;      // dh: backward only
     const float* state;    // [n][channels] or NULL
     const float* dfinal;   // backward: gradient of the final states, or NULL
