@@ -339,13 +339,14 @@ def test_calls_on_another_stream():
     T = sum(lengths)
     rec, norm = _layers(rng, lengths, C)
     z, x = _rand(rng, T, C), _rand(rng, T, C)
+    state = torch.zeros(9, C, device="cuda")  # filled on the current stream: like all inputs before the side stream's wait
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     h = rec.forward(z, x, stream=side)
     y = norm.forward(h, stream=side)
     dx, dw, db = norm.backward(x, stream=side)
     dz, dxx = rec.backward(dx, stream=side)
-    out = _seq().gated_recurrence_step(z[:9], x[:9], torch.zeros(9, C, device="cuda"), stream=side)
+    out = _seq().gated_recurrence_step(z[:9], x[:9], state, stream=side)
     side.synchronize()
     rec2, norm2 = _seq().GatedRecurrence(lengths, C, dtype=torch.float32), _seq().GroupNorm(
         lengths, norm.weight, norm.bias, 4, dtype=torch.float32, activation="silu")
