@@ -694,9 +694,9 @@ mdlstm_status mdlstm_group_norm_backward(const mdlstm_group_norm_desc* desc, int
  *     loss_i = log(sum_v exp(l_iv)) - l_i,target
  * A row whose target lies outside [0, vocab) has loss 0 and takes no part in the
  * gradients, whatever it holds. dtype: storage of x, W and their gradients. In bf16
- * the logits are products of bf16 numbers summed in fp32, and the softmax enters
- * the gradients' products rounded to bf16 once, the targets' shares without that
- * rounding; in fp32 operands are three bf16 numbers each, 2^-24 together, for
+ * the logits are products of bf16 numbers summed in fp32, the softmax enters the
+ * gradients' products as two bf16 numbers, 2^-16 together, and results are rounded
+ * once; in fp32 operands are three bf16 numbers each, 2^-24 together, for
  * magnitudes up to 3.38e38. Sums are fp32 in a fixed order. rows <= 2^22,
  * dim <= 65536, vocab <= 2^24 (UNSUPPORTED beyond).
  */

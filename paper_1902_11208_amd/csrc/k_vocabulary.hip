@@ -17,8 +17,11 @@
 // transposed for dW), and two products with the transposed W and x.
 //
 // fp32 operands are three bf16 numbers each (split.hpp), the six largest products
-// kept. In bf16, q is rounded once to a matrix operand: at most 2^-8 of each of many
-// terms beside the target's, which is exact in dx and made so in dW (k_add_rests).
+// kept. With x and W in bf16, q and c q are two bf16 numbers each, 2^-16 of
+// themselves off. One would be 2^-8 off, and the sum of q over the vocabulary is 0:
+// what W's rows have in common falls out of dx, and is left of it in proportion if
+// q is rounded (2000 rows of 128 with a common part of 10 beside a spread of 0.18 a
+// coordinate: dx 2.8e-3 off, in two pieces 1.7e-3, which is the result's own rounding).
 //
 // Matrix instructions bound it, and how fast LDS feeds them: 256 x 256 tiles in eight
 // waves of 128 x 64 read 192 KB of operands from LDS a step of 64 and write 64, beside
@@ -52,7 +55,6 @@ struct Operand {
 struct RowInfo {
     float others, scale;  // o log2(e) and c
     int target;           // -1: the row is left out
-    float rest;           // what rounding -c to bf16 left of it
 };
 
 enum { LOGSUM, GRADIENT, PLANES, RESULT };
@@ -60,7 +62,7 @@ enum { LOGSUM, GRADIENT, PLANES, RESULT };
 struct Product {
     Operand a, b;
     int steps;          // steps of one pair of pieces
-    int pairs;          // 1, or 6 of the three pieces of each
+    int pairs;          // 1; 2 of a's two pieces with b; 6 of the three pieces of each
     int splits;         // PLANES: parts of the sum
     int tiles_m, tiles_n;
     // LOGSUM
@@ -77,12 +79,9 @@ struct Product {
     float* out;         // [splits][a.rows][ldo]
     int64_t ldo;
     int add;            // to what is there
-    // RESULT: [a.rows][ldo] as stored, with the rests and times the rows' scale (k_finish)
+    // RESULT: [a.rows][ldo] as stored, times the rows' scale (k_finish)
     void* result;
     const RowInfo* rows;
-    const int* rests;
-    const uint32_t* most;
-    int64_t all_rows;
 };
 
 // A tile of a product: BM x BN, waves of WM x WN.
@@ -94,7 +93,7 @@ struct Shape {
 };
 
 // Which pieces a pair of them multiplies, two bits each, the smallest products first:
-// (2, 0) (0, 2) (1, 1) (0, 1) (1, 0) (0, 0).
+// (2, 0) (0, 2) (1, 1) (0, 1) (1, 0) (0, 0) of three; (1, 0) (0, 0) where a has two.
 constexpr uint32_t PIECES_A = 2 | 0 << 2 | 1 << 4 | 0 << 6 | 1 << 8, PIECES_B = 0 | 2 << 2 | 1 << 4 | 1 << 6 | 0 << 8;
 
 typedef __amdgpu_buffer_rsrc_t Buffer;
@@ -194,19 +193,19 @@ __device__ __forceinline__ float2 join_sums(float2 s, float2 n) {
     return make_float2(top, s.y * exp2_of(s.x - base) + n.y * exp2_of(n.x - base));
 }
 
-// The power of two that takes the rests to fixed point.
-__device__ __forceinline__ float fixed_point(uint32_t most, int64_t rows) {
-    const float all = __uint_as_float(most) * (float)rows;
-    if (!(all > 0x1p-90f && all < 0x1p90f)) return 0.0f;  // none, or beyond what this is for
-    int e;
-    (void)frexpf(all, &e);
-    return ldexpf(1.0f, 30 - e);
-}
-
 // Piece k of a number.
 __device__ __forceinline__ float piece(float v, int k) {
     for (int i = 0; i < k; ++i) v -= bf2f(f2bf(v));
     return v;
+}
+
+// To the compiler, other numbers than before.
+template <class S>
+__device__ __forceinline__ void as_new(floatx4 (&acc)[S::MI][S::NI]) {
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+        for (int j = 0; j < S::NI; ++j) asm volatile("" : "+v"(acc[i][j]));
 }
 
 // A tile's q as rows, and c q as columns, through LDS, so that whole lines leave.
@@ -287,7 +286,7 @@ __global__ __launch_bounds__(S::THREADS) void k_product(Product g) {
     const Loader<S> load(g, m0, n0);
     const bf16_t *pa = g.a.p + m0 * g.a.ld, *pb = g.b.p + n0 * g.b.ld;
     int pair = __builtin_amdgcn_readfirstlane(g.steps ? from / g.steps : 0), step = from - pair * g.steps, left = to - from;  // of the next fetch
-    const uint32_t pieces_a = g.pairs == 1 ? 0 : PIECES_A, pieces_b = g.pairs == 1 ? 0 : PIECES_B;
+    const uint32_t pieces_a = g.pairs == 6 ? PIECES_A : g.pairs - 1, pieces_b = g.pairs == 6 ? PIECES_B : 0;
     auto fetch = [&](Tile<S>& t) {  // behind the last step: that one again
         const int64_t a = (pieces_a >> 2 * pair & 3) * g.a.plane, b = (pieces_b >> 2 * pair & 3) * g.b.plane;
         load.load(t, buffer_at(pa + a + (int64_t)step * BK), buffer_at(pb + b + (int64_t)step * BK));
@@ -370,21 +369,19 @@ __global__ __launch_bounds__(S::THREADS) void k_product(Product g) {
             }
     } else if constexpr (WHAT == RESULT) {
         typedef std::conditional_t<PIECES == 1, bf16_t, float> T;
-        const float scale = g.rests ? fixed_point(*g.most, g.all_rows) : 0.0f, back = scale > 0.0f ? 1.0f / scale : 0.0f;
 #pragma unroll
         for (int i = 0; i < S::MI; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int64_t m = m0 + wm * S::WM + i * 16 + quad * 4 + r;
                 if (m >= rows) continue;
-                RowInfo f = {0.0f, 1.0f, 0, 0.0f};
+                RowInfo f = {0.0f, 1.0f, 0};
                 if (g.rows) f = g.rows[m];
 #pragma unroll
                 for (int j = 0; j < S::NI; ++j) {
                     const int64_t n = n0 + wn * S::WN + j * 16 + col;
                     if (n >= cols) continue;
                     float v = acc[i][j][r];
-                    if (g.rests) v += (float)g.rests[m * g.ldo + n] * back;
                     if (g.rows) v = f.target < 0 ? 0.0f : v * f.scale;
                     St<T>::st1(static_cast<T*>(g.result) + m * g.ldo + n, v);
                 }
@@ -468,7 +465,10 @@ __global__ __launch_bounds__(S::THREADS) void k_product(Product g) {
             }
 #pragma unroll
         for (int k = 0; k < PIECES; ++k) {
+            // each pass takes its pieces from q again: kept from the pass before they would not fit the registers
+            as_new<S>(acc);
             store_rows<S>(g, t0.a, t1.a, acc, k, m0, n0);
+            as_new<S>(acc);
             store_columns<S>(g, t0.a, t1.a, acc, scale, k, m0, n0);
         }
     }
@@ -503,55 +503,14 @@ __global__ __launch_bounds__(1024) void k_losses(VocabularyArgs a, const float2*
 
 __device__ __forceinline__ RowInfo row_info(const VocabularyArgs& a, int64_t r) {
     const int64_t t = a.targets[r];
-    RowInfo v = {0.0f, 0.0f, -1, 0.0f};
+    RowInfo v = {0.0f, 0.0f, -1};
     if (t >= 0 && t < a.vocab) {
         const float others = a.stats[r], d = sum_minus(others, a.stats[a.rows + r]);
         v.others = finite_or_0(others);  // no others: there is no q
         v.scale = a.dloss[r] * (d < 0.0f ? expf(d) / (1.0f + expf(d)) : 1.0f / (1.0f + expf(-d)));
         v.target = (int)t;
-        v.rest = bf2f(f2bf(v.scale)) - v.scale;
     }
     return v;
-}
-
-// The targets' shares of dW, -c x, enter its product with c rounded to bf16. Where all
-// losses have one gradient, c is nearly one number and its rounding, up to 2^-8 of it,
-// would be a bias of all of dW; so what it left is added, sum over the rows of a
-// target of rest x. It is small beside the share, so 32-bit fixed-point numbers hold it
-// (rows of at most the largest rest |x|, 2^30 for all rows together: 2^-16 of the
-// largest one's rest with 16384 rows), and their sums do not depend on the atomics' order.
-__global__ __launch_bounds__(256) void k_largest_rest(RowView x, int64_t rows, int dim, const RowInfo* info, uint32_t* most) {
-    __shared__ float lds[4];
-    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63;
-    float top = 0.0f;
-    for (int64_t r = (int64_t)blockIdx.x * 4 + wave; r < rows; r += (int64_t)gridDim.x * 4) {
-        const RowInfo f = info[r];
-        if (f.target < 0) continue;
-        float row = 0.0f;
-        for (int c = lane; c < dim; c += 64) row = fmaxf(row, fabsf(St<bf16_t>::ld1(static_cast<const bf16_t*>(x.p) + r * x.stride + c)));
-        row *= fabsf(f.rest);
-        if (row < __builtin_huge_valf()) top = fmaxf(top, row);
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    if (lane == 0) lds[wave] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
-    if (threadIdx.x == 0 && top > 0.0f) atomicMax(most, __float_as_uint(top));  // positive floats are ordered as their bits
-}
-
-__global__ __launch_bounds__(256) void k_add_rests(RowView x, int64_t rows, int dim, const RowInfo* info, const uint32_t* most, int64_t first,
-                                                   int64_t n, int* rests) {
-    const int64_t r = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
-    if (r >= rows) return;
-    const RowInfo f = info[r];
-    const float scale = fixed_point(*most, rows);
-    if (f.target < first || f.target >= first + n || scale == 0.0f) return;
-    int* to = rests + (f.target - first) * dim;
-    for (int c = threadIdx.x & 63; c < dim; c += 64) {
-        const float v = f.rest * St<bf16_t>::ld1(static_cast<const bf16_t*>(x.p) + r * x.stride + c) * scale;
-        if (fabsf(v) < 0x1p30f) atomicAdd(to + c, (int)rintf(v));
-    }
 }
 
 // The pieces of eight numbers at p, p + plane, ..., 16-byte aligned.
@@ -626,39 +585,35 @@ __device__ __forceinline__ void pack_transposed(const Copy& p, int64_t index, fl
 }
 
 // What a product needs first, side by side in one launch: x and W as operands, the rows'
-// info, cleared memory.
+// info.
 struct Prepare {
     Copy copy[2];
     VocabularyArgs a;
     RowInfo* info;          // or NULL
-    u32x4* zero[2];         // of `zeros` 16-byte pieces
-    int64_t zeros[2];
-    int64_t end[7];         // workgroups up to the end of each part
+    int64_t end[5];         // workgroups up to the end of each part
 };
 template <typename T>
 __global__ __launch_bounds__(256) void k_prepare(Prepare p) {
     __shared__ float lds[64][65];
     const int64_t block = block_index();
     int part = 0;
-    while (part < 7 && block >= p.end[part]) ++part;
-    if (part == 7) return;
+    while (part < 5 && block >= p.end[part]) ++part;
+    if (part == 5) return;
     const int64_t index = block - (part ? p.end[part - 1] : 0), i = index * 256 + threadIdx.x;
     if (part < 2) {
         pack_transposed<T>(p.copy[part], index, lds);
     } else if (part < 4) {
         pack<T>(p.copy[part - 2], i);
-    } else if (part == 4) {
-        if (i < p.a.rows) p.info[i] = row_info(p.a, i);
     } else {
-        if (i < p.zeros[part - 5]) p.zero[part - 5][i] = u32x4{0, 0, 0, 0};
+        if (i < p.a.rows) p.info[i] = row_info(p.a, i);
     }
 }
 
-// The planes of a product together, in order, with the rests (above) and times the
-// row's scale (info), as stored. Rows without a scale come as one.
+// The planes of a product together, in order, times the row's scale (info), as
+// stored. Rows without a scale come as one.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void k_finish(const float* planes, int splits, int64_t rows, int64_t cols, int blocks, const RowInfo* info,
-                                                const int* rests, const uint32_t* most, int64_t all_rows, T* out) {
+                                                T* out) {
     const int64_t index = block_index(), r = index / blocks, c = ((index - r * blocks) * 256 + threadIdx.x) * 4;
     if (r >= rows || c >= cols) return;
     floatx4 s = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -673,12 +628,6 @@ __global__ __launch_bounds__(256) void k_finish(const float* planes, int splits,
             for (int i = 0; i < 4; ++i)
                 if (i < n) s[i] += p[i];
         }
-    }
-    if (rests) {
-        const float scale = fixed_point(*most, all_rows), back = scale > 0.0f ? 1.0f / scale : 0.0f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < n) s[i] += (float)rests[r * cols + c + i] * back;
     }
     if (info) {
         const RowInfo f = info[r];
@@ -739,8 +688,9 @@ int splits_of(int64_t m, int64_t n, int64_t steps) {
 
 template <int WHAT, int PIECES = 1>
 hipError_t product(Product g, hipStream_t s) {
-    // three pieces of q of a large tile do not fit the registers beside it
-    return with_shape<WHAT != GRADIENT || PIECES == 1>(g.a.rows, g.b.rows, [&](auto shape) {
+    // three pieces of q leave middle tiles no slower than large ones: backward of 1537 rows of 256 over 7003 in fp32 201
+    // against 212 us, of 4000 rows of 512 over 12000 1151 against 1138
+    return with_shape<WHAT != GRADIENT || PIECES != 3>(g.a.rows, g.b.rows, [&](auto shape) {
         typedef decltype(shape) S;
         g.tiles_m = (int)((g.a.rows + S::BM - 1) / S::BM);
         g.tiles_n = (int)((g.b.rows + S::BN - 1) / S::BN);
@@ -757,12 +707,12 @@ int64_t column_tile(int64_t m, int64_t n) {
 // Where everything lies in a call's workspace, and how the vocabulary is cut.
 struct Plan {
     int64_t piece, dimp, rowsp;   // vocabulary rows of a piece, dim and rows in whole steps
-    int pieces;                   // of an operand's numbers
-    bool pack_x, pack_w;
-    int64_t x, w, part, info, most, rests, xt, wt, q, qt, dx, dw, total;  // offsets
+    int pieces, q_pieces;         // of an operand's numbers, of q's
+    int64_t x, w, part, info, xt, wt, q, qt, dx, dw, total;  // offsets
     int pairs() const { return pieces == 1 ? 1 : 6; }
-    int splits_dx(const VocabularyArgs& a) const { return splits_of(a.rows, a.dim, piece / BK * pairs()); }
-    int splits_dw(const VocabularyArgs& a, int64_t n) const { return splits_of(n, a.dim, rowsp / BK * pairs()); }
+    int q_pairs() const { return pieces == 1 ? 2 : 6; }
+    int splits_dx(const VocabularyArgs& a) const { return splits_of(a.rows, a.dim, piece / BK * q_pairs()); }
+    int splits_dw(const VocabularyArgs& a, int64_t n) const { return splits_of(n, a.dim, rowsp / BK * q_pairs()); }
 };
 
 bool direct(const VocabularyArgs& a, const RowView& v) {
@@ -772,6 +722,7 @@ bool direct(const VocabularyArgs& a, const RowView& v) {
 Plan plan_of(const VocabularyArgs& a, bool backward) {
     Plan p{};
     p.pieces = a.dtype ? 1 : 3;
+    p.q_pieces = a.dtype ? 2 : 3;
     p.dimp = up(a.dim, BK);
     p.rowsp = up(std::max<int64_t>(a.rows, 1), BK);
     // Pieces of at most 2^28 logits and 2^16 weights; where there are several, with
@@ -793,12 +744,10 @@ Plan plan_of(const VocabularyArgs& a, bool backward) {
         p.part = take((a.vocab / 128 + 2 + (a.vocab + p.piece - 1) / p.piece) * a.rows * 8);
     } else {
         p.info = take(a.rows * (int64_t)sizeof(RowInfo));
-        p.most = take(16);
-        if (p.pieces == 1) p.rests = take(std::min<int64_t>(p.piece, a.vocab) * a.dim * 4);
         p.xt = take(a.dim * p.rowsp * 2 * p.pieces);
         p.wt = take(a.dim * p.piece * 2 * p.pieces);
-        p.q = take(p.rowsp * p.piece * 2 * p.pieces);
-        p.qt = take(p.rowsp * p.piece * 2 * p.pieces);
+        p.q = take(p.rowsp * p.piece * 2 * p.q_pieces);
+        p.qt = take(p.rowsp * p.piece * 2 * p.q_pieces);
         const int64_t rest = a.vocab % p.piece;
         p.dx = take(p.splits_dx(a) * a.rows * a.dim * 4);
         p.dw = take(std::max(p.splits_dw(a, std::min<int64_t>(p.piece, a.vocab)) * p.piece, rest ? p.splits_dw(a, rest) * rest : 0) * a.dim * 4);
@@ -814,16 +763,15 @@ Plan plan_of(const VocabularyArgs& a, bool backward) {
     } while (0)
 
 template <typename T>
-hipError_t finish(const float* planes, int splits, int64_t rows, int64_t cols, const RowInfo* info, const int* rests, const uint32_t* most,
-                  int64_t all_rows, T* out, hipStream_t s) {
+hipError_t finish(const float* planes, int splits, int64_t rows, int64_t cols, const RowInfo* info, T* out, hipStream_t s) {
     const int64_t blocks = (cols + 1023) / 1024;
     dim3 grid;
     if (blocks > 0x7fffffff || !grid_of(rows * blocks, 256, grid)) return hipErrorInvalidValue;
     // a piece's rows of dW start anywhere in dW where dim is odd
     if (cols % 4 == 0 && (reinterpret_cast<uintptr_t>(out) & (4 * sizeof(T) - 1)) == 0)
-        k_finish<T, true><<<grid, 256, 0, s>>>(planes, splits, rows, cols, (int)blocks, info, rests, most, all_rows, out);
+        k_finish<T, true><<<grid, 256, 0, s>>>(planes, splits, rows, cols, (int)blocks, info, out);
     else
-        k_finish<T, false><<<grid, 256, 0, s>>>(planes, splits, rows, cols, (int)blocks, info, rests, most, all_rows, out);
+        k_finish<T, false><<<grid, 256, 0, s>>>(planes, splits, rows, cols, (int)blocks, info, out);
     return hipGetLastError();
 }
 
@@ -842,7 +790,6 @@ hipError_t prepare(Prepare p, hipStream_t s) {
     }
     if (p.info) at += (p.a.rows + 255) / 256;
     p.end[4] = at;
-    for (int k = 0; k < 2; ++k) p.end[5 + k] = at += (p.zeros[k] + 255) / 256;
     if (at == 0) return hipSuccess;
     dim3 grid;
     if (!grid_of(at, 256, grid)) return hipErrorInvalidValue;
@@ -911,11 +858,7 @@ hipError_t backward(const VocabularyArgs& a, hipStream_t s) {
     auto bf = [&](int64_t at) { return reinterpret_cast<bf16_t*>(ws + at); };
     auto f32 = [&](int64_t at) { return reinterpret_cast<float*>(ws + at); };
     RowInfo* info = reinterpret_cast<RowInfo*>(ws + p.info);
-    const int pairs = p.pairs();
     T *dx = static_cast<T*>(a.dx), *dw = static_cast<T*>(a.dw);
-    uint32_t* most = reinterpret_cast<uint32_t*>(ws + p.most);
-    int* rests = sizeof(T) == 2 && a.rows > 0 ? reinterpret_cast<int*>(ws + p.rests) : nullptr;
-    const unsigned row_waves = (unsigned)((a.rows + 3) / 4);
     const int64_t xt_plane = a.dim * p.rowsp, wt_plane = a.dim * p.piece;
     for (int64_t first = 0; first < a.vocab; first += p.piece) {
         const int64_t n = std::min<int64_t>(p.piece, a.vocab - first), np = up(n, BK);
@@ -932,8 +875,6 @@ hipError_t backward(const VocabularyArgs& a, hipStream_t s) {
             c.vocab = a.vocab;
             prep.a = a;
             prep.info = a.rows > 0 ? info : nullptr;
-            prep.zero[1] = reinterpret_cast<u32x4*>(most);
-            prep.zeros[1] = 1;
         } else {
             prep.copy[0] = Copy{};  // is there
         }
@@ -945,18 +886,10 @@ hipError_t backward(const VocabularyArgs& a, hipStream_t s) {
         } else {
             prep.copy[1] = Copy{};
         }
-        if (rests) {
-            prep.zero[0] = reinterpret_cast<u32x4*>(rests);
-            prep.zeros[0] = (n * a.dim + 3) / 4;
-        }
         OK_OR_RETURN(prepare<T>(prep, s));
-        if (rests && first == 0) {
-            k_largest_rest<<<std::min(row_waves, 512u), 256, 0, s>>>(a.x, a.rows, a.dim, info, most);
-            OK_OR_RETURN(hipGetLastError());
-        }
         if (a.rows > 0) {
             g.steps = (int)(p.dimp / BK);
-            g.pairs = pairs;
+            g.pairs = p.pairs();
             g.first = first;
             g.info = info;
             g.q = bf(p.q);
@@ -964,12 +897,12 @@ hipError_t backward(const VocabularyArgs& a, hipStream_t s) {
             g.ldq = np;
             g.ldt = p.rowsp;
             g.q_plane = g.qt_plane = p.rowsp * p.piece;
-            OK_OR_RETURN((product<GRADIENT, sizeof(T) == 2 ? 1 : 3>(g, s)));
+            OK_OR_RETURN((product<GRADIENT, sizeof(T) == 2 ? 2 : 3>(g, s)));
             Product x{};
             x.a = Operand{g.q, g.q_plane, np, a.rows};
             x.b = Operand{bf(p.wt), wt_plane, np, a.dim};
             x.steps = (int)(np / BK);
-            x.pairs = pairs;
+            x.pairs = p.q_pairs();
             x.splits = p.splits_dx(a);
             x.out = f32(p.dx);
             x.ldo = a.dim;
@@ -987,29 +920,22 @@ hipError_t backward(const VocabularyArgs& a, hipStream_t s) {
         v.a = Operand{bf(p.qt), p.rowsp * p.piece, p.rowsp, n};
         v.b = Operand{bf(p.xt), xt_plane, p.rowsp, a.dim};
         v.steps = a.rows > 0 ? (int)(p.rowsp / BK) : 0;  // no rows: dW is zero
-        v.pairs = pairs;
+        v.pairs = p.q_pairs();
         v.splits = p.splits_dw(a, n);
         v.out = f32(p.dw);
         v.ldo = a.dim;
-        if (rests) {
-            k_add_rests<<<row_waves, 256, 0, s>>>(a.x, a.rows, a.dim, info, most, first, n, rests);
-            OK_OR_RETURN(hipGetLastError());
-        }
-        // stored by the product where a launch more is what costs; of 16384 x 1024 numbers, planes stored and read
-        // again take 415 us with their product, two-byte stores beside the rests' loads 455
-        if (v.splits == 1 && n * a.dim < 1 << 22) {
+        // in one part, stored by the product: planes stored and read again took 1.4 us more where 500 rows of dW of 512
+        // leave (backward of 64 rows 35.9 against 34.5 us) and 74 where 50000 of 1024 do (280 against 207 us)
+        if (v.splits == 1) {
             v.result = dw + first * a.dim;
-            v.rests = rests;
-            v.most = most;
-            v.all_rows = a.rows;
             OK_OR_RETURN((product<RESULT, Pieces<T>::N>(v, s)));
         } else {
             OK_OR_RETURN(product<PLANES>(v, s));
-            OK_OR_RETURN(finish<T>(v.out, v.splits, 1, n * a.dim, nullptr, rests, most, a.rows, dw + first * a.dim, s));
+            OK_OR_RETURN(finish<T>(v.out, v.splits, 1, n * a.dim, nullptr, dw + first * a.dim, s));
         }
     }
     if (a.rows == 0 || !dx) return hipSuccess;  // no rows, or stored by the product
-    return finish<T>(f32(p.dx), p.splits_dx(a), a.rows, a.dim, info, nullptr, nullptr, 0, dx, s);
+    return finish<T>(f32(p.dx), p.splits_dx(a), a.rows, a.dim, info, dx, s);
 }
 
 }  // namespace
