@@ -711,7 +711,7 @@ size_t mdlstm_vocabulary_workspace_bytes(const mdlstm_vocabulary_desc* desc, int
 /*
  * d_x and d_w: rows x_stride and w_stride >= dim elements apart. d_targets [rows]
  * (int64). d_losses (out) [rows] fp32; d_stats (out) [2][rows] fp32, for the
- * backward: log2 of the sum over the tokens but the target, and the target's logit.
+ * backward: m and s of the sum over the tokens but the target, 2^m s.
  * Asynchronous on `stream`; capturable into a graph. Buffers that the call writes
  * must not overlap others (INVALID_ARG).
  */

@@ -53,8 +53,9 @@ struct Operand {
 
 // What of a row the epilogues need.
 struct RowInfo {
-    float others, scale;  // o log2(e) and c
-    int target;           // -1: the row is left out
+    float most, share;  // q = 2^(l log2(e) - most) share
+    float scale;        // c
+    int target;         // -1: the row is left out
 };
 
 enum { LOGSUM, GRADIENT, PLANES, RESULT };
@@ -375,7 +376,7 @@ __global__ __launch_bounds__(S::THREADS) void k_product(Product g) {
             for (int r = 0; r < 4; ++r) {
                 const int64_t m = m0 + wm * S::WM + i * 16 + quad * 4 + r;
                 if (m >= rows) continue;
-                RowInfo f = {0.0f, 1.0f, 0};
+                RowInfo f = {0.0f, 0.0f, 1.0f, 0};
                 if (g.rows) f = g.rows[m];
 #pragma unroll
                 for (int j = 0; j < S::NI; ++j) {
@@ -446,7 +447,7 @@ __global__ __launch_bounds__(S::THREADS) void k_product(Product g) {
                 const RowInfo f = info[wm * S::WM + i * 16 + quad * 4 + r];
                 const int t = f.target < 0 ? -(1 << 20) : (int)min(max(f.target - g.first - n0 - wn * S::WN - col, (int64_t)-1024), (int64_t)1024);
 #pragma unroll
-                for (int j = 0; j < S::NI; ++j) acc[i][j][r] = exp2_of(fmaf(acc[i][j][r], LOG2E, -f.others));
+                for (int j = 0; j < S::NI; ++j) acc[i][j][r] = exp2_of(fmaf(acc[i][j][r], LOG2E, -f.most)) * f.share;
                 if (ragged || __any(t == -(1 << 20) || (t > -16 && t < S::WN))) {
 #pragma unroll
                     for (int j = 0; j < S::NI; ++j) {
@@ -474,10 +475,15 @@ __global__ __launch_bounds__(S::THREADS) void k_product(Product g) {
     }
 }
 
-// o - l_target from log2 of the sum.
-__device__ __forceinline__ float sum_minus(float others, float logit) { return fmaf(others, 0.693147180559945309f, -logit); }
+// o - l_target of a row, from the sum over the others (m, sum). m is rounded at its own
+// size, and stays apart: every term has met the same m, and here it meets the target's logit
+// before anything smaller. In one number with the sum's logarithm, at logits of 1000,
+// losses and all q of a row were up to 4e-5 off.
+__device__ __forceinline__ float sum_minus(float m, float sum, float logit) {
+    return (fmaf(-logit, LOG2E, m) + log2f(sum)) * 0.693147180559945309f;
+}
 
-// A row's parts together: o, the target's logit and the loss. Sixteen rows a
+// A row's parts together: the sum over the others and the loss. Sixteen rows a
 // workgroup, 64 slices of the parts, joined in a fixed order.
 __global__ __launch_bounds__(1024) void k_losses(VocabularyArgs a, const float2* part, int64_t parts) {
     __shared__ float2 lds[64][16];
@@ -495,22 +501,32 @@ __global__ __launch_bounds__(1024) void k_losses(VocabularyArgs a, const float2*
     if (slice != 0 || r >= a.rows) return;
     const int64_t t = a.targets[r];
     const bool counts = t >= 0 && t < a.vocab;
-    const float d = sum_minus(s.x + log2f(s.y), a.stats[a.rows + r]);  // no others: -infinity
-    a.stats[r] = s.x + log2f(s.y);
-    if (!counts) a.stats[a.rows + r] = 0.0f;
+    const float d = sum_minus(s.x, s.y, a.stats[a.rows + r]);  // no others: -infinity
+    a.stats[r] = s.x;
+    a.stats[a.rows + r] = s.y;
     a.losses[r] = !counts ? 0.0f : d > 0.0f ? d + log1pf(expf(-d)) : log1pf(expf(d));
 }
 
-__device__ __forceinline__ RowInfo row_info(const VocabularyArgs& a, int64_t r) {
+// What the products need of row r, by a wave. The target's logit again: the forward pass leaves the sum's two numbers.
+template <typename T>
+__device__ __forceinline__ void find_row_info(const VocabularyArgs& a, int64_t r, RowInfo* info) {
+    const int lane = threadIdx.x & 63;
     const int64_t t = a.targets[r];
-    RowInfo v = {0.0f, 0.0f, -1};
+    RowInfo v = {0.0f, 0.0f, 0.0f, -1};
     if (t >= 0 && t < a.vocab) {
-        const float others = a.stats[r], d = sum_minus(others, a.stats[a.rows + r]);
-        v.others = finite_or_0(others);  // no others: there is no q
+        const T *x = static_cast<const T*>(a.x.p) + r * a.x.stride, *w = static_cast<const T*>(a.w.p) + t * a.w.stride;
+        float logit = 0.0f;
+#pragma unroll 4
+        for (int c = lane; c < a.dim; c += 64) logit = fmaf(St<T>::ld1(x + c), St<T>::ld1(w + c), logit);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) logit += __shfl_xor(logit, o);
+        const float m = a.stats[r], sum = a.stats[a.rows + r], d = sum_minus(m, sum, logit);
+        v.most = finite_or_0(m);  // no others: there is no q
+        v.share = sum == 0.0f ? 0.0f : 1.0f / sum;
         v.scale = a.dloss[r] * (d < 0.0f ? expf(d) / (1.0f + expf(d)) : 1.0f / (1.0f + expf(-d)));
         v.target = (int)t;
     }
-    return v;
+    if (lane == 0) info[r] = v;
 }
 
 // The pieces of eight numbers at p, p + plane, ..., 16-byte aligned.
@@ -599,13 +615,14 @@ __global__ __launch_bounds__(256) void k_prepare(Prepare p) {
     int part = 0;
     while (part < 5 && block >= p.end[part]) ++part;
     if (part == 5) return;
-    const int64_t index = block - (part ? p.end[part - 1] : 0), i = index * 256 + threadIdx.x;
+    const int64_t index = block - (part ? p.end[part - 1] : 0);
     if (part < 2) {
         pack_transposed<T>(p.copy[part], index, lds);
     } else if (part < 4) {
-        pack<T>(p.copy[part - 2], i);
+        pack<T>(p.copy[part - 2], index * 256 + threadIdx.x);
     } else {
-        if (i < p.a.rows) p.info[i] = row_info(p.a, i);
+        const int64_t r = index * 4 + threadIdx.x / 64;
+        if (r < p.a.rows) find_row_info<T>(p.a, r, p.info);
     }
 }
 
@@ -788,7 +805,7 @@ hipError_t prepare(Prepare p, hipStream_t s) {
         if (c.dst) at += (c.rows * c.ld / 8 + 255) / 256;
         p.end[2 + k] = at;
     }
-    if (p.info) at += (p.a.rows + 255) / 256;
+    if (p.info) at += (p.a.rows + 3) / 4;
     p.end[4] = at;
     if (at == 0) return hipSuccess;
     dim3 grid;

@@ -19,7 +19,7 @@ struct VocabularyArgs {
     RowView x, w;            // [rows][dim], [vocab][dim]
     const int64_t* targets;  // [rows]
     float* losses;           // [rows], forward output
-    float* stats;            // [2][rows]: log2 of the sum over the others, the target's logit (forward output, backward input)
+    float* stats;            // [2][rows]: m and s of the sum over the others, 2^m s (forward output, backward input)
     const float* dloss;      // [rows], backward
     void* dx;                // backward outputs
     void* dw;

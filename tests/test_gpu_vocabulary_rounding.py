@@ -94,3 +94,27 @@ def test_one_gradient_for_all_losses(rows, dim, vocab, dloss):
     _, more = _bounds(nx, nw, t, dl, 0.0)
     off = np.abs(got - want) / (2.0 ** -8 * np.abs(want) + more + 1e-40)
     assert off.max() <= 1, off.max()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,vocab", [(40, 300), (300, 2500), (1100, 20000)])
+def test_logits_of_a_thousand(rows, vocab, dtype):
+    """Logits that share 1000, all of them exact in fp32: multiples of 1/64 below 2^11. A loss is a difference from them: its
+    exponents (of terms that count: at most 2^5 below the largest) are rounded at 2^-20 and each sum at 2^-24 of itself some
+    twenty times, 2^-19 of 1 + loss in all. The q of a row add up to 1 as far, and their product with a column of ones (48
+    additions of 2^-24, pieces of 2^-24, or of 2^-16 in bf16) is 0 but for as much: 2^-18 of c, 2^-15 in bf16."""
+    from paper_1902_11208_amd import sequence
+
+    rng = np.random.default_rng(rows)
+    eighths = lambda *s: np.clip(np.rint(8 * rng.standard_normal(s)), -24, 24) / 8  # noqa: E731
+    x, w = eighths(rows, 24), eighths(vocab, 24)
+    x[:, 8:], x[:, 0], w[:, 0] = 0, 1000, 1
+    t, dl = rng.integers(0, vocab, rows), rng.uniform(0.5, 1.5, rows).astype(np.float32).astype(np.float64)
+    op = sequence.VocabularyLoss(torch.from_numpy(w).to(dtype).cuda(), rows)
+    losses = _np(op.forward(torch.from_numpy(x).to(dtype).cuda(), torch.from_numpy(t).cuda()))
+    want = orc.vocabulary_loss(x, w, t)
+    off = np.abs(losses - want) / (2.0 ** -19 * (1 + want))
+    assert off.max() <= 1, off.max()
+    dx, _ = op.backward(torch.from_numpy(dl.astype(np.float32)).cuda())
+    off = np.abs(_np(dx)[:, 0]) / dl
+    assert off.max() <= (2.0 ** -18 if dtype == torch.float32 else 2.0 ** -15), off.max()
