@@ -131,14 +131,18 @@ __device__ __forceinline__ void coefficients(float z, float x, float& f, float& 
 
 // A h + B is what the tokens give unless something leaves fp32's range on the way:
 // A may have fallen below it under a large state, 0 times infinity is no number,
-// factors may have grown and shrunk. So slices whose factors multiply to more
-// than 4 or whose B is large are marked with NaN (sixteen of them then grow a state
-// by at most 2^32), and where a mark or a large state is met the tokens are walked
-// one by one.
+// factors may have grown and shrunk. So slices whose growth (the product of the factors
+// beyond 1, which bounds every run of them) is more than 4 or whose B is large are marked
+// with NaN; sixteen of them then grow a state by at most 2^32. What A has lost below the
+// range is then at most 2^-145, and a state that a slice takes down by more than 2^-120 may
+// be that. Where a mark, a large state or such a fall is met the tokens are walked one by
+// one. Sigmoids neither grow anything nor give back what fell.
 constexpr float LARGE = 0x1p40f;
+constexpr float FALL = 0x1p-120f;
+constexpr float SEGMENT_FALL = 0x1p-68f;  // growth of at most 2^32 leaves a segment's A at most 2^-93 off
 
-__device__ __forceinline__ void mark_factor(float& A, float most) {
-    if (!(fabsf(A) <= most)) A = __builtin_nanf("");
+__device__ __forceinline__ void mark_growth(float growth, float most, float& A) {
+    if (!(growth <= most)) A = __builtin_nanf("");
 }
 __device__ __forceinline__ void mark_rest(float& B) {
     if (!(fabsf(B) <= LARGE)) B = __builtin_nanf("");
@@ -147,6 +151,7 @@ __device__ __forceinline__ void mark_rest(float& B) {
 __device__ __forceinline__ bool unsafe(float from, float joined) {
     return from == from && (joined != joined || fabsf(from) > LARGE);
 }
+__device__ __forceinline__ bool fell(float from, float joined, float by) { return fabsf(joined) < fabsf(from) * by; }
 
 // Rows of a sequence as a thread reads them: a uniform base, and 32 bits of its own
 // offset (128 rows are less than 2^32 bytes apart by the caller's check).
@@ -237,9 +242,12 @@ struct Shared {
 __device__ __forceinline__ float2 pack(const float (&v)[V]) { return make_float2(v[0], v[1]); }
 
 // The state that meets slice `mine`, from `h` that meets the tile: the slices before
-// it (REVERSE: behind it) in order. A wave goes no further than its last one.
-template <int CL, bool REVERSE>
-__device__ __forceinline__ void join_slices(const float2 (*A)[CL], const float2 (*B)[CL], int mine, int lane, float (&h)[V]) {
+// it (REVERSE: behind it) in order. A wave goes no further than its last one. True where
+// the tokens may give another state.
+template <int CL, bool REVERSE, bool SIG>
+__device__ __forceinline__ bool join_slices(const float2 (*A)[CL], const float2 (*B)[CL], int mine, int lane, float (&h)[V]) {
+    const float from[V] = {h[0], h[1]};
+    float least = 0.0f;  // below 0 after a fall
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
     const int n = REVERSE ? SLICES - 1 - wave * 64 / CL : min(SLICES - 1, (wave * 64 + 63) / CL);
     for (int k0 = 0; k0 < n; k0 += 4) {
@@ -255,10 +263,13 @@ __device__ __forceinline__ void join_slices(const float2 (*A)[CL], const float2 
             const int s = REVERSE ? SLICES - 1 - k0 - i : k0 + i;
             const bool before = REVERSE ? s > mine : s < mine;
             const float h0 = fmaf(pa[i].x, h[0], pb[i].x), h1 = fmaf(pa[i].y, h[1], pb[i].y);
-            h[0] = before ? h0 : h[0];
-            h[1] = before ? h1 : h[1];
+            const float to0 = before ? h0 : h[0], to1 = before ? h1 : h[1];
+            if (!SIG) least = fminf(fminf(least, fmaf(fabsf(h[0]), -FALL, fabsf(to0))), fmaf(fabsf(h[1]), -FALL, fabsf(to1)));
+            h[0] = to0;
+            h[1] = to1;
         }
     }
+    return least < 0.0f || unsafe(from[0], h[0]) || unsafe(from[1], h[1]);
 }
 
 // h through the tokens from .. to - 1, one by one.
@@ -298,13 +309,26 @@ __device__ __forceinline__ void walk_reverse(const Rows<T, WIDE>& z, const Rows<
 template <int CL>
 constexpr int threads_of() { return CL * SLICES; }
 
-// A segment's A and B from its tiles', by the threads of the last slice to be joined.
-__device__ __forceinline__ void add_tile(const float (&tile_a)[V], const float (&tile_b)[V], float (&A)[V], float (&B)[V]) {
+// A segment's A and B, with a tile's slices in order (REVERSE: from the last), by the threads of the last one to be joined.
+template <int CL, bool REVERSE, bool SIG>
+__device__ __forceinline__ void add_slices(const float2 (*a)[CL], const float2 (*b)[CL], int lane, float (&growth)[V], float (&A)[V], float (&B)[V]) {
+    for (int k = 0; k < SLICES; ++k) {
+        const int s = REVERSE ? SLICES - 1 - k : k;
+        const float sa[V] = {a[s][lane].x, a[s][lane].y}, sb[V] = {b[s][lane].x, b[s][lane].y};
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float next = fmaf(sa[i], B[i], sb[i]);
+            if (!SIG) {
+                growth[i] *= fmaxf(fabsf(sa[i]), 1.0f);
+                if (fell(B[i], next, FALL)) growth[i] = __builtin_huge_valf();
+            }
+            A[i] *= sa[i];
+            B[i] = next;
+        }
+    }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        B[i] = fmaf(tile_a[i], B[i], tile_b[i]);
-        A[i] *= tile_a[i];
-        mark_factor(A[i], 0x1p32f);
+        if (!SIG) mark_growth(growth[i], 0x1p32f, A[i]);
         mark_rest(B[i]);
     }
 }
@@ -321,7 +345,7 @@ __global__ __launch_bounds__(threads_of<CL>()) void k_recurrence_fwd(RecurrenceA
     const Out<T, WIDE> out(a.h, u.t0, a.channels, me.c, me.valid);
     const int64_t row = (int64_t)u.seq * a.channels + me.c, slot_row = u.slot * a.channels + me.c;
     const bool last = me.slice == SLICES - 1;
-    float h[V] = {}, A[V] = {1.0f, 1.0f}, B[V] = {};
+    float h[V] = {}, A[V] = {1.0f, 1.0f}, B[V] = {}, growth[V] = {1.0f, 1.0f};
     if (!SUMS && last) {
         if (u.from > 0) {
             load_f32(a.starts + slot_row, me.valid, h);
@@ -339,10 +363,10 @@ __global__ __launch_bounds__(threads_of<CL>()) void k_recurrence_fwd(RecurrenceA
     int parity = 0;
     for (int64_t tile = u.from; tile < u.to; tile += kRecurrenceTile, parity ^= 1) {
         const int n = (int)min(u.to - tile, (int64_t)kRecurrenceTile), mine = n - me.slice * L;  // real tokens of the tile, of the slice
-        float f[L][V], in[L][V], pa[V], pb[V];
+        float f[L][V], in[L][V], pa[V], pb[V], pg[V];
         auto sums = [&](auto whole) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) pa[i] = 1.0f, pb[i] = 0.0f;
+            for (int i = 0; i < V; ++i) pa[i] = 1.0f, pb[i] = 0.0f, pg[i] = 1.0f;
 #pragma unroll
             for (int l = 0; l < L; ++l) {
                 float vz[V], vx[V];
@@ -353,6 +377,7 @@ __global__ __launch_bounds__(threads_of<CL>()) void k_recurrence_fwd(RecurrenceA
                     coefficients<T, SIG>(vz[i], vx[i], f[l][i], in[l][i]);
                     if (!whole() && l >= mine) f[l][i] = 1.0f, in[l][i] = 0.0f;
                     pa[i] *= f[l][i];
+                    if (!SIG) pg[i] *= fmaxf(fabsf(f[l][i]), 1.0f);
                     pb[i] = fmaf(f[l][i], pb[i], in[l][i]);
                 }
             }
@@ -368,27 +393,18 @@ __global__ __launch_bounds__(threads_of<CL>()) void k_recurrence_fwd(RecurrenceA
         }
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            mark_factor(pa[i], 4.0f);
+            if (!SIG) mark_growth(pg[i], 4.0f, pa[i]);
             mark_rest(pb[i]);
         }
         lds.sum[parity][0][me.slice][me.lane] = pack(pa);
         lds.sum[parity][1][me.slice][me.lane] = pack(pb);
         lds_barrier();
         if constexpr (SUMS) {
-            if (last) {
-                float ta[V] = {1.0f, 1.0f}, tb[V] = {};
-                for (int s = 0; s < SLICES; ++s) {
-                    const float2 sa = lds.sum[parity][0][s][me.lane], sb = lds.sum[parity][1][s][me.lane];
-                    ta[0] *= sa.x, ta[1] *= sa.y;
-                    tb[0] = fmaf(sa.x, tb[0], sb.x), tb[1] = fmaf(sa.y, tb[1], sb.y);
-                }
-                add_tile(ta, tb, A, B);
-            }
+            if (last) add_slices<CL, false, SIG>(lds.sum[parity][0], lds.sum[parity][1], me.lane, growth, A, B);
         } else {
             const float2 carry = lds.carry[parity][me.lane];
             h[0] = carry.x, h[1] = carry.y;
-            join_slices<CL, false>(lds.sum[parity][0], lds.sum[parity][1], me.slice, me.lane, h);
-            if (unsafe(carry.x, h[0]) || unsafe(carry.y, h[1])) {
+            if (join_slices<CL, false, SIG>(lds.sum[parity][0], lds.sum[parity][1], me.slice, me.lane, h)) {
                 h[0] = carry.x, h[1] = carry.y;
                 walk_forward<T, SIG, WIDE>(z, x, tile, min(tile + me.slice * L, u.to), h);
             }
@@ -431,7 +447,7 @@ __global__ __launch_bounds__(threads_of<CL>(), sizeof(T) == 2 ? 4 : 2) void k_re
     const Out<T, WIDE> out_z(a.dz, u.t0, a.channels, me.c, me.valid), out_x(a.dx, u.t0, a.channels, me.c, me.valid);
     const int64_t row = (int64_t)u.seq * a.channels + me.c, slot_row = u.slot * a.channels + me.c;
     const bool first = me.slice == 0;
-    float s[V] = {}, A[V] = {1.0f, 1.0f}, B[V] = {}, mark[V] = {};
+    float s[V] = {}, A[V] = {1.0f, 1.0f}, B[V] = {}, growth[V] = {1.0f, 1.0f}, mark[V] = {};
     if (!SUMS && first) {
         if (u.to < u.len)
             load_f32(a.starts + slot_row, me.valid, s);
@@ -462,11 +478,11 @@ __global__ __launch_bounds__(threads_of<CL>(), sizeof(T) == 2 ? 4 : 2) void k_re
     for (; u.from < u.to && tile >= u.from; tile -= kRecurrenceTile, parity ^= 1) {
         const int n = (int)min(u.to - tile, (int64_t)kRecurrenceTile), mine = n - me.slice * L;
         // rest: 1 - f (or 1); cx, cg: x and dh as loaded, the registers of the fp32 numbers would halve the waves of bf16
-        float f[L][V], rest[L][V], pa[V], pb[V], pr[V];
+        float f[L][V], rest[L][V], pa[V], pb[V], pr[V], pg[V];
         Raw<T> cx[L], cg[L];
         auto sums = [&](auto whole) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) pa[i] = 1.0f, pb[i] = 0.0f, pr[i] = 0.0f;
+            for (int i = 0; i < V; ++i) pa[i] = 1.0f, pb[i] = 0.0f, pr[i] = 0.0f, pg[i] = 1.0f;
 #pragma unroll
             for (int l = 0; l < L; ++l) {
                 float vz[V], vx[V];
@@ -487,6 +503,7 @@ __global__ __launch_bounds__(threads_of<CL>(), sizeof(T) == 2 ? 4 : 2) void k_re
                     }
                     if (!real) f[l][i] = 1.0f, rest[l][i] = 0.0f;
                     pa[i] *= f[l][i];
+                    if (!SIG) pg[i] *= fmaxf(fabsf(f[l][i]), 1.0f);
                     if constexpr (!SUMS) pb[i] = fmaf(f[l][i], pb[i], SIG ? rest[l][i] * vx[i] : vx[i]);
                 }
             }
@@ -506,7 +523,7 @@ __global__ __launch_bounds__(threads_of<CL>(), sizeof(T) == 2 ? 4 : 2) void k_re
         if (tile > u.from) load(tile - kRecurrenceTile);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            mark_factor(pa[i], 4.0f);
+            if (!SIG) mark_growth(pg[i], 4.0f, pa[i]);
             mark_rest(pb[i]);
             mark_rest(pr[i]);
         }
@@ -515,26 +532,16 @@ __global__ __launch_bounds__(threads_of<CL>(), sizeof(T) == 2 ? 4 : 2) void k_re
         lds.sum[parity][2][me.slice][me.lane] = pack(pr);
         lds_barrier();
         if constexpr (SUMS) {
-            if (first) {
-                float ta[V] = {1.0f, 1.0f}, tb[V] = {};
-                for (int k = SLICES - 1; k >= 0; --k) {
-                    const float2 sa = lds.sum[parity][0][k][me.lane], sb = lds.sum[parity][2][k][me.lane];
-                    ta[0] *= sa.x, ta[1] *= sa.y;
-                    tb[0] = fmaf(sa.x, tb[0], sb.x), tb[1] = fmaf(sa.y, tb[1], sb.y);
-                }
-                add_tile(ta, tb, A, B);
-            }
+            if (first) add_slices<CL, true, SIG>(lds.sum[parity][0], lds.sum[parity][2], me.lane, growth, A, B);
         } else {
             float h[V] = {from[0], from[1]};
-            join_slices<CL, false>(lds.sum[parity][0], lds.sum[parity][1], me.slice, me.lane, h);
-            if (unsafe(from[0], h[0]) || unsafe(from[1], h[1])) {
+            if (join_slices<CL, false, SIG>(lds.sum[parity][0], lds.sum[parity][1], me.slice, me.lane, h)) {
                 h[0] = from[0], h[1] = from[1];
                 walk_forward<T, SIG, WIDE>(z, x, tile, min(tile + me.slice * L, u.to), h);
             }
             const float2 carry = lds.carry[parity][me.lane];
             s[0] = carry.x, s[1] = carry.y;
-            join_slices<CL, true>(lds.sum[parity][0], lds.sum[parity][2], me.slice, me.lane, s);
-            if (unsafe(carry.x, s[0]) || unsafe(carry.y, s[1])) {
+            if (join_slices<CL, true, SIG>(lds.sum[parity][0], lds.sum[parity][2], me.slice, me.lane, s)) {
                 s[0] = carry.x, s[1] = carry.y;
                 walk_reverse<T, SIG, WIDE>(z, g, min(tile + (me.slice + 1) * L, tile + n), tile + n, s);
             }
@@ -628,7 +635,7 @@ __global__ __launch_bounds__(64) void k_recurrence_join(RecurrenceArgs a, int bl
         for (int i = 0; i < AHEAD; ++i)
             if (i < n) {
                 const float next = fmaf(A[i], h, B[i]);
-                walk = walk || unsafe(h, next);
+                walk = walk || unsafe(h, next) || (!SIG && fell(h, next, SEGMENT_FALL));
                 h = next;
                 start_of(k0 + i) = h;
             }
@@ -637,7 +644,7 @@ __global__ __launch_bounds__(64) void k_recurrence_join(RecurrenceArgs a, int bl
         for (int i = 0; i < n; ++i) {  // each from its sums if that is safe, else token by token
             const int64_t j = REVERSE ? count - 1 - k0 - i : k0 + i, at = (slot0 + j) * a.channels + c;
             const float next = fmaf(a.sums[at], h, a.sums[all + at]);
-            if (unsafe(h, next)) {
+            if (unsafe(h, next) || (!SIG && fell(h, next, SEGMENT_FALL))) {
                 const int64_t lo = j * a.seqs.seg, hi = min(u.len, lo + a.seqs.seg);
                 for (int64_t s = lo; s < hi; ++s) {
                     const int64_t t = REVERSE ? lo + hi - 1 - s : s;
