@@ -627,7 +627,8 @@ int shape_of(GroupNormArgs& a) {
     a.held = whole ? (int)std::max<int64_t>(a.seqs.longest, 1) : held;
     a.seqs.seg = whole ? 0 : std::max<int64_t>(held * times, 1);
     a.seqs.slots = packed_slots(a.seqs, a.seqs.seg);
-    a.parts = a.seqs.seg ? a.seqs.slots : std::min<int64_t>(a.seqs.slots, std::max(1, 4096 / a.blocks));
+    // backward: each part has a row of dw and db, however many slots there are
+    a.parts = std::min<int64_t>(a.seqs.slots, std::max(1, 4096 / a.blocks));
     return threads;
 }
 
@@ -683,9 +684,10 @@ hipError_t launch(GroupNormArgs a, int threads, hipStream_t s) {
         wide = wide && aligned(a.y, V * es);
     const bool whole = a.lanes <= 64 && 64 % a.lanes == 0;
     const int rows = whole ? threads / 64 : threads / a.lanes;
-    const size_t sums = (size_t)2 * rows * a.lanes * V + 2 * (a.block / a.per), shares = (size_t)(threads / a.lanes) * a.lanes * V;
+    const size_t sums = (size_t)2 * rows * a.lanes * V + 2 * (a.block / a.per), slices = (size_t)(threads / a.lanes) * a.lanes * V;
+    const int64_t shares = a.parts;
     if (a.seqs.slots * a.blocks <= 512) a.seqs.order = nullptr;  // all start at once: the order's load would only be waited for
-    const size_t lds = std::max(sums, BACKWARD ? shares : (size_t)0) * 4;
+    const size_t lds = std::max(sums, BACKWARD ? slices : (size_t)0) * 4;
     dim3 grid, join;
     if (!grid_of(((BACKWARD ? a.parts : a.seqs.slots) + 7) / 8 * 8 * a.blocks, threads, grid) ||
         !grid_of((int64_t)a.seqs.n * a.groups, 64, join))
@@ -717,13 +719,14 @@ hipError_t launch(GroupNormArgs a, int threads, hipStream_t s) {
                 if (!BACKWARD) {  // segments of what a workgroup holds now (pages 156 us, 193 with longer ones; backward 281 against 270)
                     a.seqs.seg = a.held;
                     a.seqs.slots = packed_slots(a.seqs, a.held);
-                    if (!grid_of((a.seqs.slots + 7) / 8 * 8 * a.blocks, threads, grid)) return hipErrorInvalidValue;
                 }
+                a.parts = a.seqs.slots;
+                if (!grid_of((a.seqs.slots + 7) / 8 * 8 * a.blocks, threads, grid)) return hipErrorInvalidValue;
                 e = pass(std::integral_constant<int, AGAIN>());
             }
         }
         if (BACKWARD && e == hipSuccess) {
-            k_groupnorm_dw<<<(2 * a.channels + 15) / 16, 1024, 0, s>>>(a.channels, a.seqs.n > 0 ? a.parts : 0, a.part, a.dw, a.db);
+            k_groupnorm_dw<<<(2 * a.channels + 15) / 16, 1024, 0, s>>>(a.channels, a.seqs.n > 0 ? shares : 0, a.part, a.dw, a.db);
             e = hipGetLastError();
         }
         return e;
