@@ -230,6 +230,10 @@ __device__ __forceinline__ bool find_unit(const RecurrenceArgs& a, int blocks, U
     return true;
 }
 
+// Rows of the sums and starts: one for each edge between a sequence's segments. The `seg` tokens before an edge are those of
+// one segment, so edges `at` and their rows (at - 1) / seg are as many, however many sequences have no edge.
+__device__ __forceinline__ int64_t edge_row(const RecurrenceArgs& a, int64_t at) { return (at - 1) / a.seqs.seg; }
+
 __device__ __forceinline__ int64_t mark_row(const Unit& u, int64_t tile) { return u.t0 / kRecurrenceTile + tile / kRecurrenceTile; }
 
 // What the slices of a tile tell each other, for one of two tiles in turn (one
@@ -340,15 +344,16 @@ __global__ __launch_bounds__(threads_of<CL>()) void k_recurrence_fwd(RecurrenceA
     Unit u;
     int block;
     if (!find_unit<SUMS>(a, blocks, u, block)) return;
+    if (SUMS && u.to == u.len) return;  // nothing starts behind it
     const Place me(a.channels, CL, block);
     const Rows<T, WIDE> z(a.z, u.t0, me.c, me.valid), x(a.x, u.t0, me.c, me.valid);
     const Out<T, WIDE> out(a.h, u.t0, a.channels, me.c, me.valid);
-    const int64_t row = (int64_t)u.seq * a.channels + me.c, slot_row = u.slot * a.channels + me.c;
+    const int64_t row = (int64_t)u.seq * a.channels + me.c;
     const bool last = me.slice == SLICES - 1;
     float h[V] = {}, A[V] = {1.0f, 1.0f}, B[V] = {}, growth[V] = {1.0f, 1.0f};
     if (!SUMS && last) {
         if (u.from > 0) {
-            load_f32(a.starts + slot_row, me.valid, h);
+            load_f32(a.starts + edge_row(a, u.t0 + u.from) * a.channels + me.c, me.valid, h);
             if (a.marks && u.from < u.to) store_f32(a.marks + mark_row(u, u.from) * a.channels + me.c, me.valid, h);
         } else if (a.state) {
             load_f32(a.state + row, me.valid, h);
@@ -428,8 +433,9 @@ __global__ __launch_bounds__(threads_of<CL>()) void k_recurrence_fwd(RecurrenceA
     }
     if (!last) return;
     if constexpr (SUMS) {
-        store_f32(a.sums + slot_row, me.valid, A);
-        store_f32(a.sums + a.seqs.slots * a.channels + slot_row, me.valid, B);
+        const int64_t edge = edge_row(a, u.t0 + u.to) * a.channels + me.c;
+        store_f32(a.sums + edge, me.valid, A);
+        store_f32(a.sums + a.edges * a.channels + edge, me.valid, B);
     } else if (a.final_state && u.to == u.len) {
         store_f32(a.final_state + row, me.valid, h);
     }
@@ -442,15 +448,16 @@ __global__ __launch_bounds__(threads_of<CL>(), sizeof(T) == 2 ? 4 : 2) void k_re
     Unit u;
     int block;
     if (!find_unit<SUMS>(a, blocks, u, block)) return;
+    if (SUMS && u.from == 0) return;  // nothing ends before it
     const Place me(a.channels, CL, block);
     const Rows<T, WIDE> z(a.z, u.t0, me.c, me.valid), x(a.x, u.t0, me.c, me.valid), g(a.dh, u.t0, me.c, me.valid);
     const Out<T, WIDE> out_z(a.dz, u.t0, a.channels, me.c, me.valid), out_x(a.dx, u.t0, a.channels, me.c, me.valid);
-    const int64_t row = (int64_t)u.seq * a.channels + me.c, slot_row = u.slot * a.channels + me.c;
+    const int64_t row = (int64_t)u.seq * a.channels + me.c;
     const bool first = me.slice == 0;
     float s[V] = {}, A[V] = {1.0f, 1.0f}, B[V] = {}, growth[V] = {1.0f, 1.0f}, mark[V] = {};
     if (!SUMS && first) {
         if (u.to < u.len)
-            load_f32(a.starts + slot_row, me.valid, s);
+            load_f32(a.starts + edge_row(a, u.t0 + u.to) * a.channels + me.c, me.valid, s);
         else if (a.dfinal)
             load_f32(a.dfinal + row, me.valid, s);
         lds.carry[0][me.lane] = pack(s);
@@ -588,8 +595,9 @@ __global__ __launch_bounds__(threads_of<CL>(), sizeof(T) == 2 ? 4 : 2) void k_re
     }
     if (!first) return;
     if constexpr (SUMS) {
-        store_f32(a.sums + slot_row, me.valid, A);
-        store_f32(a.sums + a.seqs.slots * a.channels + slot_row, me.valid, B);
+        const int64_t edge = edge_row(a, u.t0 + u.from) * a.channels + me.c;
+        store_f32(a.sums + edge, me.valid, A);
+        store_f32(a.sums + a.edges * a.channels + edge, me.valid, B);
     } else if (a.dstate && u.from == 0) {
         store_f32(a.dstate + row, me.valid, s);
     }
@@ -605,7 +613,11 @@ __global__ __launch_bounds__(64) void k_recurrence_join(RecurrenceArgs a, int bl
     if (seq >= a.seqs.n || c >= a.channels) return;
     Unit u;
     sequence_of(a.seqs, seq, u);
-    const int64_t count = (u.len + a.seqs.seg - 1) / a.seqs.seg, slot0 = u.t0 / a.seqs.seg + seq, all = a.seqs.slots * a.channels;
+    const int64_t count = (u.len + a.seqs.seg - 1) / a.seqs.seg, all = a.edges * a.channels;
+    if (count < 2) return;
+    // the edge behind (REVERSE: before) the k-th segment that the pass meets
+    const int64_t edge0 = edge_row(a, u.t0 + (REVERSE ? count - 1 : 1) * a.seqs.seg);
+    auto edge = [&](int64_t k) { return (edge0 + (REVERSE ? -k : k)) * a.channels + c; };
     const float* from = REVERSE ? a.dfinal : a.state;
     float h = from ? from[(int64_t)seq * a.channels + c] : 0.0f;
     const T* z = static_cast<const T*>(a.z.p) + u.t0 * a.z.stride + c;
@@ -616,13 +628,12 @@ __global__ __launch_bounds__(64) void k_recurrence_join(RecurrenceArgs a, int bl
     auto load = [&](int64_t k0) {
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            const int64_t k = min(k0 + i, count - 1), at = (slot0 + (REVERSE ? count - 1 - k : k)) * a.channels + c;
+            const int64_t at = edge(min(k0 + i, count - 2));
             next_a[i] = a.sums[at];
             next_b[i] = a.sums[all + at];
         }
     };
-    auto start_of = [&](int64_t k) -> float& { return a.starts[(slot0 + (REVERSE ? count - 2 - k : k + 1)) * a.channels + c]; };  // behind segment k
-    if (count > 1) load(0);
+    load(0);
     for (int64_t k0 = 0; k0 + 1 < count; k0 += AHEAD) {
         const int n = (int)min(count - 1 - k0, (int64_t)AHEAD);  // nothing starts behind the last one
         float A[AHEAD], B[AHEAD];
@@ -637,12 +648,12 @@ __global__ __launch_bounds__(64) void k_recurrence_join(RecurrenceArgs a, int bl
                 const float next = fmaf(A[i], h, B[i]);
                 walk = walk || unsafe(h, next) || (!SIG && fell(h, next, SEGMENT_FALL));
                 h = next;
-                start_of(k0 + i) = h;
+                a.starts[edge(k0 + i)] = h;
             }
         if (!walk) continue;
         h = from;
         for (int i = 0; i < n; ++i) {  // each from its sums if that is safe, else token by token
-            const int64_t j = REVERSE ? count - 1 - k0 - i : k0 + i, at = (slot0 + j) * a.channels + c;
+            const int64_t j = REVERSE ? count - 1 - k0 - i : k0 + i, at = edge(k0 + i);
             const float next = fmaf(a.sums[at], h, a.sums[all + at]);
             if (unsafe(h, next) || (!SIG && fell(h, next, SEGMENT_FALL))) {
                 const int64_t lo = j * a.seqs.seg, hi = min(u.len, lo + a.seqs.seg);
@@ -656,7 +667,7 @@ __global__ __launch_bounds__(64) void k_recurrence_join(RecurrenceArgs a, int bl
             } else {
                 h = next;
             }
-            start_of(k0 + i) = h;
+            a.starts[at] = h;
         }
     }
 }
@@ -744,13 +755,16 @@ int64_t segment_of(const RecurrenceArgs& a) {
     return std::max<int64_t>(256, (share / 4 + kRecurrenceTile - 1) / kRecurrenceTile * kRecurrenceTile);
 }
 
+int64_t edges_of(const RecurrenceArgs& a, int64_t seg) { return a.seqs.tokens / seg + 1; }
+
 RecurrenceArgs plan(const RecurrenceArgs& in) {
     RecurrenceArgs a = in;
     a.seqs.seg = segment_of(a);
     a.seqs.slots = packed_slots(a.seqs, a.seqs.seg);
     if (a.seqs.seg) {
+        a.edges = edges_of(a, a.seqs.seg);
         a.sums = static_cast<float*>(a.ws);
-        a.starts = a.sums + 2 * a.seqs.slots * a.channels;
+        a.starts = a.sums + 2 * a.edges * a.channels;
     }
     return a;
 }
@@ -802,7 +816,7 @@ hipError_t launch(const RecurrenceArgs& in, hipStream_t s) {
 
 size_t recurrence_workspace_bytes(const RecurrenceArgs& a) {
     const int64_t seg = segment_of(a);
-    return seg ? (size_t)3 * packed_slots(a.seqs, seg) * a.channels * 4 : 16;
+    return seg ? (size_t)3 * edges_of(a, seg) * a.channels * 4 : 16;
 }
 
 hipError_t launch_recurrence_fwd(const RecurrenceArgs& a, hipStream_t s) { return launch<false>(a, s); }

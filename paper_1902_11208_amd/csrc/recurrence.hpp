@@ -25,8 +25,9 @@ struct RecurrenceArgs {
     void* dx;
     float* dstate;         // or NULL
     void* ws;              // recurrence_workspace_bytes
-    // set by the launchers (as seqs.seg and seqs.slots): the segments' A and B
-    // [2][slots][channels], the states that segments start from [slots][channels]
+    // set by the launchers (as seqs.seg and seqs.slots): edges between segments at most, the A and B of the segments
+    // before them (backward: behind them) [2][edges][channels], the states that meet the edges [edges][channels]
+    int64_t edges;
     float* sums;
     float* starts;
 };
