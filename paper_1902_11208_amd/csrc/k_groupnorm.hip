@@ -461,8 +461,11 @@ __global__ __launch_bounds__(H::THREADS, H::WAVES) void k_groupnorm_bwd(GroupNor
             unpack(rg[k], e);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                c[i] = (c[i] - mean[i]) * rstd[i];
-                e[i] = activate_back<ACT, sizeof(T) == 4>(e[i], fmaf(c[i], w[i], b[i]));
+                const float d = c[i] - mean[i];
+                c[i] = d * rstd[i];
+                // where it decides, u has the forward pass's own roundings: relu lets through what it let through there
+                const float u = ACT == MDLSTM_RELU ? fmaf(d, rstd[i] * w[i], b[i]) : fmaf(c[i], w[i], b[i]);
+                e[i] = activate_back<ACT, sizeof(T) == 4>(e[i], u);
             }
         };
         if constexpr (MODE != AGAIN) {
