@@ -227,12 +227,14 @@ __device__ __forceinline__ bool find_unit(const RecurrenceArgs& a, int blocks, U
     u.len = uniform(u.len);
     u.from = uniform(u.from);
     u.to = uniform(u.to);
+    u.edge = uniform(u.edge);
     return true;
 }
 
-// Rows of the sums and starts: one for each edge between a sequence's segments. The `seg` tokens before an edge are those of
-// one segment, so edges `at` and their rows (at - 1) / seg are as many, however many sequences have no edge.
-__device__ __forceinline__ int64_t edge_row(const RecurrenceArgs& a, int64_t at) { return (at - 1) / a.seqs.seg; }
+// The sums and starts have a row for each edge between a sequence's segments. The `seg` tokens before an edge are those of
+// one segment, so an edge at token t has row (t - 1) / seg to itself, and sequences without edges take none. u.edge is
+// the row of the edge before a segment; the edge behind it has the next.
+constexpr int EDGE_BEHIND = 1;
 
 __device__ __forceinline__ int64_t mark_row(const Unit& u, int64_t tile) { return u.t0 / kRecurrenceTile + tile / kRecurrenceTile; }
 
@@ -353,7 +355,7 @@ __global__ __launch_bounds__(threads_of<CL>()) void k_recurrence_fwd(RecurrenceA
     float h[V] = {}, A[V] = {1.0f, 1.0f}, B[V] = {}, growth[V] = {1.0f, 1.0f};
     if (!SUMS && last) {
         if (u.from > 0) {
-            load_f32(a.starts + edge_row(a, u.t0 + u.from) * a.channels + me.c, me.valid, h);
+            load_f32(a.starts + u.edge * a.channels + me.c, me.valid, h);
             if (a.marks && u.from < u.to) store_f32(a.marks + mark_row(u, u.from) * a.channels + me.c, me.valid, h);
         } else if (a.state) {
             load_f32(a.state + row, me.valid, h);
@@ -433,7 +435,7 @@ __global__ __launch_bounds__(threads_of<CL>()) void k_recurrence_fwd(RecurrenceA
     }
     if (!last) return;
     if constexpr (SUMS) {
-        const int64_t edge = edge_row(a, u.t0 + u.to) * a.channels + me.c;
+        const int64_t edge = (u.edge + EDGE_BEHIND) * a.channels + me.c;
         store_f32(a.sums + edge, me.valid, A);
         store_f32(a.sums + a.edges * a.channels + edge, me.valid, B);
     } else if (a.final_state && u.to == u.len) {
@@ -457,7 +459,7 @@ __global__ __launch_bounds__(threads_of<CL>(), sizeof(T) == 2 ? 4 : 2) void k_re
     float s[V] = {}, A[V] = {1.0f, 1.0f}, B[V] = {}, growth[V] = {1.0f, 1.0f}, mark[V] = {};
     if (!SUMS && first) {
         if (u.to < u.len)
-            load_f32(a.starts + edge_row(a, u.t0 + u.to) * a.channels + me.c, me.valid, s);
+            load_f32(a.starts + (u.edge + EDGE_BEHIND) * a.channels + me.c, me.valid, s);
         else if (a.dfinal)
             load_f32(a.dfinal + row, me.valid, s);
         lds.carry[0][me.lane] = pack(s);
@@ -595,7 +597,7 @@ __global__ __launch_bounds__(threads_of<CL>(), sizeof(T) == 2 ? 4 : 2) void k_re
     }
     if (!first) return;
     if constexpr (SUMS) {
-        const int64_t edge = edge_row(a, u.t0 + u.from) * a.channels + me.c;
+        const int64_t edge = u.edge * a.channels + me.c;
         store_f32(a.sums + edge, me.valid, A);
         store_f32(a.sums + a.edges * a.channels + edge, me.valid, B);
     } else if (a.dstate && u.from == 0) {
@@ -616,7 +618,7 @@ __global__ __launch_bounds__(64) void k_recurrence_join(RecurrenceArgs a, int bl
     const int64_t count = (u.len + a.seqs.seg - 1) / a.seqs.seg, all = a.edges * a.channels;
     if (count < 2) return;
     // the edge behind (REVERSE: before) the k-th segment that the pass meets
-    const int64_t edge0 = edge_row(a, u.t0 + (REVERSE ? count - 1 : 1) * a.seqs.seg);
+    const int64_t edge0 = (u.t0 + a.seqs.seg - 1) / a.seqs.seg + (REVERSE ? count - 2 : 0);
     auto edge = [&](int64_t k) { return (edge0 + (REVERSE ? -k : k)) * a.channels + c; };
     const float* from = REVERSE ? a.dfinal : a.state;
     float h = from ? from[(int64_t)seq * a.channels + c] : 0.0f;

@@ -30,6 +30,7 @@ inline int64_t packed_slots(const Packed& p, int64_t seg) { return seg ? p.n + p
 struct Unit {
     int seq;
     int64_t slot, t0, len, from, to;
+    int64_t edge;  // of a segment: (t0 + from - 1) / seg
 };
 
 __device__ __forceinline__ void sequence_of(const Packed& p, int seq, Unit& u) {
@@ -48,6 +49,7 @@ __device__ __forceinline__ bool unit_of(const Packed& p, int64_t slot, Unit& u) 
         const int seq = p.order ? p.order[slot] : (int)slot;
         if (seq < 0 || seq >= p.n) return false;
         sequence_of(p, seq, u);
+        u.edge = 0;
         return true;
     }
     // The last sequence whose first slot is not behind `slot`: a wave looks at 64 places at once, as a load
@@ -61,7 +63,9 @@ __device__ __forceinline__ bool unit_of(const Packed& p, int64_t slot, Unit& u) 
         lo += steps * step;
     }
     sequence_of(p, lo, u);
-    u.from = (slot - lo - u.t0 / p.seg) * p.seg;
+    const int64_t before = u.t0 / p.seg;
+    u.from = (slot - lo - before) * p.seg;
+    u.edge = slot - lo - (before * p.seg == u.t0);
     u.to = min(u.len, u.from + p.seg);
     return u.from >= 0 && (u.from < u.len || u.from == 0);
 }
