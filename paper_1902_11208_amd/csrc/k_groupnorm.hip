@@ -689,7 +689,6 @@ hipError_t launch(GroupNormArgs a, int threads, hipStream_t s) {
     const int rows = whole ? threads / 64 : threads / a.lanes;
     const size_t sums = (size_t)2 * rows * a.lanes * V + 2 * (a.block / a.per), slices = (size_t)(threads / a.lanes) * a.lanes * V;
     const int64_t shares = a.parts;
-    if (a.seqs.slots * a.blocks <= 512) a.seqs.order = nullptr;  // all start at once: the order's load would only be waited for
     const size_t lds = std::max(sums, BACKWARD ? slices : (size_t)0) * 4;
     dim3 grid, join;
     if (!grid_of(((BACKWARD ? a.parts : a.seqs.slots) + 7) / 8 * 8 * a.blocks, threads, grid) ||

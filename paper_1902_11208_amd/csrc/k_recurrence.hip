@@ -788,7 +788,6 @@ hipError_t launch(const RecurrenceArgs& in, hipStream_t s) {
             constexpr int CL = lanes();
             constexpr bool SIG = sig(), W = w();
             const int blocks = (vecs + CL - 1) / CL;
-            if (a.seqs.slots * blocks <= 512) a.seqs.order = nullptr;  // all start at once: the order's load would only be waited for
             dim3 grid;
             if (!grid_of(a.seqs.slots * blocks, threads_of<CL>(), grid)) return hipErrorInvalidValue;
             if (a.seqs.seg) {
