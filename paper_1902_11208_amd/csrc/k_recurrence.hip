@@ -748,12 +748,13 @@ int vecs_of(int channels) { return (channels + V - 1) / V; }
 // so sequences are cut where the longest one would hold the chip up: where it is
 // longer than all tokens spread over the CUs. Segments then give a CU four units.
 // Forward and backward in bf16 at 512 channels, whole against in segments: one
-// sequence of 4000 tokens 75 / 114 against 19 / 22 us, 8 of 2000 40 / 66 against
-// 28 / 35; 32 of 2000 42 / 83 against 69 / 97, 64 of 6000 281 / 412 against 473 / 667.
+// sequence of 600 tokens 14 / 21 against 16 / 20 us, of 800 19 / 28 against 17 / 20, of
+// 4000 75 / 114 against 19 / 22, 8 of 2000 40 / 66 against 28 / 35; 32 of 2000 42 / 83
+// against 69 / 97, 64 of 6000 281 / 412 against 473 / 667.
 int64_t segment_of(const RecurrenceArgs& a) {
     constexpr int64_t CUS = 256;
     const int64_t blocks = (vecs_of(a.channels) + 31) / 32, share = a.seqs.tokens * blocks / CUS;
-    if (a.seqs.longest <= std::max<int64_t>(1024, 2 * share)) return 0;
+    if (a.seqs.longest <= std::max<int64_t>(768, 2 * share)) return 0;
     return std::max<int64_t>(256, (share / 4 + kRecurrenceTile - 1) / kRecurrenceTile * kRecurrenceTile);
 }
 
