@@ -599,8 +599,9 @@ bool aligned(const void* p, int to) { return (reinterpret_cast<uintptr_t>(p) & (
 
 // Chooses channels of a workgroup, its threads and whether it holds whole sequences
 // (seqs.seg 0). A workgroup takes whole groups, about 128 bytes of a row; 64 where
-// it then holds the longest sequence. Measured for the wide batch of 300 to 1200
-// tokens of 512 channels: see k_groupnorm_fwd and k_groupnorm_bwd.
+// it then holds the longest sequence: forward of 128 sequences of 300 to 1200 tokens
+// of 512 bf16 channels 59 us, in segments 82; backward of 256 of 100 to 300 78 us, 96
+// in segments.
 template <typename H>
 int shape_of(GroupNormArgs& a) {
     const int es = a.dtype ? 2 : 4, hold = a.dtype ? Hold<bf16_t, H> : Hold<float, H>;
@@ -624,9 +625,12 @@ int shape_of(GroupNormArgs& a) {
     if (!whole) held = with(128);
     int threads = H::THREADS;
     while (whole && threads > 64 && threads / 2 >= a.lanes && (int64_t)threads / 2 / a.lanes * hold >= a.seqs.longest) threads /= 2;
-    // segments of up to eight times what a workgroup holds, where they still fill the chip several times: a workgroup's
-    // start (its sequence, weights, sums) takes about as long as 32 KB
-    const int64_t times = std::max<int64_t>(1, std::min<int64_t>(8, a.seqs.tokens * a.blocks / (std::max(held, 1) * (int64_t)2048)));
+    // segments of up to four times what a workgroup holds, where some 2048 of them are left: a workgroup's start (its
+    // sequence, weights, sums) takes about as long as 32 KB. Forward / backward with one, two, four and eight times, of
+    // 320 bf16 channels: 8 sequences of 65000 tokens 271 / 442, 252 / 405, 256 / 400, 255 / 418 us, one of 30000 28 / 42,
+    // 28 / 40, 32 / 47, 41 / 61. With 1024 left 8 of 8000 took 40 / 65 instead of 44 / 72, and 128 of 300 to 1200 tokens
+    // of 512 channels 12 us more, as their segments differ.
+    const int64_t times = std::max<int64_t>(1, std::min<int64_t>(4, a.seqs.tokens * a.blocks / (std::max(held, 1) * (int64_t)2048)));
     a.held = whole ? (int)std::max<int64_t>(a.seqs.longest, 1) : held;
     a.seqs.seg = whole ? 0 : std::max<int64_t>(held * times, 1);
     a.seqs.slots = packed_slots(a.seqs, a.seqs.seg);
