@@ -12,9 +12,10 @@
 // 128 sequences of 300 to 1200 tokens of 512 channels in 32 groups, forward held 66 us
 // (196 MB, 3.0 TB/s), backward in segments 75 + 75 us (196 MB read, then 295 MB: 2.6 and
 // 3.9 TB/s; held by 512 threads with 256 registers it took 175); eight pages of 60000
-// to 70000 tokens of 320 channels, 97 + 156 us and 186 + 270 us (3.4, 4.3, 3.6 and 3.7
-// TB/s). The exponentials and the sums of a thread's vectors take about as long as the
-// memory: 25 vector instructions a number backward, of the 40 that its bytes leave room for.
+// to 70000 tokens of 320 channels, 102 + 161 us and 199 + 258 us (3.3, 4.2, 3.4 and 3.9
+// TB/s). By the counters a number of the pages takes 9 and 18 vector instructions forward, 23
+// and 23 backward: at four cycles each, sixteen for the exponential and the reciprocal,
+// some 60% of the backward passes' time beside the memory's.
 //
 // The variance is the mean of squared distances from the mean, found in a second
 // look at the registers (a difference of sums of squares would lose it beside a

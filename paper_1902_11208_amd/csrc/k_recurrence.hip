@@ -11,16 +11,18 @@
 // finds the state its slice starts from and goes through its tokens once more.
 // So each input is read once and each output written once, and HBM bounds it. The
 // next tile is loaded while one is computed. Measured: 128 sequences of 300 to 1200
-// tokens of 512 bf16 channels, forward 67 us (290 MB, 4.3 TB/s), backward 128 us (490
-// MB, 3.8 TB/s); one sequence of 65536 tokens of 1024, in segments, 50 us for their
-// sums, 11 to join them, 77 for the pass itself. Its vector instructions (some thirty a
-// number with a sigmoid, the reciprocal and exponential four times one) come near the
-// memory's time in bf16: with 64-bit row addresses and masks in every tile it was 123 us.
+// tokens of 512 bf16 channels, forward 73 us (290 MB, 4.0 TB/s), backward 129 us (490
+// MB, 3.8 TB/s, and 50 MB of spilled registers); one sequence of 65536 tokens of 1024, in
+// segments, 50 us for their sums, 12 to join them, 78 for the pass itself. By the counters
+// a number takes 28 vector instructions forward and 50 backward with a sigmoid: at four
+// cycles each, sixteen for the exponential and the reciprocal, 40 and 68 us, more than half
+// of the memory's time; with 64-bit row addresses and masks in every tile the forward pass
+// took 123 us.
 //
-// The forward pass keeps the fp32 state at every tile's start (1/64 of bf16
-// inputs), and the backward pass finds h again from it instead of from the
+// The forward pass keeps the fp32 state at every tile's start (1/128 of bf16 z
+// and x), and the backward pass finds h again from it instead of from the
 // rounded output: h - x is a difference, and a rounded h would leave it with
-// an error of 2^-9 of h.
+// an error of up to 2^-8 of h.
 #include <algorithm>
 #include <type_traits>
 

@@ -23,13 +23,14 @@
 // q is rounded (2000 rows of 128 with a common part of 10 beside a spread of 0.18 a
 // coordinate: dx 2.8e-3 off, in two pieces 1.7e-3, which is the result's own rounding).
 //
-// Matrix instructions bound it, and how fast LDS feeds them: 256 x 256 tiles in eight
-// waves of 128 x 64 read 192 KB of operands from LDS a step of 64 and write 64, beside
-// 2048 cycles of products. Measured, 16383 rows of 1024 in bf16 over 50021: the
-// gradients' products 1400 TFLOP/s (sums of 16384), the logits 1020 (a tile's prologue
-// and its sums of exponentials take 10 of 33 us), the logits again with q written both
-// ways round 730 (2.1 GB of q for 16384 of the vocabulary in 755 us). 128 x 128 tiles,
-// two workgroups a CU, reach 700: they read twice as much LDS a product.
+// Matrix instructions bound it: 256 x 256 tiles in eight waves of 128 x 64 read 192 KB
+// of operands from LDS a step of 64 and write 64, beside 2048 cycles of products, without
+// bank conflicts. Measured, 16383 rows of 1024 in bf16 over 50021: dW's products 1370
+// TFLOP/s (sums of 2 x 16384, the matrix units busy 68% of the cycles), dx's 1260 (60%),
+// the logits 1000 (48%; a tile's prologue and its sums of exponentials take 10 of 33 us),
+// the logits again with q written both ways round in two pieces 600 (28%; 2.1 GB of q for
+// 16384 of the vocabulary in 920 us). 128 x 128 tiles, two workgroups a CU, reach 600 to 700:
+// they read twice as much LDS a product.
 #include <algorithm>
 #include <type_traits>
 
@@ -673,8 +674,8 @@ typedef Shape<64, 128, 64, 32> Low;
 // Low tiles where the rows fill half a middle one at most, Large ones where they
 // still give most CUs a tile. Forward at 64 rows, 1024 channels and 50000 words:
 // Low 26 us, Middle 31, Large 44. Forward and backward at 4000 rows: 4000 words of
-// 1024 channels (256 large tiles) Large 45 / 183, Middle 49 / 186 us; at 2000 rows
-// and 5000 words of 512 channels (160) Middle 31 / 117, Large 33 / 124.
+// 1024 channels (256 large tiles) Large 44 / 220, Middle 49 / 221 us; at 2000 rows
+// and 5000 words of 512 channels (160) Middle 32 / 126, Large 34 / 134.
 template <bool ANY = true, typename F>
 auto with_shape(int64_t m, int64_t n, F&& f) {
     if (m <= 64) return f(Low());

@@ -289,7 +289,8 @@ class GroupNorm(_PackedLayer):
         return self._y
 
     def backward(self, dy, stream=None):
-        """(dx, dweight, dbias) after a forward call, from the gradient of y."""
+        """(dx, dweight, dbias) after a forward call, from the gradient of y. Weight and bias have to be as they were in
+        the forward call."""
         if self._saved is None:
             raise ValueError("backward needs a forward call on this norm first")
         if self._grads is None:
@@ -373,7 +374,8 @@ class VocabularyLoss:
         loss_i = log(sum_v exp(x_i . weight_v)) - x_i . weight_target_i
 
     weight: [vocab, dim] device tensor, float32 or bfloat16, which x and the gradients share. A row whose target lies
-    outside [0, vocab) (-1, say) has loss 0 and takes no part in the gradients, whatever it holds. Sums are fp32.
+    outside [0, vocab) (-1, say) has loss 0 and takes no part in the gradients, whatever it holds. Sums are fp32, and
+    gradients are rounded to bfloat16 once.
     """
 
     def __init__(self, weight: torch.Tensor, rows: int):
