@@ -61,11 +61,17 @@ struct RowInfo {
 
 enum { LOGSUM, GRADIENT, PLANES, RESULT };
 
+// The tiles of a gradient's product and the parts of its sum (cut_of).
+struct Cut {
+    bool large = false;
+    int parts = 1;
+};
+
 struct Product {
     Operand a, b;
     int steps;          // steps of one pair of pieces
     int pairs;          // 1; 2 of a's two pieces with b; 6 of the three pieces of each
-    int splits;         // PLANES: parts of the sum
+    Cut cut;            // PLANES, RESULT: the tiles and the parts of the sum (one where nothing is set, or for a result)
     int tiles_m, tiles_n;
     // LOGSUM
     const int64_t* targets;
@@ -78,7 +84,7 @@ struct Product {
     bf16_t* qt;         // planes of [b.rows][ldt], columns a.rows to ldt are zeroed
     int64_t ldq, ldt, q_plane, qt_plane;
     // PLANES
-    float* out;         // [splits][a.rows][ldo]
+    float* out;         // [cut.parts][a.rows][ldo]
     int64_t ldo;
     int add;            // to what is there
     // RESULT: [a.rows][ldo] as stored, times the rows' scale (k_finish)
@@ -283,8 +289,8 @@ __global__ __launch_bounds__(S::THREADS) void k_product(Product g) {
     tn = __builtin_amdgcn_readfirstlane(tn);
     const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
     const int all = g.steps * g.pairs, split = blockIdx.y;
-    const int from = __builtin_amdgcn_readfirstlane((int)((int64_t)all * split / g.splits)),
-              to = __builtin_amdgcn_readfirstlane((int)((int64_t)all * (split + 1) / g.splits));
+    const int from = __builtin_amdgcn_readfirstlane((int)((int64_t)all * split / g.cut.parts)),
+              to = __builtin_amdgcn_readfirstlane((int)((int64_t)all * (split + 1) / g.cut.parts));
     const Loader<S> load(g, m0, n0);
     const bf16_t *pa = g.a.p + m0 * g.a.ld, *pb = g.b.p + n0 * g.b.ld;
     int pair = __builtin_amdgcn_readfirstlane(g.steps ? from / g.steps : 0), step = from - pair * g.steps, left = to - from;  // of the next fetch
@@ -671,7 +677,7 @@ typedef Shape<256, 256, 128, 64> Large;
 typedef Shape<128, 128, 64, 64> Middle;
 typedef Shape<64, 128, 64, 32> Low;
 
-// Low tiles where the rows fill half a middle one at most, Large ones where they
+// The logits' tiles: Low where the rows fill half a middle one at most, Large where they
 // still give most CUs a tile. Forward at 64 rows, 1024 channels and 50000 words:
 // Low 26 us, Middle 31, Large 44. Forward and backward at 4000 rows: 4000 words of
 // 1024 channels (256 large tiles) Large 44 / 220, Middle 49 / 221 us; at 2000 rows
@@ -684,38 +690,47 @@ auto with_shape(int64_t m, int64_t n, F&& f) {
     return f(Middle());
 }
 
-// Parts of the sum of a product, so that its tiles fill the chip: the number that
-// takes the least time by a model of it. A round of workgroups takes as long as
-// their steps (1.9 us of a large tile alone on its CU; 1.5 and 0.8 us of the others,
-// two on a CU) and two more to start and end; every part's plane is written and read
-// once, at 5 TB/s.
-int splits_of(int64_t m, int64_t n, int64_t steps) {
-    return with_shape(m, n, [&](auto shape) {
-        typedef decltype(shape) S;
-        const int64_t tiles = (m + S::BM - 1) / S::BM * ((n + S::BN - 1) / S::BN), slots = S::BM == 256 ? 256 : 512;
-        const double step = S::BM == 256 ? 1.9 : S::BM == 128 ? 1.5 : 0.8, plane = (double)m * n * 8 / 5e6;
-        int best = 1;
-        double least = 1e300;
-        for (int64_t k = 1; k <= std::max<int64_t>(1, std::min<int64_t>(64, steps / 4)); ++k) {
-            const double time = (double)((tiles * k + slots - 1) / slots) * ((steps + k - 1) / k + 2) * step + k * plane;
-            if (time < least) least = time, best = (int)k;
-        }
-        return best;
-    });
+// The tiles of a gradient's product and the parts of its sum, with which it fills the
+// chip: those that take the least time by a model of it. A round of workgroups takes as
+// long as their steps (1.9 us of a large tile alone on its CU; 1.5 and 0.8 us of the
+// others, two on a CU) and two more to start and end; every part's plane is written and
+// read once, at 5 TB/s. Backward with large tiles from 192 of them on, whatever the
+// parts, against this, in bf16: 4000 rows of 512 over 12000 448 and 399 us, 20000 of 256
+// over 2000 307 and 289, 5000 of 1000 over 30000 1834 and 1695, 4000 of 512 over 3000 138
+// and 141, 1000 of 256 over 100000 722 and 737.
+template <class S>
+double time_of(int64_t m, int64_t n, int64_t steps, int& parts) {
+    const int64_t tiles = (m + S::BM - 1) / S::BM * ((n + S::BN - 1) / S::BN), slots = S::BM == 256 ? 256 : 512;
+    const double step = S::BM == 256 ? 1.9 : S::BM == 128 ? 1.5 : 0.8, plane = (double)m * n * 8 / 5e6;
+    double least = 1e300;
+    for (int64_t k = 1; k <= std::max<int64_t>(1, std::min<int64_t>(64, steps / 4)); ++k) {
+        const double time = (double)((tiles * k + slots - 1) / slots) * ((steps + k - 1) / k + 2) * step + k * plane;
+        if (time < least) least = time, parts = (int)k;
+    }
+    return least;
+}
+Cut cut_of(int64_t m, int64_t n, int64_t steps) {
+    Cut large{true, 1}, small{false, 1};
+    if (m <= 64) {
+        (void)time_of<Low>(m, n, steps, small.parts);
+        return small;
+    }
+    return time_of<Large>(m, n, steps, large.parts) < time_of<Middle>(m, n, steps, small.parts) ? large : small;
 }
 
 template <int WHAT, int PIECES = 1>
 hipError_t product(Product g, hipStream_t s) {
-    // three pieces of q leave middle tiles no slower than large ones: backward of 1537 rows of 256 over 7003 in fp32 201
-    // against 212 us, of 4000 rows of 512 over 12000 1151 against 1138
-    return with_shape<WHAT != GRADIENT || PIECES != 3>(g.a.rows, g.b.rows, [&](auto shape) {
+    auto launch = [&](auto shape) {
         typedef decltype(shape) S;
         g.tiles_m = (int)((g.a.rows + S::BM - 1) / S::BM);
         g.tiles_n = (int)((g.b.rows + S::BN - 1) / S::BN);
-        if (WHAT != PLANES) g.splits = 1;  // PLANES: the caller's
-        k_product<S, WHAT, PIECES><<<dim3((unsigned)(g.tiles_m * g.tiles_n), (unsigned)g.splits), S::THREADS, 0, s>>>(g);
+        k_product<S, WHAT, PIECES><<<dim3((unsigned)(g.tiles_m * g.tiles_n), (unsigned)g.cut.parts), S::THREADS, 0, s>>>(g);
         return hipGetLastError();
-    });
+    };
+    if constexpr (WHAT == PLANES || WHAT == RESULT) return g.a.rows <= 64 ? launch(Low()) : g.cut.large ? launch(Large()) : launch(Middle());
+    // three pieces of q leave middle tiles no slower than large ones: backward of 1537 rows of 256 over 7003 in fp32 201
+    // against 212 us, of 4000 rows of 512 over 12000 1151 against 1138
+    return with_shape<WHAT != GRADIENT || PIECES != 3>(g.a.rows, g.b.rows, launch);
 }
 
 int64_t column_tile(int64_t m, int64_t n) {
@@ -729,8 +744,8 @@ struct Plan {
     int64_t x, w, part, info, xt, wt, q, qt, dx, dw, total;  // offsets
     int pairs() const { return pieces == 1 ? 1 : 6; }
     int q_pairs() const { return pieces == 1 ? 2 : 6; }
-    int splits_dx(const VocabularyArgs& a) const { return splits_of(a.rows, a.dim, piece / BK * q_pairs()); }
-    int splits_dw(const VocabularyArgs& a, int64_t n) const { return splits_of(n, a.dim, rowsp / BK * q_pairs()); }
+    Cut cut_dx(const VocabularyArgs& a) const { return cut_of(a.rows, a.dim, piece / BK * q_pairs()); }
+    Cut cut_dw(const VocabularyArgs& a, int64_t n) const { return cut_of(n, a.dim, rowsp / BK * q_pairs()); }
 };
 
 bool direct(const VocabularyArgs& a, const RowView& v) {
@@ -767,8 +782,8 @@ Plan plan_of(const VocabularyArgs& a, bool backward) {
         p.q = take(p.rowsp * p.piece * 2 * p.q_pieces);
         p.qt = take(p.rowsp * p.piece * 2 * p.q_pieces);
         const int64_t rest = a.vocab % p.piece;
-        p.dx = take(p.splits_dx(a) * a.rows * a.dim * 4);
-        p.dw = take(std::max(p.splits_dw(a, std::min<int64_t>(p.piece, a.vocab)) * p.piece, rest ? p.splits_dw(a, rest) * rest : 0) * a.dim * 4);
+        p.dx = take(p.cut_dx(a).parts * a.rows * a.dim * 4);
+        p.dw = take(std::max(p.cut_dw(a, std::min<int64_t>(p.piece, a.vocab)).parts * p.piece, rest ? p.cut_dw(a, rest).parts * rest : 0) * a.dim * 4);
     }
     p.total = std::max<int64_t>(at, 16);
     return p;
@@ -921,11 +936,11 @@ hipError_t backward(const VocabularyArgs& a, hipStream_t s) {
             x.b = Operand{bf(p.wt), wt_plane, np, a.dim};
             x.steps = (int)(np / BK);
             x.pairs = p.q_pairs();
-            x.splits = p.splits_dx(a);
+            x.cut = p.cut_dx(a);
             x.out = f32(p.dx);
             x.ldo = a.dim;
             x.add = first > 0;
-            if (x.splits == 1 && p.piece >= a.vocab) {
+            if (x.cut.parts == 1 && p.piece >= a.vocab) {
                 x.result = dx;
                 x.rows = info;
                 OK_OR_RETURN((product<RESULT, Pieces<T>::N>(x, s)));
@@ -939,21 +954,21 @@ hipError_t backward(const VocabularyArgs& a, hipStream_t s) {
         v.b = Operand{bf(p.xt), xt_plane, p.rowsp, a.dim};
         v.steps = a.rows > 0 ? (int)(p.rowsp / BK) : 0;  // no rows: dW is zero
         v.pairs = p.q_pairs();
-        v.splits = p.splits_dw(a, n);
+        v.cut = p.cut_dw(a, n);
         v.out = f32(p.dw);
         v.ldo = a.dim;
         // in one part, stored by the product: planes stored and read again took 1.4 us more where 500 rows of dW of 512
         // leave (backward of 64 rows 35.9 against 34.5 us) and 74 where 50000 of 1024 do (280 against 207 us)
-        if (v.splits == 1) {
+        if (v.cut.parts == 1) {
             v.result = dw + first * a.dim;
             OK_OR_RETURN((product<RESULT, Pieces<T>::N>(v, s)));
         } else {
             OK_OR_RETURN(product<PLANES>(v, s));
-            OK_OR_RETURN(finish<T>(v.out, v.splits, 1, n * a.dim, nullptr, dw + first * a.dim, s));
+            OK_OR_RETURN(finish<T>(v.out, v.cut.parts, 1, n * a.dim, nullptr, dw + first * a.dim, s));
         }
     }
     if (a.rows == 0 || !dx) return hipSuccess;  // no rows, or stored by the product
-    return finish<T>(f32(p.dx), p.splits_dx(a), a.rows, a.dim, info, dx, s);
+    return finish<T>(f32(p.dx), p.cut_dx(a).parts, a.rows, a.dim, info, dx, s);
 }
 
 }  // namespace
